@@ -83,6 +83,8 @@ typedef int32_t mmbev_status_t;
                                        the contract (offsets, coordinates outside the grid or of
                                        another frame; for the scatter also keys not strictly
                                        ascending inside a frame) */
+#define MMBEV_FAULT_SEQUENCES 16    /* the sequence operators: a row count outside 0 .. rows, sequence offsets not
+                                       0 .. <= rows non-decreasing, or a slot outside the states */
 
 /* ------------------------------------------------------------- inputs */
 
@@ -468,6 +470,215 @@ mmbev_status_t mmbev_voxel_clusters(const int32_t* coords, const int32_t* counts
                                     mmbev_cluster_t* out_clusters, int64_t* out_cluster_offsets,
                                     int32_t* out_voxel_labels, void* workspace, size_t workspace_bytes,
                                     void* stream);
+
+/* ------------------- sequence operators of a learned voxel encoder */
+
+/*
+ * What a learned VoxelFeatureEncoder (Alg. 1) runs over the voxel rows: layer
+ * norm, rotary positions taken from the voxel coordinates, and linear
+ * attention with a decay per head, which mixes a frame's rows in key order in
+ * time linear in their number.  Each has its forward and backward pass;
+ * attention also has the recurrent form for single rows.
+ *
+ * Rows and counts: arrays hold `rows` rows (a capacity, as num_frames *
+ * max_voxels of the voxelisation), and how many of them are in use may be
+ * known to the device alone: `row_count` is a device int64 (e.g.
+ * out_voxel_offsets + num_frames), NULL for all `rows`; attention takes the
+ * sequences' row ranges from device offsets (e.g. out_voxel_offsets).  Rows
+ * in no range are neither read nor written.  A count or offsets that break
+ * the contract are clamped into the arrays, and MMBEV_FAULT_SEQUENCES is ORed
+ * into *fault (device int32, may be NULL; the caller clears it).
+ *
+ * Element types: MMBEV_F32, MMBEV_F16, MMBEV_BF16.  Everything between the
+ * loads and the stores is held in 32 bits (a product on the matrix cores takes
+ * operands of the element type), and results are rounded once, to nearest
+ * even.  Any alignment of the element type and any row stride are taken.
+ *
+ * Ownership, streams and errors as for mmbev_roi_voxelize: caller-owned
+ * buffers, no allocation, work enqueued on `stream` (NULL = default stream)
+ * without waiting; argument errors are returned before anything is enqueued.
+ * Calls may be captured into a HIP graph.  Results do not depend on timing:
+ * every sum has a fixed order for given sizes and counts.
+ */
+#define MMBEV_F32 0
+#define MMBEV_F16 1
+#define MMBEV_BF16 2
+
+/* A matrix of rows: element c of row r is data[r*row_stride + c] (strides in
+ * elements, >= the row's width; inputs are not written). */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+} mmbev_rows_t;
+
+/* Rows of heads: element c of head h of row r is
+ * data[r*row_stride + h*head_stride + c] (head_stride >= the head's width). */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+} mmbev_heads_t;
+
+typedef struct {
+  int64_t rows;         /* >= 0 */
+  int32_t width;        /* C, 1..8192 */
+  int32_t dtype;        /* of x, residual, sum, out, dy, dskip, dx */
+  int32_t weight_dtype; /* of weight and bias: MMBEV_F32 or dtype */
+  float eps;            /* >= 0, finite */
+} mmbev_norm_t;
+
+/*
+ * Layer norm of every row, with the residual sum in front of it:
+ *   s = x + residual, rounded to dtype (x itself without a residual)
+ *   mu = mean(s), rstd = 1 / sqrt(mean((s - mu)^2) + eps)
+ *   out = (s - mu) * rstd * weight + bias
+ * residual, weight (ones), bias (zeros), out_sum, out_mean and out_rstd
+ * (fp32 [rows]) may be NULL (their structs' data NULL).  out and out_sum may
+ * be x's or residual's own rows.  width and eps as above.
+ */
+mmbev_status_t mmbev_layer_norm(const mmbev_norm_t* norm, mmbev_rows_t x, mmbev_rows_t residual, const void* weight,
+                                const void* bias, const int64_t* row_count, mmbev_rows_t out, mmbev_rows_t out_sum,
+                                float* out_mean, float* out_rstd, int32_t* fault, void* stream);
+
+size_t mmbev_layer_norm_backward_workspace_bytes(const mmbev_norm_t* norm);
+
+/*
+ * Its gradients, from s (the rows that were normalised: x, or out_sum) and
+ * the statistics that the forward call wrote:
+ *   h = (s - mean) * rstd, a = dy * weight
+ *   dx = rstd * (a - mean(a) - h * mean(a * h)) + dskip
+ *   dweight = sum over rows of dy * h, dbias = sum over rows of dy   (fp32 [C])
+ * dskip is the gradient that reaches s by another way (the residual
+ * connection past the block); dskip, weight, dweight and dbias may be NULL;
+ * dx may be dy's, s's or dskip's own rows.  The workspace is needed where
+ * dweight or dbias is asked for (256-byte aligned, no initialisation).
+ */
+mmbev_status_t mmbev_layer_norm_backward(const mmbev_norm_t* norm, mmbev_rows_t dy, mmbev_rows_t s,
+                                         const void* weight, const float* mean, const float* rstd, mmbev_rows_t dskip,
+                                         const int64_t* row_count, mmbev_rows_t dx, float* dweight, float* dbias,
+                                         int32_t* fault, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Ladders of mmbev_make_rotary for positions beyond those trained on. */
+#define MMBEV_ROTARY_PLAIN 0  /* frequencies base^(-j/n) */
+#define MMBEV_ROTARY_LINEAR 1 /* positions divided by factor */
+#define MMBEV_ROTARY_BASE 2   /* base * factor^(n/(n-1)): the slowest pair as LINEAR, the fastest as PLAIN */
+#define MMBEV_ROTARY_PARTS 3  /* pairs that turn more than `fast` times in `length` positions as PLAIN, fewer than
+                                 `slow` times as LINEAR, between them mixed in proportion to the turns */
+typedef struct {
+  int32_t rotary_dim; /* elements of a head that are turned: even, 2..1024 */
+  int32_t axes;       /* position columns, 1..8 and at most the pairs */
+  double base;        /* > 1 */
+  int32_t scaling;    /* MMBEV_ROTARY_* */
+  int32_t reserved;   /* 0 */
+  double factor;      /* >= 1 (scaling not PLAIN) */
+  double length;      /* PARTS: positions trained on, > 0 */
+  double slow, fast;  /* PARTS: 0 < slow < fast, turns in `length` */
+} mmbev_rotary_ladder_t;
+
+/*
+ * Host helper: how far each of the rotary_dim/2 pairs turns per position, in
+ * 2^-64 turns, and which position column turns it.  The pairs are shared out
+ * among the axes in order (axis a has pairs [P*a/axes, P*(a+1)/axes)); pair j
+ * of an axis' n has the frequency base^(-j/n) radians per position, scaled
+ * as asked.  out_steps and out_axis hold rotary_dim/2 entries.
+ */
+mmbev_status_t mmbev_make_rotary(const mmbev_rotary_ladder_t* ladder, uint64_t* out_steps, uint8_t* out_axis);
+
+#define MMBEV_ROTARY_HALF 0        /* pair j is elements (j, j + rotary_dim/2) */
+#define MMBEV_ROTARY_INTERLEAVED 1 /* pair j is elements (2j, 2j + 1) */
+typedef struct {
+  int64_t rows;
+  int32_t heads;      /* 1..1024 */
+  int32_t dim;        /* of a head, 1..1024 */
+  int32_t rotary_dim; /* even, 2..dim; the rest of the head is copied */
+  int32_t dtype;
+  int32_t layout;     /* MMBEV_ROTARY_HALF or _INTERLEAVED */
+  int32_t inverse;    /* 0; 1 turns back, which is also the gradient */
+} mmbev_rotary_t;
+
+/*
+ * Rotary positions: pair j = (a, b) of every head of row r becomes
+ *   (a cos t - b sin t, a sin t + b cos t),
+ *   t = 2 pi * (positions[r*position_stride + axis[j]] * steps[j] mod 2^64) / 2^64
+ * The phase is a wrapping integer product, so it has no rounding at any
+ * position; sine and cosine are taken of its top 32 bits.
+ * positions  int32, device, `axes` columns read at position_stride (the voxel
+ *            coordinates are such rows: columns (b, iz, iy, ix), stride 4);
+ *            axis[j] of steps' table must be < axes
+ * steps, axis  device copies of mmbev_make_rotary's arrays
+ * out        may be x's own rows and heads (same strides)
+ */
+mmbev_status_t mmbev_rotary(const mmbev_rotary_t* rotary, mmbev_heads_t x, const int32_t* positions,
+                            int64_t position_stride, int32_t axes, const uint64_t* steps, const uint8_t* axis,
+                            const int64_t* row_count, mmbev_heads_t out, int32_t* fault, void* stream);
+
+typedef struct {
+  int64_t rows;          /* rows that q, k, v and out hold, 0 .. 2^31-1 */
+  int64_t max_length;    /* no sequence is longer (e.g. max_voxels); 0: rows */
+  int32_t num_sequences; /* B, 1..65535 */
+  int32_t heads;         /* of q and out, 1..256 */
+  int32_t kv_heads;      /* of k and v, divides heads: head h reads k and v of head h*kv_heads/heads */
+  int32_t key_dim;       /* 1..128 */
+  int32_t value_dim;     /* 1..128 */
+  int32_t dtype;
+  float scale;           /* finite, not 0 */
+  int32_t reserved;      /* 0 */
+} mmbev_attention_t;
+
+/* Workspace of a forward (backward = 0) or backward call; 0 where the sizes
+ * are invalid, at least 256 otherwise. */
+size_t mmbev_linear_attention_workspace_bytes(const mmbev_attention_t* attention, int32_t backward);
+
+/*
+ * Linear attention with a decay per head.  Sequence b is rows [offsets[b],
+ * offsets[b+1]); within it, for every head h with lambda = exp(log_decay[h]):
+ *   S_t = lambda * S_{t-1} + k_t^T v_t        [key_dim][value_dim], fp32
+ *   out_t = scale * q_t S_t
+ * S_{-1} is initial_state[b][h] (NULL: zeros); final_state[b][h] (may be
+ * NULL) receives the state after the last row (the initial one for an empty
+ * sequence).  The two must not overlap.  log_decay (fp32 [heads]) is at most
+ * 0, -inf included (a larger value counts as 0); it is a constant of the model and
+ * has no gradient.  A sequence with a NaN or infinity in a row has
+ * unspecified outputs; other sequences and heads do not see it.
+ * The state is decayed, summed and carried in fp32 over all of a sequence;
+ * for 16-bit types its product with q takes it rounded to that type, and the
+ * decayed rows enter the state as two parts of the type, 16 bits or more
+ * together.
+ * max_length only sizes the launches: longer sequences are computed too.
+ * out must not overlap an input.
+ */
+mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* attention, mmbev_heads_t q, mmbev_heads_t k,
+                                      mmbev_heads_t v, const float* log_decay, const int64_t* offsets,
+                                      const float* initial_state, mmbev_heads_t out, float* final_state,
+                                      int32_t* fault, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients.  dfinal_state (may be NULL) is the gradient of final_state;
+ * dinitial_state (may be NULL) receives that of initial_state.  dq is like q,
+ * dk and dv like k and v (the sum over the heads that share them, taken in
+ * fp32).  dq, dk and dv must not overlap an input.
+ */
+mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* attention, mmbev_heads_t dout,
+                                               mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,
+                                               const float* log_decay, const int64_t* offsets,
+                                               const float* initial_state, const float* dfinal_state,
+                                               mmbev_heads_t dq, mmbev_heads_t dk, mmbev_heads_t dv,
+                                               float* dinitial_state, int32_t* fault, void* workspace,
+                                               size_t workspace_bytes, void* stream);
+
+/*
+ * One row for each of many streams (attention->rows of them; num_sequences
+ * and max_length are not read): row r updates state[slots[r]] in place and
+ * reads it,
+ *   S = lambda * S + k_r^T v_r;  out_r = scale * q_r S
+ * state   fp32 [num_slots][heads][key_dim][value_dim], 16-byte aligned
+ * slots   device int32 [rows], distinct where >= 0; a negative slot skips
+ *         the row (its out row is not written); NULL: row r has slot r
+ */
+mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* attention, mmbev_heads_t q, mmbev_heads_t k,
+                                           mmbev_heads_t v, const float* log_decay, const int32_t* slots,
+                                           int64_t num_slots, float* state, mmbev_heads_t out, int32_t* fault,
+                                           void* stream);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmmbev.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["api.hip", "stage.hip", "filter.hip", "sort.hip", "voxel.hip", "small_calls.hip", "bev.hip", "cc.hip", "roi_policy.cpp"]
+SOURCES = ["api.hip", "stage.hip", "filter.hip", "sort.hip", "voxel.hip", "small_calls.hip", "bev.hip", "cc.hip", "roi_policy.cpp",
+           "sequence_api.hip", "norm.hip", "rotary.hip", "attention.hip", "attention_f32.hip", "attention_f16.hip",
+           "attention_bf16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -1,0 +1,204 @@
+// The sequence operators of a learned voxel encoder (layer norm, rotary
+// positions, linear attention with decay): what their kernels share, and
+// their host-side launchers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mmbev.h"
+
+namespace mmbev {
+
+// ------------------------------------------------------------- arguments
+
+struct NormArgs {
+  const void* x;         // forward: x; backward: s
+  const void* skip;      // forward: residual; backward: dskip (null: none)
+  const void* dy;        // backward
+  const void* weight;    // null: ones
+  const void* bias;      // null: zeros
+  void* out;             // forward: out; backward: dx
+  void* sum;             // forward: out_sum (null: not written)
+  float* mean;           // backward: read
+  float* rstd;
+  float* partial;        // backward: [grid][2][width] sums of dy*h and dy, or null
+  float* dweight;
+  float* dbias;
+  const int64_t* row_count;
+  int32_t* fault;
+  int64_t rows, x_stride, skip_stride, dy_stride, out_stride, sum_stride;
+  int32_t width;
+  int32_t weight_f32;    // weight and bias are fp32 (else of the rows' type)
+  float eps, inv_width;
+};
+
+hipError_t launch_norm(const NormArgs& a, int32_t dtype, hipStream_t st);
+hipError_t launch_norm_backward(const NormArgs& a, int32_t dtype, hipStream_t st);
+int32_t norm_backward_grid(int64_t rows, int32_t width, int32_t dtype);  // workgroups, hence partial rows
+
+struct RotaryArgs {
+  const void* x;
+  void* out;
+  const int32_t* positions;
+  const uint64_t* steps;
+  const uint8_t* axis;
+  const int64_t* row_count;
+  int32_t* fault;
+  int64_t rows, x_row, x_head, out_row, out_head, position_stride;
+  int32_t heads, dim, rotary_dim, axes;
+  int32_t interleaved, inverse, copy_rest;  // copy_rest: out is not x
+};
+
+hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t st);
+
+// out_i = scale * sum_{j <= i} lambda^(i-j) (a_i . b_j) c_j + lambda^(i+1-late) scale_in a_i . init
+// over each sequence, rows counted from its end if `reversed`.  The forward
+// pass is (q, k, v), the gradients are (dout, v, k) and, reversed and with
+// `late`, (k, q, dout) and (v, dout, q).
+struct AttnArgs {
+  const void *a, *b, *c;
+  void* out;
+  int64_t a_row, a_head, b_row, b_head, c_row, c_head, o_row, o_head;
+  const float* log_decay;
+  const int64_t* offsets;
+  const float* init;      // [B][H][ad][cd], or [B][H][cd][ad] where init_swapped; null: zeros
+  float* final_state;     // [B][H][ad][cd]; null: not written
+  int32_t* fault;
+  int64_t rows;
+  int32_t B, H;
+  int32_t a_div, b_div, c_div;  // head h of the operator is head h / div of the operand
+  int32_t ad, cd;               // dims of a and b, of c and out
+  int32_t reversed;             // 0, 1: also `late`
+  int32_t init_swapped;
+  int32_t out_f32;              // out holds fp32 whatever the type
+  float scale;
+  float init_scale, final_scale;  // the state is carried divided by these
+  // a call whose sequences are cut into segments
+  int32_t segments;             // 0: one workgroup a sequence and head
+  float* seg_state;             // [segments][H][ad][cd]
+  int32_t* seg_fresh;           // [segments] a sequence begins inside the segment
+};
+
+hipError_t launch_attention(const AttnArgs& a, int32_t dtype, hipStream_t st);
+
+struct AttnSumArgs {   // out[r][g] = sum over the group's heads of part[r][g * group + i], fp32 [rows][H][dim]
+  const float* part;
+  void* out;
+  int64_t out_row, out_head, rows;
+  const int64_t* offsets;
+  int32_t B, H, group, dim;
+};
+hipError_t launch_attention_sum(const AttnSumArgs& a, int32_t dtype, hipStream_t st);
+
+struct AttnStepArgs {
+  const void *q, *k, *v;
+  void* out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  const float* log_decay;
+  const int32_t* slots;
+  float* state;
+  int32_t* fault;
+  int64_t rows, num_slots;
+  int32_t H, group, kd, vd;
+  float scale;
+};
+hipError_t launch_attention_step(const AttnStepArgs& a, int32_t dtype, hipStream_t st);
+
+// ------------------------------------------------------------ device code
+
+using f16 = _Float16;
+using bf16 = __bf16;
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+// N elements as they lie in memory, at any alignment of the element: the
+// loads and stores are still as wide as the elements together (gfx950's
+// global accesses take any byte address; an aligned row is faster).
+template <typename T, int N>
+struct Pack {
+  T v[N];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
+  Pack<T, N> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& r) {
+  __builtin_memcpy(p, &r, sizeof(r));
+}
+
+// The first `n` of N elements (n may be outside 0..N), zeros after them.
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_some(const T* p, int n) {
+  if (n >= N) return load_pack<T, N>(p);
+  Pack<T, N> r;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    r.v[e] = (T)0.0f;
+    if (e < n) r.v[e] = p[e];
+  }
+  return r;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_some(T* p, const Pack<T, N>& r, int n) {
+  if (n >= N) {
+    store_pack<T, N>(p, r);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e < n) p[e] = r.v[e];
+}
+
+template <typename T>
+constexpr int kPackOf = 16 / (int)sizeof(T);  // elements of a 16-byte access
+
+__device__ __forceinline__ float dpp_xor_step(float x, int which) {
+  // partner values of a butterfly inside 16 lanes; which is a literal
+  const int i = __builtin_bit_cast(int, x);
+  switch (which) {
+    case 1: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, 0xB1, 0xf, 0xf, true));   // lane ^ 1
+    case 2: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, 0x4E, 0xf, 0xf, true));   // lane ^ 2
+    case 4: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, 0x141, 0xf, 0xf, true));  // mirror of 8
+    default: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, 0x140, 0xf, 0xf, true)); // mirror of 16
+  }
+}
+
+// Sum over groups of LANES neighbouring lanes (a power of two up to 64),
+// known to all of them, in register moves only: quads, mirrored halves of
+// 8 and 16 (all lanes of a mirrored part hold the same sum), swapped rows.
+template <int LANES>
+__device__ __forceinline__ float group_sum(float x) {
+  if constexpr (LANES >= 2) x += dpp_xor_step(x, 1);
+  if constexpr (LANES >= 4) x += dpp_xor_step(x, 2);
+  if constexpr (LANES >= 8) x += dpp_xor_step(x, 4);
+  if constexpr (LANES >= 16) x += dpp_xor_step(x, 8);
+  if constexpr (LANES >= 32) {
+    const unsigned i = __builtin_bit_cast(unsigned, x);
+    const auto p = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    x = __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
+  }
+  if constexpr (LANES >= 64) {
+    const unsigned i = __builtin_bit_cast(unsigned, x);
+    const auto p = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    x = __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
+  }
+  return x;
+}
+
+// Rows in use: the device's count, clamped to the array.
+__device__ __forceinline__ int64_t rows_in_use(const int64_t* row_count, int64_t rows, int32_t* fault) {
+  if (!row_count) return rows;
+  const int64_t n = *row_count;
+  const int64_t use = n < 0 ? 0 : n > rows ? rows : n;
+  if (use != n && fault && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(fault, MMBEV_FAULT_SEQUENCES);
+  return use;
+}
+
+}  // namespace mmbev

@@ -1,0 +1,448 @@
+// C ABI of the sequence operators: argument validation, workspace layout and
+// launches.  No allocation, no host synchronisation, no state between calls.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "sequence.hpp"
+
+using namespace mmbev;
+
+namespace {
+
+constexpr int64_t kMaxRows = INT32_MAX;
+
+int32_t size_of(int32_t dtype) { return dtype == MMBEV_F32 ? 4 : 2; }
+
+bool known_type(int32_t dtype) { return dtype == MMBEV_F32 || dtype == MMBEV_F16 || dtype == MMBEV_BF16; }
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// Rows of `width` elements: there (or, optional, absent), aligned to the element, rows apart.
+bool rows_ok(const mmbev_rows_t& t, int64_t rows, int32_t width, int32_t dtype, bool optional) {
+  if (!t.data) return optional || rows == 0;
+  return aligned(t.data, size_of(dtype)) && (rows <= 1 || t.row_stride >= width) && t.row_stride >= 0 &&
+         t.row_stride < ((int64_t)1 << 40);
+}
+
+bool heads_ok(const mmbev_heads_t& t, int64_t rows, int32_t heads, int32_t dim, int32_t dtype) {
+  if (!t.data) return rows == 0;
+  if (!aligned(t.data, size_of(dtype)) || t.row_stride < 0 || t.head_stride < 0) return false;
+  if (t.row_stride >= ((int64_t)1 << 40) || t.head_stride >= ((int64_t)1 << 40)) return false;
+  if (heads > 1 && t.head_stride < dim) return false;
+  // heads inside a row, or rows inside a head
+  const int64_t row = (int64_t)(heads - 1) * t.head_stride + dim;
+  return rows <= 1 || t.row_stride >= row || (t.row_stride >= dim && t.head_stride >= (rows - 1) * t.row_stride + dim);
+}
+
+// First and past-the-last byte of rows of heads.
+struct Span {
+  uintptr_t lo, hi;
+};
+Span span_of(const mmbev_heads_t& t, int64_t rows, int32_t heads, int32_t dim, int32_t dtype) {
+  if (!t.data || rows == 0) return {0, 0};
+  const uintptr_t lo = (uintptr_t)t.data;
+  const int64_t last = (rows - 1) * t.row_stride + (int64_t)(heads - 1) * t.head_stride + dim;
+  return {lo, lo + (uintptr_t)last * size_of(dtype)};
+}
+bool overlap(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+
+mmbev_status_t norm_ok(const mmbev_norm_t* n) {
+  if (!n || n->rows < 0 || n->width < 1 || !known_type(n->dtype)) return MMBEV_ERR_INVALID_ARG;
+  if (n->weight_dtype != MMBEV_F32 && n->weight_dtype != n->dtype) return MMBEV_ERR_INVALID_ARG;
+  if (!(n->eps >= 0.0f) || !std::isfinite(n->eps)) return MMBEV_ERR_INVALID_ARG;
+  if (n->rows > kMaxRows || n->width > 8192) return MMBEV_ERR_UNSUPPORTED;
+  return MMBEV_OK;
+}
+
+NormArgs norm_args(const mmbev_norm_t* n, const int64_t* row_count, int32_t* fault) {
+  NormArgs a{};
+  a.rows = n->rows;
+  a.width = n->width;
+  a.weight_f32 = n->weight_dtype == MMBEV_F32;
+  a.eps = n->eps;
+  a.inv_width = (float)(1.0 / n->width);
+  a.row_count = row_count;
+  a.fault = fault;
+  return a;
+}
+
+mmbev_status_t status_of(hipError_t e) { return e == hipSuccess ? MMBEV_OK : MMBEV_ERR_HIP; }
+
+// ------------------------------------------------------------ attention
+
+// Workgroups that fill the chip: a sequence and head each where there are
+// enough of those; otherwise the rows in use are cut into as many segments as
+// make about this many with the heads.
+constexpr int64_t kAttnUnits = 768;
+// Sequences no longer than this are walked whole: cutting them would take
+// two more launches than it saves.
+constexpr int64_t kAttnWhole = 512;
+
+struct AttnPlan {
+  int32_t segments;
+  size_t off_fresh, off_state, off_part, total;
+};
+
+mmbev_status_t attention_ok(const mmbev_attention_t* t, bool step) {
+  if (!t || t->rows < 0 || t->reserved != 0 || !known_type(t->dtype)) return MMBEV_ERR_INVALID_ARG;
+  if (t->heads < 1 || t->kv_heads < 1 || t->heads % t->kv_heads != 0) return MMBEV_ERR_INVALID_ARG;
+  if (t->key_dim < 1 || t->value_dim < 1) return MMBEV_ERR_INVALID_ARG;
+  if (!std::isfinite(t->scale) || t->scale == 0.0f) return MMBEV_ERR_INVALID_ARG;
+  if (!step && (t->num_sequences < 1 || t->num_sequences > 65535 || t->max_length < 0)) return MMBEV_ERR_INVALID_ARG;
+  if (t->rows > kMaxRows || t->heads > 256 || t->key_dim > 128 || t->value_dim > 128) return MMBEV_ERR_UNSUPPORTED;
+  if (step && t->rows * t->heads > kMaxRows) return MMBEV_ERR_UNSUPPORTED;
+  return MMBEV_OK;
+}
+
+AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
+  AttnPlan p{};
+  const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
+  const int64_t units = (int64_t)t->num_sequences * t->heads;
+  if (units < kAttnUnits && longest > kAttnWhole)
+    p.segments = (int32_t)std::max<int64_t>(1, std::min((kAttnUnits + t->heads - 1) / t->heads, (t->rows + 63) / 64));
+  size_t at = 0;
+  p.off_fresh = at;
+  at = align256(at + (size_t)p.segments * 4);
+  p.off_state = at;
+  at = align256(at + (size_t)p.segments * t->heads * t->key_dim * t->value_dim * 4);
+  p.off_part = at;
+  if (backward && t->heads != t->kv_heads)
+    at = align256(at + (size_t)t->rows * t->heads * std::max(t->key_dim, t->value_dim) * 4);
+  p.total = std::max<size_t>(at, 256);
+  return p;
+}
+
+AttnArgs attention_args(const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, const AttnPlan& p, char* ws) {
+  AttnArgs a{};
+  a.log_decay = log_decay;
+  a.offsets = offsets;
+  a.rows = t->rows;
+  a.B = t->num_sequences;
+  a.H = t->heads;
+  a.scale = t->scale;
+  a.init_scale = a.final_scale = 1.0f;
+  a.segments = p.segments;
+  a.seg_fresh = (int32_t*)(ws + p.off_fresh);
+  a.seg_state = (float*)(ws + p.off_state);
+  return a;
+}
+
+void put(const mmbev_heads_t& t, int32_t div, const void** data, int64_t* row, int64_t* head, int32_t* out_div) {
+  *data = t.data;
+  *row = t.row_stride;
+  *head = t.head_stride;
+  *out_div = div;
+}
+
+bool workspace_ok(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, 256) && bytes >= need; }
+
+}  // namespace
+
+extern "C" {
+
+mmbev_status_t mmbev_layer_norm(const mmbev_norm_t* norm, mmbev_rows_t x, mmbev_rows_t residual, const void* weight,
+                                const void* bias, const int64_t* row_count, mmbev_rows_t out, mmbev_rows_t out_sum,
+                                float* out_mean, float* out_rstd, int32_t* fault, void* stream) {
+  const mmbev_status_t st = norm_ok(norm);
+  if (st != MMBEV_OK) return st;
+  const int64_t R = norm->rows;
+  const int32_t C = norm->width, T = norm->dtype;
+  if (!rows_ok(x, R, C, T, false) || !rows_ok(residual, R, C, T, true) || !rows_ok(out, R, C, T, false) ||
+      !rows_ok(out_sum, R, C, T, true))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!aligned(weight, size_of(norm->weight_dtype)) || !aligned(bias, size_of(norm->weight_dtype))) return MMBEV_ERR_INVALID_ARG;
+  NormArgs a = norm_args(norm, row_count, fault);
+  a.x = x.data;
+  a.x_stride = x.row_stride;
+  a.skip = residual.data;
+  a.skip_stride = residual.row_stride;
+  a.weight = weight;
+  a.bias = bias;
+  a.out = out.data;
+  a.out_stride = out.row_stride;
+  a.sum = out_sum.data;
+  a.sum_stride = out_sum.row_stride;
+  a.mean = out_mean;
+  a.rstd = out_rstd;
+  return status_of(launch_norm(a, T, (hipStream_t)stream));
+}
+
+size_t mmbev_layer_norm_backward_workspace_bytes(const mmbev_norm_t* norm) {
+  if (norm_ok(norm) != MMBEV_OK) return 0;
+  return align256((size_t)norm_backward_grid(norm->rows, norm->width, norm->dtype) * 2 * norm->width * 4);
+}
+
+mmbev_status_t mmbev_layer_norm_backward(const mmbev_norm_t* norm, mmbev_rows_t dy, mmbev_rows_t s,
+                                         const void* weight, const float* mean, const float* rstd, mmbev_rows_t dskip,
+                                         const int64_t* row_count, mmbev_rows_t dx, float* dweight, float* dbias,
+                                         int32_t* fault, void* workspace, size_t workspace_bytes, void* stream) {
+  const mmbev_status_t st = norm_ok(norm);
+  if (st != MMBEV_OK) return st;
+  const int64_t R = norm->rows;
+  const int32_t C = norm->width, T = norm->dtype;
+  if (!rows_ok(dy, R, C, T, false) || !rows_ok(s, R, C, T, false) || !rows_ok(dskip, R, C, T, true) ||
+      !rows_ok(dx, R, C, T, false))
+    return MMBEV_ERR_INVALID_ARG;
+  if (R > 0 && (!mean || !rstd)) return MMBEV_ERR_INVALID_ARG;
+  if (!aligned(weight, size_of(norm->weight_dtype))) return MMBEV_ERR_INVALID_ARG;
+  const bool sums = dweight || dbias;
+  if (sums && !workspace_ok(workspace, workspace_bytes, mmbev_layer_norm_backward_workspace_bytes(norm)))
+    return MMBEV_ERR_WORKSPACE;
+  NormArgs a = norm_args(norm, row_count, fault);
+  a.x = s.data;
+  a.x_stride = s.row_stride;
+  a.dy = dy.data;
+  a.dy_stride = dy.row_stride;
+  a.skip = dskip.data;
+  a.skip_stride = dskip.row_stride;
+  a.weight = weight;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.out = dx.data;
+  a.out_stride = dx.row_stride;
+  a.partial = sums ? (float*)workspace : nullptr;
+  a.dweight = dweight;
+  a.dbias = dbias;
+  return status_of(launch_norm_backward(a, T, (hipStream_t)stream));
+}
+
+mmbev_status_t mmbev_make_rotary(const mmbev_rotary_ladder_t* t, uint64_t* out_steps, uint8_t* out_axis) {
+  if (!t || !out_steps || !out_axis || t->reserved != 0) return MMBEV_ERR_INVALID_ARG;
+  if (t->rotary_dim < 2 || t->rotary_dim > 1024 || t->rotary_dim % 2 != 0) return MMBEV_ERR_INVALID_ARG;
+  const int32_t P = t->rotary_dim / 2;
+  if (t->axes < 1 || t->axes > 8 || t->axes > P) return MMBEV_ERR_INVALID_ARG;
+  if (!(t->base > 1.0) || !std::isfinite(t->base)) return MMBEV_ERR_INVALID_ARG;
+  if (t->scaling < MMBEV_ROTARY_PLAIN || t->scaling > MMBEV_ROTARY_PARTS) return MMBEV_ERR_INVALID_ARG;
+  if (t->scaling != MMBEV_ROTARY_PLAIN && (!(t->factor >= 1.0) || !std::isfinite(t->factor))) return MMBEV_ERR_INVALID_ARG;
+  if (t->scaling == MMBEV_ROTARY_PARTS &&
+      (!(t->length > 0.0) || !std::isfinite(t->length) || !(t->slow > 0.0) || !(t->fast > t->slow) || !std::isfinite(t->fast)))
+    return MMBEV_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int32_t a = 0; a < t->axes; ++a) {
+    const int32_t first = P * a / t->axes, n = P * (a + 1) / t->axes - first;
+    for (int32_t j = 0; j < n; ++j) {
+      double base = t->base;
+      if (t->scaling == MMBEV_ROTARY_BASE && n > 1) base *= std::pow(t->factor, (double)n / (n - 1));
+      double turns = std::pow(base, -(double)j / n) / two_pi;
+      if (t->scaling == MMBEV_ROTARY_LINEAR) turns /= t->factor;
+      if (t->scaling == MMBEV_ROTARY_PARTS) {
+        const double share = std::min(1.0, std::max(0.0, (turns * t->length - t->slow) / (t->fast - t->slow)));
+        turns = share * turns + (1.0 - share) * turns / t->factor;
+      }
+      // at most 1 / (2 pi) of a turn, so the product fits; the double's 53 bits are exact in it
+      out_steps[first + j] = (uint64_t)std::ldexp(turns, 64);
+      out_axis[first + j] = (uint8_t)a;
+    }
+  }
+  return MMBEV_OK;
+}
+
+mmbev_status_t mmbev_rotary(const mmbev_rotary_t* t, mmbev_heads_t x, const int32_t* positions, int64_t position_stride,
+                            int32_t axes, const uint64_t* steps, const uint8_t* axis, const int64_t* row_count,
+                            mmbev_heads_t out, int32_t* fault, void* stream) {
+  if (!t || t->rows < 0 || t->heads < 1 || t->dim < 1 || !known_type(t->dtype)) return MMBEV_ERR_INVALID_ARG;
+  if (t->rotary_dim < 2 || t->rotary_dim % 2 != 0 || t->rotary_dim > t->dim) return MMBEV_ERR_INVALID_ARG;
+  if (t->layout != MMBEV_ROTARY_HALF && t->layout != MMBEV_ROTARY_INTERLEAVED) return MMBEV_ERR_INVALID_ARG;
+  if (t->inverse != 0 && t->inverse != 1) return MMBEV_ERR_INVALID_ARG;
+  if (axes < 1 || axes > 8) return MMBEV_ERR_INVALID_ARG;
+  if (t->rows > kMaxRows || t->heads > 1024 || t->dim > 1024) return MMBEV_ERR_UNSUPPORTED;
+  if (!heads_ok(x, t->rows, t->heads, t->dim, t->dtype) || !heads_ok(out, t->rows, t->heads, t->dim, t->dtype))
+    return MMBEV_ERR_INVALID_ARG;
+  if (t->rows > 0 && (!positions || !aligned(positions, 4) || !steps || !aligned(steps, 8) || !axis)) return MMBEV_ERR_INVALID_ARG;
+  if (position_stride < 0 || (t->rows > 1 && position_stride < axes) || position_stride >= ((int64_t)1 << 40))
+    return MMBEV_ERR_INVALID_ARG;
+  const bool same = x.data == out.data && x.row_stride == out.row_stride && x.head_stride == out.head_stride;
+  if (!same && overlap(span_of(x, t->rows, t->heads, t->dim, t->dtype), span_of(out, t->rows, t->heads, t->dim, t->dtype)) &&
+      x.data == out.data)
+    return MMBEV_ERR_INVALID_ARG;
+  RotaryArgs a{};
+  a.x = x.data;
+  a.out = out.data;
+  a.positions = positions;
+  a.steps = steps;
+  a.axis = axis;
+  a.row_count = row_count;
+  a.fault = fault;
+  a.rows = t->rows;
+  a.x_row = x.row_stride;
+  a.x_head = x.head_stride;
+  a.out_row = out.row_stride;
+  a.out_head = out.head_stride;
+  a.position_stride = position_stride;
+  a.heads = t->heads;
+  a.dim = t->dim;
+  a.rotary_dim = t->rotary_dim;
+  a.axes = axes;
+  a.interleaved = t->layout == MMBEV_ROTARY_INTERLEAVED;
+  a.inverse = t->inverse;
+  a.copy_rest = !same;
+  return status_of(launch_rotary(a, t->dtype, (hipStream_t)stream));
+}
+
+size_t mmbev_linear_attention_workspace_bytes(const mmbev_attention_t* attention, int32_t backward) {
+  if (attention_ok(attention, false) != MMBEV_OK) return 0;
+  return attention_plan(attention, backward != 0).total;
+}
+
+mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,
+                                      const float* log_decay, const int64_t* offsets, const float* initial_state,
+                                      mmbev_heads_t out, float* final_state, int32_t* fault, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  const mmbev_status_t st = attention_ok(t, false);
+  if (st != MMBEV_OK) return st;
+  if (!heads_ok(q, t->rows, t->heads, t->key_dim, t->dtype) || !heads_ok(k, t->rows, t->kv_heads, t->key_dim, t->dtype) ||
+      !heads_ok(v, t->rows, t->kv_heads, t->value_dim, t->dtype) || !heads_ok(out, t->rows, t->heads, t->value_dim, t->dtype))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!log_decay || !aligned(log_decay, 4) || !offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) ||
+      !aligned(final_state, 4))
+    return MMBEV_ERR_INVALID_ARG;
+  const size_t state = (size_t)t->num_sequences * t->heads * t->key_dim * t->value_dim * 4;
+  if (initial_state && final_state &&
+      overlap({(uintptr_t)initial_state, (uintptr_t)initial_state + state}, {(uintptr_t)final_state, (uintptr_t)final_state + state}))
+    return MMBEV_ERR_INVALID_ARG;
+  for (const void* in : {q.data, k.data, v.data})
+    if (in && in == out.data) return MMBEV_ERR_INVALID_ARG;
+  const AttnPlan p = attention_plan(t, false);
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
+  AttnArgs a = attention_args(t, log_decay, offsets, p, (char*)workspace);
+  const int32_t group = t->heads / t->kv_heads;
+  put(q, 1, &a.a, &a.a_row, &a.a_head, &a.a_div);
+  put(k, group, &a.b, &a.b_row, &a.b_head, &a.b_div);
+  put(v, group, &a.c, &a.c_row, &a.c_head, &a.c_div);
+  a.ad = t->key_dim;
+  a.cd = t->value_dim;
+  a.out = out.data;
+  a.o_row = out.row_stride;
+  a.o_head = out.head_stride;
+  a.init = initial_state;
+  a.final_state = final_state;
+  a.fault = fault;
+  return status_of(launch_attention(a, t->dtype, (hipStream_t)stream));
+}
+
+mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev_heads_t dout, mmbev_heads_t q,
+                                               mmbev_heads_t k, mmbev_heads_t v, const float* log_decay,
+                                               const int64_t* offsets, const float* initial_state,
+                                               const float* dfinal_state, mmbev_heads_t dq, mmbev_heads_t dk,
+                                               mmbev_heads_t dv, float* dinitial_state, int32_t* fault, void* workspace,
+                                               size_t workspace_bytes, void* stream) {
+  const mmbev_status_t ok = attention_ok(t, false);
+  if (ok != MMBEV_OK) return ok;
+  const int32_t T = t->dtype, H = t->heads, K = t->kv_heads, group = H / K;
+  const int64_t R = t->rows;
+  if (!heads_ok(dout, R, H, t->value_dim, T) || !heads_ok(q, R, H, t->key_dim, T) || !heads_ok(k, R, K, t->key_dim, T) ||
+      !heads_ok(v, R, K, t->value_dim, T) || !heads_ok(dq, R, H, t->key_dim, T) || !heads_ok(dk, R, K, t->key_dim, T) ||
+      !heads_ok(dv, R, K, t->value_dim, T))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!log_decay || !aligned(log_decay, 4) || !offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) ||
+      !aligned(dfinal_state, 4) || !aligned(dinitial_state, 4))
+    return MMBEV_ERR_INVALID_ARG;
+  const size_t state = (size_t)t->num_sequences * H * t->key_dim * t->value_dim * 4;
+  const Span di = {(uintptr_t)dinitial_state, (uintptr_t)dinitial_state + (dinitial_state ? state : 0)};
+  for (const float* in : {initial_state, dfinal_state})
+    if (in && dinitial_state && overlap(di, {(uintptr_t)in, (uintptr_t)in + state})) return MMBEV_ERR_INVALID_ARG;
+  for (const void* to : {dq.data, dk.data, dv.data})
+    for (const void* in : {dout.data, q.data, k.data, v.data})
+      if (in && in == to) return MMBEV_ERR_INVALID_ARG;
+  const AttnPlan p = attention_plan(t, true);
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  hipStream_t st = (hipStream_t)stream;
+
+  // dq: the forward walk of (dout, v, k), whose state is the transposed one
+  AttnArgs a = attention_args(t, log_decay, offsets, p, ws);
+  put(dout, 1, &a.a, &a.a_row, &a.a_head, &a.a_div);
+  put(v, group, &a.b, &a.b_row, &a.b_head, &a.b_div);
+  put(k, group, &a.c, &a.c_row, &a.c_head, &a.c_div);
+  a.ad = t->value_dim;
+  a.cd = t->key_dim;
+  a.init = initial_state;
+  a.init_swapped = 1;
+  a.out = dq.data;
+  a.o_row = dq.row_stride;
+  a.o_head = dq.head_stride;
+  a.fault = fault;
+  if (launch_attention(a, T, st) != hipSuccess) return MMBEV_ERR_HIP;
+
+  // dv and dk: backwards, the carried state that of q and dout, divided by scale
+  for (int which = 0; which < 2; ++which) {
+    const mmbev_heads_t& to = which ? dk : dv;
+    a = attention_args(t, log_decay, offsets, p, ws);
+    a.reversed = 1;
+    put(which ? v : k, group, &a.a, &a.a_row, &a.a_head, &a.a_div);
+    put(which ? dout : q, 1, &a.b, &a.b_row, &a.b_head, &a.b_div);
+    put(which ? q : dout, 1, &a.c, &a.c_row, &a.c_head, &a.c_div);
+    a.ad = which ? t->value_dim : t->key_dim;
+    a.cd = which ? t->key_dim : t->value_dim;
+    a.init = dfinal_state;
+    a.init_swapped = which;
+    a.init_scale = 1.0f / t->scale;
+    a.final_scale = t->scale;
+    a.final_state = which ? nullptr : dinitial_state;
+    if (group == 1) {
+      a.out = to.data;
+      a.o_row = to.row_stride;
+      a.o_head = to.head_stride;
+    } else {
+      a.out = ws + p.off_part;
+      a.o_row = (int64_t)H * a.cd;
+      a.o_head = a.cd;
+      a.out_f32 = 1;
+    }
+    if (launch_attention(a, T, st) != hipSuccess) return MMBEV_ERR_HIP;
+    if (group > 1 && R > 0) {
+      AttnSumArgs s{};
+      s.part = (const float*)(ws + p.off_part);
+      s.out = to.data;
+      s.out_row = to.row_stride;
+      s.out_head = to.head_stride;
+      s.rows = R;
+      s.offsets = offsets;
+      s.B = t->num_sequences;
+      s.H = H;
+      s.group = group;
+      s.dim = a.cd;
+      if (launch_attention_sum(s, T, st) != hipSuccess) return MMBEV_ERR_HIP;
+    }
+  }
+  return MMBEV_OK;
+}
+
+mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* t, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,
+                                           const float* log_decay, const int32_t* slots, int64_t num_slots, float* state,
+                                           mmbev_heads_t out, int32_t* fault, void* stream) {
+  const mmbev_status_t ok = attention_ok(t, true);
+  if (ok != MMBEV_OK) return ok;
+  if (!heads_ok(q, t->rows, t->heads, t->key_dim, t->dtype) || !heads_ok(k, t->rows, t->kv_heads, t->key_dim, t->dtype) ||
+      !heads_ok(v, t->rows, t->kv_heads, t->value_dim, t->dtype) || !heads_ok(out, t->rows, t->heads, t->value_dim, t->dtype))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!log_decay || !aligned(log_decay, 4) || !aligned(slots, 4) || num_slots < 0) return MMBEV_ERR_INVALID_ARG;
+  if (num_slots > kMaxRows) return MMBEV_ERR_UNSUPPORTED;
+  if (t->rows > 0 && num_slots > 0 && (!state || !aligned(state, 16))) return MMBEV_ERR_INVALID_ARG;
+  if (!slots && num_slots < t->rows) return MMBEV_ERR_INVALID_ARG;
+  AttnStepArgs a{};
+  int32_t unused;
+  put(q, 1, &a.q, &a.q_row, &a.q_head, &unused);
+  put(k, 1, &a.k, &a.k_row, &a.k_head, &unused);
+  put(v, 1, &a.v, &a.v_row, &a.v_head, &unused);
+  a.out = out.data;
+  a.o_row = out.row_stride;
+  a.o_head = out.head_stride;
+  a.log_decay = log_decay;
+  a.slots = slots;
+  a.num_slots = num_slots;
+  a.state = state;
+  a.fault = fault;
+  a.rows = t->rows;
+  a.H = t->heads;
+  a.group = t->heads / t->kv_heads;
+  a.kd = t->key_dim;
+  a.vd = t->value_dim;
+  a.scale = t->scale;
+  return status_of(launch_attention_step(a, t->dtype, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmmbev.so")
 
 OK, ERR_INVALID_ARG, ERR_WORKSPACE, ERR_UNSUPPORTED, ERR_HIP = 0, -1, -2, -3, -4
-FAULT_POINT_OFFSETS, FAULT_ROI_OFFSETS, FAULT_INTERNAL, FAULT_VOXELS = 1, 2, 4, 8
+FAULT_POINT_OFFSETS, FAULT_ROI_OFFSETS, FAULT_INTERNAL, FAULT_VOXELS, FAULT_SEQUENCES = 1, 2, 4, 8, 16
 
 ROI_DTYPE = np.dtype([("cx", "<f4"), ("cy", "<f4"), ("cos_yaw", "<f4"), ("sin_yaw", "<f4"),
                       ("ext_x", "<f4"), ("ext_y", "<f4"), ("reserved0", "<f4"), ("reserved1", "<f4")])
@@ -45,6 +45,38 @@ class mmbev_options_t(ctypes.Structure):
 class mmbev_cluster_params_t(ctypes.Structure):
     _fields_ = [("z_min", ctypes.c_int32), ("z_max", ctypes.c_int32), ("cell_shift", ctypes.c_int32),
                 ("connectivity", ctypes.c_int32), ("min_cells", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class mmbev_rows_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class mmbev_heads_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class mmbev_norm_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class mmbev_rotary_ladder_t(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32), ("base", ctypes.c_double),
+                ("scaling", ctypes.c_int32), ("reserved", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("length", ctypes.c_double), ("slow", ctypes.c_double), ("fast", ctypes.c_double)]
+
+
+class mmbev_rotary_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("inverse", ctypes.c_int32)]
+
+
+class mmbev_attention_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("max_length", ctypes.c_int64), ("num_sequences", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("key_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
 
 
 CLUSTER_DTYPE = np.dtype([("frame", "<i4"), ("root", "<i4"), ("cells", "<i4"), ("voxels", "<i4"), ("points", "<i4"),
@@ -130,6 +162,28 @@ def load() -> ctypes.CDLL:
         L.mmbev_voxel_clusters.restype = ctypes.c_int32
         L.mmbev_build_rois.argtypes = [p, p, ctypes.c_int32, p, ctypes.POINTER(mmbev_policy_t), p, p, p, p, p]
         L.mmbev_build_rois.restype = ctypes.c_int32
+        rows, heads = mmbev_rows_t, mmbev_heads_t
+        size, i32, i64 = ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
+        norm, attention = ctypes.POINTER(mmbev_norm_t), ctypes.POINTER(mmbev_attention_t)
+        L.mmbev_layer_norm.argtypes = [norm, rows, rows, p, p, p, rows, rows, p, p, p, p]
+        L.mmbev_layer_norm.restype = i32
+        L.mmbev_layer_norm_backward_workspace_bytes.argtypes = [norm]
+        L.mmbev_layer_norm_backward_workspace_bytes.restype = size
+        L.mmbev_layer_norm_backward.argtypes = [norm, rows, rows, p, p, p, rows, p, rows, p, p, p, p, size, p]
+        L.mmbev_layer_norm_backward.restype = i32
+        L.mmbev_make_rotary.argtypes = [ctypes.POINTER(mmbev_rotary_ladder_t), p, p]
+        L.mmbev_make_rotary.restype = i32
+        L.mmbev_rotary.argtypes = [ctypes.POINTER(mmbev_rotary_t), heads, p, i64, i32, p, p, p, heads, p, p]
+        L.mmbev_rotary.restype = i32
+        L.mmbev_linear_attention_workspace_bytes.argtypes = [attention, i32]
+        L.mmbev_linear_attention_workspace_bytes.restype = size
+        L.mmbev_linear_attention.argtypes = [attention, heads, heads, heads, p, p, p, heads, p, p, p, size, p]
+        L.mmbev_linear_attention.restype = i32
+        L.mmbev_linear_attention_backward.argtypes = [attention, heads, heads, heads, heads, p, p, p, p, heads, heads, heads,
+                                                      p, p, p, size, p]
+        L.mmbev_linear_attention_backward.restype = i32
+        L.mmbev_linear_attention_step.argtypes = [attention, heads, heads, heads, p, p, i64, p, heads, p, p]
+        L.mmbev_linear_attention_step.restype = i32
         _lib = L
     return _lib
 
@@ -451,3 +505,295 @@ def roi_voxelize_workload(wl, device) -> dict:
     vz = voxelizer_for_workload(wl, device)
     vz.run()
     return vz.result()
+
+
+# ------------------------------------------------- sequence operators of a learned voxel encoder
+#
+# Rows are torch tensors on the current device, of float32, float16 or bfloat16, elements of a row (of a head) next to
+# each other and any stride between rows.  Outputs and workspaces that are not given are allocated for the stream that
+# the call is enqueued on.
+
+F32, F16, BF16 = 0, 1, 2
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+_DTYPE_CODES: dict = {}
+
+
+def _dtype_code(t) -> int:
+    if not _DTYPE_CODES:
+        import torch
+
+        _DTYPE_CODES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise MmbevError(f"float32, float16 or bfloat16 rows are needed, not {t.dtype}")
+    return code
+
+
+def _like(name, t, dtype, shape):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise MmbevError(f"{name} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+    return t
+
+
+def _rows(name, t) -> mmbev_rows_t:
+    if t is None:
+        return mmbev_rows_t(None, 0)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1 and t.numel()):
+        raise MmbevError(f"{name} must be [rows][width] with the elements of a row next to each other")
+    return mmbev_rows_t(_ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _heads(name, t) -> mmbev_heads_t:
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1 and t.numel()):
+        raise MmbevError(f"{name} must be [rows][heads][dim] with the elements of a head next to each other")
+    head = t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return mmbev_heads_t(_ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1] * head, head)
+
+
+def _vector(name, t, dtype, n):
+    """The data pointer of a contiguous tensor of at least n elements (None: no tensor)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise MmbevError(f"{name} must be contiguous, {dtype}, with {n} elements or more")
+    return _ptr(t)
+
+
+def _on_device(*tensors) -> None:
+    import torch
+
+    current = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    for t in tensors:
+        if t is not None and t.device.type != "cuda":
+            raise MmbevError(f"a tensor on the GPU is needed, not one on {t.device}")
+        if t is not None and t.device.index != current:
+            raise MmbevError(f"tensor on {t.device}, current device cuda:{current}")
+
+
+def _empty(stream, shape, dtype, device):
+    """Memory that the allocator knows to be used on `stream`."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(given, nbytes, stream, device):
+    import torch
+
+    if given is None:
+        given = _empty(stream, (nbytes,), torch.uint8, device)
+    return given, given.numel() * given.element_size()
+
+
+def _norm_of(x, weight, bias, eps) -> mmbev_norm_t:
+    code = _dtype_code(x)
+    wcode = F32
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            continue
+        _vector(name, t, t.dtype, x.shape[1])
+        if t.numel() != x.shape[1]:
+            raise MmbevError(f"{name} must have {x.shape[1]} elements")
+        wcode = _dtype_code(t)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise MmbevError("weight and bias must have one type")
+    return mmbev_norm_t(x.shape[0], x.shape[1], code, wcode, float(eps))
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stats: bool = False, row_count=None, out=None,
+               out_sum=None, fault=None, stream=None):
+    """Enqueue mmbev_layer_norm: x [rows][width], weight and bias [width] (float32 or x's type).
+
+    Returns (out, sum, mean, rstd): sum is x + residual (x itself without a residual), the rows that the backward pass
+    needs; mean and rstd (float32 [rows]) are None unless `stats`.  row_count: int64 device tensor of one element, the
+    rows in use (others keep what out holds).
+    """
+    import torch
+
+    _on_device(x, weight, bias, residual, row_count, out, out_sum, fault)
+    rows = _rows("x", x)
+    desc = _norm_of(x, weight, bias, eps)
+    if residual is not None:
+        _like("residual", residual, x.dtype, x.shape)
+    out = _empty(stream, x.shape, x.dtype, x.device) if out is None else _like("out", out, x.dtype, x.shape)
+    if residual is not None and out_sum is None:
+        out_sum = _empty(stream, x.shape, x.dtype, x.device)
+    elif out_sum is not None:
+        _like("out_sum", out_sum, x.dtype, x.shape)
+    mean = rstd = None
+    if stats:
+        mean, rstd = (_empty(stream, (x.shape[0],), torch.float32, x.device) for _ in range(2))
+    _check(load().mmbev_layer_norm(ctypes.byref(desc), rows, _rows("residual", residual), _ptr_of(weight), _ptr_of(bias),
+                                   _vector("row_count", row_count, torch.int64, 1), _rows("out", out),
+                                   _rows("out_sum", out_sum), _ptr_of(mean), _ptr_of(rstd),
+                                   _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_layer_norm")
+    return out, (x if out_sum is None else out_sum), mean, rstd
+
+
+def _ptr_of(t) -> int | None:
+    return None if t is None else _ptr(t)
+
+
+def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, dx=None, dweight=None, dbias=None,
+                        weight_grads: bool = True, fault=None, workspace=None, stream=None):
+    """Enqueue mmbev_layer_norm_backward: the gradients of layer_norm from s (its second result) and its statistics.
+
+    dskip: the gradient that reaches s past the norm, added to dx.  Returns (dx, dweight, dbias), the last two float32
+    [width], None without `weight_grads`.
+    """
+    import torch
+
+    _on_device(dy, s, weight, mean, rstd, dskip, row_count, dx, dweight, dbias, fault, workspace)
+    desc = _norm_of(s, weight, None, 0.0)
+    _like("dy", dy, s.dtype, s.shape)
+    if dskip is not None:
+        _like("dskip", dskip, s.dtype, s.shape)
+    dx = _empty(stream, s.shape, s.dtype, s.device) if dx is None else _like("dx", dx, s.dtype, s.shape)
+    nbytes = 0
+    if weight_grads:
+        if dweight is None:
+            dweight = _empty(stream, (s.shape[1],), torch.float32, s.device)
+        if dbias is None:
+            dbias = _empty(stream, (s.shape[1],), torch.float32, s.device)
+        workspace, nbytes = _workspace(workspace, int(load().mmbev_layer_norm_backward_workspace_bytes(ctypes.byref(desc))),
+                                       stream, s.device)
+    else:
+        workspace = dweight = dbias = None
+    _check(load().mmbev_layer_norm_backward(
+        ctypes.byref(desc), _rows("dy", dy), _rows("s", s), _ptr_of(weight), _vector("mean", mean, torch.float32, s.shape[0]),
+        _vector("rstd", rstd, torch.float32, s.shape[0]), _rows("dskip", dskip),
+        _vector("row_count", row_count, torch.int64, 1), _rows("dx", dx),
+        _vector("dweight", dweight, torch.float32, s.shape[1]), _vector("dbias", dbias, torch.float32, s.shape[1]),
+        _vector("fault", fault, torch.int32, 1), _ptr_of(workspace), nbytes, _stream(stream)), "mmbev_layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def make_rotary(rotary_dim: int, axes: int = 1, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                length: float = 0.0, slow: float = 1.0, fast: float = 32.0):
+    """mmbev_make_rotary: (steps int64 [rotary_dim/2], the 2^-64 turns per position as bit patterns; axis uint8)."""
+    ladder = mmbev_rotary_ladder_t(int(rotary_dim), int(axes), float(base), ROTARY_SCALINGS[scaling], 0, float(factor),
+                                   float(length), float(slow), float(fast))
+    pairs = max(int(rotary_dim) // 2, 1)
+    steps, axis = np.zeros(pairs, dtype=np.uint64), np.zeros(pairs, dtype=np.uint8)
+    _check(load().mmbev_make_rotary(ctypes.byref(ladder), steps.ctypes.data, axis.ctypes.data), "mmbev_make_rotary")
+    return steps.view(np.int64), axis
+
+
+def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = False, row_count=None, out=None, fault=None,
+           stream=None):
+    """Enqueue mmbev_rotary: x [rows][heads][dim]; positions int32 [rows] or [rows][axes] (a view of the voxeliser's
+    coordinates will do: coords[:, 1:]); steps, axis: make_rotary's arrays on the GPU.  Returns out (may be x)."""
+    import torch
+
+    _on_device(x, positions, steps, axis, row_count, out, fault)
+    if positions.dtype != torch.int32 or positions.shape[0] != x.shape[0] or positions.dim() > 2 or \
+            (positions.dim() == 2 and positions.shape[1] > 1 and positions.stride(1) != 1):
+        raise MmbevError("positions must be int32 [rows] or [rows][axes], a row's columns next to each other")
+    axes = positions.shape[1] if positions.dim() == 2 else 1
+    pairs = steps.numel()
+    xs = _heads("x", x)
+    out = _empty(stream, x.shape, x.dtype, x.device) if out is None else _like("out", out, x.dtype, x.shape)
+    desc = mmbev_rotary_t(x.shape[0], x.shape[1], x.shape[2], 2 * pairs, _dtype_code(x), ROTARY_LAYOUTS[layout],
+                          1 if inverse else 0)
+    _check(load().mmbev_rotary(ctypes.byref(desc), xs, _ptr(positions), positions.stride(0) if x.shape[0] > 1 else axes, axes,
+                               _vector("steps", steps, torch.int64, pairs), _vector("axis", axis, torch.uint8, pairs),
+                               _vector("row_count", row_count, torch.int64, 1), _heads("out", out),
+                               _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_rotary")
+    return out
+
+
+def _attention_of(q, k, v, num_sequences, scale, max_length) -> mmbev_attention_t:
+    rows, heads, key_dim = q.shape
+    if k.shape[0] != rows or v.shape[:2] != k.shape[:2] or k.shape[2] != key_dim or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise MmbevError("k must be [rows][kv_heads][key_dim] and v [rows][kv_heads][value_dim] of q's type and rows")
+    return mmbev_attention_t(rows, int(max_length or 0), num_sequences, heads, k.shape[1], key_dim, v.shape[2],
+                             _dtype_code(q), key_dim ** -0.5 if scale is None else float(scale), 0)
+
+
+def _state(name, t, desc, n):
+    import torch
+
+    if t is None:
+        return None
+    _like(name, t, torch.float32, (n, desc.heads, desc.key_dim, desc.value_dim))
+    return _vector(name, t, torch.float32, 0)
+
+
+def linear_attention_workspace_bytes(desc: mmbev_attention_t, backward: bool = False) -> int:
+    return int(load().mmbev_linear_attention_workspace_bytes(ctypes.byref(desc), 1 if backward else 0))
+
+
+def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None, final_state=False, max_length=None,
+                     out=None, fault=None, workspace=None, stream=None):
+    """Enqueue mmbev_linear_attention: q [rows][heads][key_dim], k and v [rows][kv_heads][..], log_decay float32 [heads],
+    offsets int64 [B+1] (the voxeliser's out_voxel_offsets).  scale: key_dim ** -0.5 when None.  final_state: True, or
+    the tensor to write.  max_length: a bound on the sequences' rows, if known (the grid's max_voxels).
+
+    Returns (out, final state or None).  Rows of no sequence keep what `out` holds.
+    """
+    import torch
+
+    _on_device(q, k, v, log_decay, offsets, initial_state, out, fault, workspace)
+    n = offsets.numel() - 1
+    qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
+    desc = _attention_of(q, k, v, n, scale, max_length)
+    shape = (desc.rows, desc.heads, desc.value_dim)
+    out = _empty(stream, shape, q.dtype, q.device) if out is None else _like("out", out, q.dtype, shape)
+    if final_state is True:
+        final_state = _empty(stream, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32, q.device)
+    final = None if final_state is False else final_state
+    workspace, nbytes = _workspace(workspace, linear_attention_workspace_bytes(desc), stream, q.device)
+    _check(load().mmbev_linear_attention(
+        ctypes.byref(desc), qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
+        _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n), _heads("out", out),
+        _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), _ptr(workspace), nbytes,
+        _stream(stream)), "mmbev_linear_attention")
+    return out, final
+
+
+def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, initial_state=None, dfinal_state=None,
+                              dinitial_state=False, max_length=None, dq=None, dk=None, dv=None, fault=None,
+                              workspace=None, stream=None):
+    """Enqueue mmbev_linear_attention_backward: the gradients of linear_attention's q, k and v and, where
+    `dinitial_state` is True or a tensor to write, of its initial state.  Returns (dq, dk, dv, dinitial_state or None)."""
+    import torch
+
+    _on_device(dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, dq, dk, dv, fault, workspace)
+    n = offsets.numel() - 1
+    desc = _attention_of(q, k, v, n, scale, max_length)
+    _like("dout", dout, q.dtype, (desc.rows, desc.heads, desc.value_dim))
+    ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
+    dq, dk, dv = (_empty(stream, t.shape, t.dtype, t.device) if d is None else _like(name, d, t.dtype, t.shape)
+                  for name, d, t in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    if dinitial_state is True:
+        dinitial_state = _empty(stream, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32, q.device)
+    dinitial = None if dinitial_state is False else dinitial_state
+    workspace, nbytes = _workspace(workspace, linear_attention_workspace_bytes(desc, True), stream, q.device)
+    _check(load().mmbev_linear_attention_backward(
+        ctypes.byref(desc), *ins, _vector("log_decay", log_decay, torch.float32, desc.heads),
+        _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n),
+        _state("dfinal_state", dfinal_state, desc, n), _heads("dq", dq), _heads("dk", dk), _heads("dv", dv),
+        _state("dinitial_state", dinitial, desc, n), _vector("fault", fault, torch.int32, 1), _ptr(workspace), nbytes,
+        _stream(stream)), "mmbev_linear_attention_backward")
+    return dq, dk, dv, dinitial
+
+
+def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=None, fault=None, stream=None):
+    """Enqueue mmbev_linear_attention_step: one row for each of many streams.  state float32 [slots][heads][key_dim]
+    [value_dim] is updated in place; slots int32 [rows] names each row's state (negative: the row is skipped)."""
+    import torch
+
+    _on_device(q, k, v, log_decay, state, slots, out, fault)
+    qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
+    desc = _attention_of(q, k, v, 1, scale, 0)
+    shape = (desc.rows, desc.heads, desc.value_dim)
+    out = _empty(stream, shape, q.dtype, q.device) if out is None else _like("out", out, q.dtype, shape)
+    _check(load().mmbev_linear_attention_step(
+        ctypes.byref(desc), qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
+        _vector("slots", slots, torch.int32, desc.rows), state.shape[0], _state("state", state, desc, state.shape[0]),
+        _heads("out", out), _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_linear_attention_step")
+    return out
