@@ -22,20 +22,23 @@
 //   rounded copy is put into LDS for the product with a;
 // - the next chunk's loads are issued before this one's products.
 //
-// The gradients are the same recurrence (dout, v, k), and backwards in time
-// (k, q, dout) and (v, dout, q); backwards the state is carried one decay
-// later, S' = lambda^n S + sum_j lambda^(n-j) b_j^T c_j with lambda^i in the
-// first sum's place of lambda^(i+1), so that a gradient of the final state
-// enters undecayed and the last S is the initial state's.
+// The gradients are the same recurrence: dq forwards as (dout, v, k); dv and dk
+// backwards in time as (k, q, dout) and (v, dout, q), whose states are one
+// another's transposes, so one walk makes both (attention_grad_kernel).
+// Backwards the state is carried one decay later, S' = lambda^n S + sum_j
+// lambda^(n-j) b_j^T c_j with lambda^i in place of lambda^(i+1), so that a
+// gradient of the final state enters undecayed and the last S is the initial
+// state's.
 //
 // 16-bit types: P and the state's copy are rounded to the type for their
 // products.  The rows that enter the state are c times its decay in two parts
 // (the rounded product and what the rounding left), so the state has 16 or 22
 // bits and not the type's 8 or 11; in bf16 a third part makes them 24 where
 // the state is asked for.  fp16 has too few exponents for a state that sums
-// many rows: its copy is scaled by a power of two per column.
+// many rows: its copy is scaled by a power of two.
 #pragma once
 
+#include "common.hpp"
 #include "sequence.hpp"
 
 namespace mmbev {
@@ -65,6 +68,17 @@ __device__ __forceinline__ Frag<T> load_rows(const T* s, int stride, int row0, i
   const T* p = s + (row0 + (l & 15)) * stride + col0 + (l >> 4) * 8;
   Frag<T> f;
   __builtin_memcpy(&f, __builtin_assume_aligned(p, 16), sizeof(f));
+  return f;
+}
+
+// Along a row in load_cols' order.
+template <typename T>
+__device__ __forceinline__ Frag<T> load_rows_split(const T* s, int stride, int row0, int col0) {
+  const int l = threadIdx.x & 63;
+  const T* p = s + (row0 + (l & 15)) * stride + col0 + (l >> 4) * 4;
+  Frag<T> f;
+  __builtin_memcpy(&f.v[0], __builtin_assume_aligned(p, 4 * sizeof(T)), 4 * sizeof(T));
+  __builtin_memcpy(&f.v[4], __builtin_assume_aligned(p + 16, 4 * sizeof(T)), 4 * sizeof(T));
   return f;
 }
 
@@ -111,388 +125,731 @@ __device__ __forceinline__ f32x4 mma(const Frag<float>& a, const Frag<float>& b,
 // call is reversed; sequence k in that order begins at bound(k).
 struct Order {
   const int64_t* offsets;
-  int64_t used;
-  int32_t B, reversed;
-  __device__ __forceinline__ int64_t bound(int32_t k) const {
+  int32_t used, B, reversed;
+  __device__ __forceinline__ int32_t bound(int32_t k) const {
     const int64_t o = offsets[reversed ? B - k : k];
-    const int64_t c = o < 0 ? 0 : o > used ? used : o;
+    const int32_t c = o < 0 ? 0 : o > used ? used : (int32_t)o;
     return reversed ? used - c : c;
   }
-  __device__ __forceinline__ int64_t row(int64_t p) const { return reversed ? used - 1 - p : p; }
+  __device__ __forceinline__ int32_t row(int32_t p) const { return reversed ? used - 1 - p : p; }
   __device__ __forceinline__ int32_t sequence(int32_t k) const { return reversed ? B - 1 - k : k; }
 };
 
-__device__ __forceinline__ Order order_of(const AttnArgs& a) {
+__device__ __forceinline__ Order order_of(const AttnWalk& a) {
   Order o;
   o.offsets = a.offsets;
   o.B = a.B;
   o.reversed = a.reversed;
   const int64_t end = a.offsets[a.B];
-  o.used = end < 0 ? 0 : end > a.rows ? a.rows : end;
+  o.used = end < 0 ? 0 : end > a.rows ? (int32_t)a.rows : (int32_t)end;
   return o;
 }
 
-// Rows of a segment: the rows in use shared out evenly, in whole chunks.
-__device__ __forceinline__ int64_t segment_rows(int64_t used, int32_t segments) {
-  const int64_t each = (used + segments - 1) / segments;
-  return max((each + kChunk - 1) / kChunk * kChunk, (int64_t)kChunk);
-}
+// A run of rows that one workgroup walks: a sequence, or a part of one.
+struct Part {
+  int32_t lo, hi;  // positions
+  int32_t b;       // sequence
+  int32_t before;  // parts that go on (into another of their sequence) before this one
+  bool began;      // a part of the sequence comes before it
+  bool goes_on;    // and after it
+};
 
-// First sequence that ends after position p (B if none): the bounds do not
-// decrease where the offsets keep their contract, and any k is in bounds.
-__device__ __forceinline__ int32_t first_ending_after(const Order& o, int64_t p) {
-  int32_t lo = 0, hi = o.B;
-  while (lo < hi) {
-    const int32_t mid = (lo + hi) >> 1;
-    if (o.bound(mid + 1) > p)
-      hi = mid;
-    else
-      lo = mid + 1;
+// Sequences longer than `rows in use / a.cuts` are cut into equal parts of at
+// most that, in whole chunks; there are at most a.cuts + B parts, of which at
+// most a.cuts go on.  Finds part `index` in the order of positions, counting
+// all parts or those that go on; false if there are fewer.  Every wave looks
+// for itself, 64 sequences at a time: a load, a sum over the lanes and a
+// ballot (about a microsecond for 64 sequences).
+__device__ __forceinline__ bool find_part(Part& q, const Order& o, const AttnWalk& a, int32_t index, bool going_on) {
+  if (!a.cuts) {
+    q.lo = o.bound(index);
+    q.hi = max(o.bound(index + 1), q.lo);
+    q.b = o.sequence(index);
+    q.before = 0;
+    q.began = q.goes_on = false;
+    return true;
   }
-  return lo;
+  const int32_t each = (int32_t)(((int64_t)o.used + a.cuts - 1) / a.cuts);
+  const int32_t most = max((int32_t)(((int64_t)each + kChunk - 1) / kChunk * kChunk), a.least);
+  const int lane = threadIdx.x & 63;
+  int32_t seen = 0;
+  for (int32_t k0 = 0; k0 < o.B; k0 += 64) {
+    const int32_t k = min(k0 + lane, o.B - 1);
+    const int32_t s0 = o.bound(k), s1 = max(o.bound(k + 1), s0);
+    const int32_t parts = max((int32_t)(((int64_t)(s1 - s0) + most - 1) / most), 1);
+    const uint32_t count = k0 + lane < o.B ? (uint32_t)(parts - (going_on ? 1 : 0)) : 0u;
+    const uint32_t upto = wave_inclusive_sum(count);
+    const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    if ((uint32_t)index < seen + all) {
+      const int at = __builtin_ctzll(__ballot(seen + upto > (uint32_t)index));
+      const int32_t n0 = __builtin_amdgcn_readlane(s0, at), n1 = __builtin_amdgcn_readlane(s1, at);
+      const int32_t c = __builtin_amdgcn_readlane(parts, at);
+      const int32_t j = index - seen - (int32_t)__builtin_amdgcn_readlane((int)(upto - count), at);
+      const int32_t step = (int32_t)((((int64_t)(n1 - n0) + c - 1) / c + kChunk - 1) / kChunk * kChunk);  // <= most
+      q.lo = n0 + j * step;
+      q.hi = j + 1 < c ? min(q.lo + step, n1) : n1;
+      q.b = o.sequence(k0 + at);
+      q.before = going_on ? index : index - (k0 + at);
+      q.began = j > 0 && q.before <= a.cuts;  // more parts than that go on only where the offsets break their contract
+      q.goes_on = j + 1 < c;
+      return true;
+    }
+    seen += (int32_t)all;
+  }
+  return false;
 }
 
 __device__ __forceinline__ float decay_exponent(const float* log_decay, int h) {
-  // at most 0; -1e4 stands for -inf, whose products with 0 rows would be NaN
+  // at most 0; -1e4 stands for -inf, whose product with no rows would be NaN
   return fmaxf(fminf(log_decay[h], 0.0f), -1.0e4f) * 1.44269504088896341f;
 }
 
+// ------------------------------------------------------ parts of a step
+
 template <typename T>
 constexpr int kRowPad = 16 / (int)sizeof(T);  // one 16-byte step: rows of a column fall into different banks
+template <int D>
+constexpr int kTiles = D / 16;
+template <int D>
+constexpr int kSteps = D / 32;  // 32-deep products along a dim
+template <int D>
+constexpr int kOwnTiles = D >= 64 ? D / 64 : 1;  // column tiles of the state that a wave owns
+template <int D>
+constexpr int kPacks = kChunk * D / 8 / kAttnThreads;  // 8-element packs of a thread and tile
 
-// ------------------------------------------------------ the walk
+// A value that every lane holds, in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
 
-// STATE_ONLY: the state at the end of every segment that a sequence goes on
-// beyond, from nothing (or the initial state, where the sequence begins
-// inside); attention_join_kernel then carries them on.
-template <typename T, int D, bool STATE_ONLY>
-__global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
+// The same value, of which the compiler knows nothing: what is computed from
+// it stays where it is used, instead of being kept in registers all through a
+// loop that is around it.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+struct Lane {
+  int w, g, n;  // wave; lane / 16; lane % 16
+};
+
+// Powers of the decay that do not change from chunk to chunk.
+struct Powers {
+  float g2;
+  float diag[4], off[4], gap[3];  // scale * lambda^(i-j): of the wave's own tile, and as off * gap of those before it
+  float left[4];                  // lambda^(rows after j) of the chunk's last 16 rows; the tiles before them 16 rows more each
+  float fade16, fade32, fade48, fade_chunk;
+
+  __device__ __forceinline__ float of(int x) const { return __builtin_amdgcn_exp2f(g2 * (float)x); }
+  __device__ __forceinline__ void set(float exponent, const Lane& l, float scale, int late) {
+    g2 = exponent;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      diag[r] = l.n >= 4 * l.g + r ? of(l.n - 4 * l.g - r) * scale : 0.0f;
+      off[r] = of(l.n - 4 * l.g - r + 15) * scale;
+      left[r] = of(15 - 4 * l.g - r + late);
+    }
+#pragma unroll
+    for (int d = 0; d < 3; ++d) gap[d] = uniform(of(16 * d + 1));
+    fade16 = uniform(of(16));
+    fade32 = uniform(of(32));
+    fade48 = uniform(of(48));
+    fade_chunk = uniform(of(kChunk));
+  }
+};
+
+// Eight elements into LDS at a multiple of 16 bytes; zeros if they are not to be seen.
+template <typename T>
+__device__ __forceinline__ void put_pack(T* s, const Pack<T, 8>& r, bool seen) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * 2)));
+  words x = __builtin_bit_cast(words, r);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) * 2; ++i) x[i] = seen ? x[i] : 0u;
+  __builtin_memcpy(__builtin_assume_aligned(s, 16), &x, sizeof(x));
+}
+
+// WHOLE: both dims are multiples of eight, so a pack of eight elements lies in
+// a row or past it.  Its loads are unconditional, at an address that is always
+// a row's (what lies before the sequence or past the row is zeroed on the way
+// into LDS): a load under a condition is waited for where the paths meet.
+template <typename T, int N, bool WHOLE>
+__device__ __forceinline__ Pack<T, N> load_part(const T* row, int c, int dim) {
+  if constexpr (WHOLE)
+    return load_pack<T, N>(row + (c < dim ? c : 0));
+  else
+    return load_some<T, N>(row + c, dim - c);
+}
+
+// A chunk's 64 rows of an operand, shared out among the threads.
+template <typename T, int D, bool WHOLE>
+__device__ __forceinline__ void fetch_tile(Pack<T, 8> (&r)[kPacks<D>], const T* p, int32_t stride, int dim, const Order& o, int32_t c0,
+                                           int32_t lo) {
+#pragma unroll
+  for (int i = 0; i < kPacks<D>; ++i) {
+    const int idx = threadIdx.x + i * kAttnThreads;
+    const int64_t row = o.row(max(c0 + idx / (D / 8), lo));
+    r[i] = load_part<T, 8, WHOLE>(p + row * stride, idx % (D / 8) * 8, dim);
+  }
+}
+
+template <typename T, int D, bool WHOLE>
+__device__ __forceinline__ void put_tile(T* s, const Pack<T, 8> (&r)[kPacks<D>], int dim, int skip) {
+#pragma unroll
+  for (int i = 0; i < kPacks<D>; ++i) {
+    const int idx = threadIdx.x + i * kAttnThreads, row = idx / (D / 8), c = idx % (D / 8) * 8;
+    put_pack(s + row * (D + kRowPad<T>) + c, r[i], row >= skip && (!WHOLE || c < dim));
+  }
+}
+
+// The wave's 16 rows as operands, lane n its row n: in load_rows' order, or in load_cols'.
+template <typename T, int D, bool WHOLE, bool SPLIT>
+__device__ __forceinline__ void fetch_rows(Frag<T> (&q)[kSteps<D>], const T* p, int32_t stride, int dim, const Order& o, int32_t at,
+                                           int32_t lo, const Lane& l) {
+  // a row before the first makes a column of the result that is not stored
+  const T* row = p + (int64_t)o.row(max(at + l.n, lo)) * stride;
+#pragma unroll
+  for (int s = 0; s < kSteps<D>; ++s) {
+    if constexpr (SPLIT) {
+      const Pack<T, 4> x = load_part<T, 4, WHOLE>(row, 32 * s + 4 * l.g, dim), y = load_part<T, 4, WHOLE>(row, 32 * s + 16 + 4 * l.g, dim);
+      __builtin_memcpy(&q[s].v[0], &x, sizeof(x));
+      __builtin_memcpy(&q[s].v[4], &y, sizeof(y));
+    } else {
+      const Pack<T, 8> x = load_part<T, 8, WHOLE>(row, 32 * s + 8 * l.g, dim);
+      __builtin_memcpy(&q[s], &x, sizeof(x));
+    }
+  }
+}
+
+// What lies past the row's end is zeroed before it is used.
+template <typename T, int D, bool WHOLE, bool SPLIT>
+__device__ __forceinline__ void take_rows(Frag<T> (&to)[kSteps<D>], const Frag<T> (&from)[kSteps<D>], int dim, const Lane& l) {
+#pragma unroll
+  for (int s = 0; s < kSteps<D>; ++s) {
+    to[s] = from[s];
+    if constexpr (WHOLE) {
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (32 * s + 4 * l.g >= dim) to[s].v[e] = (T)0.0f;
+          if (32 * s + 16 + 4 * l.g >= dim) to[s].v[4 + e] = (T)0.0f;
+        }
+      } else {
+        if (32 * s + 8 * l.g >= dim) to[s] = Frag<T>{};
+      }
+    }
+  }
+}
+
+// ---- the state: wave w has columns 16 * own * w .., all rows; lane n of a tile column n, rows 4g .. 4g+3
+
+template <int D>
+using State = f32x4[kTiles<D>][kOwnTiles<D>];
+
+template <int D>
+__device__ __forceinline__ bool owns_state(const Lane& l) {
+  return l.w * kOwnTiles<D> < kTiles<D>;
+}
+
+template <int D>
+__device__ __forceinline__ void load_state(State<D>& st, const float* from, int ad, int cd, bool swapped, float times, const Lane& l) {
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt) st[kt][vt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (!from) return;
+  // unconditional loads of an element that is there: they do not wait for each other
+  const int row0 = opaque(4 * l.g), col0 = opaque(16 * l.w * kOwnTiles<D> + l.n);
+  const int step_r = swapped ? 1 : cd, step_c = swapped ? ad : 1;
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        st[kt][vt][r] = from[min(row0 + 16 * kt + r, ad - 1) * step_r + min(col0 + 16 * vt, cd - 1) * step_c];
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        st[kt][vt][r] = row0 + 16 * kt + r < ad && col0 + 16 * vt < cd ? st[kt][vt][r] * times : 0.0f;
+}
+
+template <int D>
+__device__ __forceinline__ void store_state(float* to, const State<D>& st, int ad, int cd, float times, const Lane& l) {
+  const int row0 = opaque(4 * l.g), col0 = opaque(16 * l.w * kOwnTiles<D> + l.n);
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = row0 + 16 * kt + r, col = col0 + 16 * vt;
+        if (row < ad && col < cd) to[row * cd + col] = st[kt][vt][r] * times;
+      }
+}
+
+// fp16: the wave's largest magnitude, for the copy's scale (s_max: a word a wave).
+template <int D>
+__device__ __forceinline__ void put_max(float* s_max, const State<D>& st, const Lane& l) {
+  float m = 0.0f;
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m = fmaxf(m, __builtin_fabsf(st[kt][vt][r]));
+  m = group_max(m);
+  s_max[l.w] = owns_state<D>(l) ? m : 0.0f;
+}
+
+// The exponent that brings the state's copy below 1.
+__device__ __forceinline__ int copy_exponent(const float* s_max) {
+  const float m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  const int ex = m > 0.0f && m < 3.0e38f ? max(-100, min(126, __builtin_amdgcn_frexp_expf(m))) : 0;
+  return __builtin_amdgcn_readfirstlane(ex);
+}
+
+// The state's copy in LDS, [column][row].
+template <typename T, int D>
+__device__ __forceinline__ void put_state(T* s, const State<D>& st, float times, const Lane& l) {
+#pragma unroll
+  for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+    for (int kt = 0; kt < kTiles<D>; ++kt) {
+      Pack<T, 4> q;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) q.v[r] = (T)(__is_same(T, f16) ? st[kt][vt][r] * times : st[kt][vt][r]);
+      __builtin_memcpy(__builtin_assume_aligned(
+                           s + (16 * (l.w * kOwnTiles<D> + vt) + l.n) * (D + kRowPad<T>) + 16 * kt + 4 * l.g, 4 * sizeof(T)),
+                       &q, sizeof(q));
+    }
+}
+
+// S += times * sum_j lambda^(rows after j in the chunk) b_j^T c_j.
+template <typename T, int D>
+__device__ __forceinline__ void add_to_state(State<D>& st, const T* s_b, const T* s_c, const Powers& p, float times, bool third,
+                                             const Lane& l) {
+  constexpr int SD = D + kRowPad<T>, VT = kOwnTiles<D>;
+  constexpr bool HALF = sizeof(T) == 2, THIRD = __is_same(T, bf16);
+#pragma unroll
+  for (int s2 = 0; s2 < 2; ++s2) {
+    Frag<T> hi_part[VT], lo_part[VT], end_part[VT];
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt) {
+      const Frag<T> c = load_cols(s_c, SD, 32 * s2, 16 * (l.w * VT + vt));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = (s2 == 0 ? (e < 4 ? p.fade48 : p.fade32) : e < 4 ? p.fade16 : 1.0f) * times;
+        float x = (float)c.v[e] * (p.left[e & 3] * f);
+        // the product as rounded to fp32: a multiply fused with one of its two conversions to fp16, but not with the
+        // other, would leave the parts a step of fp16 apart where x lies next to a tie
+        if constexpr (__is_same(T, f16)) asm("" : "+v"(x));
+        hi_part[vt].v[e] = (T)x;
+        if constexpr (HALF) {
+          const float rest = x - (float)hi_part[vt].v[e];
+          lo_part[vt].v[e] = (T)rest;
+          if constexpr (THIRD) end_part[vt].v[e] = (T)(rest - (float)lo_part[vt].v[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int kt = 0; kt < kTiles<D>; ++kt) {
+      const Frag<T> bk = load_cols(s_b, SD, 32 * s2, 16 * kt);
+#pragma unroll
+      for (int vt = 0; vt < VT; ++vt) {
+        st[kt][vt] = mma(bk, hi_part[vt], st[kt][vt]);
+        if constexpr (HALF) st[kt][vt] = mma(bk, lo_part[vt], st[kt][vt]);
+      }
+    }
+    if constexpr (THIRD)
+      if (third) {
+#pragma unroll
+        for (int kt = 0; kt < kTiles<D>; ++kt) {
+          const Frag<T> bk = load_cols(s_b, SD, 32 * s2, 16 * kt);
+#pragma unroll
+          for (int vt = 0; vt < VT; ++vt) st[kt][vt] = mma(bk, end_part[vt], st[kt][vt]);
+        }
+      }
+  }
+}
+
+// The state after the chunk.
+template <typename T, int D>
+__device__ __forceinline__ void update_state(State<D>& st, const T* s_b, const T* s_c, const Powers& p, float fade, bool third,
+                                             const Lane& l) {
+#pragma unroll
+  for (int kt = 0; kt < kTiles<D>; ++kt)
+#pragma unroll
+    for (int vt = 0; vt < kOwnTiles<D>; ++vt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st[kt][vt][r] *= fade;
+  add_to_state<T, D>(st, s_b, s_c, p, 1.0f, third, l);
+}
+
+// ---- products for the wave's 16 rows, transposed: lane n its row n, elements 16t + 4g .. of it
+
+template <int D>
+using Rows = f32x4[kTiles<D>];
+
+template <int D>
+__device__ __forceinline__ void clear(Rows<D>& acc) {
+#pragma unroll
+  for (int t = 0; t < kTiles<D>; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// acc += times * (the rows' a) S.  SPLIT: S transposed, a in load_cols' order.
+template <typename T, int D, bool SPLIT>
+__device__ __forceinline__ void add_state_product(Rows<D>& acc, const T* s_s, const Frag<T> (&q)[kSteps<D>], float times) {
   constexpr int SD = D + kRowPad<T>;
-  constexpr int KT = D / 16;                     // tiles of 16 along a dim
-  constexpr int VT = D >= 64 ? D / 64 : 1;       // state column tiles of a wave
-  constexpr int KS = D / 32;                     // 32-deep steps along a dim
-  constexpr int PACKS = kChunk * D / 8 / kAttnThreads;  // 8-element packs of a thread, per operand
-  constexpr bool HALF = sizeof(T) == 2;
-  constexpr bool SCALED = __is_same(T, f16);
-  constexpr bool THIRD = __is_same(T, bf16);
+#pragma unroll
+  for (int t = 0; t < kTiles<D>; ++t) {
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < kSteps<D>; ++s)
+      x = mma(SPLIT ? load_cols(s_s, SD, 32 * s, 16 * t) : load_rows(s_s, SD, 16 * t, 32 * s), q[s], x);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[t][r] = __builtin_fmaf(x[r], times, acc[t][r]);
+  }
+}
+
+// acc += sum over the rows j of the chunk up to the wave's own, scale * lambda^(i-j) (a_i . b_j) c_j.
+template <typename T, int D, bool SPLIT>
+__device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s_c, const Frag<T> (&q)[kSteps<D>], const Powers& pw,
+                                          const Lane& l) {
+  constexpr int SD = D + kRowPad<T>;
+#pragma unroll
+  for (int s2 = 0; s2 < 2; ++s2) {
+    if (2 * s2 > l.w) continue;
+    f32x4 p[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      p[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      const int j = 2 * s2 + u;
+      if (j > l.w) continue;
+#pragma unroll
+      for (int s = 0; s < kSteps<D>; ++s)
+        p[u] = mma(SPLIT ? load_rows_split(s_b, SD, 16 * j, 32 * s) : load_rows(s_b, SD, 16 * j, 32 * s), q[s], p[u]);
+      if (j == l.w) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[u][r] = l.n >= 4 * l.g + r ? p[u][r] * pw.diag[r] : 0.0f;
+      } else {
+        const float f = l.w - j == 1 ? pw.gap[0] : l.w - j == 2 ? pw.gap[1] : pw.gap[2];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[u][r] *= pw.off[r] * f;
+      }
+    }
+    Frag<T> pf;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      pf.v[r] = (T)p[0][r];
+      pf.v[4 + r] = (T)p[1][r];
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles<D>; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
+  }
+}
+
+template <bool WHOLE, int D, typename T>
+__device__ __forceinline__ void store_rows(T* p, const Rows<D>& acc, int dim) {
+#pragma unroll
+  for (int t = 0; t < kTiles<D>; ++t) {
+    Pack<T, 4> q;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) q.v[r] = (T)acc[t][r];
+    const int c = 16 * t + 4 * ((threadIdx.x & 63) >> 4);
+    if constexpr (WHOLE) {
+      if (c < dim) store_pack<T, 4>(p + c, q);
+    } else {
+      store_some<T, 4>(p + c, q, dim - c);
+    }
+  }
+}
+
+__device__ __forceinline__ Lane lane_of() {
+  Lane l;
+  l.w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  l.g = (threadIdx.x & 63) >> 4;
+  l.n = threadIdx.x & 15;
+  return l;
+}
+
+template <typename T, int D>
+#ifndef W64
+#define W64 3
+#endif
+constexpr int kWavesSimd = (D == 128 ? 2 : D == 64 ? W64 : 4) - (sizeof(T) == 4 ? 1 : 0);  // waves a SIMD, as the registers allow
+
+// ------------------------------------------------------ the kernels
+
+// The state at the end of every part that goes on, from nothing (or the
+// initial state, where the part begins the sequence); attention_join_kernel
+// then carries them on.
+template <typename T, int D, bool WHOLE>
+__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_state_kernel(AttnArgs a) {
+  constexpr int SD = D + kRowPad<T>;
   __shared__ __attribute__((aligned(16))) T s_b[kChunk * SD];
   __shared__ __attribute__((aligned(16))) T s_c[kChunk * SD];
-  __shared__ __attribute__((aligned(16))) T s_s[STATE_ONLY ? 8 : D * SD];  // state copy, [column][row]
-  __shared__ __attribute__((aligned(16))) float s_scale[SCALED && !STATE_ONLY ? D : 4];
-
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l = threadIdx.x & 63, g = l >> 4, n = l & 15;
+  const Lane l = lane_of();
   const int h = blockIdx.x % a.H, unit = blockIdx.x / a.H;
   const Order o = order_of(a);
+  Part q;
+  const bool found = find_part(q, o, a, unit, true);
+  if (h == 0 && threadIdx.x == 0) a.cut_rows[unit] = !found ? -1 : q.began ? q.hi - q.lo : 0;
+  if (!found) return;
+  const int32_t lo = q.lo, hi = q.hi;
+  const T* pb = static_cast<const T*>(a.b) + (int64_t)(h / a.b_div) * a.b_head;
+  const T* pc = static_cast<const T*>(a.c) + (int64_t)(h / a.c_div) * a.c_head;
 
-  int64_t p_lo, p_hi;
-  int32_t k = unit, k_end = unit + 1;
-  if (a.segments) {
-    const int64_t per = segment_rows(o.used, a.segments);
-    p_lo = unit * per;
-    p_hi = min(p_lo + per, o.used);
-    if (unit > 0 && p_lo >= o.used) return;
-    k = unit == 0 ? 0 : first_ending_after(o, p_lo);
-    k_end = a.B;
-  } else {
-    p_lo = 0;
-    p_hi = o.used;
+  // from the end back: the walk that follows begins with the rows read last here
+  Pack<T, 8> rb[kPacks<D>], rc[kPacks<D>];
+  fetch_tile<T, D, WHOLE>(rb, pb, a.b_row, a.ad, o, hi - kChunk, lo);
+  fetch_tile<T, D, WHOLE>(rc, pc, a.c_row, a.cd, o, hi - kChunk, lo);
+  State<D> st;
+  const bool own = owns_state<D>(l);
+  Powers pw;
+  pw.set(decay_exponent(a.log_decay, h), l, a.scale, a.reversed);
+  load_state<D>(st, !q.began && a.init && own ? a.init + ((int64_t)q.b * a.H + h) * a.ad * a.cd : nullptr, a.ad, a.cd, a.init_swapped,
+                a.init_scale * pw.of(hi - lo), l);
+  for (int32_t c0 = hi - kChunk; c0 + kChunk > lo; c0 -= kChunk) {
+    const int skip = max(lo - c0, 0);
+    __syncthreads();  // the chunk before has been read
+    put_tile<T, D, WHOLE>(s_b, rb, a.ad, skip);
+    put_tile<T, D, WHOLE>(s_c, rc, a.cd, skip);
+    __syncthreads();
+    if (c0 > lo) {
+      fetch_tile<T, D, WHOLE>(rb, pb, a.b_row, a.ad, o, c0 - kChunk, lo);
+      fetch_tile<T, D, WHOLE>(rc, pc, a.c_row, a.cd, o, c0 - kChunk, lo);
+    }
+    if (own) add_to_state<T, D>(st, s_b, s_c, pw, uniform(pw.of(hi - c0 - kChunk)), a.exact_state, l);
   }
-  if (STATE_ONLY) {
-    // only the sequence that goes on beyond the segment counts
-    k = first_ending_after(o, p_hi);
-    k_end = k + 1;
-    const bool goes_on = k < a.B && o.bound(k) < p_hi;
-    if (h == 0 && threadIdx.x == 0) a.seg_fresh[unit] = !goes_on || o.bound(k) >= p_lo;
-    if (!goes_on) return;
-  }
+  if (own) store_state<D>(a.cut_state + ((int64_t)unit * a.H + h) * a.ad * a.cd, st, a.ad, a.cd, 1.0f, l);
+}
 
+// out: the walk of (a, b, c).
+template <typename T, int D, bool WHOLE>
+__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_kernel(AttnArgs a) {
+  constexpr int SD = D + kRowPad<T>;
+  constexpr bool SCALED = __is_same(T, f16);
+  __shared__ __attribute__((aligned(16))) T s_b[kChunk * SD];
+  __shared__ __attribute__((aligned(16))) T s_c[kChunk * SD];
+  __shared__ __attribute__((aligned(16))) T s_s[D * SD];  // the state's copy
+  __shared__ float s_max[kAttnWaves];
+  const Lane l = lane_of();
+  const int h = blockIdx.x % a.H, unit = blockIdx.x / a.H;
+  const Order o = order_of(a);
+  Part q;
+  if (!find_part(q, o, a, unit, false)) return;
   const T* pa = static_cast<const T*>(a.a) + (int64_t)(h / a.a_div) * a.a_head;
   const T* pb = static_cast<const T*>(a.b) + (int64_t)(h / a.b_div) * a.b_head;
   const T* pc = static_cast<const T*>(a.c) + (int64_t)(h / a.c_div) * a.c_head;
-  const int late = a.reversed;
+  T* po = static_cast<T*>(a.out) + (int64_t)h * a.o_head;
+  const bool own = owns_state<D>(l);
+  const int64_t state = (int64_t)a.ad * a.cd;
 
-  // powers of the decay that do not change from chunk to chunk
-  const float g2 = decay_exponent(a.log_decay, h);
-  auto power = [&](int x) { return __builtin_amdgcn_exp2f(g2 * (float)x); };
-  const float fade_in = power(16 * w + n + 1 - late) * a.scale;  // of the state, for this lane's row
-  float diag[4], off[4], gap[3];  // lambda^(i-j) of the wave's own tile, and as off * gap of those before it
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    diag[r] = n >= 4 * g + r ? power(n - 4 * g - r) * a.scale : 0.0f;
-    off[r] = power(n - 4 * g - r + 15) * a.scale;
+  // whole chunks up to the end, so the first one may begin `skip` rows before the first row: those are zeros in LDS
+  const int32_t first = q.hi - (q.hi - q.lo + kChunk - 1) / kChunk * kChunk;
+  Pack<T, 8> rb[kPacks<D>], rc[kPacks<D>];
+  Frag<T> qa[kSteps<D>], qn[kSteps<D>];
+  auto fetch = [&](int32_t c0) {
+    fetch_tile<T, D, WHOLE>(rb, pb, a.b_row, a.ad, o, c0, q.lo);
+    fetch_tile<T, D, WHOLE>(rc, pc, a.c_row, a.cd, o, c0, q.lo);
+    fetch_rows<T, D, WHOLE, false>(qn, pa, a.a_row, a.ad, o, c0 + 16 * l.w, q.lo, l);
+  };
+  if (q.lo < q.hi) fetch(first);
+  const float* from = q.began ? a.cut_state + ((int64_t)(q.before - 1) * a.H + h) * state
+                      : a.init ? a.init + ((int64_t)q.b * a.H + h) * state
+                               : nullptr;
+  bool have_state = from != nullptr;
+  State<D> st;
+  load_state<D>(st, own ? from : nullptr, a.ad, a.cd, !q.began && a.init_swapped, q.began ? 1.0f : a.init_scale, l);
+  if (SCALED && have_state) put_max<D>(s_max, st, l);
+  Powers pw;
+  pw.set(decay_exponent(a.log_decay, h), l, a.scale, 0);
+
+  for (int32_t c0 = first; c0 < q.hi; c0 += kChunk) {
+    const int skip = max(q.lo - c0, 0);
+    __syncthreads();  // the chunk before has been read
+    put_tile<T, D, WHOLE>(s_b, rb, a.ad, skip);
+    put_tile<T, D, WHOLE>(s_c, rc, a.cd, skip);
+    take_rows<T, D, WHOLE, false>(qa, qn, a.ad, l);
+    const int ex = SCALED && have_state ? copy_exponent(s_max) : 0;
+    if (have_state && own) put_state<T, D>(s_s, st, __builtin_ldexpf(1.0f, -ex), l);
+    __syncthreads();
+    if (c0 + kChunk < q.hi) fetch(c0 + kChunk);
+
+    if (16 * l.w + 15 >= skip) {
+      Rows<D> acc;
+      clear<D>(acc);
+      if (have_state)
+        add_state_product<T, D, false>(acc, s_s, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
+      add_pairs<T, D, false>(acc, s_b, s_c, qa, pw, l);
+      if (16 * l.w + l.n >= skip) store_rows<WHOLE, D>(po + (int64_t)o.row(c0 + 16 * l.w + l.n) * a.o_row, acc, a.cd);
+    }
+    // the state after the chunk, where something reads it
+    if (c0 + kChunk < q.hi || (!q.goes_on && a.final_state)) {
+      if (own) update_state<T, D>(st, s_b, s_c, pw, skip ? pw.of(kChunk - skip) : pw.fade_chunk, a.exact_state, l);
+      if constexpr (SCALED) put_max<D>(s_max, st, l);
+    }
+    have_state = true;
   }
-#pragma unroll
-  for (int d = 0; d < 3; ++d) gap[d] = power(16 * d + 1);
-  float left[2][8];  // lambda^(rows after j), of a whole chunk
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) left[s][e] = power(kChunk - 1 + late - (32 * s + (e < 4 ? 0 : 12) + 4 * g + e));
-  const float fade_chunk = power(kChunk);
+  if (!q.goes_on && a.final_state && own)
+    store_state<D>(a.final_state + ((int64_t)q.b * a.H + h) * state, st, a.ad, a.cd, 1.0f, l);
+}
 
-  const bool owns_state = w * VT < KT;
-  f32x4 st[KT][VT];
+// dv and dk: one walk backwards, whose state is that of (q, dout) divided by
+// scale.  A workgroup takes GROUP of the heads that share its keys and values:
+// each chunk it goes through them with a state each, and their sums stay in
+// registers.  Where GROUP is not all of them, the sums are fp32 parts that
+// attention_sum_kernel adds.
+template <typename T, int D, int GROUP, bool WHOLE>
+__global__ __launch_bounds__(kAttnThreads, (D == 128 ? (sizeof(T) == 2 ? 2 : 1) : 2)) void attention_grad_kernel(AttnGradArgs a) {
+  constexpr int SD = D + kRowPad<T>;
+  constexpr bool SCALED = __is_same(T, f16);
+  __shared__ __attribute__((aligned(16))) T s_q[kChunk * SD];
+  __shared__ __attribute__((aligned(16))) T s_d[kChunk * SD];
+  __shared__ __attribute__((aligned(16))) T s_s[D * SD];
+  __shared__ float s_max[GROUP][kAttnWaves];
+  const Lane l = lane_of();
+  const int groups = a.H / GROUP, u = blockIdx.x % groups, unit = blockIdx.x / groups;
+  const int h0 = u * GROUP, hk = h0 / a.kv_div;
+  const Order o = order_of(a);
+  Part q;
+  if (!find_part(q, o, a, unit, false)) return;
+  const T* pq = static_cast<const T*>(a.q) + (int64_t)h0 * a.q_head;
+  const T* pd = static_cast<const T*>(a.dout) + (int64_t)h0 * a.d_head;
+  const T* pk = static_cast<const T*>(a.k) + (int64_t)hk * a.k_head;
+  const T* pv = static_cast<const T*>(a.v) + (int64_t)hk * a.v_head;
+  const bool own = owns_state<D>(l);
+  const int64_t state = (int64_t)a.ad * a.cd;
 
-  for (; k < k_end; ++k) {
-    const int64_t s0 = o.bound(k), s1 = max(o.bound(k + 1), s0);
-    if (a.segments && s1 > p_hi && s0 >= p_hi) break;
-    const int64_t lo = max(s0, p_lo), hi = min(s1, p_hi);
-    const int32_t b = o.sequence(k);
-    const bool goes_on = s1 > p_hi;
-
-    // the state before `lo`
-    const float* from = nullptr;
-    int64_t step_r = a.cd, step_c = 1;
-    float times = a.init_scale;
-    if (s0 < p_lo) {
-      if (!STATE_ONLY) {
-        from = a.seg_state + ((int64_t)(unit - 1) * a.H + h) * a.ad * a.cd;
-        times = 1.0f;
-      }
-    } else if (a.init) {
-      from = a.init + ((int64_t)b * a.H + h) * a.ad * a.cd;
-      if (a.init_swapped) {
-        step_r = 1;
-        step_c = a.ad;
-      }
+  const int32_t first = q.hi - (q.hi - q.lo + kChunk - 1) / kChunk * kChunk;
+  Pack<T, 8> rq[kPacks<D>], rd[kPacks<D>];
+  Frag<T> fk[kSteps<D>], fv[kSteps<D>], nk[kSteps<D>], nv[kSteps<D>];
+  auto fetch = [&](int32_t c0, int j) {
+    fetch_tile<T, D, WHOLE>(rq, pq + j * a.q_head, a.q_row, a.ad, o, c0, q.lo);
+    fetch_tile<T, D, WHOLE>(rd, pd + j * a.d_head, a.d_row, a.cd, o, c0, q.lo);
+    if (j == 0) {
+      fetch_rows<T, D, WHOLE, false>(nk, pk, a.k_row, a.ad, o, c0 + 16 * l.w, q.lo, l);
+      fetch_rows<T, D, WHOLE, true>(nv, pv, a.v_row, a.cd, o, c0 + 16 * l.w, q.lo, l);
     }
-    bool have_state = from != nullptr;
+  };
+  if (q.lo < q.hi) fetch(first, 0);
+  const float* from = q.began ? a.cut_state + ((int64_t)(q.before - 1) * a.H + h0) * state
+                      : a.init ? a.init + ((int64_t)q.b * a.H + h0) * state
+                               : nullptr;
+  bool have_state = from != nullptr;
+  State<D> st[GROUP];
+  Powers pw[GROUP];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int vt = 0; vt < VT; ++vt) {
-        const int col = 16 * (w * VT + vt) + n;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * kt + 4 * g + r;
-          st[kt][vt][r] = from && row < a.ad && col < a.cd ? from[row * step_r + col * step_c] * times : 0.0f;
-        }
-      }
+  for (int j = 0; j < GROUP; ++j) {
+    load_state<D>(st[j], own && from ? from + j * state : nullptr, a.ad, a.cd, false, q.began ? 1.0f : a.init_scale, l);
+    if (SCALED && have_state) put_max<D>(s_max[j], st[j], l);
+    pw[j].set(decay_exponent(a.log_decay, h0 + j), l, a.scale, 1);
+  }
 
-    Pack<T, 8> rb[PACKS], rc[PACKS];
-    Frag<T> qa[KS], qn[KS];
-    auto fetch = [&](int64_t c0) {
+  for (int32_t c0 = first; c0 < q.hi; c0 += kChunk) {
+    const int skip = max(q.lo - c0, 0);
+    const bool needed = c0 + kChunk < q.hi || (!q.goes_on && a.final_state);
+    const bool there = 16 * l.w + l.n >= skip;
+    const int64_t row = o.row(max(c0 + 16 * l.w + l.n, q.lo));
+    Rows<D> acc_v, acc_k;  // of one head: live one after the other
 #pragma unroll
-      for (int i = 0; i < PACKS; ++i) {
-        const int idx = threadIdx.x + i * kAttnThreads, r = idx / (D / 8), c = idx % (D / 8) * 8;
-        const bool in = c0 + r < hi;
-        const int64_t row = o.row(c0 + r);
-        rb[i] = load_some<T, 8>(pb + row * a.b_row + c, in ? a.ad - c : 0);
-        rc[i] = load_some<T, 8>(pc + row * a.c_row + c, in ? a.cd - c : 0);
+    for (int j = 0; j < GROUP; ++j) {
+      __syncthreads();  // what was in LDS has been read
+      put_tile<T, D, WHOLE>(s_q, rq, a.ad, skip);
+      put_tile<T, D, WHOLE>(s_d, rd, a.cd, skip);
+      if (j == 0) {
+        take_rows<T, D, WHOLE, false>(fk, nk, a.ad, l);
+        take_rows<T, D, WHOLE, true>(fv, nv, a.cd, l);
       }
-      if constexpr (!STATE_ONLY) {
-        const int64_t p = c0 + 16 * w + n;
-        const int64_t row = o.row(p);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const int c = 32 * s + 8 * g;
-          const Pack<T, 8> q = load_some<T, 8>(pa + row * a.a_row + c, p < hi ? a.ad - c : 0);
-          __builtin_memcpy(&qn[s], &q, sizeof(q));
-        }
-      }
-    };
-    if (lo < hi) fetch(lo);
-
-    for (int64_t c0 = lo; c0 < hi; c0 += kChunk) {
-      const int len = (int)min((int64_t)kChunk, hi - c0);
-      __syncthreads();  // the chunk before has been read
-#pragma unroll
-      for (int i = 0; i < PACKS; ++i) {
-        const int idx = threadIdx.x + i * kAttnThreads, r = idx / (D / 8), c = idx % (D / 8) * 8;
-        __builtin_memcpy(__builtin_assume_aligned(s_b + r * SD + c, 16), &rb[i], sizeof(rb[i]));
-        __builtin_memcpy(__builtin_assume_aligned(s_c + r * SD + c, 16), &rc[i], sizeof(rc[i]));
-      }
-      if constexpr (!STATE_ONLY) {
-#pragma unroll
-        for (int s = 0; s < KS; ++s) qa[s] = qn[s];
-        if (have_state && owns_state) {
-#pragma unroll
-          for (int vt = 0; vt < VT; ++vt) {
-            const int col = 16 * (w * VT + vt) + n;
-            float shrink = 1.0f;
-            if constexpr (SCALED) {
-              float m = 0.0f;
-#pragma unroll
-              for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) m = fmaxf(m, __builtin_fabsf(st[kt][vt][r]));
-              m = fmaxf(m, __shfl_xor(m, 16));
-              m = fmaxf(m, __shfl_xor(m, 32));
-              const int ex = m > 0.0f && m < 3.0e38f ? max(-100, min(100, __builtin_amdgcn_frexp_expf(m))) : 0;
-              shrink = __builtin_ldexpf(1.0f, -ex);
-              if (g == 0) s_scale[col] = __builtin_ldexpf(1.0f, ex);
-            }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-              Pack<T, 4> q;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) q.v[r] = (T)(SCALED ? st[kt][vt][r] * shrink : st[kt][vt][r]);
-              __builtin_memcpy(__builtin_assume_aligned(s_s + col * SD + 16 * kt + 4 * g, 4 * sizeof(T)), &q, sizeof(q));
-            }
-          }
-        }
-      }
+      const int ex = SCALED && have_state ? copy_exponent(s_max[j]) : 0;
+      if (have_state && own) put_state<T, D>(s_s, st[j], __builtin_ldexpf(1.0f, -ex), l);
       __syncthreads();
-      if (c0 + kChunk < hi) fetch(c0 + kChunk);
-
-      if (!STATE_ONLY && 16 * w < len) {
-        f32x4 acc[KT];
-#pragma unroll
-        for (int t = 0; t < KT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (have_state) {
-#pragma unroll
-          for (int t = 0; t < KT; ++t) {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) acc[t] = mma(load_rows(s_s, SD, 16 * t, 32 * s), qa[s], acc[t]);
-            if constexpr (SCALED) {
-              f32x4 sc;
-              __builtin_memcpy(&sc, __builtin_assume_aligned(s_scale + 16 * t + 4 * g, 16), 16);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) acc[t][r] *= sc[r];
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][r] *= fade_in;
-          }
+      if (j + 1 < GROUP)
+        fetch(c0, j + 1);
+      else if (c0 + kChunk < q.hi)
+        fetch(c0 + kChunk, 0);
+      if (16 * l.w + 15 >= skip) {
+        const float fade_in = have_state ? __builtin_ldexpf(pw[j].of(max(16 * l.w + l.n - skip, 0)) * a.scale, ex) : 0.0f;
+        if (j == 0) clear<D>(acc_v);
+        if (have_state) add_state_product<T, D, false>(acc_v, s_s, fk, fade_in);
+        add_pairs<T, D, false>(acc_v, s_q, s_d, fk, pw[j], l);
+        if (j == GROUP - 1 && there) {
+          if (a.parts)
+            store_rows<WHOLE, D>(a.part_v + (row * groups + u) * a.cd, acc_v, a.cd);
+          else
+            store_rows<WHOLE, D>(static_cast<T*>(a.dv) + row * a.dv_row + (int64_t)hk * a.dv_head, acc_v, a.cd);
         }
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-          if (2 * s2 > w) continue;
-          f32x4 p[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            p[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const int j = 2 * s2 + u;
-            if (j > w) continue;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) p[u] = mma(load_rows(s_b, SD, 16 * j, 32 * s), qa[s], p[u]);
-            if (j == w) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r) p[u][r] = n >= 4 * g + r ? p[u][r] * diag[r] : 0.0f;
-            } else {
-              const float f = w - j == 1 ? gap[0] : w - j == 2 ? gap[1] : gap[2];
-#pragma unroll
-              for (int r = 0; r < 4; ++r) p[u][r] *= off[r] * f;
-            }
-          }
-          Frag<T> pf;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            pf.v[r] = (T)p[0][r];
-            pf.v[4 + r] = (T)p[1][r];
-          }
-#pragma unroll
-          for (int t = 0; t < KT; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
-        }
-        if (16 * w + n < len) {
-          const int64_t row = o.row(c0 + 16 * w + n);
-          if (a.out_f32) {
-            float* out = static_cast<float*>(a.out) + row * a.o_row + h * a.o_head;
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-              Pack<float, 4> q;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) q.v[r] = acc[t][r];
-              store_some<float, 4>(out + 16 * t + 4 * g, q, a.cd - 16 * t - 4 * g);
-            }
-          } else {
-            T* out = static_cast<T*>(a.out) + row * a.o_row + h * a.o_head;
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-              Pack<T, 4> q;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) q.v[r] = (T)acc[t][r];
-              store_some<T, 4>(out + 16 * t + 4 * g, q, a.cd - 16 * t - 4 * g);
-            }
-          }
+        if (j == 0) clear<D>(acc_k);
+        if (have_state) add_state_product<T, D, true>(acc_k, s_s, fv, fade_in);
+        add_pairs<T, D, true>(acc_k, s_d, s_q, fv, pw[j], l);
+        if (j == GROUP - 1 && there) {
+          if (a.parts)
+            store_rows<WHOLE, D>(a.part_k + (row * groups + u) * a.ad, acc_k, a.ad);
+          else
+            store_rows<WHOLE, D>(static_cast<T*>(a.dk) + row * a.dk_row + (int64_t)hk * a.dk_head, acc_k, a.ad);
         }
       }
-
-      // the state after the chunk, where something reads it
-      if (owns_state && (c0 + kChunk < hi || (STATE_ONLY ? goes_on : (!goes_on && a.final_state)))) {
-        float fade = fade_chunk;
-        if (len < kChunk) fade = power(len);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int vt = 0; vt < VT; ++vt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) st[kt][vt][r] *= fade;
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-          if (32 * s2 >= len) continue;
-          Frag<T> hi_part[VT], lo_part[VT], end_part[VT];
-#pragma unroll
-          for (int vt = 0; vt < VT; ++vt) {
-            const Frag<T> c = load_cols(s_c, SD, 32 * s2, 16 * (w * VT + vt));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float f = left[s2][e];
-              if (len < kChunk) f = power(max(len - 1 - (32 * s2 + (e < 4 ? 0 : 12) + 4 * g + e), 0) + late);
-              float x = (float)c.v[e] * f;
-              // the product as rounded to fp32: a multiply fused with one of its two conversions to fp16, but not with
-              // the other, would leave the parts a step of fp16 apart where x lies next to a tie
-              if constexpr (SCALED) asm("" : "+v"(x));
-              hi_part[vt].v[e] = (T)x;
-              if constexpr (HALF) {
-                const float rest = x - (float)hi_part[vt].v[e];
-                lo_part[vt].v[e] = (T)rest;
-                if constexpr (THIRD) end_part[vt].v[e] = (T)(rest - (float)lo_part[vt].v[e]);
-              }
-            }
-          }
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            const Frag<T> bk = load_cols(s_b, SD, 32 * s2, 16 * kt);
-#pragma unroll
-            for (int vt = 0; vt < VT; ++vt) {
-              st[kt][vt] = mma(bk, hi_part[vt], st[kt][vt]);
-              if constexpr (HALF) st[kt][vt] = mma(bk, lo_part[vt], st[kt][vt]);
-              if (THIRD && a.final_state) st[kt][vt] = mma(bk, end_part[vt], st[kt][vt]);
-            }
-          }
-        }
+      if (needed) {
+        if (own) update_state<T, D>(st[j], s_q, s_d, pw[j], skip ? pw[j].of(kChunk - skip) : pw[j].fade_chunk, a.exact_state, l);
+        if constexpr (SCALED) put_max<D>(s_max[j], st[j], l);
       }
-      have_state = true;
     }
-
-    float* to = nullptr;
-    float scaled = 1.0f;
-    if (STATE_ONLY) {
-      to = a.seg_state + ((int64_t)unit * a.H + h) * a.ad * a.cd;
-    } else if (!goes_on && a.final_state) {
-      to = a.final_state + ((int64_t)b * a.H + h) * a.ad * a.cd;
-      scaled = a.final_scale;
-    }
-    if (to && owns_state) {
+    have_state = true;
+  }
+  if (!q.goes_on && a.final_state && own) {
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int vt = 0; vt < VT; ++vt) {
-          const int col = 16 * (w * VT + vt) + n;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int row = 16 * kt + 4 * g + r;
-            if (row < a.ad && col < a.cd) to[(int64_t)row * a.cd + col] = st[kt][vt][r] * scaled;
-          }
-        }
-    }
-    if (goes_on) break;
+    for (int j = 0; j < GROUP; ++j)
+      store_state<D>(a.final_state + ((int64_t)q.b * a.H + h0 + j) * state, st[j], a.ad, a.cd, a.final_scale, l);
   }
 }
 
 // Instances by the wider of the two dims: 32, 64 or 128, the rest zeros.
-template <typename T>
-hipError_t attention_of(const AttnArgs& a, bool state_only, hipStream_t st) {
+template <typename T, bool WHOLE>
+void launch_walk(const AttnArgs& a, bool state_only, hipStream_t st) {
   const int wide = a.ad > a.cd ? a.ad : a.cd;
-  const dim3 grid((uint32_t)((a.segments ? a.segments : a.B) * (int64_t)a.H));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kAttnThreads), 0, st, a); };
+  const dim3 grid((uint32_t)((state_only ? a.cuts : a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
   if (wide <= 32)
-    state_only ? go(attention_kernel<T, 32, true>) : go(attention_kernel<T, 32, false>);
+    state_only ? go(attention_state_kernel<T, 32, WHOLE>) : go(attention_kernel<T, 32, WHOLE>);
   else if (wide <= 64)
-    state_only ? go(attention_kernel<T, 64, true>) : go(attention_kernel<T, 64, false>);
+    state_only ? go(attention_state_kernel<T, 64, WHOLE>) : go(attention_kernel<T, 64, WHOLE>);
   else
-    state_only ? go(attention_kernel<T, 128, true>) : go(attention_kernel<T, 128, false>);
+    state_only ? go(attention_state_kernel<T, 128, WHOLE>) : go(attention_kernel<T, 128, WHOLE>);
+}
+
+template <typename T>
+hipError_t walk_of(const AttnArgs& a, bool state_only, hipStream_t st) {
+  if (a.ad % 8 == 0 && a.cd % 8 == 0)
+    launch_walk<T, true>(a, state_only, st);
+  else
+    launch_walk<T, false>(a, state_only, st);
+  return hipGetLastError();
+}
+
+template <typename T, bool WHOLE>
+void launch_grad(const AttnGradArgs& a, hipStream_t st) {
+  const int wide = a.ad > a.cd ? a.ad : a.cd;
+  const dim3 grid((uint32_t)((a.cuts + a.B) * (int64_t)(a.H / a.group))), block(kAttnThreads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
+  if (wide <= 32)
+    a.group == 4 ? go(attention_grad_kernel<T, 32, 4, WHOLE>) : a.group == 2 ? go(attention_grad_kernel<T, 32, 2, WHOLE>)
+                                                                             : go(attention_grad_kernel<T, 32, 1, WHOLE>);
+  else if (wide <= 64)
+    a.group == 2 ? go(attention_grad_kernel<T, 64, 2, WHOLE>) : go(attention_grad_kernel<T, 64, 1, WHOLE>);
+  else
+    go(attention_grad_kernel<T, 128, 1, WHOLE>);
+}
+
+template <typename T>
+hipError_t grad_of(const AttnGradArgs& a, hipStream_t st) {
+  if (a.ad % 8 == 0 && a.cd % 8 == 0)
+    launch_grad<T, true>(a, st);
+  else
+    launch_grad<T, false>(a, st);
   return hipGetLastError();
 }
 

@@ -52,14 +52,9 @@ struct RotaryArgs {
 
 hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t st);
 
-// out_i = scale * sum_{j <= i} lambda^(i-j) (a_i . b_j) c_j + lambda^(i+1-late) scale_in a_i . init
-// over each sequence, rows counted from its end if `reversed`.  The forward
-// pass is (q, k, v), the gradients are (dout, v, k) and, reversed and with
-// `late`, (k, q, dout) and (v, dout, q).
-struct AttnArgs {
-  const void *a, *b, *c;
-  void* out;
-  int64_t a_row, a_head, b_row, b_head, c_row, c_head, o_row, o_head;
+// What the walks over ragged sequences share.  Positions may run backwards;
+// `ad` and `cd` are the state's rows and columns.
+struct AttnWalk {
   const float* log_decay;
   const int64_t* offsets;
   const float* init;      // [B][H][ad][cd], or [B][H][cd][ad] where init_swapped; null: zeros
@@ -67,27 +62,53 @@ struct AttnArgs {
   int32_t* fault;
   int64_t rows;
   int32_t B, H;
-  int32_t a_div, b_div, c_div;  // head h of the operator is head h / div of the operand
-  int32_t ad, cd;               // dims of a and b, of c and out
-  int32_t reversed;             // 0, 1: also `late`
+  int32_t ad, cd;
+  int32_t reversed;
   int32_t init_swapped;
-  int32_t out_f32;              // out holds fp32 whatever the type
+  int32_t exact_state;    // the state is an output: as exact as fp32
   float scale;
   float init_scale, final_scale;  // the state is carried divided by these
-  // a call whose sequences are cut into segments
-  int32_t segments;             // 0: one workgroup a sequence and head
-  float* seg_state;             // [segments][H][ad][cd]
-  int32_t* seg_fresh;           // [segments] a sequence begins inside the segment
+  // sequences longer than (rows in use) / cuts are cut, into parts of at least `least` rows; 0: none is
+  int32_t cuts;
+  int32_t least;          // whole chunks
+  float* cut_state;       // [cuts][H][ad][cd]: the state at the end of every part that goes on
+  int32_t* cut_rows;      // [cuts] its rows, 0 where it begins its sequence, -1: there is no such part
 };
 
-hipError_t launch_attention(const AttnArgs& a, int32_t dtype, hipStream_t st);
+// out_i = scale * sum_{j <= i} lambda^(i-j) (a_i . b_j) c_j + scale * lambda^(i+1) a_i . init over each sequence: the
+// forward pass is (q, k, v), dq is (dout, v, k).  The state alone (of b and c) is also made backwards.
+struct AttnArgs : AttnWalk {
+  const void *a, *b, *c;
+  void* out;
+  int64_t a_head, b_head, c_head, o_head;
+  int32_t a_row, b_row, c_row, o_row;
+  int32_t a_div, b_div, c_div;  // head h of the operator is head h / div of the operand
+};
 
-struct AttnSumArgs {   // out[r][g] = sum over the group's heads of part[r][g * group + i], fp32 [rows][H][dim]
+struct AttnGradArgs : AttnWalk {  // dv and dk, backwards; the state's rows are q's, its columns dout's
+  const void *q, *dout, *k, *v;
+  void *dk, *dv;
+  int64_t q_head, d_head, k_head, v_head, dk_head, dv_head;
+  int32_t q_row, d_row, k_row, v_row, dk_row, dv_row;
+  int32_t kv_div;         // heads that share keys and values
+  int32_t group;          // of them a workgroup's: 1, 2 or 4
+  int32_t parts;          // not all of them: the sums go to part_k and part_v, fp32 [rows][H / group][dim]
+  float *part_k, *part_v;
+};
+
+constexpr int32_t kAttnGroupMost(int32_t wide) { return wide <= 32 ? 4 : wide <= 64 ? 2 : 1; }
+
+hipError_t launch_attention(const AttnArgs& a, int32_t dtype, hipStream_t st);
+// states: the arguments of the walk that makes the cut sequences' states, (., q, dout) reversed
+hipError_t launch_attention_grad(const AttnGradArgs& a, const AttnArgs& states, int32_t dtype, hipStream_t st);
+
+struct AttnSumArgs {   // out[r][g] = sum over the group's parts of part[r][g * group + i], fp32 [rows][parts][dim]
   const float* part;
   void* out;
-  int64_t out_row, out_head, rows;
+  int64_t out_head, rows;
   const int64_t* offsets;
-  int32_t B, H, group, dim;
+  int32_t out_row;
+  int32_t B, parts, group, dim;
 };
 hipError_t launch_attention_sum(const AttnSumArgs& a, int32_t dtype, hipStream_t st);
 
@@ -190,6 +211,20 @@ __device__ __forceinline__ float group_sum(float x) {
     x = __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
   }
   return x;
+}
+
+// Largest value of a wave, known to all lanes.
+__device__ __forceinline__ float group_max(float x) {
+  x = fmaxf(x, dpp_xor_step(x, 1));
+  x = fmaxf(x, dpp_xor_step(x, 2));
+  x = fmaxf(x, dpp_xor_step(x, 4));
+  x = fmaxf(x, dpp_xor_step(x, 8));
+  unsigned i = __builtin_bit_cast(unsigned, x);
+  const auto p = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+  x = fmaxf(__builtin_bit_cast(float, (unsigned)p[0]), __builtin_bit_cast(float, (unsigned)p[1]));
+  i = __builtin_bit_cast(unsigned, x);
+  const auto q = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+  return fmaxf(__builtin_bit_cast(float, (unsigned)q[0]), __builtin_bit_cast(float, (unsigned)q[1]));
 }
 
 // Rows in use: the device's count, clamped to the array.

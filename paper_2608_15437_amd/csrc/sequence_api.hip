@@ -30,7 +30,7 @@ bool rows_ok(const mmbev_rows_t& t, int64_t rows, int32_t width, int32_t dtype, 
 bool heads_ok(const mmbev_heads_t& t, int64_t rows, int32_t heads, int32_t dim, int32_t dtype) {
   if (!t.data) return rows == 0;
   if (!aligned(t.data, size_of(dtype)) || t.row_stride < 0 || t.head_stride < 0) return false;
-  if (t.row_stride >= ((int64_t)1 << 40) || t.head_stride >= ((int64_t)1 << 40)) return false;
+  if (t.row_stride > INT32_MAX || t.head_stride >= ((int64_t)1 << 40)) return false;
   if (heads > 1 && t.head_stride < dim) return false;
   // heads inside a row, or rows inside a head
   const int64_t row = (int64_t)(heads - 1) * t.head_stride + dim;
@@ -73,17 +73,23 @@ mmbev_status_t status_of(hipError_t e) { return e == hipSuccess ? MMBEV_OK : MMB
 
 // ------------------------------------------------------------ attention
 
-// Workgroups that fill the chip: a sequence and head each where there are
-// enough of those; otherwise the rows in use are cut into as many segments as
-// make about this many with the heads.
-constexpr int64_t kAttnUnits = 768;
-// Sequences no longer than this are walked whole: cutting them would take
-// two more launches than it saves.
+// A sequence and head is a workgroup's work, but one that is longer than the
+// rows' share of kAttnUnits workgroups is cut into parts.
+#ifndef UNITS
+#define UNITS 768
+#endif
+constexpr int64_t kAttnUnits = UNITS;
+// None is cut where none can be longer than this (it would take two more
+// launches than it saves), nor among more sequences than a workgroup can look
+// through in passing.
 constexpr int64_t kAttnWhole = 512;
+constexpr int32_t kAttnCutSequences = 1024;
 
 struct AttnPlan {
-  int32_t segments;
-  size_t off_fresh, off_state, off_part, total;
+  int32_t cuts;       // of the forward walks
+  int32_t grad_cuts;  // of the backward walk
+  int32_t group;      // its heads a workgroup
+  size_t off_rows, off_state, off_part, total;
 };
 
 mmbev_status_t attention_ok(const mmbev_attention_t* t, bool step) {
@@ -97,26 +103,47 @@ mmbev_status_t attention_ok(const mmbev_attention_t* t, bool step) {
   return MMBEV_OK;
 }
 
+// Heads that one workgroup of the backward walk takes of those that share keys and values.
+int32_t grad_group(const mmbev_attention_t* t) {
+  const int32_t shared = t->heads / t->kv_heads;
+  int32_t group = kAttnGroupMost(std::max(t->key_dim, t->value_dim));
+  while (shared % group != 0) group /= 2;
+  return group;
+}
+
+// Rows of a part, at least: enough that its state is a small part of what is read for them.
+int32_t least_rows(const mmbev_attention_t* t) { return std::max(t->key_dim, t->value_dim) <= 64 ? 128 : 256; }
+
+int32_t cuts_for(const mmbev_attention_t* t, int64_t heads) {
+  const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
+  if (longest <= kAttnWhole || t->num_sequences > kAttnCutSequences) return 0;
+  const int64_t least = least_rows(t);
+  return (int32_t)std::max<int64_t>(1, std::min((kAttnUnits + heads - 1) / heads, (t->rows + least - 1) / least));
+}
+
 AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   AttnPlan p{};
-  const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
-  const int64_t units = (int64_t)t->num_sequences * t->heads;
-  if (units < kAttnUnits && longest > kAttnWhole)
-    p.segments = (int32_t)std::max<int64_t>(1, std::min((kAttnUnits + t->heads - 1) / t->heads, (t->rows + 63) / 64));
+  p.cuts = cuts_for(t, t->heads);
+  int32_t most = p.cuts;
+  if (backward) {
+    p.group = grad_group(t);
+    p.grad_cuts = cuts_for(t, t->heads / p.group);
+    most = std::max(most, p.grad_cuts);
+  }
   size_t at = 0;
-  p.off_fresh = at;
-  at = align256(at + (size_t)p.segments * 4);
+  p.off_rows = at;
+  at = align256(at + (size_t)most * 4);
   p.off_state = at;
-  at = align256(at + (size_t)p.segments * t->heads * t->key_dim * t->value_dim * 4);
+  at = align256(at + (size_t)most * t->heads * t->key_dim * t->value_dim * 4);
   p.off_part = at;
-  if (backward && t->heads != t->kv_heads)
-    at = align256(at + (size_t)t->rows * t->heads * std::max(t->key_dim, t->value_dim) * 4);
+  if (backward && t->heads != t->kv_heads * p.group)
+    at = align256(at + (size_t)t->rows * (t->heads / p.group) * (t->key_dim + t->value_dim) * 4);
   p.total = std::max<size_t>(at, 256);
   return p;
 }
 
-AttnArgs attention_args(const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, const AttnPlan& p, char* ws) {
-  AttnArgs a{};
+void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, int32_t cuts, const AttnPlan& p,
+              char* ws) {
   a.log_decay = log_decay;
   a.offsets = offsets;
   a.rows = t->rows;
@@ -124,17 +151,17 @@ AttnArgs attention_args(const mmbev_attention_t* t, const float* log_decay, cons
   a.H = t->heads;
   a.scale = t->scale;
   a.init_scale = a.final_scale = 1.0f;
-  a.segments = p.segments;
-  a.seg_fresh = (int32_t*)(ws + p.off_fresh);
-  a.seg_state = (float*)(ws + p.off_state);
-  return a;
+  a.cuts = cuts;
+  a.least = least_rows(t);
+  a.cut_rows = (int32_t*)(ws + p.off_rows);
+  a.cut_state = (float*)(ws + p.off_state);
 }
 
-void put(const mmbev_heads_t& t, int32_t div, const void** data, int64_t* row, int64_t* head, int32_t* out_div) {
+template <typename P, typename R>
+void put(const mmbev_heads_t& t, P** data, R* row, int64_t* head) {
   *data = t.data;
-  *row = t.row_stride;
+  *row = (R)t.row_stride;
   *head = t.head_stride;
-  *out_div = div;
 }
 
 bool workspace_ok(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, 256) && bytes >= need; }
@@ -307,18 +334,19 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t 
     if (in && in == out.data) return MMBEV_ERR_INVALID_ARG;
   const AttnPlan p = attention_plan(t, false);
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
-  AttnArgs a = attention_args(t, log_decay, offsets, p, (char*)workspace);
-  const int32_t group = t->heads / t->kv_heads;
-  put(q, 1, &a.a, &a.a_row, &a.a_head, &a.a_div);
-  put(k, group, &a.b, &a.b_row, &a.b_head, &a.b_div);
-  put(v, group, &a.c, &a.c_row, &a.c_head, &a.c_div);
+  AttnArgs a{};
+  put_walk(a, t, log_decay, offsets, p.cuts, p, (char*)workspace);
+  put(q, &a.a, &a.a_row, &a.a_head);
+  put(k, &a.b, &a.b_row, &a.b_head);
+  put(v, &a.c, &a.c_row, &a.c_head);
+  put(out, &a.out, &a.o_row, &a.o_head);
+  a.a_div = 1;
+  a.b_div = a.c_div = t->heads / t->kv_heads;
   a.ad = t->key_dim;
   a.cd = t->value_dim;
-  a.out = out.data;
-  a.o_row = out.row_stride;
-  a.o_head = out.head_stride;
   a.init = initial_state;
   a.final_state = final_state;
+  a.exact_state = final_state != nullptr;
   a.fault = fault;
   return status_of(launch_attention(a, t->dtype, (hipStream_t)stream));
 }
@@ -353,60 +381,61 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   hipStream_t st = (hipStream_t)stream;
 
   // dq: the forward walk of (dout, v, k), whose state is the transposed one
-  AttnArgs a = attention_args(t, log_decay, offsets, p, ws);
-  put(dout, 1, &a.a, &a.a_row, &a.a_head, &a.a_div);
-  put(v, group, &a.b, &a.b_row, &a.b_head, &a.b_div);
-  put(k, group, &a.c, &a.c_row, &a.c_head, &a.c_div);
+  AttnArgs a{};
+  put_walk(a, t, log_decay, offsets, p.cuts, p, ws);
+  put(dout, &a.a, &a.a_row, &a.a_head);
+  put(v, &a.b, &a.b_row, &a.b_head);
+  put(k, &a.c, &a.c_row, &a.c_head);
+  put(dq, &a.out, &a.o_row, &a.o_head);
+  a.a_div = 1;
+  a.b_div = a.c_div = group;
   a.ad = t->value_dim;
   a.cd = t->key_dim;
   a.init = initial_state;
   a.init_swapped = 1;
-  a.out = dq.data;
-  a.o_row = dq.row_stride;
-  a.o_head = dq.head_stride;
   a.fault = fault;
   if (launch_attention(a, T, st) != hipSuccess) return MMBEV_ERR_HIP;
 
   // dv and dk: backwards, the carried state that of q and dout, divided by scale
-  for (int which = 0; which < 2; ++which) {
-    const mmbev_heads_t& to = which ? dk : dv;
-    a = attention_args(t, log_decay, offsets, p, ws);
-    a.reversed = 1;
-    put(which ? v : k, group, &a.a, &a.a_row, &a.a_head, &a.a_div);
-    put(which ? dout : q, 1, &a.b, &a.b_row, &a.b_head, &a.b_div);
-    put(which ? q : dout, 1, &a.c, &a.c_row, &a.c_head, &a.c_div);
-    a.ad = which ? t->value_dim : t->key_dim;
-    a.cd = which ? t->key_dim : t->value_dim;
-    a.init = dfinal_state;
-    a.init_swapped = which;
-    a.init_scale = 1.0f / t->scale;
-    a.final_scale = t->scale;
-    a.final_state = which ? nullptr : dinitial_state;
-    if (group == 1) {
-      a.out = to.data;
-      a.o_row = to.row_stride;
-      a.o_head = to.head_stride;
-    } else {
-      a.out = ws + p.off_part;
-      a.o_row = (int64_t)H * a.cd;
-      a.o_head = a.cd;
-      a.out_f32 = 1;
-    }
-    if (launch_attention(a, T, st) != hipSuccess) return MMBEV_ERR_HIP;
-    if (group > 1 && R > 0) {
-      AttnSumArgs s{};
-      s.part = (const float*)(ws + p.off_part);
-      s.out = to.data;
-      s.out_row = to.row_stride;
-      s.out_head = to.head_stride;
-      s.rows = R;
-      s.offsets = offsets;
-      s.B = t->num_sequences;
-      s.H = H;
-      s.group = group;
-      s.dim = a.cd;
-      if (launch_attention_sum(s, T, st) != hipSuccess) return MMBEV_ERR_HIP;
-    }
+  AttnGradArgs b{};
+  put_walk(b, t, log_decay, offsets, p.grad_cuts, p, ws);
+  b.reversed = 1;
+  put(q, &b.q, &b.q_row, &b.q_head);
+  put(dout, &b.dout, &b.d_row, &b.d_head);
+  put(k, &b.k, &b.k_row, &b.k_head);
+  put(v, &b.v, &b.v_row, &b.v_head);
+  put(dk, &b.dk, &b.dk_row, &b.dk_head);
+  put(dv, &b.dv, &b.dv_row, &b.dv_head);
+  b.ad = t->key_dim;
+  b.cd = t->value_dim;
+  b.init = dfinal_state;
+  b.init_scale = 1.0f / t->scale;
+  b.final_state = dinitial_state;
+  b.final_scale = t->scale;
+  b.exact_state = dinitial_state != nullptr;
+  b.kv_div = group;
+  b.group = p.group;
+  b.parts = group != p.group;
+  const int32_t parts = H / p.group;
+  b.part_k = (float*)(ws + p.off_part);
+  b.part_v = b.part_k + (size_t)R * parts * t->key_dim;
+  AttnArgs s{};
+  static_cast<AttnWalk&>(s) = b;
+  put(q, &s.b, &s.b_row, &s.b_head);
+  put(dout, &s.c, &s.c_row, &s.c_head);
+  s.b_div = s.c_div = 1;
+  if (launch_attention_grad(b, s, T, st) != hipSuccess) return MMBEV_ERR_HIP;
+  for (int which = 0; b.parts && which < 2; ++which) {
+    AttnSumArgs u{};
+    u.part = which ? b.part_v : b.part_k;
+    put(which ? dv : dk, &u.out, &u.out_row, &u.out_head);
+    u.rows = R;
+    u.offsets = offsets;
+    u.B = t->num_sequences;
+    u.parts = parts;
+    u.group = group / p.group;
+    u.dim = which ? t->value_dim : t->key_dim;
+    if (launch_attention_sum(u, T, st) != hipSuccess) return MMBEV_ERR_HIP;
   }
   return MMBEV_OK;
 }
@@ -424,10 +453,9 @@ mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* t, mmbev_hea
   if (t->rows > 0 && num_slots > 0 && (!state || !aligned(state, 16))) return MMBEV_ERR_INVALID_ARG;
   if (!slots && num_slots < t->rows) return MMBEV_ERR_INVALID_ARG;
   AttnStepArgs a{};
-  int32_t unused;
-  put(q, 1, &a.q, &a.q_row, &a.q_head, &unused);
-  put(k, 1, &a.k, &a.k_row, &a.k_head, &unused);
-  put(v, 1, &a.v, &a.v_row, &a.v_head, &unused);
+  put(q, &a.q, &a.q_row, &a.q_head);
+  put(k, &a.k, &a.k_row, &a.k_head);
+  put(v, &a.v, &a.v_row, &a.v_head);
   a.out = out.data;
   a.o_row = out.row_stride;
   a.o_head = out.head_stride;
