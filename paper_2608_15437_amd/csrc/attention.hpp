@@ -154,47 +154,117 @@ struct Part {
   bool goes_on;    // and after it
 };
 
-// Sequences longer than `rows in use / a.cuts` are cut into equal parts of at
-// most that, in whole chunks; there are at most a.cuts + B parts, of which at
-// most a.cuts go on.  Finds part `index` in the order of positions, counting
-// all parts or those that go on; false if there are fewer.  Every wave looks
-// for itself, 64 sequences at a time: a load, a sum over the lanes and a
-// ballot (about a microsecond for 64 sequences).
+// The r-th longest of up to 256 sequences that are not longer than `most`
+// (ties: the first ones first), found bit by bit: the largest length that more
+// than r of them reach.  False: there are no more than r.
+
+__device__ __forceinline__ bool find_longest(Part& q, const Order& o, int32_t most, int32_t r) {
+  constexpr int N = kOrderedSequences / 64;
+  const int lane = threadIdx.x & 63;
+  int32_t n[N], s0[N];
+  int32_t there = 0;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    n[u] = -1;
+    s0[u] = 0;
+    if (64 * u < o.B) {
+      const int32_t k = 64 * u + lane;
+      s0[u] = o.bound(min(k, o.B - 1));
+      const int32_t len = max(o.bound(min(k, o.B - 1) + 1) - s0[u], 0);
+      n[u] = k < o.B && len <= most ? len : -1;
+    }
+    there += __popcll(__ballot(n[u] >= 0));
+  }
+  if (r >= there) return false;
+  auto reach = [&](int32_t len) {
+    int32_t c = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) c += __popcll(__ballot(n[u] >= len));
+    return c;
+  };
+  int32_t len = 0;
+  for (int32_t bit = most > 0 ? 1 << (31 - __builtin_clz(most)) : 0; bit; bit >>= 1)
+    if (reach(len | bit) > r) len |= bit;
+  int32_t tie = r - reach(len + 1);
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const uint64_t same = __ballot(n[u] == len);
+    const int c = __popcll(same);
+    if (tie >= 0 && tie < c) {
+      const int at = __builtin_ctzll(__ballot(n[u] == len && (int32_t)count_below(same) == tie));
+      q.lo = __builtin_amdgcn_readlane(s0[u], at);
+      q.hi = q.lo + len;
+      q.b = o.sequence(64 * u + at);
+    }
+    tie -= c;
+  }
+  return true;
+}
+
+// A workgroup's share is the rows in use over a.cuts.  Sequences longer than
+// two shares are cut into equal parts of at most one, in whole chunks; the
+// others are walked whole.  There are at most a.cuts + B parts, of which at
+// most a.cuts go on.  Finds part `index`: the cut sequences' parts come first,
+// then the whole ones, the longest first where there are more than the chip
+// takes at once (so that the last ones to begin are short).  Or, `going_on`,
+// the part of that number among those that go on.  False if there are fewer.
+// Every wave looks for itself, 64 sequences at a time: loads, a sum over the
+// lanes and ballots, about a microsecond.
 __device__ __forceinline__ bool find_part(Part& q, const Order& o, const AttnWalk& a, int32_t index, bool going_on) {
+  q.before = 0;
+  q.began = q.goes_on = false;
   if (!a.cuts) {
     q.lo = o.bound(index);
     q.hi = max(o.bound(index + 1), q.lo);
     q.b = o.sequence(index);
-    q.before = 0;
-    q.began = q.goes_on = false;
     return true;
   }
   const int32_t each = (int32_t)(((int64_t)o.used + a.cuts - 1) / a.cuts);
-  const int32_t most = max((int32_t)(((int64_t)each + kChunk - 1) / kChunk * kChunk), a.least);
+  const int32_t share = max((int32_t)(((int64_t)each + kChunk - 1) / kChunk * kChunk), a.least);
+  const int32_t most = (int32_t)min((int64_t)share * 2, (int64_t)INT32_MAX);
   const int lane = threadIdx.x & 63;
-  int32_t seen = 0;
+  int32_t seen = 0, cut = 0;
   for (int32_t k0 = 0; k0 < o.B; k0 += 64) {
     const int32_t k = min(k0 + lane, o.B - 1);
-    const int32_t s0 = o.bound(k), s1 = max(o.bound(k + 1), s0);
-    const int32_t parts = max((int32_t)(((int64_t)(s1 - s0) + most - 1) / most), 1);
-    const uint32_t count = k0 + lane < o.B ? (uint32_t)(parts - (going_on ? 1 : 0)) : 0u;
-    const uint32_t upto = wave_inclusive_sum(count);
+    const int32_t s0 = o.bound(k), n = max(o.bound(k + 1) - s0, 0);
+    const uint32_t parts = k0 + lane < o.B && n > most ? (uint32_t)(((int64_t)n + share - 1) / share) : 0u;
+    const uint64_t cuts = __ballot(parts != 0);
+    if (cuts == 0) continue;
+    const uint32_t count = parts - (going_on && parts ? 1u : 0u), upto = wave_inclusive_sum(count);
     const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-    if ((uint32_t)index < seen + all) {
-      const int at = __builtin_ctzll(__ballot(seen + upto > (uint32_t)index));
-      const int32_t n0 = __builtin_amdgcn_readlane(s0, at), n1 = __builtin_amdgcn_readlane(s1, at);
-      const int32_t c = __builtin_amdgcn_readlane(parts, at);
+    if ((uint32_t)(index - seen) < all) {
+      const int at = __builtin_ctzll(__ballot(upto > (uint32_t)(index - seen)));
+      const int32_t n0 = __builtin_amdgcn_readlane(s0, at), len = __builtin_amdgcn_readlane(n, at);
+      const int32_t c = __builtin_amdgcn_readlane((int)parts, at);
       const int32_t j = index - seen - (int32_t)__builtin_amdgcn_readlane((int)(upto - count), at);
-      const int32_t step = (int32_t)((((int64_t)(n1 - n0) + c - 1) / c + kChunk - 1) / kChunk * kChunk);  // <= most
+      const int32_t step = (int32_t)((((int64_t)len + c - 1) / c + kChunk - 1) / kChunk * kChunk);  // <= share
       q.lo = n0 + j * step;
-      q.hi = j + 1 < c ? min(q.lo + step, n1) : n1;
+      q.hi = j + 1 < c ? q.lo + step : n0 + len;
       q.b = o.sequence(k0 + at);
-      q.before = going_on ? index : index - (k0 + at);
+      q.before = going_on ? index : index - cut - __popcll(cuts & ((1ull << at) - 1));
       q.began = j > 0 && q.before <= a.cuts;  // more parts than that go on only where the offsets break their contract
       q.goes_on = j + 1 < c;
       return true;
     }
     seen += (int32_t)all;
+    cut += __popcll(cuts);
+  }
+  if (going_on) return false;
+  if (a.longest_first) return find_longest(q, o, most, index - seen);
+  int32_t r = index - seen;
+  for (int32_t k0 = 0; k0 < o.B; k0 += 64) {
+    const int32_t k = min(k0 + lane, o.B - 1);
+    const int32_t s0 = o.bound(k), n = max(o.bound(k + 1) - s0, 0);
+    const uint64_t whole = __ballot(k0 + lane < o.B && n <= most);
+    const int c = __popcll(whole);
+    if (r < c) {
+      const int at = __builtin_ctzll(__ballot((whole >> lane & 1) && (int32_t)count_below(whole) == r));
+      q.lo = __builtin_amdgcn_readlane(s0, at);
+      q.hi = q.lo + __builtin_amdgcn_readlane(n, at);
+      q.b = o.sequence(k0 + at);
+      return true;
+    }
+    r -= c;
   }
   return false;
 }
@@ -552,18 +622,83 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
   }
 }
 
+// The wave's 16 rows from position `at` on, those before `lo` left out.
+//
+// 16-bit results: a lane's four elements of a tile are eight bytes, and stores
+// of 32 bytes a row cost more than the loads of all operands (128 frames: 450
+// of 1,190 us).  So two tiles' elements are exchanged among the four lanes of
+// a row, in registers, until a lane has 16 bytes and the row's lanes 64 in a
+// line; and then two such lines of a row with the row eight further, until a
+// store covers eight rows of 128 bytes, a cache line each.
 template <bool WHOLE, int D, typename T>
-__device__ __forceinline__ void store_rows(T* p, const Rows<D>& acc, int dim) {
+__device__ __forceinline__ void store_rows(T* base, int32_t stride, const Order& o, int32_t at, int32_t lo, const Rows<D>& acc, int dim) {
+  const int g = (threadIdx.x & 63) >> 4, n = threadIdx.x & 15;
+  if constexpr (sizeof(T) == 2) {
+    uint32_t line[kTiles<D> / 2][4];
 #pragma unroll
-  for (int t = 0; t < kTiles<D>; ++t) {
-    Pack<T, 4> q;
+    for (int t = 0; t < kTiles<D>; t += 2) {
+      uint32_t x[2], y[2];
+      Pack<T, 4> u, v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) q.v[r] = (T)acc[t][r];
-    const int c = 16 * t + 4 * ((threadIdx.x & 63) >> 4);
-    if constexpr (WHOLE) {
-      if (c < dim) store_pack<T, 4>(p + c, q);
+      for (int r = 0; r < 4; ++r) {
+        u.v[r] = (T)acc[t][r];
+        v.v[r] = (T)acc[t + 1][r];
+      }
+      __builtin_memcpy(x, &u, 8);
+      __builtin_memcpy(y, &v, 8);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        // lanes of g 0, 1 take tile t's elements of g and g + 2, those of g 2, 3 tile t + 1's of g - 2 and g
+        const auto a = __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false);
+        // and then neighbours: g has eighths 2g and 2g + 1 of the 32 elements
+        const auto b = __builtin_amdgcn_permlane16_swap(a[0], a[1], false, false);
+        line[t / 2][i] = b[0];
+        line[t / 2][2 + i] = b[1];
+      }
+    }
+    auto put = [&](const uint32_t (&q)[4], int32_t p, int c) {
+      if (p < lo) return;
+      T* to = base + (int64_t)o.row(p) * stride + c;
+      Pack<T, 8> r;
+      __builtin_memcpy(&r, q, 16);
+      if constexpr (WHOLE) {
+        if (c < dim) store_pack<T, 8>(to, r);
+      } else {
+        store_some<T, 8>(to, r, dim - c);
+      }
+    };
+    if constexpr (D == 32) {
+      put(line[0], at + n, 8 * g);
     } else {
-      store_some<T, 4>(p + c, q, dim - c);
+#pragma unroll
+      for (int t = 0; t < kTiles<D> / 2; t += 2) {
+        uint32_t low[4], high[4];  // of rows n % 8 and n % 8 + 8
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)line[t][i], 0x128, 0xf, 0xf, true);  // lane n ^ 8's
+          const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)line[t + 1][i], 0x128, 0xf, 0xf, true);
+          low[i] = n < 8 ? line[t][i] : y;
+          high[i] = n < 8 ? x : line[t + 1][i];
+        }
+        const int c = 32 * t + (n < 8 ? 0 : 32) + 8 * g;
+        put(low, at + (n & 7), c);
+        put(high, at + (n & 7) + 8, c);
+      }
+    }
+  } else {
+    if (at + n < lo) return;
+    T* to = base + (int64_t)o.row(at + n) * stride;
+#pragma unroll
+    for (int t = 0; t < kTiles<D>; ++t) {
+      Pack<T, 4> q;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) q.v[r] = (T)acc[t][r];
+      const int c = 16 * t + 4 * g;
+      if constexpr (WHOLE) {
+        if (c < dim) store_pack<T, 4>(to + c, q);
+      } else {
+        store_some<T, 4>(to + c, q, dim - c);
+      }
     }
   }
 }
@@ -577,10 +712,7 @@ __device__ __forceinline__ Lane lane_of() {
 }
 
 template <typename T, int D>
-#ifndef W64
-#define W64 3
-#endif
-constexpr int kWavesSimd = (D == 128 ? 2 : D == 64 ? W64 : 4) - (sizeof(T) == 4 ? 1 : 0);  // waves a SIMD, as the registers allow
+constexpr int kWavesSimd = walk_waves(sizeof(T) == 2, D);
 
 // ------------------------------------------------------ the kernels
 
@@ -686,7 +818,7 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_ke
       if (have_state)
         add_state_product<T, D, false>(acc, s_s, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
       add_pairs<T, D, false>(acc, s_b, s_c, qa, pw, l);
-      if (16 * l.w + l.n >= skip) store_rows<WHOLE, D>(po + (int64_t)o.row(c0 + 16 * l.w + l.n) * a.o_row, acc, a.cd);
+      store_rows<WHOLE, D>(po, a.o_row, o, c0 + 16 * l.w, q.lo, acc, a.cd);
     }
     // the state after the chunk, where something reads it
     if (c0 + kChunk < q.hi || (!q.goes_on && a.final_state)) {
@@ -705,7 +837,7 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_ke
 // registers.  Where GROUP is not all of them, the sums are fp32 parts that
 // attention_sum_kernel adds.
 template <typename T, int D, int GROUP, bool WHOLE>
-__global__ __launch_bounds__(kAttnThreads, (D == 128 ? (sizeof(T) == 2 ? 2 : 1) : 2)) void attention_grad_kernel(AttnGradArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_grad_kernel(AttnGradArgs a) {
   constexpr int SD = D + kRowPad<T>;
   constexpr bool SCALED = __is_same(T, f16);
   __shared__ __attribute__((aligned(16))) T s_q[kChunk * SD];
@@ -753,8 +885,7 @@ __global__ __launch_bounds__(kAttnThreads, (D == 128 ? (sizeof(T) == 2 ? 2 : 1) 
   for (int32_t c0 = first; c0 < q.hi; c0 += kChunk) {
     const int skip = max(q.lo - c0, 0);
     const bool needed = c0 + kChunk < q.hi || (!q.goes_on && a.final_state);
-    const bool there = 16 * l.w + l.n >= skip;
-    const int64_t row = o.row(max(c0 + 16 * l.w + l.n, q.lo));
+    const int32_t at = c0 + 16 * l.w;
     Rows<D> acc_v, acc_k;  // of one head: live one after the other
 #pragma unroll
     for (int j = 0; j < GROUP; ++j) {
@@ -777,20 +908,20 @@ __global__ __launch_bounds__(kAttnThreads, (D == 128 ? (sizeof(T) == 2 ? 2 : 1) 
         if (j == 0) clear<D>(acc_v);
         if (have_state) add_state_product<T, D, false>(acc_v, s_s, fk, fade_in);
         add_pairs<T, D, false>(acc_v, s_q, s_d, fk, pw[j], l);
-        if (j == GROUP - 1 && there) {
+        if (j == GROUP - 1) {
           if (a.parts)
-            store_rows<WHOLE, D>(a.part_v + (row * groups + u) * a.cd, acc_v, a.cd);
+            store_rows<WHOLE, D>(a.part_v + (int64_t)u * a.cd, groups * a.cd, o, at, q.lo, acc_v, a.cd);
           else
-            store_rows<WHOLE, D>(static_cast<T*>(a.dv) + row * a.dv_row + (int64_t)hk * a.dv_head, acc_v, a.cd);
+            store_rows<WHOLE, D>(static_cast<T*>(a.dv) + (int64_t)hk * a.dv_head, a.dv_row, o, at, q.lo, acc_v, a.cd);
         }
         if (j == 0) clear<D>(acc_k);
         if (have_state) add_state_product<T, D, true>(acc_k, s_s, fv, fade_in);
         add_pairs<T, D, true>(acc_k, s_d, s_q, fv, pw[j], l);
-        if (j == GROUP - 1 && there) {
+        if (j == GROUP - 1) {
           if (a.parts)
-            store_rows<WHOLE, D>(a.part_k + (row * groups + u) * a.ad, acc_k, a.ad);
+            store_rows<WHOLE, D>(a.part_k + (int64_t)u * a.ad, groups * a.ad, o, at, q.lo, acc_k, a.ad);
           else
-            store_rows<WHOLE, D>(static_cast<T*>(a.dk) + row * a.dk_row + (int64_t)hk * a.dk_head, acc_k, a.ad);
+            store_rows<WHOLE, D>(static_cast<T*>(a.dk) + (int64_t)hk * a.dk_head, a.dk_row, o, at, q.lo, acc_k, a.ad);
         }
       }
       if (needed) {

@@ -241,30 +241,32 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormArgs a)
   }
 }
 
-// dweight and dbias: the workgroups' partial rows added up.  A workgroup takes
-// 32 columns of the 2*width; its eight rows of threads each every eighth
-// partial row, then the eight sums in order.
-__global__ __launch_bounds__(256) void norm_weight_sum_kernel(const float* partial, int32_t parts, int32_t width,
-                                                              float* dweight, float* dbias) {
-  __shared__ float s_sum[8][33];
-  const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + col;
+// dweight and dbias: the workgroups' partial rows added up, few columns a
+// workgroup so that its threads' loads are all in flight together (32 columns
+// and eight threads a column, one after the other: 13 us for 1,024 rows).
+constexpr int kSumCols = 16, kSumParts = 64;
+
+__global__ __launch_bounds__(kSumCols * kSumParts) void norm_weight_sum_kernel(const float* partial, int32_t parts, int32_t width,
+                                                                               float* dweight, float* dbias) {
+  __shared__ float s_sum[kSumParts][kSumCols + 1];
+  const int col = threadIdx.x % kSumCols, part = threadIdx.x / kSumCols;
+  const int c = blockIdx.x * kSumCols + col, at = min(c, 2 * width - 1);
+  float x[kNormGrid / kSumParts];
+#pragma unroll
+  for (int i = 0; i < kNormGrid / kSumParts; ++i) x[i] = partial[(int64_t)min(part + i * kSumParts, parts - 1) * 2 * width + at];
   float t = 0.0f;
-  if (c < 2 * width) {
-#pragma unroll 4
-    for (int i = part; i < parts; i += 8) t += partial[(int64_t)i * 2 * width + c];
-  }
+#pragma unroll
+  for (int i = 0; i < kNormGrid / kSumParts; ++i) t += part + i * kSumParts < parts ? x[i] : 0.0f;
   s_sum[part][col] = t;
   __syncthreads();
-  if (part == 0 && c < 2 * width) {
-    t = 0.0f;
+  if (part != 0 || c >= 2 * width) return;
+  t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t += s_sum[i][col];
-    if (c < width) {
-      if (dweight) dweight[c] = t;
-    } else if (dbias) {
-      dbias[c - width] = t;
-    }
+  for (int i = 0; i < kSumParts; ++i) t += s_sum[i][col];
+  if (c < width) {
+    if (dweight) dweight[c] = t;
+  } else if (dbias) {
+    dbias[c - width] = t;
   }
 }
 
@@ -348,7 +350,8 @@ hipError_t launch_norm_backward(const NormArgs& a, int32_t dtype, hipStream_t st
                        : dtype == MMBEV_F16 ? norm_backward_of<f16>(a, s, grid, st)
                                             : norm_backward_of<bf16>(a, s, grid, st);
   if (e != hipSuccess || !a.partial) return e;
-  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((uint32_t)((2 * a.width + 31) / 32)), dim3(256), 0, st, a.partial, grid,
+  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((uint32_t)((2 * a.width + kSumCols - 1) / kSumCols)),
+                     dim3(kSumCols * kSumParts), 0, st, a.partial, grid,
                      a.width, a.dweight, a.dbias);
   return hipGetLastError();
 }

@@ -6,8 +6,9 @@
 // radians) to the Taylor polynomials of sine and cosine: terms to x^11 and
 // x^10, whose next terms are below 2^-29.
 //
-// A thread owns as many neighbouring pairs as two 16-byte accesses hold, works
-// their sines and cosines out once, and turns those pairs of several heads
+// A thread owns the neighbouring pairs of a 16-byte access (of two, where a
+// pair's elements lie apart), works their sines and cosines out once, and turns
+// those pairs of several heads
 // (the fewer rows, the fewer heads a thread, so that small calls spread out).
 // The operator moves bytes: 7 operations a pair and head beside the loads, and
 // some 50 a pair for its angle.
@@ -48,9 +49,51 @@ __device__ __forceinline__ void sincos_of_phase(uint32_t phase, float& s, float&
   c = ((quarter + 1) & 2) ? -b : b;
 }
 
+// A thread's elements of a head: one pack of neighbouring pairs, or the packs
+// of their first and of their second elements.
+template <typename T, bool INTERLEAVED>
+struct Turned {
+  static constexpr int V = kPackOf<T>, PAIRS = INTERLEAVED ? V / 2 : V;
+  Pack<T, V> p, q;
+
+  __device__ __forceinline__ void load(const T* x, int j0, int half) {
+    const int left = half - j0;
+    if constexpr (INTERLEAVED) {
+      p = load_some<T, V>(x + 2 * j0, 2 * left);
+    } else {
+      p = load_some<T, V>(x + j0, left);
+      q = load_some<T, V>(x + half + j0, left);
+    }
+  }
+  __device__ __forceinline__ void store(T* x, int j0, int half) const {
+    const int left = half - j0;
+    if constexpr (INTERLEAVED) {
+      store_some<T, V>(x + 2 * j0, p, 2 * left);
+    } else {
+      store_some<T, V>(x + j0, p, left);
+      store_some<T, V>(x + half + j0, q, left);
+    }
+  }
+  __device__ __forceinline__ void turn(const float (&sn)[PAIRS], const float (&cs)[PAIRS]) {
+#pragma unroll
+    for (int e = 0; e < PAIRS; ++e) {
+      const float a = (float)(INTERLEAVED ? p.v[2 * e] : p.v[e]), b = (float)(INTERLEAVED ? p.v[2 * e + 1] : q.v[e]);
+      const T u = (T)__builtin_fmaf(a, cs[e], -(b * sn[e])), v = (T)__builtin_fmaf(a, sn[e], b * cs[e]);
+      if constexpr (INTERLEAVED) {
+        p.v[2 * e] = u;
+        p.v[2 * e + 1] = v;
+      } else {
+        p.v[e] = u;
+        q.v[e] = v;
+      }
+    }
+  }
+};
+
 template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotShape s) {
-  constexpr int V = kPackOf<T>;  // pairs of a thread
+  using Elements = Turned<T, INTERLEAVED>;
+  constexpr int V = kPackOf<T>, PAIRS = Elements::PAIRS;
   const int64_t n = rows_in_use(a.row_count, a.rows, a.fault);
   const int per_row = s.items * s.head_parts;
   const int64_t row0 = (int64_t)blockIdx.x * s.rows_block;
@@ -70,45 +113,34 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotSh
         store_some<T, V>(out + c, load_some<T, V>(x + c, a.dim - c), a.dim - c);
       continue;
     }
-    const int j0 = item * V, pairs = half - j0;
-    float sn[V], cs[V];
+    const int j0 = item * PAIRS;
+    float sn[PAIRS], cs[PAIRS];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sn[e] = 0.0f;
-      cs[e] = 1.0f;
-      if (e < pairs) {
-        const int ax = min((int)a.axis[j0 + e], a.axes - 1);
-        const uint64_t phase = (uint64_t)(int64_t)a.positions[row * a.position_stride + ax] * a.steps[j0 + e];
-        sincos_of_phase((uint32_t)(phase >> 32), sn[e], cs[e]);
-        if (a.inverse) sn[e] = -sn[e];
+    for (int e = 0; e < PAIRS; ++e) {
+      // pairs past the last turn by its angle; they are not stored
+      const int j = min(j0 + e, half - 1);
+      const int ax = min((int)a.axis[j], a.axes - 1);
+      const uint64_t phase = (uint64_t)(int64_t)a.positions[row * a.position_stride + ax] * a.steps[j];
+      sincos_of_phase((uint32_t)(phase >> 32), sn[e], cs[e]);
+      if (a.inverse) sn[e] = -sn[e];
+    }
+    // four heads' loads before their stores: out may be x, so the compiler keeps a load behind the store before it
+    int h = h0;
+    for (; h + 4 <= h1; h += 4, x += 4 * a.x_head, out += 4 * a.out_head) {
+      Elements e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i].load(x + i * a.x_head, j0, half);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[i].turn(sn, cs);
+        e[i].store(out + i * a.out_head, j0, half);
       }
     }
-    for (int h = h0; h < h1; ++h, x += a.x_head, out += a.out_head) {
-      if constexpr (INTERLEAVED) {
-        const int c = 2 * j0;
-        Pack<T, V> p = load_some<T, V>(x + c, 2 * pairs), q = load_some<T, V>(x + c + V, 2 * pairs - V);
-#pragma unroll
-        for (int e = 0; e < V / 2; ++e) {
-          const float p0 = (float)p.v[2 * e], p1 = (float)p.v[2 * e + 1];
-          const float q0 = (float)q.v[2 * e], q1 = (float)q.v[2 * e + 1];
-          p.v[2 * e] = (T)__builtin_fmaf(p0, cs[e], -(p1 * sn[e]));
-          p.v[2 * e + 1] = (T)__builtin_fmaf(p0, sn[e], p1 * cs[e]);
-          q.v[2 * e] = (T)__builtin_fmaf(q0, cs[e + V / 2], -(q1 * sn[e + V / 2]));
-          q.v[2 * e + 1] = (T)__builtin_fmaf(q0, sn[e + V / 2], q1 * cs[e + V / 2]);
-        }
-        store_some<T, V>(out + c, p, 2 * pairs);
-        store_some<T, V>(out + c + V, q, 2 * pairs - V);
-      } else {
-        Pack<T, V> p = load_some<T, V>(x + j0, pairs), q = load_some<T, V>(x + half + j0, pairs);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float u0 = (float)p.v[e], u1 = (float)q.v[e];
-          p.v[e] = (T)__builtin_fmaf(u0, cs[e], -(u1 * sn[e]));
-          q.v[e] = (T)__builtin_fmaf(u0, sn[e], u1 * cs[e]);
-        }
-        store_some<T, V>(out + j0, p, pairs);
-        store_some<T, V>(out + half + j0, q, pairs);
-      }
+    for (; h < h1; ++h, x += a.x_head, out += a.out_head) {
+      Elements e;
+      e.load(x, j0, half);
+      e.turn(sn, cs);
+      e.store(out, j0, half);
     }
   }
 }
@@ -116,7 +148,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotSh
 template <typename T>
 hipError_t rotary_of(const RotaryArgs& a, hipStream_t st) {
   RotShape s;
-  s.turned = (a.rotary_dim / 2 + kPackOf<T> - 1) / kPackOf<T>;
+  const int pairs = a.interleaved ? kPackOf<T> / 2 : kPackOf<T>;
+  s.turned = (a.rotary_dim / 2 + pairs - 1) / pairs;
   const int rest = a.dim - a.rotary_dim;
   s.items = s.turned + (a.copy_rest ? (rest + kPackOf<T> - 1) / kPackOf<T> : 0);
   // eight heads share an angle unless that leaves the chip under four waves a SIMD

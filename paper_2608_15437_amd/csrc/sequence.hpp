@@ -52,6 +52,13 @@ struct RotaryArgs {
 
 hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t st);
 
+// Waves a SIMD of the walks' kernels, as their registers allow, hence the
+// workgroups of four waves that a compute unit takes; `wide`: 32, 64 or 128.
+constexpr int walk_waves(bool half, int wide) { return (wide > 64 ? 2 : wide > 32 ? 3 : 4) - (half ? 0 : 1); }
+constexpr int grad_waves(bool half, int wide) { return wide > 64 && !half ? 1 : 2; }
+
+constexpr int kOrderedSequences = 256;
+
 // What the walks over ragged sequences share.  Positions may run backwards;
 // `ad` and `cd` are the state's rows and columns.
 struct AttnWalk {
@@ -68,8 +75,9 @@ struct AttnWalk {
   int32_t exact_state;    // the state is an output: as exact as fp32
   float scale;
   float init_scale, final_scale;  // the state is carried divided by these
-  // sequences longer than (rows in use) / cuts are cut, into parts of at least `least` rows; 0: none is
+  // sequences are cut at shares of (rows in use) / cuts, at least `least` rows; 0: none is
   int32_t cuts;
+  int32_t longest_first;  // the sequences that are not cut, up to kOrderedSequences of them
   int32_t least;          // whole chunks
   float* cut_state;       // [cuts][H][ad][cd]: the state at the end of every part that goes on
   int32_t* cut_rows;      // [cuts] its rows, 0 where it begins its sequence, -1: there is no such part

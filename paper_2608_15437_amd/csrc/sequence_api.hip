@@ -73,12 +73,9 @@ mmbev_status_t status_of(hipError_t e) { return e == hipSuccess ? MMBEV_OK : MMB
 
 // ------------------------------------------------------------ attention
 
-// A sequence and head is a workgroup's work, but one that is longer than the
-// rows' share of kAttnUnits workgroups is cut into parts.
-#ifndef UNITS
-#define UNITS 768
-#endif
-constexpr int64_t kAttnUnits = UNITS;
+// A sequence and head is a workgroup's work, but long ones are cut so that the
+// workgroups fill the chip's compute units once.
+constexpr int64_t kComputeUnits = 256;
 // None is cut where none can be longer than this (it would take two more
 // launches than it saves), nor among more sequences than a workgroup can look
 // through in passing.
@@ -86,6 +83,7 @@ constexpr int64_t kAttnWhole = 512;
 constexpr int32_t kAttnCutSequences = 1024;
 
 struct AttnPlan {
+  int64_t slots, grad_slots;  // workgroups that the chip takes at once
   int32_t cuts;       // of the forward walks
   int32_t grad_cuts;  // of the backward walk
   int32_t group;      // its heads a workgroup
@@ -114,20 +112,28 @@ int32_t grad_group(const mmbev_attention_t* t) {
 // Rows of a part, at least: enough that its state is a small part of what is read for them.
 int32_t least_rows(const mmbev_attention_t* t) { return std::max(t->key_dim, t->value_dim) <= 64 ? 128 : 256; }
 
-int32_t cuts_for(const mmbev_attention_t* t, int64_t heads) {
+// Parts that rows are shared out over, so that with the sequences that are
+// not cut there are about `units` of them and no second round of a few: at
+// least half the units. `heads`: workgroups of a part.
+int32_t cuts_for(const mmbev_attention_t* t, int64_t heads, int64_t slots) {
   const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
   if (longest <= kAttnWhole || t->num_sequences > kAttnCutSequences) return 0;
-  const int64_t least = least_rows(t);
-  return (int32_t)std::max<int64_t>(1, std::min((kAttnUnits + heads - 1) / heads, (t->rows + least - 1) / least));
+  const int64_t least = least_rows(t), units = std::max<int64_t>(2, slots / heads);
+  const int64_t parts = units - std::min<int64_t>(t->num_sequences, units / 2);
+  return (int32_t)std::max<int64_t>(1, std::min(parts, (t->rows + least - 1) / least));
 }
 
 AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   AttnPlan p{};
-  p.cuts = cuts_for(t, t->heads);
+  const bool half = t->dtype != MMBEV_F32;
+  const int32_t wide = std::max(t->key_dim, t->value_dim);
+  p.slots = kComputeUnits * walk_waves(half, wide);
+  p.grad_slots = kComputeUnits * grad_waves(half, wide);
+  p.cuts = cuts_for(t, t->heads, p.slots);
   int32_t most = p.cuts;
   if (backward) {
     p.group = grad_group(t);
-    p.grad_cuts = cuts_for(t, t->heads / p.group);
+    p.grad_cuts = cuts_for(t, t->heads / p.group, p.grad_slots);
     most = std::max(most, p.grad_cuts);
   }
   size_t at = 0;
@@ -142,8 +148,8 @@ AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   return p;
 }
 
-void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, int32_t cuts, const AttnPlan& p,
-              char* ws) {
+void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, int32_t cuts, int64_t slots,
+              int64_t heads, const AttnPlan& p, char* ws) {
   a.log_decay = log_decay;
   a.offsets = offsets;
   a.rows = t->rows;
@@ -152,6 +158,7 @@ void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, c
   a.scale = t->scale;
   a.init_scale = a.final_scale = 1.0f;
   a.cuts = cuts;
+  a.longest_first = t->num_sequences <= kOrderedSequences && t->num_sequences * heads > slots;
   a.least = least_rows(t);
   a.cut_rows = (int32_t*)(ws + p.off_rows);
   a.cut_state = (float*)(ws + p.off_state);
@@ -335,7 +342,7 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t 
   const AttnPlan p = attention_plan(t, false);
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
   AttnArgs a{};
-  put_walk(a, t, log_decay, offsets, p.cuts, p, (char*)workspace);
+  put_walk(a, t, log_decay, offsets, p.cuts, p.slots, t->heads, p, (char*)workspace);
   put(q, &a.a, &a.a_row, &a.a_head);
   put(k, &a.b, &a.b_row, &a.b_head);
   put(v, &a.c, &a.c_row, &a.c_head);
@@ -382,7 +389,7 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
 
   // dq: the forward walk of (dout, v, k), whose state is the transposed one
   AttnArgs a{};
-  put_walk(a, t, log_decay, offsets, p.cuts, p, ws);
+  put_walk(a, t, log_decay, offsets, p.cuts, p.slots, t->heads, p, ws);
   put(dout, &a.a, &a.a_row, &a.a_head);
   put(v, &a.b, &a.b_row, &a.b_head);
   put(k, &a.c, &a.c_row, &a.c_head);
@@ -398,7 +405,7 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
 
   // dv and dk: backwards, the carried state that of q and dout, divided by scale
   AttnGradArgs b{};
-  put_walk(b, t, log_decay, offsets, p.grad_cuts, p, ws);
+  put_walk(b, t, log_decay, offsets, p.grad_cuts, p.grad_slots, H / p.group, p, ws);
   b.reversed = 1;
   put(q, &b.q, &b.q_row, &b.q_head);
   put(dout, &b.dout, &b.d_row, &b.d_head);

@@ -511,19 +511,29 @@ def roi_voxelize_workload(wl, device) -> dict:
 #
 # Rows are torch tensors on the current device, of float32, float16 or bfloat16, elements of a row (of a head) next to
 # each other and any stride between rows.  Outputs and workspaces that are not given are allocated for the stream that
-# the call is enqueued on.
+# the call is enqueued on.  A short call takes longer to issue than to run, so the helpers below touch each tensor as
+# few times as they can.
 
 F32, F16, BF16 = 0, 1, 2
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 _DTYPE_CODES: dict = {}
+_torch = None
 
 
-def _dtype_code(t) -> int:
-    if not _DTYPE_CODES:
+def _with_torch():
+    """torch, imported with the first call that needs it."""
+    global _torch
+    if _torch is None:
         import torch
 
         _DTYPE_CODES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+        _torch = torch
+    return _torch
+
+
+def _dtype_code(t) -> int:
+    _with_torch()
     code = _DTYPE_CODES.get(t.dtype)
     if code is None:
         raise MmbevError(f"float32, float16 or bfloat16 rows are needed, not {t.dtype}")
@@ -531,24 +541,29 @@ def _dtype_code(t) -> int:
 
 
 def _like(name, t, dtype, shape):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise MmbevError(f"{name} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
     return t
 
 
+_NO_ROWS = mmbev_rows_t(None, 0)
+
+
 def _rows(name, t) -> mmbev_rows_t:
     if t is None:
-        return mmbev_rows_t(None, 0)
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1 and t.numel()):
+        return _NO_ROWS
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1 and t.numel()):
         raise MmbevError(f"{name} must be [rows][width] with the elements of a row next to each other")
-    return mmbev_rows_t(_ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return mmbev_rows_t(t.data_ptr(), stride[0] if shape[0] > 1 else shape[1])
 
 
 def _heads(name, t) -> mmbev_heads_t:
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1 and t.numel()):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or (shape[2] > 1 and stride[2] != 1 and t.numel()):
         raise MmbevError(f"{name} must be [rows][heads][dim] with the elements of a head next to each other")
-    head = t.stride(1) if t.shape[1] > 1 else t.shape[2]
-    return mmbev_heads_t(_ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1] * head, head)
+    head = stride[1] if shape[1] > 1 else shape[2]
+    return mmbev_heads_t(t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * head, head)
 
 
 def _vector(name, t, dtype, n):
@@ -557,51 +572,49 @@ def _vector(name, t, dtype, n):
         return None
     if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
         raise MmbevError(f"{name} must be contiguous, {dtype}, with {n} elements or more")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _on_device(*tensors) -> None:
-    import torch
-
-    current = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+def _issue_on(stream, *tensors) -> int | None:
+    """The handle of the stream to issue on (the current device's current one if None), after a look at where the
+    tensors are: all of them on that device."""
+    device = tensors[0].get_device()  # -1: not on a GPU
     for t in tensors:
-        if t is not None and t.device.type != "cuda":
-            raise MmbevError(f"a tensor on the GPU is needed, not one on {t.device}")
-        if t is not None and t.device.index != current:
-            raise MmbevError(f"tensor on {t.device}, current device cuda:{current}")
+        if t is not None and t.get_device() != device or device < 0:
+            raise MmbevError("tensors on one GPU are needed")
+    torch = _with_torch()
+    if device != torch._C._cuda_getDevice():
+        raise MmbevError(f"tensors on cuda:{device}, current device cuda:{torch.cuda.current_device()}")
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    return int(handle) or None
 
 
-def _empty(stream, shape, dtype, device):
-    """Memory that the allocator knows to be used on `stream`."""
-    import torch
-
+def _empty(stream, like, shape, dtype):
+    """Memory on `like`'s device that the allocator knows to be used on `stream`."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _workspace(given, nbytes, stream, device):
-    import torch
-
-    if given is None:
-        given = _empty(stream, (nbytes,), torch.uint8, device)
-    return given, given.numel() * given.element_size()
+        return like.new_empty(shape, dtype=dtype)
+    with _torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _norm_of(x, weight, bias, eps) -> mmbev_norm_t:
     code = _dtype_code(x)
+    if x.dim() != 2:
+        raise MmbevError("rows must be [rows][width]")
+    rows, width = x.shape
     wcode = F32
     for name, t in (("weight", weight), ("bias", bias)):
-        if t is None:
-            continue
-        _vector(name, t, t.dtype, x.shape[1])
-        if t.numel() != x.shape[1]:
-            raise MmbevError(f"{name} must have {x.shape[1]} elements")
-        wcode = _dtype_code(t)
+        if t is not None:
+            if t.numel() != width or not t.is_contiguous():
+                raise MmbevError(f"{name} must be contiguous with {width} elements")
+            wcode = _dtype_code(t)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise MmbevError("weight and bias must have one type")
-    return mmbev_norm_t(x.shape[0], x.shape[1], code, wcode, float(eps))
+    return mmbev_norm_t(rows, width, code, wcode, eps)
+
+
+def _ptr_of(t) -> int | None:
+    return None if t is None else t.data_ptr()
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stats: bool = False, row_count=None, out=None,
@@ -612,30 +625,25 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stat
     needs; mean and rstd (float32 [rows]) are None unless `stats`.  row_count: int64 device tensor of one element, the
     rows in use (others keep what out holds).
     """
-    import torch
-
-    _on_device(x, weight, bias, residual, row_count, out, out_sum, fault)
-    rows = _rows("x", x)
+    handle = _issue_on(stream, x, weight, bias, residual, row_count, out, out_sum, fault)
+    torch = _torch
     desc = _norm_of(x, weight, bias, eps)
+    dtype, shape = x.dtype, x.shape
     if residual is not None:
-        _like("residual", residual, x.dtype, x.shape)
-    out = _empty(stream, x.shape, x.dtype, x.device) if out is None else _like("out", out, x.dtype, x.shape)
-    if residual is not None and out_sum is None:
-        out_sum = _empty(stream, x.shape, x.dtype, x.device)
-    elif out_sum is not None:
-        _like("out_sum", out_sum, x.dtype, x.shape)
+        _like("residual", residual, dtype, shape)
+        if out_sum is None:
+            out_sum = _empty(stream, x, shape, dtype)
+    if out_sum is not None:
+        _like("out_sum", out_sum, dtype, shape)
+    out = _empty(stream, x, shape, dtype) if out is None else _like("out", out, dtype, shape)
     mean = rstd = None
     if stats:
-        mean, rstd = (_empty(stream, (x.shape[0],), torch.float32, x.device) for _ in range(2))
-    _check(load().mmbev_layer_norm(ctypes.byref(desc), rows, _rows("residual", residual), _ptr_of(weight), _ptr_of(bias),
-                                   _vector("row_count", row_count, torch.int64, 1), _rows("out", out),
-                                   _rows("out_sum", out_sum), _ptr_of(mean), _ptr_of(rstd),
-                                   _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_layer_norm")
+        mean, rstd = _empty(stream, x, shape[:1], torch.float32), _empty(stream, x, shape[:1], torch.float32)
+    _check((_lib or load()).mmbev_layer_norm(
+        desc, _rows("x", x), _rows("residual", residual), _ptr_of(weight), _ptr_of(bias),
+        _vector("row_count", row_count, torch.int64, 1), _rows("out", out), _rows("out_sum", out_sum), _ptr_of(mean),
+        _ptr_of(rstd), _vector("fault", fault, torch.int32, 1), handle), "mmbev_layer_norm")
     return out, (x if out_sum is None else out_sum), mean, rstd
-
-
-def _ptr_of(t) -> int | None:
-    return None if t is None else _ptr(t)
 
 
 def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, dx=None, dweight=None, dbias=None,
@@ -645,30 +653,28 @@ def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, d
     dskip: the gradient that reaches s past the norm, added to dx.  Returns (dx, dweight, dbias), the last two float32
     [width], None without `weight_grads`.
     """
-    import torch
-
-    _on_device(dy, s, weight, mean, rstd, dskip, row_count, dx, dweight, dbias, fault, workspace)
+    handle = _issue_on(stream, dy, s, weight, mean, rstd, dskip, row_count, dx, dweight, dbias, fault, workspace)
+    torch, lib = _torch, _lib or load()
     desc = _norm_of(s, weight, None, 0.0)
-    _like("dy", dy, s.dtype, s.shape)
+    dtype, shape = s.dtype, s.shape
+    _like("dy", dy, dtype, shape)
     if dskip is not None:
-        _like("dskip", dskip, s.dtype, s.shape)
-    dx = _empty(stream, s.shape, s.dtype, s.device) if dx is None else _like("dx", dx, s.dtype, s.shape)
-    nbytes = 0
+        _like("dskip", dskip, dtype, shape)
+    dx = _empty(stream, s, shape, dtype) if dx is None else _like("dx", dx, dtype, shape)
     if weight_grads:
-        if dweight is None:
-            dweight = _empty(stream, (s.shape[1],), torch.float32, s.device)
-        if dbias is None:
-            dbias = _empty(stream, (s.shape[1],), torch.float32, s.device)
-        workspace, nbytes = _workspace(workspace, int(load().mmbev_layer_norm_backward_workspace_bytes(ctypes.byref(desc))),
-                                       stream, s.device)
+        dweight = _empty(stream, s, shape[1:], torch.float32) if dweight is None else dweight
+        dbias = _empty(stream, s, shape[1:], torch.float32) if dbias is None else dbias
+        if workspace is None:
+            workspace = _empty(stream, s, (int(lib.mmbev_layer_norm_backward_workspace_bytes(desc)),), torch.uint8)
     else:
         workspace = dweight = dbias = None
-    _check(load().mmbev_layer_norm_backward(
-        ctypes.byref(desc), _rows("dy", dy), _rows("s", s), _ptr_of(weight), _vector("mean", mean, torch.float32, s.shape[0]),
-        _vector("rstd", rstd, torch.float32, s.shape[0]), _rows("dskip", dskip),
+    _check(lib.mmbev_layer_norm_backward(
+        desc, _rows("dy", dy), _rows("s", s), _ptr_of(weight), _vector("mean", mean, torch.float32, shape[0]),
+        _vector("rstd", rstd, torch.float32, shape[0]), _rows("dskip", dskip),
         _vector("row_count", row_count, torch.int64, 1), _rows("dx", dx),
-        _vector("dweight", dweight, torch.float32, s.shape[1]), _vector("dbias", dbias, torch.float32, s.shape[1]),
-        _vector("fault", fault, torch.int32, 1), _ptr_of(workspace), nbytes, _stream(stream)), "mmbev_layer_norm_backward")
+        _vector("dweight", dweight, torch.float32, shape[1]), _vector("dbias", dbias, torch.float32, shape[1]),
+        _vector("fault", fault, torch.int32, 1), _ptr_of(workspace), 0 if workspace is None else workspace.nbytes,
+        handle), "mmbev_layer_norm_backward")
     return dx, dweight, dbias
 
 
@@ -687,44 +693,42 @@ def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = Fals
            stream=None):
     """Enqueue mmbev_rotary: x [rows][heads][dim]; positions int32 [rows] or [rows][axes] (a view of the voxeliser's
     coordinates will do: coords[:, 1:]); steps, axis: make_rotary's arrays on the GPU.  Returns out (may be x)."""
-    import torch
-
-    _on_device(x, positions, steps, axis, row_count, out, fault)
-    if positions.dtype != torch.int32 or positions.shape[0] != x.shape[0] or positions.dim() > 2 or \
-            (positions.dim() == 2 and positions.shape[1] > 1 and positions.stride(1) != 1):
+    handle = _issue_on(stream, x, positions, steps, axis, row_count, out, fault)
+    torch = _torch
+    xs, shape = _heads("x", x), x.shape
+    at, step = positions.shape, positions.stride()
+    if positions.dtype != torch.int32 or at[0] != shape[0] or len(at) > 2 or (len(at) == 2 and at[1] > 1 and step[1] != 1):
         raise MmbevError("positions must be int32 [rows] or [rows][axes], a row's columns next to each other")
-    axes = positions.shape[1] if positions.dim() == 2 else 1
+    axes = at[1] if len(at) == 2 else 1
     pairs = steps.numel()
-    xs = _heads("x", x)
-    out = _empty(stream, x.shape, x.dtype, x.device) if out is None else _like("out", out, x.dtype, x.shape)
-    desc = mmbev_rotary_t(x.shape[0], x.shape[1], x.shape[2], 2 * pairs, _dtype_code(x), ROTARY_LAYOUTS[layout],
-                          1 if inverse else 0)
-    _check(load().mmbev_rotary(ctypes.byref(desc), xs, _ptr(positions), positions.stride(0) if x.shape[0] > 1 else axes, axes,
-                               _vector("steps", steps, torch.int64, pairs), _vector("axis", axis, torch.uint8, pairs),
-                               _vector("row_count", row_count, torch.int64, 1), _heads("out", out),
-                               _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_rotary")
+    out = _empty(stream, x, shape, x.dtype) if out is None else _like("out", out, x.dtype, shape)
+    desc = mmbev_rotary_t(*shape, 2 * pairs, _dtype_code(x), ROTARY_LAYOUTS[layout], 1 if inverse else 0)
+    _check((_lib or load()).mmbev_rotary(
+        desc, xs, positions.data_ptr(), step[0] if shape[0] > 1 else axes, axes, _vector("steps", steps, torch.int64, pairs),
+        _vector("axis", axis, torch.uint8, pairs), _vector("row_count", row_count, torch.int64, 1), _heads("out", out),
+        _vector("fault", fault, torch.int32, 1), handle), "mmbev_rotary")
     return out
 
 
 def _attention_of(q, k, v, num_sequences, scale, max_length) -> mmbev_attention_t:
-    rows, heads, key_dim = q.shape
-    if k.shape[0] != rows or v.shape[:2] != k.shape[:2] or k.shape[2] != key_dim or k.dtype != q.dtype or v.dtype != q.dtype:
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise MmbevError("q, k and v must be [rows][heads][dim]")
+    (rows, heads, key_dim), (krows, kv_heads, kdim), (vrows, vheads, value_dim) = q.shape, k.shape, v.shape
+    if krows != rows or vrows != rows or vheads != kv_heads or kdim != key_dim or k.dtype != q.dtype or v.dtype != q.dtype:
         raise MmbevError("k must be [rows][kv_heads][key_dim] and v [rows][kv_heads][value_dim] of q's type and rows")
-    return mmbev_attention_t(rows, int(max_length or 0), num_sequences, heads, k.shape[1], key_dim, v.shape[2],
-                             _dtype_code(q), key_dim ** -0.5 if scale is None else float(scale), 0)
+    return mmbev_attention_t(rows, max_length or 0, num_sequences, heads, kv_heads, key_dim, value_dim, _dtype_code(q),
+                             key_dim ** -0.5 if scale is None else scale, 0)
 
 
 def _state(name, t, desc, n):
-    import torch
-
     if t is None:
         return None
-    _like(name, t, torch.float32, (n, desc.heads, desc.key_dim, desc.value_dim))
-    return _vector(name, t, torch.float32, 0)
+    _like(name, t, _torch.float32, (n, desc.heads, desc.key_dim, desc.value_dim))
+    return _vector(name, t, _torch.float32, 0)
 
 
 def linear_attention_workspace_bytes(desc: mmbev_attention_t, backward: bool = False) -> int:
-    return int(load().mmbev_linear_attention_workspace_bytes(ctypes.byref(desc), 1 if backward else 0))
+    return int(load().mmbev_linear_attention_workspace_bytes(desc, 1 if backward else 0))
 
 
 def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None, final_state=False, max_length=None,
@@ -735,23 +739,23 @@ def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None
 
     Returns (out, final state or None).  Rows of no sequence keep what `out` holds.
     """
-    import torch
-
-    _on_device(q, k, v, log_decay, offsets, initial_state, out, fault, workspace)
+    handle = _issue_on(stream, q, k, v, log_decay, offsets, initial_state, out, fault, workspace)
+    torch = _torch
     n = offsets.numel() - 1
     qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
     desc = _attention_of(q, k, v, n, scale, max_length)
     shape = (desc.rows, desc.heads, desc.value_dim)
-    out = _empty(stream, shape, q.dtype, q.device) if out is None else _like("out", out, q.dtype, shape)
+    out = _empty(stream, q, shape, q.dtype) if out is None else _like("out", out, q.dtype, shape)
     if final_state is True:
-        final_state = _empty(stream, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32, q.device)
+        final_state = _empty(stream, q, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32)
     final = None if final_state is False else final_state
-    workspace, nbytes = _workspace(workspace, linear_attention_workspace_bytes(desc), stream, q.device)
-    _check(load().mmbev_linear_attention(
-        ctypes.byref(desc), qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
+    if workspace is None:
+        workspace = _empty(stream, q, (linear_attention_workspace_bytes(desc),), torch.uint8)
+    _check(_lib.mmbev_linear_attention(
+        desc, qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
         _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n), _heads("out", out),
-        _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), _ptr(workspace), nbytes,
-        _stream(stream)), "mmbev_linear_attention")
+        _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), workspace.data_ptr(),
+        workspace.nbytes, handle), "mmbev_linear_attention")
     return out, final
 
 
@@ -760,40 +764,40 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
                               workspace=None, stream=None):
     """Enqueue mmbev_linear_attention_backward: the gradients of linear_attention's q, k and v and, where
     `dinitial_state` is True or a tensor to write, of its initial state.  Returns (dq, dk, dv, dinitial_state or None)."""
-    import torch
-
-    _on_device(dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, dq, dk, dv, fault, workspace)
+    handle = _issue_on(stream, dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, dq, dk, dv, fault, workspace)
+    torch = _torch
     n = offsets.numel() - 1
+    ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
     desc = _attention_of(q, k, v, n, scale, max_length)
     _like("dout", dout, q.dtype, (desc.rows, desc.heads, desc.value_dim))
-    ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
-    dq, dk, dv = (_empty(stream, t.shape, t.dtype, t.device) if d is None else _like(name, d, t.dtype, t.shape)
+    dq, dk, dv = (_empty(stream, t, t.shape, t.dtype) if d is None else _like(name, d, t.dtype, t.shape)
                   for name, d, t in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
     if dinitial_state is True:
-        dinitial_state = _empty(stream, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32, q.device)
+        dinitial_state = _empty(stream, q, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32)
     dinitial = None if dinitial_state is False else dinitial_state
-    workspace, nbytes = _workspace(workspace, linear_attention_workspace_bytes(desc, True), stream, q.device)
-    _check(load().mmbev_linear_attention_backward(
-        ctypes.byref(desc), *ins, _vector("log_decay", log_decay, torch.float32, desc.heads),
-        _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n),
-        _state("dfinal_state", dfinal_state, desc, n), _heads("dq", dq), _heads("dk", dk), _heads("dv", dv),
-        _state("dinitial_state", dinitial, desc, n), _vector("fault", fault, torch.int32, 1), _ptr(workspace), nbytes,
-        _stream(stream)), "mmbev_linear_attention_backward")
+    if workspace is None:
+        workspace = _empty(stream, q, (linear_attention_workspace_bytes(desc, True),), torch.uint8)
+    _check(_lib.mmbev_linear_attention_backward(
+        desc, *ins, _vector("log_decay", log_decay, torch.float32, desc.heads), _vector("offsets", offsets, torch.int64, 2),
+        _state("initial_state", initial_state, desc, n), _state("dfinal_state", dfinal_state, desc, n), _heads("dq", dq),
+        _heads("dk", dk), _heads("dv", dv), _state("dinitial_state", dinitial, desc, n),
+        _vector("fault", fault, torch.int32, 1), workspace.data_ptr(), workspace.nbytes, handle),
+        "mmbev_linear_attention_backward")
     return dq, dk, dv, dinitial
 
 
 def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=None, fault=None, stream=None):
     """Enqueue mmbev_linear_attention_step: one row for each of many streams.  state float32 [slots][heads][key_dim]
     [value_dim] is updated in place; slots int32 [rows] names each row's state (negative: the row is skipped)."""
-    import torch
-
-    _on_device(q, k, v, log_decay, state, slots, out, fault)
+    handle = _issue_on(stream, q, k, v, log_decay, state, slots, out, fault)
+    torch = _torch
     qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
     desc = _attention_of(q, k, v, 1, scale, 0)
     shape = (desc.rows, desc.heads, desc.value_dim)
-    out = _empty(stream, shape, q.dtype, q.device) if out is None else _like("out", out, q.dtype, shape)
-    _check(load().mmbev_linear_attention_step(
-        ctypes.byref(desc), qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
-        _vector("slots", slots, torch.int32, desc.rows), state.shape[0], _state("state", state, desc, state.shape[0]),
-        _heads("out", out), _vector("fault", fault, torch.int32, 1), _stream(stream)), "mmbev_linear_attention_step")
+    out = _empty(stream, q, shape, q.dtype) if out is None else _like("out", out, q.dtype, shape)
+    held = state.shape[0]
+    _check((_lib or load()).mmbev_linear_attention_step(
+        desc, qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
+        _vector("slots", slots, torch.int32, desc.rows), held, _state("state", state, desc, held), _heads("out", out),
+        _vector("fault", fault, torch.int32, 1), handle), "mmbev_linear_attention_step")
     return out
