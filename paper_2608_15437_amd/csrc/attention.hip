@@ -19,14 +19,16 @@ namespace {
 // time: 11.8 us).
 constexpr int kJoinWaves = 8, kJoinRun = 12;
 
-__global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnPair pair) {
   __shared__ float s_end[kJoinWaves][64];
   __shared__ int32_t s_rows[kJoinWaves];  // of a run that no sequence begins in, else -1
+  const AttnArgs& a = pair.walk[blockIdx.z];
   const int64_t each = (int64_t)a.ad * a.cd, all = each * a.H;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const bool there = (int64_t)blockIdx.x * 64 + lane < all;
-  const int64_t i = min((int64_t)blockIdx.x * 64 + lane, all - 1);
-  const float g2 = decay_exponent(a.log_decay, (int)(i / each));
+  const int at = blockIdx.x * 64 + lane;
+  const bool there = at < each;
+  const int64_t i = blockIdx.y * each + min(at, (int)each - 1);
+  const float g2 = decay_exponent(a.log_decay, blockIdx.y);
   float carry = 0.0f;
   for (int32_t s0 = 0; s0 < a.cuts; s0 += kJoinWaves * kJoinRun) {
     const int32_t first = s0 + w * kJoinRun;
@@ -161,37 +163,50 @@ __global__ __launch_bounds__(256) void attention_check_kernel(const int64_t* off
   if ((b == 0 && o0 != 0) || o1 < o0 || o1 > rows) atomicOr(fault, MMBEV_FAULT_SEQUENCES);
 }
 
-hipError_t chunks_of(const AttnArgs& a, int32_t dtype, bool state_only, hipStream_t st) {
-  return dtype == MMBEV_F32   ? launch_attention_f32(a, state_only, st)
-         : dtype == MMBEV_F16 ? launch_attention_f16(a, state_only, st)
-                              : launch_attention_bf16(a, state_only, st);
+void check_offsets(const AttnWalk& a, hipStream_t st) {
+  if (a.fault)
+    hipLaunchKernelGGL(attention_check_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a.offsets, a.B, a.rows, a.fault);
 }
 
-// The states that go into the parts of cut sequences.
-hipError_t cut_states(const AttnArgs& a, int32_t dtype, hipStream_t st) {
-  if (!a.cuts) return hipSuccess;
-  const hipError_t e = chunks_of(a, dtype, true, st);
+// The states that go into the parts of cut sequences: made, and carried on.
+hipError_t cut_states(const AttnPair& p, int32_t dtype, hipStream_t st) {
+  const hipError_t e = dtype == MMBEV_F32   ? launch_attention_states_f32(p, st)
+                       : dtype == MMBEV_F16 ? launch_attention_states_f16(p, st)
+                                            : launch_attention_states_bf16(p, st);
   if (e != hipSuccess) return e;
-  const int64_t all = (int64_t)a.H * a.ad * a.cd;
-  hipLaunchKernelGGL(attention_join_kernel, dim3((uint32_t)((all + 63) / 64)), dim3(kJoinWaves * 64), 0, st, a);
+  const AttnArgs& a = p.walk[0];
+  hipLaunchKernelGGL(attention_join_kernel, dim3((a.ad * a.cd + 63) / 64, a.H, p.items[1] ? 2 : 1), dim3(kJoinWaves * 64), 0, st, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attention(const AttnArgs& a, int32_t dtype, hipStream_t st) {
-  if (a.fault)
-    hipLaunchKernelGGL(attention_check_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a.offsets, a.B, a.rows, a.fault);
-  const hipError_t e = cut_states(a, dtype, st);
-  return e != hipSuccess ? e : chunks_of(a, dtype, false, st);
+  check_offsets(a, st);
+  if (a.cuts) {
+    AttnPair p{};
+    p.walk[0] = a;
+    p.items[0] = (uint32_t)(a.cuts * a.H);
+    const hipError_t e = cut_states(p, dtype, st);
+    if (e != hipSuccess) return e;
+  }
+  return dtype == MMBEV_F32 ? launch_attention_f32(a, st) : dtype == MMBEV_F16 ? launch_attention_f16(a, st) : launch_attention_bf16(a, st);
 }
 
-hipError_t launch_attention_grad(const AttnGradArgs& a, const AttnArgs& states, int32_t dtype, hipStream_t st) {
-  const hipError_t e = cut_states(states, dtype, st);
-  if (e != hipSuccess) return e;
-  return dtype == MMBEV_F32   ? launch_attention_grad_f32(a, st)
-         : dtype == MMBEV_F16 ? launch_attention_grad_f16(a, st)
-                              : launch_attention_grad_bf16(a, st);
+hipError_t launch_attention_backward(const AttnArgs& a, const AttnGradArgs& b, const AttnArgs& states, int32_t dtype, hipStream_t st) {
+  check_offsets(a, st);
+  if (a.cuts) {  // and then b's are cut too
+    AttnPair p{};
+    p.walk[0] = a;
+    p.walk[1] = states;
+    p.items[0] = (uint32_t)(a.cuts * a.H);
+    p.items[1] = (uint32_t)(states.cuts * states.H);
+    const hipError_t e = cut_states(p, dtype, st);
+    if (e != hipSuccess) return e;
+  }
+  return dtype == MMBEV_F32   ? launch_attention_backward_f32(a, b, st)
+         : dtype == MMBEV_F16 ? launch_attention_backward_f16(a, b, st)
+                              : launch_attention_backward_bf16(a, b, st);
 }
 
 hipError_t launch_attention_sum(const AttnSumArgs& a, int32_t dtype, hipStream_t st) {

@@ -720,12 +720,15 @@ constexpr int kWavesSimd = walk_waves(sizeof(T) == 2, D);
 // initial state, where the part begins the sequence); attention_join_kernel
 // then carries them on.
 template <typename T, int D, bool WHOLE>
-__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_state_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_state_kernel(AttnPair pair) {
   constexpr int SD = D + kRowPad<T>;
   __shared__ __attribute__((aligned(16))) T s_b[kChunk * SD];
   __shared__ __attribute__((aligned(16))) T s_c[kChunk * SD];
   const Lane l = lane_of();
-  const int h = blockIdx.x % a.H, unit = blockIdx.x / a.H;
+  const bool second = blockIdx.x >= pair.items[0];
+  const AttnArgs& a = pair.walk[second];
+  const int item = blockIdx.x - (second ? pair.items[0] : 0);
+  const int h = item % a.H, unit = item / a.H;
   const Order o = order_of(a);
   Part q;
   const bool found = find_part(q, o, a, unit, true);
@@ -760,17 +763,23 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_st
   if (own) store_state<D>(a.cut_state + ((int64_t)unit * a.H + h) * a.ad * a.cd, st, a.ad, a.cd, 1.0f, l);
 }
 
+// LDS of a walk: two operands' chunks, the state's copy, fp16's largest values.
+template <typename T, int D>
+struct WalkShared {
+  __attribute__((aligned(16))) T b[kChunk * (D + kRowPad<T>)];
+  __attribute__((aligned(16))) T c[kChunk * (D + kRowPad<T>)];
+  __attribute__((aligned(16))) T s[D * (D + kRowPad<T>)];
+  float most[4][kAttnWaves];  // of each head that the workgroup takes
+};
+
 // out: the walk of (a, b, c).
 template <typename T, int D, bool WHOLE>
-__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_kernel(AttnArgs a) {
-  constexpr int SD = D + kRowPad<T>;
+__device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, D>& shared) {
   constexpr bool SCALED = __is_same(T, f16);
-  __shared__ __attribute__((aligned(16))) T s_b[kChunk * SD];
-  __shared__ __attribute__((aligned(16))) T s_c[kChunk * SD];
-  __shared__ __attribute__((aligned(16))) T s_s[D * SD];  // the state's copy
-  __shared__ float s_max[kAttnWaves];
+  T *s_b = shared.b, *s_c = shared.c, *s_s = shared.s;
+  float* s_max = shared.most[0];
   const Lane l = lane_of();
-  const int h = blockIdx.x % a.H, unit = blockIdx.x / a.H;
+  const int h = item % a.H, unit = item / a.H;
   const Order o = order_of(a);
   Part q;
   if (!find_part(q, o, a, unit, false)) return;
@@ -831,21 +840,24 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_ke
     store_state<D>(a.final_state + ((int64_t)q.b * a.H + h) * state, st, a.ad, a.cd, 1.0f, l);
 }
 
+template <typename T, int D, bool WHOLE>
+__global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_kernel(AttnArgs a) {
+  __shared__ WalkShared<T, D> shared;
+  walk<T, D, WHOLE>(a, blockIdx.x, shared);
+}
+
 // dv and dk: one walk backwards, whose state is that of (q, dout) divided by
 // scale.  A workgroup takes GROUP of the heads that share its keys and values:
 // each chunk it goes through them with a state each, and their sums stay in
 // registers.  Where GROUP is not all of them, the sums are fp32 parts that
 // attention_sum_kernel adds.
 template <typename T, int D, int GROUP, bool WHOLE>
-__global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_grad_kernel(AttnGradArgs a) {
-  constexpr int SD = D + kRowPad<T>;
+__device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkShared<T, D>& shared) {
   constexpr bool SCALED = __is_same(T, f16);
-  __shared__ __attribute__((aligned(16))) T s_q[kChunk * SD];
-  __shared__ __attribute__((aligned(16))) T s_d[kChunk * SD];
-  __shared__ __attribute__((aligned(16))) T s_s[D * SD];
-  __shared__ float s_max[GROUP][kAttnWaves];
+  T *s_q = shared.b, *s_d = shared.c, *s_s = shared.s;
+  float(&s_max)[4][kAttnWaves] = shared.most;
   const Lane l = lane_of();
-  const int groups = a.H / GROUP, u = blockIdx.x % groups, unit = blockIdx.x / groups;
+  const int groups = a.H / GROUP, u = item % groups, unit = item / groups;
   const int h0 = u * GROUP, hk = h0 / a.kv_div;
   const Order o = order_of(a);
   Part q;
@@ -938,49 +950,69 @@ __global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void
   }
 }
 
+// The backward pass: both walks in one launch, the longer one's workgroups
+// first (one after the other their last workgroups, and twice two more
+// launches for the cut sequences' states, left the chip idle: 167 us for one
+// robot frame instead of 113).
+template <typename T, int D, int GROUP, bool WHOLE>
+__global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_backward_kernel(AttnArgs a, AttnGradArgs b,
+                                                                                                       uint32_t back_items) {
+  __shared__ WalkShared<T, D> shared;
+  if (blockIdx.x < back_items)
+    walk_back<T, D, GROUP, WHOLE>(b, blockIdx.x, shared);
+  else
+    walk<T, D, WHOLE>(a, blockIdx.x - back_items, shared);
+}
+
 // Instances by the wider of the two dims: 32, 64 or 128, the rest zeros.
 template <typename T, bool WHOLE>
-void launch_walk(const AttnArgs& a, bool state_only, hipStream_t st) {
-  const int wide = a.ad > a.cd ? a.ad : a.cd;
-  const dim3 grid((uint32_t)((state_only ? a.cuts : a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  if (wide <= 32)
-    state_only ? go(attention_state_kernel<T, 32, WHOLE>) : go(attention_kernel<T, 32, WHOLE>);
-  else if (wide <= 64)
-    state_only ? go(attention_state_kernel<T, 64, WHOLE>) : go(attention_kernel<T, 64, WHOLE>);
-  else
-    state_only ? go(attention_state_kernel<T, 128, WHOLE>) : go(attention_kernel<T, 128, WHOLE>);
-}
-
-template <typename T>
-hipError_t walk_of(const AttnArgs& a, bool state_only, hipStream_t st) {
-  if (a.ad % 8 == 0 && a.cd % 8 == 0)
-    launch_walk<T, true>(a, state_only, st);
-  else
-    launch_walk<T, false>(a, state_only, st);
-  return hipGetLastError();
+void launch_states(const AttnPair& p, hipStream_t st) {
+  const int wide = p.walk[0].ad > p.walk[0].cd ? p.walk[0].ad : p.walk[0].cd;
+  const dim3 grid(p.items[0] + p.items[1]), block(kAttnThreads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, p); };
+  wide <= 32 ? go(attention_state_kernel<T, 32, WHOLE>) : wide <= 64 ? go(attention_state_kernel<T, 64, WHOLE>)
+                                                                     : go(attention_state_kernel<T, 128, WHOLE>);
 }
 
 template <typename T, bool WHOLE>
-void launch_grad(const AttnGradArgs& a, hipStream_t st) {
+void launch_walk(const AttnArgs& a, hipStream_t st) {
   const int wide = a.ad > a.cd ? a.ad : a.cd;
-  const dim3 grid((uint32_t)((a.cuts + a.B) * (int64_t)(a.H / a.group))), block(kAttnThreads);
+  const dim3 grid((uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  if (wide <= 32)
-    a.group == 4 ? go(attention_grad_kernel<T, 32, 4, WHOLE>) : a.group == 2 ? go(attention_grad_kernel<T, 32, 2, WHOLE>)
-                                                                             : go(attention_grad_kernel<T, 32, 1, WHOLE>);
-  else if (wide <= 64)
-    a.group == 2 ? go(attention_grad_kernel<T, 64, 2, WHOLE>) : go(attention_grad_kernel<T, 64, 1, WHOLE>);
-  else
-    go(attention_grad_kernel<T, 128, 1, WHOLE>);
+  wide <= 32 ? go(attention_kernel<T, 32, WHOLE>) : wide <= 64 ? go(attention_kernel<T, 64, WHOLE>) : go(attention_kernel<T, 128, WHOLE>);
 }
 
-template <typename T>
-hipError_t grad_of(const AttnGradArgs& a, hipStream_t st) {
-  if (a.ad % 8 == 0 && a.cd % 8 == 0)
-    launch_grad<T, true>(a, st);
+template <typename T, bool WHOLE>
+void launch_backward(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
+  const int wide = b.ad > b.cd ? b.ad : b.cd;
+  const uint32_t back = (uint32_t)((b.cuts + b.B) * (int64_t)(b.H / b.group));
+  const dim3 grid(back + (uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, b, back); };
+  if (wide <= 32)
+    b.group == 4 ? go(attention_backward_kernel<T, 32, 4, WHOLE>) : b.group == 2 ? go(attention_backward_kernel<T, 32, 2, WHOLE>)
+                                                                                 : go(attention_backward_kernel<T, 32, 1, WHOLE>);
+  else if (wide <= 64)
+    b.group == 2 ? go(attention_backward_kernel<T, 64, 2, WHOLE>) : go(attention_backward_kernel<T, 64, 1, WHOLE>);
   else
-    launch_grad<T, false>(a, st);
+    go(attention_backward_kernel<T, 128, 1, WHOLE>);
+}
+
+// WHOLE: see load_part; both walks' dims are the same two.
+bool whole_packs(const AttnWalk& a) { return a.ad % 8 == 0 && a.cd % 8 == 0; }
+
+template <typename T>
+hipError_t states_of(const AttnPair& p, hipStream_t st) {
+  whole_packs(p.walk[0]) ? launch_states<T, true>(p, st) : launch_states<T, false>(p, st);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t walk_of(const AttnArgs& a, hipStream_t st) {
+  whole_packs(a) ? launch_walk<T, true>(a, st) : launch_walk<T, false>(a, st);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t backward_of(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
+  whole_packs(b) ? launch_backward<T, true>(a, b, st) : launch_backward<T, false>(a, b, st);
   return hipGetLastError();
 }
 

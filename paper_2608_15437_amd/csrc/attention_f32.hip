@@ -4,8 +4,10 @@
 
 namespace mmbev {
 
-hipError_t launch_attention_f32(const AttnArgs& a, bool state_only, hipStream_t st) { return walk_of<float>(a, state_only, st); }
+hipError_t launch_attention_states_f32(const AttnPair& p, hipStream_t st) { return states_of<float>(p, st); }
 
-hipError_t launch_attention_grad_f32(const AttnGradArgs& a, hipStream_t st) { return grad_of<float>(a, st); }
+hipError_t launch_attention_f32(const AttnArgs& a, hipStream_t st) { return walk_of<float>(a, st); }
+
+hipError_t launch_attention_backward_f32(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) { return backward_of<float>(a, b, st); }
 
 }  // namespace mmbev

@@ -5,11 +5,14 @@
 
 namespace mmbev {
 
-hipError_t launch_attention_f32(const AttnArgs& a, bool state_only, hipStream_t st);
-hipError_t launch_attention_grad_f32(const AttnGradArgs& a, hipStream_t st);
-hipError_t launch_attention_f16(const AttnArgs& a, bool state_only, hipStream_t st);
-hipError_t launch_attention_grad_f16(const AttnGradArgs& a, hipStream_t st);
-hipError_t launch_attention_bf16(const AttnArgs& a, bool state_only, hipStream_t st);
-hipError_t launch_attention_grad_bf16(const AttnGradArgs& a, hipStream_t st);
+hipError_t launch_attention_states_f32(const AttnPair& p, hipStream_t st);
+hipError_t launch_attention_f32(const AttnArgs& a, hipStream_t st);
+hipError_t launch_attention_backward_f32(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st);
+hipError_t launch_attention_states_f16(const AttnPair& p, hipStream_t st);
+hipError_t launch_attention_f16(const AttnArgs& a, hipStream_t st);
+hipError_t launch_attention_backward_f16(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st);
+hipError_t launch_attention_states_bf16(const AttnPair& p, hipStream_t st);
+hipError_t launch_attention_bf16(const AttnArgs& a, hipStream_t st);
+hipError_t launch_attention_backward_bf16(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st);
 
 }  // namespace mmbev

@@ -106,9 +106,15 @@ struct AttnGradArgs : AttnWalk {  // dv and dk, backwards; the state's rows are 
 
 constexpr int32_t kAttnGroupMost(int32_t wide) { return wide <= 32 ? 4 : wide <= 64 ? 2 : 1; }
 
+// One or two walks whose cut sequences' states one launch makes, and their workgroups.
+struct AttnPair {
+  AttnArgs walk[2];
+  uint32_t items[2];
+};
+
 hipError_t launch_attention(const AttnArgs& a, int32_t dtype, hipStream_t st);
-// states: the arguments of the walk that makes the cut sequences' states, (., q, dout) reversed
-hipError_t launch_attention_grad(const AttnGradArgs& a, const AttnArgs& states, int32_t dtype, hipStream_t st);
+// states: the arguments of the walk that makes the states of b's cut sequences, (., q, dout) reversed
+hipError_t launch_attention_backward(const AttnArgs& a, const AttnGradArgs& b, const AttnArgs& states, int32_t dtype, hipStream_t st);
 
 struct AttnSumArgs {   // out[r][g] = sum over the group's parts of part[r][g * group + i], fp32 [rows][parts][dim]
   const float* part;

@@ -83,7 +83,7 @@ constexpr int64_t kAttnWhole = 512;
 constexpr int32_t kAttnCutSequences = 1024;
 
 struct AttnPlan {
-  int64_t slots, grad_slots;  // workgroups that the chip takes at once
+  int64_t slots;      // workgroups that the chip takes at once
   int32_t cuts;       // of the forward walks
   int32_t grad_cuts;  // of the backward walk
   int32_t group;      // its heads a workgroup
@@ -127,20 +127,19 @@ AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   AttnPlan p{};
   const bool half = t->dtype != MMBEV_F32;
   const int32_t wide = std::max(t->key_dim, t->value_dim);
-  p.slots = kComputeUnits * walk_waves(half, wide);
-  p.grad_slots = kComputeUnits * grad_waves(half, wide);
+  p.slots = kComputeUnits * (backward ? grad_waves(half, wide) : walk_waves(half, wide));
   p.cuts = cuts_for(t, t->heads, p.slots);
-  int32_t most = p.cuts;
   if (backward) {
     p.group = grad_group(t);
-    p.grad_cuts = cuts_for(t, t->heads / p.group, p.grad_slots);
-    most = std::max(most, p.grad_cuts);
+    p.grad_cuts = cuts_for(t, t->heads / p.group, p.slots);
   }
+  // the forward walk's, then the backward one's
+  const size_t all = p.cuts + p.grad_cuts;
   size_t at = 0;
   p.off_rows = at;
-  at = align256(at + (size_t)most * 4);
+  at = align256(at + all * 4);
   p.off_state = at;
-  at = align256(at + (size_t)most * t->heads * t->key_dim * t->value_dim * 4);
+  at = align256(at + all * t->heads * t->key_dim * t->value_dim * 4);
   p.off_part = at;
   if (backward && t->heads != t->kv_heads * p.group)
     at = align256(at + (size_t)t->rows * (t->heads / p.group) * (t->key_dim + t->value_dim) * 4);
@@ -148,8 +147,10 @@ AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   return p;
 }
 
-void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, int32_t cuts, int64_t slots,
-              int64_t heads, const AttnPlan& p, char* ws) {
+void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, const int64_t* offsets, bool backwards, const AttnPlan& p,
+              char* ws) {
+  const int32_t cuts = backwards ? p.grad_cuts : p.cuts, before = backwards ? p.cuts : 0;
+  const int64_t heads = backwards ? t->heads / p.group : t->heads;
   a.log_decay = log_decay;
   a.offsets = offsets;
   a.rows = t->rows;
@@ -158,10 +159,11 @@ void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, c
   a.scale = t->scale;
   a.init_scale = a.final_scale = 1.0f;
   a.cuts = cuts;
-  a.longest_first = t->num_sequences <= kOrderedSequences && t->num_sequences * heads > slots;
+  a.longest_first = t->num_sequences <= kOrderedSequences && t->num_sequences * heads > p.slots;
   a.least = least_rows(t);
-  a.cut_rows = (int32_t*)(ws + p.off_rows);
-  a.cut_state = (float*)(ws + p.off_state);
+  a.reversed = backwards;
+  a.cut_rows = (int32_t*)(ws + p.off_rows) + before;
+  a.cut_state = (float*)(ws + p.off_state) + (int64_t)before * t->heads * t->key_dim * t->value_dim;
 }
 
 template <typename P, typename R>
@@ -342,7 +344,7 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t 
   const AttnPlan p = attention_plan(t, false);
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
   AttnArgs a{};
-  put_walk(a, t, log_decay, offsets, p.cuts, p.slots, t->heads, p, (char*)workspace);
+  put_walk(a, t, log_decay, offsets, false, p, (char*)workspace);
   put(q, &a.a, &a.a_row, &a.a_head);
   put(k, &a.b, &a.b_row, &a.b_head);
   put(v, &a.c, &a.c_row, &a.c_head);
@@ -387,9 +389,10 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   char* ws = (char*)workspace;
   hipStream_t st = (hipStream_t)stream;
 
-  // dq: the forward walk of (dout, v, k), whose state is the transposed one
+  // dq: the forward walk of (dout, v, k), whose state is the transposed one; it
+  // shares its launches, hence the chip, with the other
   AttnArgs a{};
-  put_walk(a, t, log_decay, offsets, p.cuts, p.slots, t->heads, p, ws);
+  put_walk(a, t, log_decay, offsets, false, p, ws);
   put(dout, &a.a, &a.a_row, &a.a_head);
   put(v, &a.b, &a.b_row, &a.b_head);
   put(k, &a.c, &a.c_row, &a.c_head);
@@ -401,12 +404,10 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   a.init = initial_state;
   a.init_swapped = 1;
   a.fault = fault;
-  if (launch_attention(a, T, st) != hipSuccess) return MMBEV_ERR_HIP;
 
   // dv and dk: backwards, the carried state that of q and dout, divided by scale
   AttnGradArgs b{};
-  put_walk(b, t, log_decay, offsets, p.grad_cuts, p.grad_slots, H / p.group, p, ws);
-  b.reversed = 1;
+  put_walk(b, t, log_decay, offsets, true, p, ws);
   put(q, &b.q, &b.q_row, &b.q_head);
   put(dout, &b.dout, &b.d_row, &b.d_head);
   put(k, &b.k, &b.k_row, &b.k_head);
@@ -431,7 +432,7 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   put(q, &s.b, &s.b_row, &s.b_head);
   put(dout, &s.c, &s.c_row, &s.c_head);
   s.b_div = s.c_div = 1;
-  if (launch_attention_grad(b, s, T, st) != hipSuccess) return MMBEV_ERR_HIP;
+  if (launch_attention_backward(a, b, s, T, st) != hipSuccess) return MMBEV_ERR_HIP;
   for (int which = 0; b.parts && which < 2; ++which) {
     AttnSumArgs u{};
     u.part = which ? b.part_v : b.part_k;
