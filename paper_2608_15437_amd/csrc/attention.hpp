@@ -24,18 +24,20 @@
 //
 // The gradients are the same recurrence: dq forwards as (dout, v, k); dv and dk
 // backwards in time as (k, q, dout) and (v, dout, q), whose states are one
-// another's transposes, so one walk makes both (attention_grad_kernel).
+// another's transposes, so one walk makes both (walk_back).
 // Backwards the state is carried one decay later, S' = lambda^n S + sum_j
 // lambda^(n-j) b_j^T c_j with lambda^i in place of lambda^(i+1), so that a
 // gradient of the final state enters undecayed and the last S is the initial
 // state's.
 //
-// 16-bit types: P and the state's copy are rounded to the type for their
-// products.  The rows that enter the state are c times its decay in two parts
-// (the rounded product and what the rounding left), so the state has 16 or 22
-// bits and not the type's 8 or 11; in bf16 a third part makes them 24 where
-// the state is asked for.  fp16 has too few exponents for a state that sums
-// many rows: its copy is scaled by a power of two.
+// 16-bit types: the rows that enter the state are c times its decay in two
+// parts, the rounded value and what the rounding left: 16 or 22 bits instead of
+// the type's 8 or 11; in bf16 a third part makes them 24 where the state is
+// asked for.  P and the state's copy are rounded to the type for their
+// products, together an error like the result's own rounding.  Calls of short
+// sequences take P in two parts too, which costs them nothing (long ones 4%).
+// fp16 has too few exponents for a state that sums many rows: its copy is
+// scaled by a power of two.
 #pragma once
 
 #include "common.hpp"
@@ -586,7 +588,8 @@ __device__ __forceinline__ void add_state_product(Rows<D>& acc, const T* s_s, co
 }
 
 // acc += sum over the rows j of the chunk up to the wave's own, scale * lambda^(i-j) (a_i . b_j) c_j.
-template <typename T, int D, bool SPLIT>
+// FINE: the pairs' factors in both parts.
+template <typename T, int D, bool SPLIT, bool FINE>
 __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s_c, const Frag<T> (&q)[kSteps<D>], const Powers& pw,
                                           const Lane& l) {
   constexpr int SD = D + kRowPad<T>;
@@ -613,12 +616,18 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
     }
     Frag<T> pf;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      pf.v[r] = (T)p[0][r];
-      pf.v[4 + r] = (T)p[1][r];
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (FINE && __is_same(T, f16)) asm("" : "+v"(p[e >> 2][e & 3]));  // see add_to_state
+      pf.v[e] = (T)p[e >> 2][e & 3];
     }
 #pragma unroll
     for (int t = 0; t < kTiles<D>; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
+    if constexpr (FINE && sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf.v[e] = (T)(p[e >> 2][e & 3] - (float)pf.v[e]);
+#pragma unroll
+      for (int t = 0; t < kTiles<D>; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
+    }
   }
 }
 
@@ -773,7 +782,7 @@ struct WalkShared {
 };
 
 // out: the walk of (a, b, c).
-template <typename T, int D, bool WHOLE>
+template <typename T, int D, bool WHOLE, bool FINE>
 __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, D>& shared) {
   constexpr bool SCALED = __is_same(T, f16);
   T *s_b = shared.b, *s_c = shared.c, *s_s = shared.s;
@@ -826,7 +835,7 @@ __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, 
       clear<D>(acc);
       if (have_state)
         add_state_product<T, D, false>(acc, s_s, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
-      add_pairs<T, D, false>(acc, s_b, s_c, qa, pw, l);
+      add_pairs<T, D, false, FINE>(acc, s_b, s_c, qa, pw, l);
       store_rows<WHOLE, D>(po, a.o_row, o, c0 + 16 * l.w, q.lo, acc, a.cd);
     }
     // the state after the chunk, where something reads it
@@ -840,10 +849,10 @@ __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, 
     store_state<D>(a.final_state + ((int64_t)q.b * a.H + h) * state, st, a.ad, a.cd, 1.0f, l);
 }
 
-template <typename T, int D, bool WHOLE>
+template <typename T, int D, bool WHOLE, bool FINE>
 __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_kernel(AttnArgs a) {
   __shared__ WalkShared<T, D> shared;
-  walk<T, D, WHOLE>(a, blockIdx.x, shared);
+  walk<T, D, WHOLE, FINE>(a, blockIdx.x, shared);
 }
 
 // dv and dk: one walk backwards, whose state is that of (q, dout) divided by
@@ -851,7 +860,7 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_ke
 // each chunk it goes through them with a state each, and their sums stay in
 // registers.  Where GROUP is not all of them, the sums are fp32 parts that
 // attention_sum_kernel adds.
-template <typename T, int D, int GROUP, bool WHOLE>
+template <typename T, int D, int GROUP, bool WHOLE, bool FINE>
 __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkShared<T, D>& shared) {
   constexpr bool SCALED = __is_same(T, f16);
   T *s_q = shared.b, *s_d = shared.c, *s_s = shared.s;
@@ -919,7 +928,7 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
         const float fade_in = have_state ? __builtin_ldexpf(pw[j].of(max(16 * l.w + l.n - skip, 0)) * a.scale, ex) : 0.0f;
         if (j == 0) clear<D>(acc_v);
         if (have_state) add_state_product<T, D, false>(acc_v, s_s, fk, fade_in);
-        add_pairs<T, D, false>(acc_v, s_q, s_d, fk, pw[j], l);
+        add_pairs<T, D, false, FINE>(acc_v, s_q, s_d, fk, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
             store_rows<WHOLE, D>(a.part_v + (int64_t)u * a.cd, groups * a.cd, o, at, q.lo, acc_v, a.cd);
@@ -928,7 +937,7 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
         }
         if (j == 0) clear<D>(acc_k);
         if (have_state) add_state_product<T, D, true>(acc_k, s_s, fv, fade_in);
-        add_pairs<T, D, true>(acc_k, s_d, s_q, fv, pw[j], l);
+        add_pairs<T, D, true, FINE>(acc_k, s_d, s_q, fv, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
             store_rows<WHOLE, D>(a.part_k + (int64_t)u * a.ad, groups * a.ad, o, at, q.lo, acc_k, a.ad);
@@ -954,14 +963,14 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
 // first (one after the other their last workgroups, and twice two more
 // launches for the cut sequences' states, left the chip idle: 167 us for one
 // robot frame instead of 113).
-template <typename T, int D, int GROUP, bool WHOLE>
+template <typename T, int D, int GROUP, bool WHOLE, bool FINE>
 __global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_backward_kernel(AttnArgs a, AttnGradArgs b,
                                                                                                        uint32_t back_items) {
   __shared__ WalkShared<T, D> shared;
   if (blockIdx.x < back_items)
-    walk_back<T, D, GROUP, WHOLE>(b, blockIdx.x, shared);
+    walk_back<T, D, GROUP, WHOLE, FINE>(b, blockIdx.x, shared);
   else
-    walk<T, D, WHOLE>(a, blockIdx.x - back_items, shared);
+    walk<T, D, WHOLE, FINE>(a, blockIdx.x - back_items, shared);
 }
 
 // Instances by the wider of the two dims: 32, 64 or 128, the rest zeros.
@@ -974,27 +983,27 @@ void launch_states(const AttnPair& p, hipStream_t st) {
                                                                      : go(attention_state_kernel<T, 128, WHOLE>);
 }
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool FINE>
 void launch_walk(const AttnArgs& a, hipStream_t st) {
   const int wide = a.ad > a.cd ? a.ad : a.cd;
   const dim3 grid((uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  wide <= 32 ? go(attention_kernel<T, 32, WHOLE>) : wide <= 64 ? go(attention_kernel<T, 64, WHOLE>) : go(attention_kernel<T, 128, WHOLE>);
+  wide <= 32 ? go(attention_kernel<T, 32, WHOLE, FINE>) : wide <= 64 ? go(attention_kernel<T, 64, WHOLE, FINE>) : go(attention_kernel<T, 128, WHOLE, FINE>);
 }
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool FINE>
 void launch_backward(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
   const int wide = b.ad > b.cd ? b.ad : b.cd;
   const uint32_t back = (uint32_t)((b.cuts + b.B) * (int64_t)(b.H / b.group));
   const dim3 grid(back + (uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, b, back); };
   if (wide <= 32)
-    b.group == 4 ? go(attention_backward_kernel<T, 32, 4, WHOLE>) : b.group == 2 ? go(attention_backward_kernel<T, 32, 2, WHOLE>)
-                                                                                 : go(attention_backward_kernel<T, 32, 1, WHOLE>);
+    b.group == 4 ? go(attention_backward_kernel<T, 32, 4, WHOLE, FINE>) : b.group == 2 ? go(attention_backward_kernel<T, 32, 2, WHOLE, FINE>)
+                                                                                 : go(attention_backward_kernel<T, 32, 1, WHOLE, FINE>);
   else if (wide <= 64)
-    b.group == 2 ? go(attention_backward_kernel<T, 64, 2, WHOLE>) : go(attention_backward_kernel<T, 64, 1, WHOLE>);
+    b.group == 2 ? go(attention_backward_kernel<T, 64, 2, WHOLE, FINE>) : go(attention_backward_kernel<T, 64, 1, WHOLE, FINE>);
   else
-    go(attention_backward_kernel<T, 128, 1, WHOLE>);
+    go(attention_backward_kernel<T, 128, 1, WHOLE, FINE>);
 }
 
 // WHOLE: see load_part; both walks' dims are the same two.
@@ -1007,12 +1016,18 @@ hipError_t states_of(const AttnPair& p, hipStream_t st) {
 }
 template <typename T>
 hipError_t walk_of(const AttnArgs& a, hipStream_t st) {
-  whole_packs(a) ? launch_walk<T, true>(a, st) : launch_walk<T, false>(a, st);
+  if (sizeof(T) == 2 && a.fine)
+    whole_packs(a) ? launch_walk<T, true, sizeof(T) == 2>(a, st) : launch_walk<T, false, sizeof(T) == 2>(a, st);
+  else
+    whole_packs(a) ? launch_walk<T, true, false>(a, st) : launch_walk<T, false, false>(a, st);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t backward_of(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
-  whole_packs(b) ? launch_backward<T, true>(a, b, st) : launch_backward<T, false>(a, b, st);
+  if (sizeof(T) == 2 && a.fine)
+    whole_packs(b) ? launch_backward<T, true, sizeof(T) == 2>(a, b, st) : launch_backward<T, false, sizeof(T) == 2>(a, b, st);
+  else
+    whole_packs(b) ? launch_backward<T, true, false>(a, b, st) : launch_backward<T, false, false>(a, b, st);
   return hipGetLastError();
 }
 

@@ -73,6 +73,7 @@ struct AttnWalk {
   int32_t reversed;
   int32_t init_swapped;
   int32_t exact_state;    // the state is an output: as exact as fp32
+  int32_t fine;           // all sequences are short: P in two parts
   float scale;
   float init_scale, final_scale;  // the state is carried divided by these
   // sequences are cut at shares of (rows in use) / cuts, at least `least` rows; 0: none is

@@ -597,6 +597,14 @@ def _empty(stream, like, shape, dtype):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _empty_like(stream, like):
+    """The same with `like`'s own shape and type."""
+    if stream is None:
+        return _torch.empty_like(like)
+    with _torch.cuda.stream(stream):
+        return _torch.empty_like(like)
+
+
 def _norm_of(x, weight, bias, eps) -> mmbev_norm_t:
     code = _dtype_code(x)
     if x.dim() != 2:
@@ -632,13 +640,13 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stat
     if residual is not None:
         _like("residual", residual, dtype, shape)
         if out_sum is None:
-            out_sum = _empty(stream, x, shape, dtype)
+            out_sum = _empty_like(stream, x)
     if out_sum is not None:
         _like("out_sum", out_sum, dtype, shape)
-    out = _empty(stream, x, shape, dtype) if out is None else _like("out", out, dtype, shape)
+    out = _empty_like(stream, x) if out is None else _like("out", out, dtype, shape)
     mean = rstd = None
     if stats:
-        mean, rstd = _empty(stream, x, shape[:1], torch.float32), _empty(stream, x, shape[:1], torch.float32)
+        mean, rstd = _empty(stream, x, (2, shape[0]), torch.float32).unbind(0)
     _check((_lib or load()).mmbev_layer_norm(
         desc, _rows("x", x), _rows("residual", residual), _ptr_of(weight), _ptr_of(bias),
         _vector("row_count", row_count, torch.int64, 1), _rows("out", out), _rows("out_sum", out_sum), _ptr_of(mean),
@@ -660,7 +668,7 @@ def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, d
     _like("dy", dy, dtype, shape)
     if dskip is not None:
         _like("dskip", dskip, dtype, shape)
-    dx = _empty(stream, s, shape, dtype) if dx is None else _like("dx", dx, dtype, shape)
+    dx = _empty_like(stream, s) if dx is None else _like("dx", dx, dtype, shape)
     if weight_grads:
         dweight = _empty(stream, s, shape[1:], torch.float32) if dweight is None else dweight
         dbias = _empty(stream, s, shape[1:], torch.float32) if dbias is None else dbias
@@ -701,7 +709,7 @@ def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = Fals
         raise MmbevError("positions must be int32 [rows] or [rows][axes], a row's columns next to each other")
     axes = at[1] if len(at) == 2 else 1
     pairs = steps.numel()
-    out = _empty(stream, x, shape, x.dtype) if out is None else _like("out", out, x.dtype, shape)
+    out = _empty_like(stream, x) if out is None else _like("out", out, x.dtype, shape)
     desc = mmbev_rotary_t(*shape, 2 * pairs, _dtype_code(x), ROTARY_LAYOUTS[layout], 1 if inverse else 0)
     _check((_lib or load()).mmbev_rotary(
         desc, xs, positions.data_ptr(), step[0] if shape[0] > 1 else axes, axes, _vector("steps", steps, torch.int64, pairs),
@@ -770,7 +778,7 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
     ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
     desc = _attention_of(q, k, v, n, scale, max_length)
     _like("dout", dout, q.dtype, (desc.rows, desc.heads, desc.value_dim))
-    dq, dk, dv = (_empty(stream, t, t.shape, t.dtype) if d is None else _like(name, d, t.dtype, t.shape)
+    dq, dk, dv = (_empty_like(stream, t) if d is None else _like(name, d, t.dtype, t.shape)
                   for name, d, t in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
     if dinitial_state is True:
         dinitial_state = _empty(stream, q, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32)
