@@ -127,12 +127,13 @@ __device__ __forceinline__ f32x4 mma(const Frag<float>& a, const Frag<float>& b,
 // call is reversed; sequence k in that order begins at bound(k).
 struct Order {
   const int64_t* offsets;
+  int64_t ahead[2];  // offsets of this lane's sequence, if it is one of the first 64
   int32_t used, B, reversed;
-  __device__ __forceinline__ int32_t bound(int32_t k) const {
-    const int64_t o = offsets[reversed ? B - k : k];
+  __device__ __forceinline__ int32_t clamped(int64_t o) const {
     const int32_t c = o < 0 ? 0 : o > used ? used : (int32_t)o;
     return reversed ? used - c : c;
   }
+  __device__ __forceinline__ int32_t bound(int32_t k) const { return clamped(offsets[reversed ? B - k : k]); }
   __device__ __forceinline__ int32_t row(int32_t p) const { return reversed ? used - 1 - p : p; }
   __device__ __forceinline__ int32_t sequence(int32_t k) const { return reversed ? B - 1 - k : k; }
 };
@@ -142,6 +143,10 @@ __device__ __forceinline__ Order order_of(const AttnWalk& a) {
   o.offsets = a.offsets;
   o.B = a.B;
   o.reversed = a.reversed;
+  // all of these loads before the first is waited for
+  const int k = min((int)(threadIdx.x & 63), a.B - 1);
+  o.ahead[0] = a.offsets[a.reversed ? a.B - k : k];
+  o.ahead[1] = a.offsets[a.reversed ? a.B - k - 1 : k + 1];
   const int64_t end = a.offsets[a.B];
   o.used = end < 0 ? 0 : end > a.rows ? (int32_t)a.rows : (int32_t)end;
   return o;
@@ -228,7 +233,8 @@ __device__ __forceinline__ bool find_part(Part& q, const Order& o, const AttnWal
   int32_t seen = 0, cut = 0;
   for (int32_t k0 = 0; k0 < o.B; k0 += 64) {
     const int32_t k = min(k0 + lane, o.B - 1);
-    const int32_t s0 = o.bound(k), n = max(o.bound(k + 1) - s0, 0);
+    const int32_t s0 = k0 == 0 ? o.clamped(o.ahead[0]) : o.bound(k);
+    const int32_t n = max((k0 == 0 ? o.clamped(o.ahead[1]) : o.bound(k + 1)) - s0, 0);
     const uint32_t parts = k0 + lane < o.B && n > most ? (uint32_t)(((int64_t)n + share - 1) / share) : 0u;
     const uint64_t cuts = __ballot(parts != 0);
     if (cuts == 0) continue;
