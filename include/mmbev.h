@@ -615,7 +615,7 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* rotary, mmbev_heads_t x, const
 typedef struct {
   int64_t rows;          /* rows that q, k, v and out hold, 0 .. 2^31-1 */
   int64_t max_length;    /* no sequence is longer (e.g. max_voxels); 0: rows */
-  int32_t num_sequences; /* B, 1..65535 */
+  int32_t num_sequences; /* B, 1..65535; (B + 1024) * heads <= 2^23 */
   int32_t heads;         /* of q and out, 1..256 */
   int32_t kv_heads;      /* of k and v, divides heads: head h reads k and v of head h*kv_heads/heads */
   int32_t key_dim;       /* 1..128 */
@@ -667,8 +667,8 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* attentio
                                                size_t workspace_bytes, void* stream);
 
 /*
- * One row for each of many streams (attention->rows of them; num_sequences
- * and max_length are not read): row r updates state[slots[r]] in place and
+ * One row for each of many streams (attention->rows of them, rows * heads <=
+ * 2^23; num_sequences and max_length are not read): row r updates state[slots[r]] in place and
  * reads it,
  *   S = lambda * S + k_r^T v_r;  out_r = scale * q_r S
  * state   fp32 [num_slots][heads][key_dim][value_dim], 16-byte aligned

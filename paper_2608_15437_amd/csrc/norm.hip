@@ -68,9 +68,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
   constexpr int VEC = kPackOf<T>, ROWS = kNormThreads / LANES;
   __shared__ float s_part[4];
   const int64_t n = rows_in_use(a.row_count, a.rows, a.fault);
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  const int64_t row0 = a.first_row + (int64_t)blockIdx.x * ROWS, row = row0 + threadIdx.x / LANES;
   const int lane = threadIdx.x % LANES;
-  if ((int64_t)blockIdx.x * ROWS >= n) return;
+  if (row0 >= n) return;
   const bool live = row < n;
   float f[PACKS][VEC];
   float sum = 0.0f;
@@ -316,8 +316,11 @@ template <typename T>
 hipError_t norm_of(const NormArgs& a, NormShape s, hipStream_t st) {
   return with_shape<T>(s, [&](auto lanes, auto packs) {
     constexpr int rows = kNormThreads / lanes.value;
-    hipLaunchKernelGGL((norm_kernel<T, lanes.value, packs.value>), dim3((uint32_t)((a.rows + rows - 1) / rows)),
-                       dim3(kNormThreads), 0, st, a);
+    NormArgs part = a;
+    for (; part.first_row < a.rows; part.first_row += kMostGroups * rows) {
+      const int64_t groups = std::min((a.rows - part.first_row + rows - 1) / rows, kMostGroups);
+      hipLaunchKernelGGL((norm_kernel<T, lanes.value, packs.value>), dim3((uint32_t)groups), dim3(kNormThreads), 0, st, part);
+    }
   });
 }
 

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotSh
   constexpr int V = kPackOf<T>, PAIRS = Elements::PAIRS;
   const int64_t n = rows_in_use(a.row_count, a.rows, a.fault);
   const int per_row = s.items * s.head_parts;
-  const int64_t row0 = (int64_t)blockIdx.x * s.rows_block;
+  const int64_t row0 = a.first_row + (int64_t)blockIdx.x * s.rows_block;
   if (row0 >= n) return;
   const int half = a.rotary_dim / 2;
   for (int t = threadIdx.x; t < s.rows_block * per_row; t += kRotThreads) {
@@ -157,11 +157,14 @@ hipError_t rotary_of(const RotaryArgs& a, hipStream_t st) {
   s.heads_each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(8, a.rows * s.items * a.heads / wanted));
   s.head_parts = (a.heads + s.heads_each - 1) / s.heads_each;
   s.rows_block = std::max(1, kRotThreads / (s.items * s.head_parts));
-  const uint64_t grid = ((uint64_t)a.rows + s.rows_block - 1) / s.rows_block;
-  if (a.interleaved)
-    hipLaunchKernelGGL((rotary_kernel<T, true>), dim3((uint32_t)grid), dim3(kRotThreads), 0, st, a, s);
-  else
-    hipLaunchKernelGGL((rotary_kernel<T, false>), dim3((uint32_t)grid), dim3(kRotThreads), 0, st, a, s);
+  RotaryArgs part = a;
+  for (; part.first_row < a.rows; part.first_row += kMostGroups * s.rows_block) {
+    const int64_t groups = std::min((a.rows - part.first_row + s.rows_block - 1) / s.rows_block, kMostGroups);
+    if (a.interleaved)
+      hipLaunchKernelGGL((rotary_kernel<T, true>), dim3((uint32_t)groups), dim3(kRotThreads), 0, st, part, s);
+    else
+      hipLaunchKernelGGL((rotary_kernel<T, false>), dim3((uint32_t)groups), dim3(kRotThreads), 0, st, part, s);
+  }
   return hipGetLastError();
 }
 

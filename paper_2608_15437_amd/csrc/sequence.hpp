@@ -12,6 +12,10 @@ namespace mmbev {
 
 // ------------------------------------------------------------- arguments
 
+// Workgroups of a launch: with 256 threads each they stay under the 2^32
+// threads that one may have.  More rows take more launches.
+constexpr int64_t kMostGroups = (int64_t)1 << 23;
+
 struct NormArgs {
   const void* x;         // forward: x; backward: s
   const void* skip;      // forward: residual; backward: dskip (null: none)
@@ -28,6 +32,7 @@ struct NormArgs {
   const int64_t* row_count;
   int32_t* fault;
   int64_t rows, x_stride, skip_stride, dy_stride, out_stride, sum_stride;
+  int64_t first_row;     // of the launch
   int32_t width;
   int32_t weight_f32;    // weight and bias are fp32 (else of the rows' type)
   float eps, inv_width;
@@ -46,6 +51,7 @@ struct RotaryArgs {
   const int64_t* row_count;
   int32_t* fault;
   int64_t rows, x_row, x_head, out_row, out_head, position_stride;
+  int64_t first_row;     // of the launch
   int32_t heads, dim, rotary_dim, axes;
   int32_t interleaved, inverse, copy_rest;  // copy_rest: out is not x
 };

@@ -98,7 +98,8 @@ mmbev_status_t attention_ok(const mmbev_attention_t* t, bool step) {
   if (!std::isfinite(t->scale) || t->scale == 0.0f) return MMBEV_ERR_INVALID_ARG;
   if (!step && (t->num_sequences < 1 || t->num_sequences > 65535 || t->max_length < 0)) return MMBEV_ERR_INVALID_ARG;
   if (t->rows > kMaxRows || t->heads > 256 || t->key_dim > 128 || t->value_dim > 128) return MMBEV_ERR_UNSUPPORTED;
-  if (step && t->rows * t->heads > kMaxRows) return MMBEV_ERR_UNSUPPORTED;
+  // a workgroup each, and the parts of cut sequences
+  if ((step ? t->rows : (int64_t)t->num_sequences + 1024) * t->heads > kMostGroups) return MMBEV_ERR_UNSUPPORTED;
   return MMBEV_OK;
 }
 

@@ -189,3 +189,12 @@ def test_binding_refuses_what_the_kernels_cannot_take(mb):
         mb._dtype_code(x.double())
     with pytest.raises(mb.MmbevError, match="contiguous"):
         mb._vector("log_decay", torch.zeros(8, dtype=torch.float64), torch.float32, 8)
+
+
+def test_more_workgroups_than_a_launch_may_have_are_refused(mb):
+    assert mb.linear_attention_workspace_bytes(attention(mb, num_sequences=65535, heads=128, kv_heads=128)) == 0
+    assert mb.linear_attention_workspace_bytes(attention(mb, num_sequences=65535, heads=64, kv_heads=64)) > 0
+    L = mb.load()
+    q = mb.mmbev_heads_t(FAKE, 256, 64)
+    d = attention(mb, rows=(1 << 21) + 1, kv_heads=4, value_dim=64)
+    assert L.mmbev_linear_attention_step(ctypes.byref(d), q, q, q, FAKE, FAKE, 50, FAKE, q, None, None) == mb.ERR_UNSUPPORTED
