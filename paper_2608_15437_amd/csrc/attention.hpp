@@ -886,16 +886,22 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
 
   const int32_t first = q.hi - (q.hi - q.lo + kChunk - 1) / kChunk * kChunk;
   Pack<T, 8> rq[kPacks<D>], rd[kPacks<D>];
+  // the next chunk's rows of k and v are loaded with its tiles where the registers allow, else when this chunk's are
+  // done with
+  constexpr bool AHEAD = D < 128;
   Frag<T> fk[kSteps<D>], fv[kSteps<D>], nk[kSteps<D>], nv[kSteps<D>];
   auto fetch = [&](int32_t c0, int j) {
     fetch_tile<T, D, WHOLE>(rq, pq + j * a.q_head, a.q_row, a.ad, o, c0, q.lo);
     fetch_tile<T, D, WHOLE>(rd, pd + j * a.d_head, a.d_row, a.cd, o, c0, q.lo);
-    if (j == 0) {
-      fetch_rows<T, D, WHOLE, false>(nk, pk, a.k_row, a.ad, o, c0 + 16 * l.w, q.lo, l);
-      fetch_rows<T, D, WHOLE, true>(nv, pv, a.v_row, a.cd, o, c0 + 16 * l.w, q.lo, l);
-    }
   };
-  if (q.lo < q.hi) fetch(first, 0);
+  auto fetch_own = [&](int32_t c0) {
+    fetch_rows<T, D, WHOLE, false>(nk, pk, a.k_row, a.ad, o, c0 + 16 * l.w, q.lo, l);
+    fetch_rows<T, D, WHOLE, true>(nv, pv, a.v_row, a.cd, o, c0 + 16 * l.w, q.lo, l);
+  };
+  if (q.lo < q.hi) {
+    fetch(first, 0);
+    fetch_own(first);
+  }
   const float* from = q.began ? a.cut_state + ((int64_t)(q.before - 1) * a.H + h0) * state
                       : a.init ? a.init + ((int64_t)q.b * a.H + h0) * state
                                : nullptr;
@@ -926,10 +932,12 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
       const int ex = SCALED && have_state ? copy_exponent(s_max[j]) : 0;
       if (have_state && own) put_state<T, D>(s_s, st[j], __builtin_ldexpf(1.0f, -ex), l);
       __syncthreads();
-      if (j + 1 < GROUP)
+      if (j + 1 < GROUP) {
         fetch(c0, j + 1);
-      else if (c0 + kChunk < q.hi)
+      } else if (c0 + kChunk < q.hi) {
         fetch(c0 + kChunk, 0);
+        if (AHEAD) fetch_own(c0 + kChunk);
+      }
       if (16 * l.w + 15 >= skip) {
         const float fade_in = have_state ? __builtin_ldexpf(pw[j].of(max(16 * l.w + l.n - skip, 0)) * a.scale, ex) : 0.0f;
         if (j == 0) clear<D>(acc_v);
@@ -951,6 +959,7 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
             store_rows<WHOLE, D>(static_cast<T*>(a.dk) + (int64_t)hk * a.dk_head, a.dk_row, o, at, q.lo, acc_k, a.ad);
         }
       }
+      if (!AHEAD && j == GROUP - 1 && c0 + kChunk < q.hi) fetch_own(c0 + kChunk);
       if (needed) {
         if (own) update_state<T, D>(st[j], s_q, s_d, pw[j], skip ? pw[j].of(kChunk - skip) : pw[j].fade_chunk, a.exact_state, l);
         if constexpr (SCALED) put_max<D>(s_max[j], st[j], l);
