@@ -646,7 +646,8 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
 // line; and then two such lines of a row with the row eight further, until a
 // store covers eight rows of 128 bytes, a cache line each.
 template <bool WHOLE, int D, typename T>
-__device__ __forceinline__ void store_rows(T* base, int32_t stride, const Order& o, int32_t at, int32_t lo, const Rows<D>& acc, int dim) {
+__device__ __forceinline__ void store_rows(T* base, int32_t stride, const Order& o, int32_t at, int32_t lo, const Rows<D>& acc, int dim,
+                                           bool past) {
   const int g = (threadIdx.x & 63) >> 4, n = threadIdx.x & 15;
   if constexpr (sizeof(T) == 2) {
     uint32_t line[kTiles<D> / 2][4];
@@ -677,9 +678,9 @@ __device__ __forceinline__ void store_rows(T* base, int32_t stride, const Order&
       Pack<T, 8> r;
       __builtin_memcpy(&r, q, 16);
       if constexpr (WHOLE) {
-        if (c < dim) store_pack<T, 8>(to, r);
+        if (c < dim) store_some<T, 8>(to, r, 8, past);
       } else {
-        store_some<T, 8>(to, r, dim - c);
+        store_some<T, 8>(to, r, dim - c, past);
       }
     };
     if constexpr (D == 32) {
@@ -710,9 +711,9 @@ __device__ __forceinline__ void store_rows(T* base, int32_t stride, const Order&
       for (int r = 0; r < 4; ++r) q.v[r] = (T)acc[t][r];
       const int c = 16 * t + 4 * g;
       if constexpr (WHOLE) {
-        if (c < dim) store_pack<T, 4>(to + c, q);
+        if (c < dim) store_some<T, 4>(to + c, q, 4, past);
       } else {
-        store_some<T, 4>(to + c, q, dim - c);
+        store_some<T, 4>(to + c, q, dim - c, past);
       }
     }
   }
@@ -842,7 +843,7 @@ __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, 
       if (have_state)
         add_state_product<T, D, false>(acc, s_s, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
       add_pairs<T, D, false, FINE>(acc, s_b, s_c, qa, pw, l);
-      store_rows<WHOLE, D>(po, a.o_row, o, c0 + 16 * l.w, q.lo, acc, a.cd);
+      store_rows<WHOLE, D>(po, a.o_row, o, c0 + 16 * l.w, q.lo, acc, a.cd, a.past);
     }
     // the state after the chunk, where something reads it
     if (c0 + kChunk < q.hi || (!q.goes_on && a.final_state)) {
@@ -945,18 +946,18 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
         add_pairs<T, D, false, FINE>(acc_v, s_q, s_d, fk, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
-            store_rows<WHOLE, D>(a.part_v + (int64_t)u * a.cd, groups * a.cd, o, at, q.lo, acc_v, a.cd);
+            store_rows<WHOLE, D>(a.part_v + (int64_t)u * a.cd, groups * a.cd, o, at, q.lo, acc_v, a.cd, a.past);
           else
-            store_rows<WHOLE, D>(static_cast<T*>(a.dv) + (int64_t)hk * a.dv_head, a.dv_row, o, at, q.lo, acc_v, a.cd);
+            store_rows<WHOLE, D>(static_cast<T*>(a.dv) + (int64_t)hk * a.dv_head, a.dv_row, o, at, q.lo, acc_v, a.cd, a.past);
         }
         if (j == 0) clear<D>(acc_k);
         if (have_state) add_state_product<T, D, true>(acc_k, s_s, fv, fade_in);
         add_pairs<T, D, true, FINE>(acc_k, s_d, s_q, fv, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
-            store_rows<WHOLE, D>(a.part_k + (int64_t)u * a.ad, groups * a.ad, o, at, q.lo, acc_k, a.ad);
+            store_rows<WHOLE, D>(a.part_k + (int64_t)u * a.ad, groups * a.ad, o, at, q.lo, acc_k, a.ad, a.past);
           else
-            store_rows<WHOLE, D>(static_cast<T*>(a.dk) + (int64_t)hk * a.dk_head, a.dk_row, o, at, q.lo, acc_k, a.ad);
+            store_rows<WHOLE, D>(static_cast<T*>(a.dk) + (int64_t)hk * a.dk_head, a.dk_row, o, at, q.lo, acc_k, a.ad, a.past);
         }
       }
       if (!AHEAD && j == GROUP - 1 && c0 + kChunk < q.hi) fetch_own(c0 + kChunk);

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
           r.v[e] = (T)(f[p][e] + (float)r.v[e]);
           f[p][e] = (float)r.v[e];
         }
-        if (a.sum) store_some<T, VEC>(static_cast<T*>(a.sum) + row * a.sum_stride + c, r, a.width - c);
+        if (a.sum) store_some<T, VEC>(static_cast<T*>(a.sum) + row * a.sum_stride + c, r, a.width - c, a.past);
       }
     } else if (a.sum) {
 #pragma unroll
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
         Pack<T, VEC> r;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) r.v[e] = (T)f[p][e];
-        store_some<T, VEC>(static_cast<T*>(a.sum) + row * a.sum_stride + c, r, a.width - c);
+        store_some<T, VEC>(static_cast<T*>(a.sum) + row * a.sum_stride + c, r, a.width - c, a.past);
       }
     }
 #pragma unroll
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
     Pack<T, VEC> r;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) r.v[e] = (T)__builtin_fmaf(f[p][e] * rstd, w[e], b[e]);
-    store_some<T, VEC>(out + c, r, left);
+    store_some<T, VEC>(out + c, r, left, a.past);
   }
 }
 
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormArgs a)
       Pack<T, VEC> r;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) r.v[e] = (T)k[e];
-      store_some<T, VEC>(dx + c, r, left);
+      store_some<T, VEC>(dx + c, r, left, a.past);
     }
   }
   if (!a.partial) return;

@@ -56,22 +56,25 @@ struct Turned {
   static constexpr int V = kPackOf<T>, PAIRS = INTERLEAVED ? V / 2 : V;
   Pack<T, V> p, q;
 
-  __device__ __forceinline__ void load(const T* x, int j0, int half) {
+  static __device__ __forceinline__ Pack<T, V> load_one(const T* x, int left, bool past) {
+    return past && left >= V ? load_past<T, V>(x) : load_some<T, V>(x, left);
+  }
+  __device__ __forceinline__ void load(const T* x, int j0, int half, bool past) {
     const int left = half - j0;
     if constexpr (INTERLEAVED) {
-      p = load_some<T, V>(x + 2 * j0, 2 * left);
+      p = load_one(x + 2 * j0, 2 * left, past);
     } else {
-      p = load_some<T, V>(x + j0, left);
-      q = load_some<T, V>(x + half + j0, left);
+      p = load_one(x + j0, left, past);
+      q = load_one(x + half + j0, left, past);
     }
   }
-  __device__ __forceinline__ void store(T* x, int j0, int half) const {
+  __device__ __forceinline__ void store(T* x, int j0, int half, bool past) const {
     const int left = half - j0;
     if constexpr (INTERLEAVED) {
-      store_some<T, V>(x + 2 * j0, p, 2 * left);
+      store_some<T, V>(x + 2 * j0, p, 2 * left, past);
     } else {
-      store_some<T, V>(x + j0, p, left);
-      store_some<T, V>(x + half + j0, q, left);
+      store_some<T, V>(x + j0, p, left, past);
+      store_some<T, V>(x + half + j0, q, left, past);
     }
   }
   __device__ __forceinline__ void turn(const float (&sn)[PAIRS], const float (&cs)[PAIRS]) {
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotSh
     if (item >= s.turned) {  // the head's rest, copied
       const int c = a.rotary_dim + (item - s.turned) * V;
       for (int h = h0; h < h1; ++h, x += a.x_head, out += a.out_head)
-        store_some<T, V>(out + c, load_some<T, V>(x + c, a.dim - c), a.dim - c);
+        store_some<T, V>(out + c, load_some<T, V>(x + c, a.dim - c), a.dim - c, a.past);
       continue;
     }
     const int j0 = item * PAIRS;
@@ -129,18 +132,18 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotSh
     for (; h + 4 <= h1; h += 4, x += 4 * a.x_head, out += 4 * a.out_head) {
       Elements e[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[i].load(x + i * a.x_head, j0, half);
+      for (int i = 0; i < 4; ++i) e[i].load(x + i * a.x_head, j0, half, a.past);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         e[i].turn(sn, cs);
-        e[i].store(out + i * a.out_head, j0, half);
+        e[i].store(out + i * a.out_head, j0, half, a.past);
       }
     }
     for (; h < h1; ++h, x += a.x_head, out += a.out_head) {
       Elements e;
-      e.load(x, j0, half);
+      e.load(x, j0, half, a.past);
       e.turn(sn, cs);
-      e.store(out, j0, half);
+      e.store(out, j0, half, a.past);
     }
   }
 }

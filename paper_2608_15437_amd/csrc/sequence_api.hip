@@ -57,8 +57,9 @@ mmbev_status_t norm_ok(const mmbev_norm_t* n) {
   return MMBEV_OK;
 }
 
-NormArgs norm_args(const mmbev_norm_t* n, const int64_t* row_count, int32_t* fault) {
+NormArgs norm_args(const mmbev_norm_t* n, int32_t arrays, const int64_t* row_count, int32_t* fault) {
   NormArgs a{};
+  a.past = arrays * n->rows * n->width * size_of(n->dtype) > kPastCaches;
   a.rows = n->rows;
   a.width = n->width;
   a.weight_f32 = n->weight_dtype == MMBEV_F32;
@@ -175,6 +176,7 @@ void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, c
   a.cuts = cuts;
   a.longest_first = t->num_sequences <= kOrderedSequences && t->num_sequences * heads > p.slots;
   a.fine = short_rows(t);
+  a.past = t->rows * (t->heads + t->kv_heads) * (t->key_dim + t->value_dim) * size_of(t->dtype) > kPastCaches;
   a.least = p.least;
   a.reversed = backwards;
   a.cut_rows = (int32_t*)(ws + p.off_rows) + before;
@@ -205,7 +207,7 @@ mmbev_status_t mmbev_layer_norm(const mmbev_norm_t* norm, mmbev_rows_t x, mmbev_
       !rows_ok(out_sum, R, C, T, true))
     return MMBEV_ERR_INVALID_ARG;
   if (!aligned(weight, size_of(norm->weight_dtype)) || !aligned(bias, size_of(norm->weight_dtype))) return MMBEV_ERR_INVALID_ARG;
-  NormArgs a = norm_args(norm, row_count, fault);
+  NormArgs a = norm_args(norm, 2 + (residual.data != nullptr) + (out_sum.data != nullptr), row_count, fault);
   a.x = x.data;
   a.x_stride = x.row_stride;
   a.skip = residual.data;
@@ -242,7 +244,7 @@ mmbev_status_t mmbev_layer_norm_backward(const mmbev_norm_t* norm, mmbev_rows_t 
   const bool sums = dweight || dbias;
   if (sums && !workspace_ok(workspace, workspace_bytes, mmbev_layer_norm_backward_workspace_bytes(norm)))
     return MMBEV_ERR_WORKSPACE;
-  NormArgs a = norm_args(norm, row_count, fault);
+  NormArgs a = norm_args(norm, 3 + (dskip.data != nullptr), row_count, fault);
   a.x = s.data;
   a.x_stride = s.row_stride;
   a.dy = dy.data;
@@ -330,6 +332,7 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* t, mmbev_heads_t x, const int3
   a.interleaved = t->layout == MMBEV_ROTARY_INTERLEAVED;
   a.inverse = t->inverse;
   a.copy_rest = !same;
+  a.past = 2 * t->rows * t->heads * t->dim * size_of(t->dtype) > kPastCaches;
   return status_of(launch_rotary(a, t->dtype, (hipStream_t)stream));
 }
 
