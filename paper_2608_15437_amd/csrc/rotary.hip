@@ -11,7 +11,7 @@
 // those pairs of several heads
 // (the fewer rows, the fewer heads a thread, so that small calls spread out).
 // The operator moves bytes: 7 operations a pair and head beside the loads, and
-// some 50 a pair for its angle.
+// some 50 a pair for its angle.  213,879 x 16 x 64 bf16: 151 us, 5.8 TB/s.
 #include <algorithm>
 
 #include "sequence.hpp"
