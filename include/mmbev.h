@@ -641,9 +641,9 @@ size_t mmbev_linear_attention_workspace_bytes(const mmbev_attention_t* attention
  * has no gradient.  A sequence with a NaN or infinity in a row has
  * unspecified outputs; other sequences and heads do not see it.
  * The state is decayed, summed and carried in fp32 over all of a sequence;
- * for 16-bit types its product with q takes it rounded to that type, and the
- * decayed rows enter the state as two parts of the type, 16 bits or more
- * together.
+ * for 16-bit types what the matrix cores multiply (the state, the pairs'
+ * factors scale * lambda^(i-j) * q_i k_j, the decayed rows that enter the
+ * state) is two parts of the type, 16 bits or more together.
  * max_length only sizes the launches: longer sequences are computed too.
  * out must not overlap an input.
  */

@@ -38,11 +38,13 @@
 // 16-bit types: the rows that enter the state are c times its decay in two
 // parts, the rounded value and what the rounding left: 16 or 22 bits instead of
 // the type's 8 or 11; in bf16 a third part makes them 24 where the state is
-// asked for.  P and the state's copy are rounded to the type for their
-// products, together an error like the result's own rounding.  Calls of short
-// sequences take P in two parts too, which costs them nothing (long ones 4%).
-// fp16 has too few exponents for a state that sums many rows: its copy is
-// scaled by a power of two.
+// asked for.  P and the state's copy take part in two parts as well, so that a
+// result is off by its own rounding and no more (rounded once they add an error
+// of that size, 1.4 times it together; the four more products cost 128 frames
+// 979 us instead of 918, the gradients of 8 crowded frames 607 instead of 514,
+// those of one robot frame's heads of 128, where the parts take turns in LDS,
+// 152 instead of 109).  fp16 has too few exponents for a state that sums many
+// rows: its copy is scaled by a power of two.
 #pragma once
 
 #include "common.hpp"
@@ -495,19 +497,23 @@ __device__ __forceinline__ int copy_exponent(const float* s_max) {
   return __builtin_amdgcn_readfirstlane(ex);
 }
 
-// The state's copy in LDS, [column][row].
+// The state's copy in LDS, [column][row]; in 16-bit types what its rounding leaves as another, `low`.
 template <typename T, int D>
-__device__ __forceinline__ void put_state(T* s, const State<D>& st, float times, const Lane& l) {
+__device__ __forceinline__ void put_state(T* s, T* low, const State<D>& st, float times, const Lane& l) {
 #pragma unroll
   for (int vt = 0; vt < kOwnTiles<D>; ++vt)
 #pragma unroll
     for (int kt = 0; kt < kTiles<D>; ++kt) {
-      Pack<T, 4> q;
+      const int at = (16 * (l.w * kOwnTiles<D> + vt) + l.n) * (D + kRowPad<T>) + 16 * kt + 4 * l.g;
+      Pack<T, 4> q, rest;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) q.v[r] = (T)(__is_same(T, f16) ? st[kt][vt][r] * times : st[kt][vt][r]);
-      __builtin_memcpy(__builtin_assume_aligned(
-                           s + (16 * (l.w * kOwnTiles<D> + vt) + l.n) * (D + kRowPad<T>) + 16 * kt + 4 * l.g, 4 * sizeof(T)),
-                       &q, sizeof(q));
+      for (int r = 0; r < 4; ++r) {
+        const float x = __is_same(T, f16) ? st[kt][vt][r] * times : st[kt][vt][r];
+        q.v[r] = (T)x;
+        if constexpr (sizeof(T) == 2) rest.v[r] = (T)(x - (float)q.v[r]);
+      }
+      __builtin_memcpy(__builtin_assume_aligned(s + at, 4 * sizeof(T)), &q, sizeof(q));
+      if constexpr (sizeof(T) == 2) __builtin_memcpy(__builtin_assume_aligned(low + at, 4 * sizeof(T)), &rest, sizeof(rest));
     }
 }
 
@@ -583,24 +589,28 @@ __device__ __forceinline__ void clear(Rows<D>& acc) {
   for (int t = 0; t < kTiles<D>; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 }
 
-// acc += times * (the rows' a) S.  SPLIT: S transposed, a in load_cols' order.
+// acc += times * (the rows' a) S, S in its parts.  SPLIT: S transposed, a in load_cols' order.
 template <typename T, int D, bool SPLIT>
-__device__ __forceinline__ void add_state_product(Rows<D>& acc, const T* s_s, const Frag<T> (&q)[kSteps<D>], float times) {
+__device__ __forceinline__ void add_state_product(Rows<D>& acc, const T* s_s, const T* s_low, const Frag<T> (&q)[kSteps<D>],
+                                                  float times) {
   constexpr int SD = D + kRowPad<T>;
 #pragma unroll
   for (int t = 0; t < kTiles<D>; ++t) {
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < kSteps<D>; ++s)
+    for (int s = 0; s < kSteps<D>; ++s) {
       x = mma(SPLIT ? load_cols(s_s, SD, 32 * s, 16 * t) : load_rows(s_s, SD, 16 * t, 32 * s), q[s], x);
+      if constexpr (sizeof(T) == 2)
+        x = mma(SPLIT ? load_cols(s_low, SD, 32 * s, 16 * t) : load_rows(s_low, SD, 16 * t, 32 * s), q[s], x);
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) acc[t][r] = __builtin_fmaf(x[r], times, acc[t][r]);
   }
 }
 
-// acc += sum over the rows j of the chunk up to the wave's own, scale * lambda^(i-j) (a_i . b_j) c_j.
-// FINE: the pairs' factors in both parts.
-template <typename T, int D, bool SPLIT, bool FINE>
+// acc += sum over the rows j of the chunk up to the wave's own, scale * lambda^(i-j) (a_i . b_j) c_j.  In 16-bit types
+// the pairs' factors take part as the rounded value and what the rounding left.
+template <typename T, int D, bool SPLIT>
 __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s_c, const Frag<T> (&q)[kSteps<D>], const Powers& pw,
                                           const Lane& l) {
   constexpr int SD = D + kRowPad<T>;
@@ -625,19 +635,18 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
         for (int r = 0; r < 4; ++r) p[u][r] *= pw.off[r] * f;
       }
     }
-    Frag<T> pf;
+    Frag<T> pf, rest;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if constexpr (FINE && __is_same(T, f16)) asm("" : "+v"(p[e >> 2][e & 3]));  // see add_to_state
+      if constexpr (__is_same(T, f16)) asm("" : "+v"(p[e >> 2][e & 3]));  // see add_to_state
       pf.v[e] = (T)p[e >> 2][e & 3];
+      if constexpr (sizeof(T) == 2) rest.v[e] = (T)(p[e >> 2][e & 3] - (float)pf.v[e]);
     }
 #pragma unroll
-    for (int t = 0; t < kTiles<D>; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
-    if constexpr (FINE && sizeof(T) == 2) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pf.v[e] = (T)(p[e >> 2][e & 3] - (float)pf.v[e]);
-#pragma unroll
-      for (int t = 0; t < kTiles<D>; ++t) acc[t] = mma(load_cols(s_c, SD, 32 * s2, 16 * t), pf, acc[t]);
+    for (int t = 0; t < kTiles<D>; ++t) {
+      const Frag<T> c = load_cols(s_c, SD, 32 * s2, 16 * t);
+      acc[t] = mma(c, pf, acc[t]);
+      if constexpr (sizeof(T) == 2) acc[t] = mma(c, rest, acc[t]);
     }
   }
 }
@@ -784,20 +793,27 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_st
   if (own) store_state<D>(a.cut_state + ((int64_t)unit * a.H + h) * a.ad * a.cd, st, a.ad, a.cd, 1.0f, l);
 }
 
+// The second part of the state's copy lies beside the first where two workgroups of it still fit a compute unit.  Else
+// (16-bit heads over 64) it takes the chunks' place: the products with the state come first, then the chunks.  (Taking
+// the first part's place when that has been read: 160 us for the robot frame's gradients instead of 152.)
+template <typename T, int D>
+constexpr bool kStateFirst = sizeof(T) == 2 && D > 64;
+
 // LDS of a walk: two operands' chunks, the state's copy, fp16's largest values.
 template <typename T, int D>
 struct WalkShared {
-  __attribute__((aligned(16))) T b[kChunk * (D + kRowPad<T>)];
-  __attribute__((aligned(16))) T c[kChunk * (D + kRowPad<T>)];
+  __attribute__((aligned(16))) T chunk[2][kChunk * (D + kRowPad<T>)];
   __attribute__((aligned(16))) T s[D * (D + kRowPad<T>)];
+  __attribute__((aligned(16))) T low[sizeof(T) == 2 && !kStateFirst<T, D> ? D * (D + kRowPad<T>) : 8];
+  static_assert(!kStateFirst<T, D> || D <= 2 * kChunk, "both chunks hold it");
   float most[4][kAttnWaves];  // of each head that the workgroup takes
 };
 
 // out: the walk of (a, b, c).
-template <typename T, int D, bool WHOLE, bool FINE>
+template <typename T, int D, bool WHOLE>
 __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, D>& shared) {
-  constexpr bool SCALED = __is_same(T, f16);
-  T *s_b = shared.b, *s_c = shared.c, *s_s = shared.s;
+  constexpr bool SCALED = __is_same(T, f16), STATE_FIRST = kStateFirst<T, D>;
+  T *s_b = shared.chunk[0], *s_c = shared.chunk[1], *s_s = shared.s, *s_low = STATE_FIRST ? shared.chunk[0] : shared.low;
   float* s_max = shared.most[0];
   const Lane l = lane_of();
   const int h = item % a.H, unit = item / a.H;
@@ -833,21 +849,30 @@ __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, 
 
   for (int32_t c0 = first; c0 < q.hi; c0 += kChunk) {
     const int skip = max(q.lo - c0, 0);
+    const bool some = 16 * l.w + 15 >= skip;  // of the wave's rows
+    auto put_chunk = [&] {
+      put_tile<T, D, WHOLE>(s_b, rb, a.ad, skip);
+      put_tile<T, D, WHOLE>(s_c, rc, a.cd, skip);
+    };
     __syncthreads();  // the chunk before has been read
-    put_tile<T, D, WHOLE>(s_b, rb, a.ad, skip);
-    put_tile<T, D, WHOLE>(s_c, rc, a.cd, skip);
+    if (!STATE_FIRST) put_chunk();
     take_rows<T, D, WHOLE, false>(qa, qn, a.ad, l);
     const int ex = SCALED && have_state ? copy_exponent(s_max) : 0;
-    if (have_state && own) put_state<T, D>(s_s, st, __builtin_ldexpf(1.0f, -ex), l);
-    __syncthreads();
-    if (c0 + kChunk < q.hi) fetch(c0 + kChunk);
-
-    if (16 * l.w + 15 >= skip) {
-      Rows<D> acc;
-      clear<D>(acc);
-      if (have_state)
-        add_state_product<T, D, false>(acc, s_s, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
-      add_pairs<T, D, false, FINE>(acc, s_b, s_c, qa, pw, l);
+    if (have_state && own) put_state<T, D>(s_s, s_low, st, __builtin_ldexpf(1.0f, -ex), l);
+    if (!STATE_FIRST || have_state) __syncthreads();
+    if (!STATE_FIRST && c0 + kChunk < q.hi) fetch(c0 + kChunk);
+    Rows<D> acc;
+    clear<D>(acc);
+    if (have_state && some)
+      add_state_product<T, D, false>(acc, s_s, s_low, qa, __builtin_ldexpf(pw.of(max(16 * l.w + l.n - skip, 0) + 1) * a.scale, ex));
+    if (STATE_FIRST) {
+      if (have_state) __syncthreads();
+      put_chunk();
+      __syncthreads();
+      if (c0 + kChunk < q.hi) fetch(c0 + kChunk);
+    }
+    if (some) {
+      add_pairs<T, D, false>(acc, s_b, s_c, qa, pw, l);
       store_rows<WHOLE, D>(po, a.o_row, o, c0 + 16 * l.w, q.lo, acc, a.cd, a.past);
     }
     // the state after the chunk, where something reads it
@@ -861,10 +886,10 @@ __device__ __forceinline__ void walk(const AttnArgs& a, int item, WalkShared<T, 
     store_state<D>(a.final_state + ((int64_t)q.b * a.H + h) * state, st, a.ad, a.cd, 1.0f, l);
 }
 
-template <typename T, int D, bool WHOLE, bool FINE>
+template <typename T, int D, bool WHOLE>
 __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_kernel(AttnArgs a) {
   __shared__ WalkShared<T, D> shared;
-  walk<T, D, WHOLE, FINE>(a, blockIdx.x, shared);
+  walk<T, D, WHOLE>(a, blockIdx.x, shared);
 }
 
 // dv and dk: one walk backwards, whose state is that of (q, dout) divided by
@@ -872,10 +897,10 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesSimd<T, D>)) void attention_ke
 // each chunk it goes through them with a state each, and their sums stay in
 // registers.  Where GROUP is not all of them, the sums are fp32 parts that
 // attention_sum_kernel adds.
-template <typename T, int D, int GROUP, bool WHOLE, bool FINE>
+template <typename T, int D, int GROUP, bool WHOLE>
 __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkShared<T, D>& shared) {
-  constexpr bool SCALED = __is_same(T, f16);
-  T *s_q = shared.b, *s_d = shared.c, *s_s = shared.s;
+  constexpr bool SCALED = __is_same(T, f16), STATE_FIRST = kStateFirst<T, D>;
+  T *s_q = shared.chunk[0], *s_d = shared.chunk[1], *s_s = shared.s, *s_low = STATE_FIRST ? shared.chunk[0] : shared.low;
   float(&s_max)[4][kAttnWaves] = shared.most;
   const Lane l = lane_of();
   const int groups = a.H / GROUP, u = item % groups, unit = item / groups;
@@ -925,39 +950,60 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
     const int skip = max(q.lo - c0, 0);
     const bool needed = c0 + kChunk < q.hi || (!q.goes_on && a.final_state);
     const int32_t at = c0 + 16 * l.w;
-    Rows<D> acc_v, acc_k;  // of one head: live one after the other
+    const bool some = 16 * l.w + 15 >= skip;  // of the wave's rows
+    Rows<D> acc_v, acc_k;  // of one head and not STATE_FIRST: live one after the other
 #pragma unroll
     for (int j = 0; j < GROUP; ++j) {
+      auto put_chunk = [&] {
+        put_tile<T, D, WHOLE>(s_q, rq, a.ad, skip);
+        put_tile<T, D, WHOLE>(s_d, rd, a.cd, skip);
+      };
+      auto fetch_next = [&] {
+        if (j + 1 < GROUP) {
+          fetch(c0, j + 1);
+        } else if (c0 + kChunk < q.hi) {
+          fetch(c0 + kChunk, 0);
+          if (AHEAD) fetch_own(c0 + kChunk);
+        }
+      };
       __syncthreads();  // what was in LDS has been read
-      put_tile<T, D, WHOLE>(s_q, rq, a.ad, skip);
-      put_tile<T, D, WHOLE>(s_d, rd, a.cd, skip);
+      if (!STATE_FIRST) put_chunk();
       if (j == 0) {
         take_rows<T, D, WHOLE, false>(fk, nk, a.ad, l);
         take_rows<T, D, WHOLE, true>(fv, nv, a.cd, l);
       }
       const int ex = SCALED && have_state ? copy_exponent(s_max[j]) : 0;
-      if (have_state && own) put_state<T, D>(s_s, st[j], __builtin_ldexpf(1.0f, -ex), l);
-      __syncthreads();
-      if (j + 1 < GROUP) {
-        fetch(c0, j + 1);
-      } else if (c0 + kChunk < q.hi) {
-        fetch(c0 + kChunk, 0);
-        if (AHEAD) fetch_own(c0 + kChunk);
-      }
-      if (16 * l.w + 15 >= skip) {
-        const float fade_in = have_state ? __builtin_ldexpf(pw[j].of(max(16 * l.w + l.n - skip, 0)) * a.scale, ex) : 0.0f;
+      if (have_state && own) put_state<T, D>(s_s, s_low, st[j], __builtin_ldexpf(1.0f, -ex), l);
+      if (!STATE_FIRST || have_state) __syncthreads();
+      if (!STATE_FIRST) fetch_next();
+      const float fade_in = have_state ? __builtin_ldexpf(pw[j].of(max(16 * l.w + l.n - skip, 0)) * a.scale, ex) : 0.0f;
+      auto state_v = [&] {
         if (j == 0) clear<D>(acc_v);
-        if (have_state) add_state_product<T, D, false>(acc_v, s_s, fk, fade_in);
-        add_pairs<T, D, false, FINE>(acc_v, s_q, s_d, fk, pw[j], l);
+        if (have_state && some) add_state_product<T, D, false>(acc_v, s_s, s_low, fk, fade_in);
+      };
+      auto state_k = [&] {
+        if (j == 0) clear<D>(acc_k);
+        if (have_state && some) add_state_product<T, D, true>(acc_k, s_s, s_low, fv, fade_in);
+      };
+      if (STATE_FIRST) {
+        state_v();
+        state_k();
+        if (have_state) __syncthreads();
+        put_chunk();
+        __syncthreads();
+        fetch_next();
+      }
+      if (some) {
+        if (!STATE_FIRST) state_v();
+        add_pairs<T, D, false>(acc_v, s_q, s_d, fk, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
             store_rows<WHOLE, D>(a.part_v + (int64_t)u * a.cd, groups * a.cd, o, at, q.lo, acc_v, a.cd, a.past);
           else
             store_rows<WHOLE, D>(static_cast<T*>(a.dv) + (int64_t)hk * a.dv_head, a.dv_row, o, at, q.lo, acc_v, a.cd, a.past);
         }
-        if (j == 0) clear<D>(acc_k);
-        if (have_state) add_state_product<T, D, true>(acc_k, s_s, fv, fade_in);
-        add_pairs<T, D, true, FINE>(acc_k, s_d, s_q, fv, pw[j], l);
+        if (!STATE_FIRST) state_k();
+        add_pairs<T, D, true>(acc_k, s_d, s_q, fv, pw[j], l);
         if (j == GROUP - 1) {
           if (a.parts)
             store_rows<WHOLE, D>(a.part_k + (int64_t)u * a.ad, groups * a.ad, o, at, q.lo, acc_k, a.ad, a.past);
@@ -984,14 +1030,14 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
 // first (one after the other their last workgroups, and twice two more
 // launches for the cut sequences' states, left the chip idle: 167 us for one
 // robot frame instead of 113).
-template <typename T, int D, int GROUP, bool WHOLE, bool FINE>
+template <typename T, int D, int GROUP, bool WHOLE>
 __global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_backward_kernel(AttnArgs a, AttnGradArgs b,
                                                                                                        uint32_t back_items) {
   __shared__ WalkShared<T, D> shared;
   if (blockIdx.x < back_items)
-    walk_back<T, D, GROUP, WHOLE, FINE>(b, blockIdx.x, shared);
+    walk_back<T, D, GROUP, WHOLE>(b, blockIdx.x, shared);
   else
-    walk<T, D, WHOLE, FINE>(a, blockIdx.x - back_items, shared);
+    walk<T, D, WHOLE>(a, blockIdx.x - back_items, shared);
 }
 
 // Instances by the wider of the two dims: 32, 64 or 128, the rest zeros.
@@ -1004,27 +1050,27 @@ void launch_states(const AttnPair& p, hipStream_t st) {
                                                                      : go(attention_state_kernel<T, 128, WHOLE>);
 }
 
-template <typename T, bool WHOLE, bool FINE>
+template <typename T, bool WHOLE>
 void launch_walk(const AttnArgs& a, hipStream_t st) {
   const int wide = a.ad > a.cd ? a.ad : a.cd;
   const dim3 grid((uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  wide <= 32 ? go(attention_kernel<T, 32, WHOLE, FINE>) : wide <= 64 ? go(attention_kernel<T, 64, WHOLE, FINE>) : go(attention_kernel<T, 128, WHOLE, FINE>);
+  wide <= 32 ? go(attention_kernel<T, 32, WHOLE>) : wide <= 64 ? go(attention_kernel<T, 64, WHOLE>) : go(attention_kernel<T, 128, WHOLE>);
 }
 
-template <typename T, bool WHOLE, bool FINE>
+template <typename T, bool WHOLE>
 void launch_backward(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
   const int wide = b.ad > b.cd ? b.ad : b.cd;
   const uint32_t back = (uint32_t)((b.cuts + b.B) * (int64_t)(b.H / b.group));
   const dim3 grid(back + (uint32_t)((a.cuts + a.B) * (int64_t)a.H)), block(kAttnThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, b, back); };
   if (wide <= 32)
-    b.group == 4 ? go(attention_backward_kernel<T, 32, 4, WHOLE, FINE>) : b.group == 2 ? go(attention_backward_kernel<T, 32, 2, WHOLE, FINE>)
-                                                                                 : go(attention_backward_kernel<T, 32, 1, WHOLE, FINE>);
+    b.group == 4 ? go(attention_backward_kernel<T, 32, 4, WHOLE>) : b.group == 2 ? go(attention_backward_kernel<T, 32, 2, WHOLE>)
+                                                                                 : go(attention_backward_kernel<T, 32, 1, WHOLE>);
   else if (wide <= 64)
-    b.group == 2 ? go(attention_backward_kernel<T, 64, 2, WHOLE, FINE>) : go(attention_backward_kernel<T, 64, 1, WHOLE, FINE>);
+    b.group == 2 ? go(attention_backward_kernel<T, 64, 2, WHOLE>) : go(attention_backward_kernel<T, 64, 1, WHOLE>);
   else
-    go(attention_backward_kernel<T, 128, 1, WHOLE, FINE>);
+    go(attention_backward_kernel<T, 128, 1, WHOLE>);
 }
 
 // WHOLE: see load_part; both walks' dims are the same two.
@@ -1037,18 +1083,12 @@ hipError_t states_of(const AttnPair& p, hipStream_t st) {
 }
 template <typename T>
 hipError_t walk_of(const AttnArgs& a, hipStream_t st) {
-  if (sizeof(T) == 2 && a.fine)
-    whole_packs(a) ? launch_walk<T, true, sizeof(T) == 2>(a, st) : launch_walk<T, false, sizeof(T) == 2>(a, st);
-  else
-    whole_packs(a) ? launch_walk<T, true, false>(a, st) : launch_walk<T, false, false>(a, st);
+  whole_packs(a) ? launch_walk<T, true>(a, st) : launch_walk<T, false>(a, st);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t backward_of(const AttnArgs& a, const AttnGradArgs& b, hipStream_t st) {
-  if (sizeof(T) == 2 && a.fine)
-    whole_packs(b) ? launch_backward<T, true, sizeof(T) == 2>(a, b, st) : launch_backward<T, false, sizeof(T) == 2>(a, b, st);
-  else
-    whole_packs(b) ? launch_backward<T, true, false>(a, b, st) : launch_backward<T, false, false>(a, b, st);
+  whole_packs(b) ? launch_backward<T, true>(a, b, st) : launch_backward<T, false>(a, b, st);
   return hipGetLastError();
 }
 

@@ -88,7 +88,6 @@ struct AttnWalk {
   int32_t reversed;
   int32_t init_swapped;
   int32_t exact_state;    // the state is an output: as exact as fp32
-  int32_t fine;           // all sequences are short: P in two parts
   int32_t past;           // store past the caches
   float scale;
   float init_scale, final_scale;  // the state is carried divided by these

@@ -175,7 +175,6 @@ void put_walk(AttnWalk& a, const mmbev_attention_t* t, const float* log_decay, c
   a.init_scale = a.final_scale = 1.0f;
   a.cuts = cuts;
   a.longest_first = t->num_sequences <= kOrderedSequences && t->num_sequences * heads > p.slots;
-  a.fine = short_rows(t);
   a.past = t->rows * (t->heads + t->kv_heads) * (t->key_dim + t->value_dim) * size_of(t->dtype) > kPastCaches;
   a.least = p.least;
   a.reversed = backwards;
