@@ -28,7 +28,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnPai
   const int at = blockIdx.x * 64 + lane;
   const bool there = at < each;
   const int64_t i = blockIdx.y * each + min(at, (int)each - 1);
-  const float g2 = decay_exponent(a.log_decay, blockIdx.y);
+  const Exponent log2 = decay_exponent(a.log_decay, blockIdx.y);
   float carry = 0.0f;
   for (int32_t s0 = 0; s0 < a.cuts; s0 += kJoinWaves * kJoinRun) {
     const int32_t first = s0 + w * kJoinRun;
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnPai
     int32_t run = rows[0] > 0 ? rows[0] : -1;
 #pragma unroll
     for (int j = 1; j < kJoinRun; ++j) {
-      if (rows[j] > 0) x[j] = __builtin_fmaf(__builtin_amdgcn_exp2f(g2 * (float)rows[j]), x[j - 1], x[j]);
+      if (rows[j] > 0) x[j] = __builtin_fmaf(power(log2, rows[j]), x[j - 1], x[j]);
       run = rows[j] > 0 && run > 0 ? run + rows[j] : -1;
     }
     s_end[w][lane] = x[kJoinRun - 1];
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnPai
     for (int v = 0; v < kJoinWaves; ++v) {
       if (v == w) in = carry;
       const int32_t r = s_rows[v];
-      carry = r > 0 ? __builtin_fmaf(__builtin_amdgcn_exp2f(g2 * (float)r), carry, s_end[v][lane]) : s_end[v][lane];
+      carry = r > 0 ? __builtin_fmaf(power(log2, r), carry, s_end[v][lane]) : s_end[v][lane];
     }
     __syncthreads();
     bool open = true;  // no sequence has begun since the run's first part
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void attention_join_kernel(AttnPai
     for (int j = 0; j < kJoinRun; ++j) {
       open = open && rows[j] > 0;
       upto += rows[j];
-      if (open) x[j] = __builtin_fmaf(__builtin_amdgcn_exp2f(g2 * (float)upto), in, x[j]);
+      if (open) x[j] = __builtin_fmaf(power(log2, upto), in, x[j]);
       if (there && first + j < a.cuts && rows[j] > 0) a.cut_state[(first + j) * all + i] = x[j];
     }
   }
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(AttnStepArgs a) {
   }
   const int lane = threadIdx.x % LANES, part = threadIdx.x / LANES, c = lane * 4;
   const Pack<T, 4> rv = load_some<T, 4>(static_cast<const T*>(a.v) + r * a.v_row + hk * a.v_head + c, a.vd - c);
-  const float lambda = __expf(fmaxf(fminf(a.log_decay[h], 0.0f), -1.0e4f));
+  const float lambda = power(decay_exponent(a.log_decay, h), 1);
   float* state = a.state + (slot * a.H + h) * a.kd * a.vd;
   __syncthreads();
   float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};

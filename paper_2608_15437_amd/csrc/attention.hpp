@@ -284,9 +284,24 @@ __device__ __forceinline__ bool find_part(Part& q, const Order& o, const AttnWal
   return false;
 }
 
-__device__ __forceinline__ float decay_exponent(const float* log_decay, int h) {
+// log2 of a decay, in two parts: its product with many rows is to keep the power's last bits, not the
+// exponent's (e^-60 taken of the product rounded once is off by up to 5e-6 of itself).
+struct Exponent {
+  float hi, lo;
+};
+
+__device__ __forceinline__ Exponent decay_exponent(const float* log_decay, int h) {
   // at most 0; -1e4 stands for -inf, whose product with no rows would be NaN
-  return fmaxf(fminf(log_decay[h], 0.0f), -1.0e4f) * 1.44269504088896341f;
+  const float x = fmaxf(fminf(log_decay[h], 0.0f), -1.0e4f);
+  const float hi = x * 1.44269504088896341f;
+  return {hi, __builtin_fmaf(x, 1.44269504088896341f, -hi) + x * 1.92596299e-8f};  // 1 / ln 2 and what fp32 leaves of it
+}
+
+// The decay of n rows.
+__device__ __forceinline__ float power(const Exponent& e, int n) {
+  const float t = e.hi * (float)n, p = __builtin_amdgcn_exp2f(t);
+  const float rest = __builtin_fmaf(e.hi, (float)n, -t) + e.lo * (float)n;
+  return __builtin_fmaf(p, rest * 0.693147181f, p);
 }
 
 // ------------------------------------------------------ parts of a step
@@ -321,14 +336,14 @@ struct Lane {
 
 // Powers of the decay that do not change from chunk to chunk.
 struct Powers {
-  float g2;
+  Exponent log2;
   float diag[4], off[4], gap[3];  // scale * lambda^(i-j): of the wave's own tile, and as off * gap of those before it
   float left[4];                  // lambda^(rows after j) of the chunk's last 16 rows; the tiles before them 16 rows more each
   float fade16, fade32, fade48, fade_chunk;
 
-  __device__ __forceinline__ float of(int x) const { return __builtin_amdgcn_exp2f(g2 * (float)x); }
-  __device__ __forceinline__ void set(float exponent, const Lane& l, float scale, int late) {
-    g2 = exponent;
+  __device__ __forceinline__ float of(int x) const { return power(log2, x); }
+  __device__ __forceinline__ void set(const Exponent& exponent, const Lane& l, float scale, int late) {
+    log2 = {uniform(exponent.hi), uniform(exponent.lo)};
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       diag[r] = l.n >= 4 * l.g + r ? of(l.n - 4 * l.g - r) * scale : 0.0f;
