@@ -643,7 +643,8 @@ size_t mmbev_linear_attention_workspace_bytes(const mmbev_attention_t* attention
  * The state is decayed, summed and carried in fp32 over all of a sequence;
  * for 16-bit types what the matrix cores multiply (the state, the pairs'
  * factors scale * lambda^(i-j) * q_i k_j, the decayed rows that enter the
- * state) is two parts of the type, 16 bits or more together.
+ * state) is two parts of the type, 16 bits or more together; in fp16 these
+ * are scaled by powers of two, so that they may lie outside the type's range.
  * max_length only sizes the launches: longer sequences are computed too.
  * out must not overlap an input.
  */

@@ -43,8 +43,14 @@
 // of that size, 1.4 times it together; the four more products cost 128 frames
 // 979 us instead of 918, the gradients of 8 crowded frames 607 instead of 514,
 // those of one robot frame's heads of 128, where the parts take turns in LDS,
-// 152 instead of 109).  fp16 has too few exponents for a state that sums many
-// rows: its copy is scaled by a power of two.
+// 152 instead of 109).
+//
+// fp16 has too few exponents for what its own values make: a product of two
+// rows passes 65,504, a small gradient's decayed rows fall under 2^-24.  So
+// whatever becomes fp16 inside is divided by a power of two first and the
+// product multiplied by it in fp32: the state's copy (one power), the pairs'
+// factors (one a row of the result and 32 rows of the chunk), the decayed rows
+// (one a column of the state).  The robot frame's gradients 166 us, 152 without.
 #pragma once
 
 #include "common.hpp"
@@ -505,11 +511,15 @@ __device__ __forceinline__ void put_max(float* s_max, const State<D>& st, const 
   s_max[l.w] = owns_state<D>(l) ? m : 0.0f;
 }
 
-// The exponent that brings the state's copy below 1.
+// The exponent of the power of two that values are divided by before they become fp16, the largest of them being m: it
+// then lies in 2^14 .. 2^15, and a value's second part keeps its bits down to 2^-25 of m.
+__device__ __forceinline__ int exponent_under(float m) {
+  return m > 0.0f && m < 3.0e38f ? max(-126, __builtin_amdgcn_frexp_expf(m) - 15) : 0;
+}
+
+// That of the state's copy.
 __device__ __forceinline__ int copy_exponent(const float* s_max) {
-  const float m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const int ex = m > 0.0f && m < 3.0e38f ? max(-100, min(126, __builtin_amdgcn_frexp_expf(m))) : 0;
-  return __builtin_amdgcn_readfirstlane(ex);
+  return __builtin_amdgcn_readfirstlane(exponent_under(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]))));
 }
 
 // The state's copy in LDS, [column][row]; in 16-bit types what its rounding leaves as another, `low`.
@@ -537,44 +547,70 @@ template <typename T, int D>
 __device__ __forceinline__ void add_to_state(State<D>& st, const T* s_b, const T* s_c, const Powers& p, float times, bool third,
                                              const Lane& l) {
   constexpr int SD = D + kRowPad<T>, VT = kOwnTiles<D>;
-  constexpr bool HALF = sizeof(T) == 2, THIRD = __is_same(T, bf16);
+  constexpr bool HALF = sizeof(T) == 2, THIRD = __is_same(T, bf16), SCALED = __is_same(T, f16);
+  // 32 rows at a time; in fp16 all 64, as a column's largest value is looked for among them
+  constexpr int STEPS = SCALED ? 2 : 1;
 #pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2) {
-    Frag<T> hi_part[VT], lo_part[VT], end_part[VT];
+  for (int s0 = 0; s0 < 2; s0 += STEPS) {
+    Frag<T> hi_part[STEPS][VT], lo_part[STEPS][VT], end_part[STEPS][VT];
+    float up[VT];  // fp16: the power of two that the lane's column is divided by
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) {
-      const Frag<T> c = load_cols(s_c, SD, 32 * s2, 16 * (l.w * VT + vt));
+      float x[STEPS][8], m = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float f = (s2 == 0 ? (e < 4 ? p.fade48 : p.fade32) : e < 4 ? p.fade16 : 1.0f) * times;
-        float x = (float)c.v[e] * (p.left[e & 3] * f);
-        // the product as rounded to fp32: a multiply fused with one of its two conversions to fp16, but not with the
-        // other, would leave the parts a step of fp16 apart where x lies next to a tie
-        if constexpr (__is_same(T, f16)) asm("" : "+v"(x));
-        hi_part[vt].v[e] = (T)x;
-        if constexpr (HALF) {
-          const float rest = x - (float)hi_part[vt].v[e];
-          lo_part[vt].v[e] = (T)rest;
-          if constexpr (THIRD) end_part[vt].v[e] = (T)(rest - (float)lo_part[vt].v[e]);
+      for (int u = 0; u < STEPS; ++u) {
+        const Frag<T> c = load_cols(s_c, SD, 32 * (s0 + u), 16 * (l.w * VT + vt));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f = (s0 + u == 0 ? (e < 4 ? p.fade48 : p.fade32) : e < 4 ? p.fade16 : 1.0f) * times;
+          x[u][e] = (float)c.v[e] * (p.left[e & 3] * f);
+          if constexpr (SCALED) m = fmaxf(m, __builtin_fabsf(x[u][e]));
         }
       }
+      const int ex = SCALED ? exponent_under(column_max(m)) : 0;
+      if constexpr (SCALED) up[vt] = __builtin_ldexpf(1.0f, ex);
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float y = SCALED ? __builtin_ldexpf(x[u][e], -ex) : x[u][e];
+          // the value as rounded to fp32: a multiply fused with one of its two conversions to fp16, but not with the
+          // other, would leave the parts a step of fp16 apart where it lies next to a tie
+          if constexpr (SCALED) asm("" : "+v"(y));
+          hi_part[u][vt].v[e] = (T)y;
+          if constexpr (HALF) {
+            const float rest = y - (float)hi_part[u][vt].v[e];
+            lo_part[u][vt].v[e] = (T)rest;
+            if constexpr (THIRD) end_part[u][vt].v[e] = (T)(rest - (float)lo_part[u][vt].v[e]);
+          }
+        }
     }
 #pragma unroll
     for (int kt = 0; kt < kTiles<D>; ++kt) {
-      const Frag<T> bk = load_cols(s_b, SD, 32 * s2, 16 * kt);
+      f32x4 sum[VT];
 #pragma unroll
-      for (int vt = 0; vt < VT; ++vt) {
-        st[kt][vt] = mma(bk, hi_part[vt], st[kt][vt]);
-        if constexpr (HALF) st[kt][vt] = mma(bk, lo_part[vt], st[kt][vt]);
+      for (int vt = 0; vt < VT; ++vt) sum[vt] = SCALED ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : st[kt][vt];
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        const Frag<T> bk = load_cols(s_b, SD, 32 * (s0 + u), 16 * kt);
+#pragma unroll
+        for (int vt = 0; vt < VT; ++vt) {
+          sum[vt] = mma(bk, hi_part[u][vt], sum[vt]);
+          if constexpr (HALF) sum[vt] = mma(bk, lo_part[u][vt], sum[vt]);
+        }
       }
+#pragma unroll
+      for (int vt = 0; vt < VT; ++vt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st[kt][vt][r] = SCALED ? __builtin_fmaf(sum[vt][r], up[vt], st[kt][vt][r]) : sum[vt][r];
     }
     if constexpr (THIRD)
       if (third) {
 #pragma unroll
         for (int kt = 0; kt < kTiles<D>; ++kt) {
-          const Frag<T> bk = load_cols(s_b, SD, 32 * s2, 16 * kt);
+          const Frag<T> bk = load_cols(s_b, SD, 32 * s0, 16 * kt);
 #pragma unroll
-          for (int vt = 0; vt < VT; ++vt) st[kt][vt] = mma(bk, end_part[vt], st[kt][vt]);
+          for (int vt = 0; vt < VT; ++vt) st[kt][vt] = mma(bk, end_part[0][vt], st[kt][vt]);
         }
       }
   }
@@ -624,7 +660,8 @@ __device__ __forceinline__ void add_state_product(Rows<D>& acc, const T* s_s, co
 }
 
 // acc += sum over the rows j of the chunk up to the wave's own, scale * lambda^(i-j) (a_i . b_j) c_j.  In 16-bit types
-// the pairs' factors take part as the rounded value and what the rounding left.
+// the pairs' factors take part as the rounded value and what the rounding left; fp16 has too few exponents for products
+// of its own values, so there a row's factors are first divided by a power of two.
 template <typename T, int D, bool SPLIT>
 __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s_c, const Frag<T> (&q)[kSteps<D>], const Powers& pw,
                                           const Lane& l) {
@@ -650,6 +687,15 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
         for (int r = 0; r < 4; ++r) p[u][r] *= pw.off[r] * f;
       }
     }
+    int ex = 0;  // of the lane's row of the result
+    if constexpr (__is_same(T, f16)) {
+      float m = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, __builtin_fabsf(p[e >> 2][e & 3]));
+      ex = exponent_under(column_max(m));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e >> 2][e & 3] = __builtin_ldexpf(p[e >> 2][e & 3], -ex);
+    }
     Frag<T> pf, rest;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -660,8 +706,15 @@ __device__ __forceinline__ void add_pairs(Rows<D>& acc, const T* s_b, const T* s
 #pragma unroll
     for (int t = 0; t < kTiles<D>; ++t) {
       const Frag<T> c = load_cols(s_c, SD, 32 * s2, 16 * t);
-      acc[t] = mma(c, pf, acc[t]);
-      if constexpr (sizeof(T) == 2) acc[t] = mma(c, rest, acc[t]);
+      if constexpr (__is_same(T, f16)) {
+        const f32x4 x = mma(c, rest, mma(c, pf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}));
+        const float up = __builtin_ldexpf(1.0f, ex);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[t][r] = __builtin_fmaf(x[r], up, acc[t][r]);
+      } else {
+        acc[t] = mma(c, pf, acc[t]);
+        if constexpr (sizeof(T) == 2) acc[t] = mma(c, rest, acc[t]);
+      }
     }
   }
 }

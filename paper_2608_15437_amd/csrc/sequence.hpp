@@ -276,18 +276,22 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// Largest value of a wave, known to all lanes.
-__device__ __forceinline__ float group_max(float x) {
-  x = fmaxf(x, dpp_xor_step(x, 1));
-  x = fmaxf(x, dpp_xor_step(x, 2));
-  x = fmaxf(x, dpp_xor_step(x, 4));
-  x = fmaxf(x, dpp_xor_step(x, 8));
+// Largest value of the four lanes of the same number in the wave's rows of 16, known to all of them.
+__device__ __forceinline__ float column_max(float x) {
   unsigned i = __builtin_bit_cast(unsigned, x);
   const auto p = __builtin_amdgcn_permlane16_swap(i, i, false, false);
   x = fmaxf(__builtin_bit_cast(float, (unsigned)p[0]), __builtin_bit_cast(float, (unsigned)p[1]));
   i = __builtin_bit_cast(unsigned, x);
   const auto q = __builtin_amdgcn_permlane32_swap(i, i, false, false);
   return fmaxf(__builtin_bit_cast(float, (unsigned)q[0]), __builtin_bit_cast(float, (unsigned)q[1]));
+}
+
+// Largest value of a wave, known to all lanes.
+__device__ __forceinline__ float group_max(float x) {
+  x = fmaxf(x, dpp_xor_step(x, 1));
+  x = fmaxf(x, dpp_xor_step(x, 2));
+  x = fmaxf(x, dpp_xor_step(x, 4));
+  return column_max(fmaxf(x, dpp_xor_step(x, 8)));
 }
 
 // Rows in use: the device's count, clamped to the array.

@@ -8,7 +8,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows", [3, 40, 200, 2000])
 def test_a_single_row_after_many(gpu_lib, rows, dtype):
     """The state that one row (or the initial state) leaves after many rows of zeros: one power of the decay, down to e^-80."""
