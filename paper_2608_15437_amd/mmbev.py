@@ -735,6 +735,11 @@ def _state(name, t, desc, n):
     return _vector(name, t, _torch.float32, 0)
 
 
+def _given(t):
+    """A tensor to write, of an argument that may also be True or False."""
+    return None if t is True or t is False else t
+
+
 def linear_attention_workspace_bytes(desc: mmbev_attention_t, backward: bool = False) -> int:
     return int(load().mmbev_linear_attention_workspace_bytes(desc, 1 if backward else 0))
 
@@ -747,7 +752,7 @@ def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None
 
     Returns (out, final state or None).  Rows of no sequence keep what `out` holds.
     """
-    handle = _issue_on(stream, q, k, v, log_decay, offsets, initial_state, out, fault, workspace)
+    handle = _issue_on(stream, q, k, v, log_decay, offsets, initial_state, _given(final_state), out, fault, workspace)
     torch = _torch
     n = offsets.numel() - 1
     qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
@@ -772,7 +777,8 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
                               workspace=None, stream=None):
     """Enqueue mmbev_linear_attention_backward: the gradients of linear_attention's q, k and v and, where
     `dinitial_state` is True or a tensor to write, of its initial state.  Returns (dq, dk, dv, dinitial_state or None)."""
-    handle = _issue_on(stream, dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, dq, dk, dv, fault, workspace)
+    handle = _issue_on(stream, dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, _given(dinitial_state), dq, dk,
+                       dv, fault, workspace)
     torch = _torch
     n = offsets.numel() - 1
     ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]

@@ -1,0 +1,65 @@
+"""The binding of the sequence operators without a GPU: what it looks at before it hands addresses to the library.
+
+Tensors here say that they are on GPU 0 and lie in host memory; the library is the real one for sizes, and a recorder for
+calls, which run nothing."""
+import pytest
+import torch
+
+from test_abi_host import mb  # noqa: F401  (the loaded library)
+
+
+class OnGpu(torch.Tensor):
+    where = 0
+
+    def get_device(self):
+        return self.where
+
+
+class OnOtherGpu(OnGpu):
+    where = 1
+
+
+def gpu(t, where=OnGpu):
+    return t.as_subclass(where)
+
+
+class Recorder:
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def __getattr__(self, name):
+        if name.endswith("workspace_bytes"):
+            return getattr(self.real, name)
+        return lambda *a: self.calls.append((name, a)) or 0
+
+
+@pytest.fixture
+def lib(mb, monkeypatch):
+    rec = Recorder(mb.load())
+    monkeypatch.setattr(mb, "_lib", rec)
+    monkeypatch.setattr(mb, "load", lambda: rec)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0, raising=False)
+    return rec
+
+
+def attention_tensors(rows=6, heads=2, dim=4, sequences=2):
+    q, k, v, g = (gpu(torch.zeros(rows, heads, dim)) for _ in range(4))
+    decay = gpu(torch.zeros(heads))
+    off = gpu(torch.tensor([0, 2, rows]))
+    state = gpu(torch.zeros(sequences, heads, dim, dim))
+    return q, k, v, g, decay, off, state
+
+
+@pytest.mark.parametrize("wrong", [lambda t: t.as_subclass(torch.Tensor), lambda t: gpu(t, OnOtherGpu)], ids=["host", "other"])
+def test_states_to_write_must_be_on_the_gpu(mb, lib, wrong):  # noqa: F811
+    q, k, v, g, decay, off, state = attention_tensors()
+    mb.linear_attention(q, k, v, decay, off, final_state=state)
+    mb.linear_attention_backward(g, q, k, v, decay, off, initial_state=state, dinitial_state=gpu(torch.zeros_like(state)))
+    assert [c[0] for c in lib.calls] == ["mmbev_linear_attention", "mmbev_linear_attention_backward"]
+    lib.calls.clear()
+    with pytest.raises(mb.MmbevError, match="one GPU"):
+        mb.linear_attention(q, k, v, decay, off, final_state=wrong(state))
+    with pytest.raises(mb.MmbevError, match="one GPU"):
+        mb.linear_attention_backward(g, q, k, v, decay, off, initial_state=state, dinitial_state=wrong(state))
+    assert not lib.calls
