@@ -764,7 +764,7 @@ def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None
     final = None if final_state is False else final_state
     if workspace is None:
         workspace = _empty(stream, q, (linear_attention_workspace_bytes(desc),), torch.uint8)
-    _check(_lib.mmbev_linear_attention(
+    _check((_lib or load()).mmbev_linear_attention(
         desc, qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
         _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n), _heads("out", out),
         _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), workspace.data_ptr(),
@@ -791,7 +791,7 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
     dinitial = None if dinitial_state is False else dinitial_state
     if workspace is None:
         workspace = _empty(stream, q, (linear_attention_workspace_bytes(desc, True),), torch.uint8)
-    _check(_lib.mmbev_linear_attention_backward(
+    _check((_lib or load()).mmbev_linear_attention_backward(
         desc, *ins, _vector("log_decay", log_decay, torch.float32, desc.heads), _vector("offsets", offsets, torch.int64, 2),
         _state("initial_state", initial_state, desc, n), _state("dfinal_state", dfinal_state, desc, n), _heads("dq", dq),
         _heads("dk", dk), _heads("dv", dv), _state("dinitial_state", dinitial, desc, n),

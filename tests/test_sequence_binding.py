@@ -63,3 +63,12 @@ def test_states_to_write_must_be_on_the_gpu(mb, lib, wrong):  # noqa: F811
     with pytest.raises(mb.MmbevError, match="one GPU"):
         mb.linear_attention_backward(g, q, k, v, decay, off, initial_state=state, dinitial_state=wrong(state))
     assert not lib.calls
+
+
+def test_a_first_call_with_its_own_workspace_loads_the_library(mb, lib, monkeypatch):  # noqa: F811
+    q, k, v, g, decay, off, state = attention_tensors()
+    room = gpu(torch.zeros(1 << 20, dtype=torch.uint8))
+    monkeypatch.setattr(mb, "_lib", None)
+    mb.linear_attention(q, k, v, decay, off, workspace=room)
+    mb.linear_attention_backward(g, q, k, v, decay, off, workspace=room)
+    assert len(lib.calls) == 2
