@@ -493,6 +493,8 @@ mmbev_status_t mmbev_voxel_clusters(const int32_t* coords, const int32_t* counts
  * loads and the stores is held in 32 bits (a product on the matrix cores takes
  * operands of the element type), and results are rounded once, to nearest
  * even.  Any alignment of the element type and any row stride are taken.
+ * Arrays that a call writes share no element with its other arrays, except
+ * where it says so; they may interleave in rows of one stride.
  *
  * Ownership, streams and errors as for mmbev_roi_voxelize: caller-owned
  * buffers, no allocation, work enqueued on `stream` (NULL = default stream)
@@ -534,7 +536,7 @@ typedef struct {
  *   out = (s - mu) * rstd * weight + bias
  * residual, weight (ones), bias (zeros), out_sum, out_mean and out_rstd
  * (fp32 [rows]) may be NULL (their structs' data NULL).  out and out_sum may
- * be x's or residual's own rows.  width and eps as above.
+ * be x's or residual's own rows (not each other's).  width and eps as above.
  */
 mmbev_status_t mmbev_layer_norm(const mmbev_norm_t* norm, mmbev_rows_t x, mmbev_rows_t residual, const void* weight,
                                 const void* bias, const int64_t* row_count, mmbev_rows_t out, mmbev_rows_t out_sum,
@@ -657,7 +659,7 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* attention, mmbev_
  * Its gradients.  dfinal_state (may be NULL) is the gradient of final_state;
  * dinitial_state (may be NULL) receives that of initial_state.  dq is like q,
  * dk and dv like k and v (the sum over the heads that share them, taken in
- * fp32).  dq, dk and dv must not overlap an input.
+ * fp32).  dq, dk and dv must not overlap an input or each other.
  */
 mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* attention, mmbev_heads_t dout,
                                                mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,

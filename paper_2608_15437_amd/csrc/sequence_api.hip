@@ -49,6 +49,71 @@ Span span_of(const mmbev_heads_t& t, int64_t rows, int32_t heads, int32_t dim, i
 }
 bool overlap(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
 
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b != 0 && a < 0); }
+
+// Runs of `width` elements every `stride`, `count` of them.
+struct Runs {
+  int64_t stride, count, width;
+};
+
+// Whether any run of y, whose first is `shift` elements behind x's first, has an element of a run of x.
+bool runs_meet(const Runs& x, const Runs& y, int64_t shift) {
+  if (shift >= (x.count - 1) * x.stride + x.width || shift + (y.count - 1) * y.stride + y.width <= 0) return false;
+  if (x.stride == y.stride || y.count == 1) {
+    // y's run j begins m elements into x's run first + j and may reach into the next
+    const int64_t first = floor_div(shift, x.stride), m = shift - first * x.stride;
+    auto there = [&](int64_t i) { return i < x.count && i + y.count > 0; };  // one of x's runs i .. i + y.count - 1
+    if (m < x.width && there(first)) return true;
+    // (a single run of y may reach over several of x's)
+    return m + y.width > x.stride && first + 1 < x.count && first + (m + y.width - 1) / x.stride + y.count > 0;
+  }
+  if (x.count == 1) return runs_meet(y, x, -shift);
+  if (x.count + y.count > 4096) return true;  // not told apart
+  for (int64_t i = 0, j = 0; i < x.count && j < y.count;) {
+    const int64_t a = i * x.stride, b = shift + j * y.stride;
+    if (a < b + y.width && b < a + x.width) return true;
+    a < b ? ++i : ++j;
+  }
+  return false;
+}
+
+// Whether two arrays of `rows` rows of heads have an element in common.  Exact where both have their heads inside rows of
+// one stride, or their rows inside heads of one; else arrays whose first and last elements enclose one another's count as
+// having one.
+bool meet(const mmbev_heads_t& x, int32_t x_heads, int32_t x_dim, const mmbev_heads_t& y, int32_t y_heads, int32_t y_dim, int64_t rows,
+          int32_t dtype) {
+  if (!x.data || !y.data || rows == 0) return false;
+  if (!overlap(span_of(x, rows, x_heads, x_dim, dtype), span_of(y, rows, y_heads, y_dim, dtype))) return false;
+  const int64_t bytes = (int64_t)((uintptr_t)y.data - (uintptr_t)x.data);  // both are aligned to the element
+  const int64_t shift = bytes / size_of(dtype);
+  const Runs xh{x_heads > 1 ? x.head_stride : x_dim, x_heads, x_dim}, yh{y_heads > 1 ? y.head_stride : y_dim, y_heads, y_dim};
+  if (rows == 1) return runs_meet(xh, yh, shift);
+  auto extent = [](const Runs& r) { return (r.count - 1) * r.stride + r.width; };
+  // `step` elements a time, x's and y's runs inside each
+  auto nested = [&](int64_t step, int64_t x_count, int64_t y_count, const Runs& xr, const Runs& yr) {
+    const int64_t k = floor_div(shift, step), o = shift - k * step;  // y's item j lies o behind x's item j + k
+    auto both = [&](int64_t d) { return d < x_count && d + y_count > 0; };
+    return (both(k) && runs_meet(xr, yr, o)) || (both(k + 1) && runs_meet(xr, yr, o - step));
+  };
+  if (x.row_stride == y.row_stride && x.row_stride >= extent(xh) && x.row_stride >= extent(yh))
+    return nested(x.row_stride, rows, rows, xh, yh);
+  const Runs xr{x.row_stride, rows, x_dim}, yr{y.row_stride, rows, y_dim};
+  if (x_heads > 1 && y_heads > 1 && x.head_stride == y.head_stride && x.head_stride >= extent(xr) && x.head_stride >= extent(yr))
+    return nested(x.head_stride, x_heads, y_heads, xr, yr);
+  return true;
+}
+
+// The same rows, heads and strides.
+bool same(const mmbev_heads_t& x, const mmbev_heads_t& y) {
+  return x.data == y.data && x.row_stride == y.row_stride && x.head_stride == y.head_stride;
+}
+
+// The same for rows without heads: apart, or (own) the very same rows.
+bool rows_apart(const mmbev_rows_t& x, const mmbev_rows_t& y, int64_t rows, int32_t width, int32_t dtype, bool own) {
+  if (own && x.data == y.data && (rows <= 1 || x.row_stride == y.row_stride)) return true;
+  return !meet({x.data, x.row_stride, width}, 1, width, {y.data, y.row_stride, width}, 1, width, rows, dtype);
+}
+
 mmbev_status_t norm_ok(const mmbev_norm_t* n) {
   if (!n || n->rows < 0 || n->width < 1 || !known_type(n->dtype)) return MMBEV_ERR_INVALID_ARG;
   if (n->weight_dtype != MMBEV_F32 && n->weight_dtype != n->dtype) return MMBEV_ERR_INVALID_ARG;
@@ -206,6 +271,10 @@ mmbev_status_t mmbev_layer_norm(const mmbev_norm_t* norm, mmbev_rows_t x, mmbev_
       !rows_ok(out_sum, R, C, T, true))
     return MMBEV_ERR_INVALID_ARG;
   if (!aligned(weight, size_of(norm->weight_dtype)) || !aligned(bias, size_of(norm->weight_dtype))) return MMBEV_ERR_INVALID_ARG;
+  for (const mmbev_rows_t* in : {&x, &residual})
+    for (const mmbev_rows_t* to : {&out, &out_sum})
+      if (!rows_apart(*in, *to, R, C, T, true)) return MMBEV_ERR_INVALID_ARG;
+  if (!rows_apart(out, out_sum, R, C, T, false)) return MMBEV_ERR_INVALID_ARG;
   NormArgs a = norm_args(norm, 2 + (residual.data != nullptr) + (out_sum.data != nullptr), row_count, fault);
   a.x = x.data;
   a.x_stride = x.row_stride;
@@ -239,6 +308,8 @@ mmbev_status_t mmbev_layer_norm_backward(const mmbev_norm_t* norm, mmbev_rows_t 
       !rows_ok(dx, R, C, T, false))
     return MMBEV_ERR_INVALID_ARG;
   if (R > 0 && (!mean || !rstd)) return MMBEV_ERR_INVALID_ARG;
+  for (const mmbev_rows_t* in : {&dy, &s, &dskip})
+    if (!rows_apart(*in, dx, R, C, T, true)) return MMBEV_ERR_INVALID_ARG;
   if (!aligned(weight, size_of(norm->weight_dtype))) return MMBEV_ERR_INVALID_ARG;
   const bool sums = dweight || dbias;
   if (sums && !workspace_ok(workspace, workspace_bytes, mmbev_layer_norm_backward_workspace_bytes(norm)))
@@ -306,10 +377,7 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* t, mmbev_heads_t x, const int3
   if (t->rows > 0 && (!positions || !aligned(positions, 4) || !steps || !aligned(steps, 8) || !axis)) return MMBEV_ERR_INVALID_ARG;
   if (position_stride < 0 || (t->rows > 1 && position_stride < axes) || position_stride >= ((int64_t)1 << 40))
     return MMBEV_ERR_INVALID_ARG;
-  const bool same = x.data == out.data && x.row_stride == out.row_stride && x.head_stride == out.head_stride;
-  if (!same && overlap(span_of(x, t->rows, t->heads, t->dim, t->dtype), span_of(out, t->rows, t->heads, t->dim, t->dtype)) &&
-      x.data == out.data)
-    return MMBEV_ERR_INVALID_ARG;
+  if (!same(x, out) && meet(x, t->heads, t->dim, out, t->heads, t->dim, t->rows, t->dtype)) return MMBEV_ERR_INVALID_ARG;
   RotaryArgs a{};
   a.x = x.data;
   a.out = out.data;
@@ -330,7 +398,7 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* t, mmbev_heads_t x, const int3
   a.axes = axes;
   a.interleaved = t->layout == MMBEV_ROTARY_INTERLEAVED;
   a.inverse = t->inverse;
-  a.copy_rest = !same;
+  a.copy_rest = !same(x, out);
   a.past = 2 * t->rows * t->heads * t->dim * size_of(t->dtype) > kPastCaches;
   return status_of(launch_rotary(a, t->dtype, (hipStream_t)stream));
 }
@@ -356,8 +424,10 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t 
   if (initial_state && final_state &&
       overlap({(uintptr_t)initial_state, (uintptr_t)initial_state + state}, {(uintptr_t)final_state, (uintptr_t)final_state + state}))
     return MMBEV_ERR_INVALID_ARG;
-  for (const void* in : {q.data, k.data, v.data})
-    if (in && in == out.data) return MMBEV_ERR_INVALID_ARG;
+  if (meet(q, t->heads, t->key_dim, out, t->heads, t->value_dim, t->rows, t->dtype) ||
+      meet(k, t->kv_heads, t->key_dim, out, t->heads, t->value_dim, t->rows, t->dtype) ||
+      meet(v, t->kv_heads, t->value_dim, out, t->heads, t->value_dim, t->rows, t->dtype))
+    return MMBEV_ERR_INVALID_ARG;
   const AttnPlan p = attention_plan(t, false);
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
   AttnArgs a{};
@@ -398,9 +468,16 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   const Span di = {(uintptr_t)dinitial_state, (uintptr_t)dinitial_state + (dinitial_state ? state : 0)};
   for (const float* in : {initial_state, dfinal_state})
     if (in && dinitial_state && overlap(di, {(uintptr_t)in, (uintptr_t)in + state})) return MMBEV_ERR_INVALID_ARG;
-  for (const void* to : {dq.data, dk.data, dv.data})
-    for (const void* in : {dout.data, q.data, k.data, v.data})
-      if (in && in == to) return MMBEV_ERR_INVALID_ARG;
+  struct Array {
+    const mmbev_heads_t& t;
+    int32_t heads, dim;
+  };
+  // the gradients against the inputs and against each other
+  const Array arrays[] = {{dq, H, t->key_dim},  {dk, K, t->key_dim}, {dv, K, t->value_dim}, {dout, H, t->value_dim},
+                          {q, H, t->key_dim}, {k, K, t->key_dim},  {v, K, t->value_dim}};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 7; ++j)
+      if (meet(arrays[i].t, arrays[i].heads, arrays[i].dim, arrays[j].t, arrays[j].heads, arrays[j].dim, R, T)) return MMBEV_ERR_INVALID_ARG;
   const AttnPlan p = attention_plan(t, true);
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
   char* ws = (char*)workspace;
