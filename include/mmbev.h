@@ -677,6 +677,8 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* attentio
  * state   fp32 [num_slots][heads][key_dim][value_dim], 16-byte aligned
  * slots   device int32 [rows], distinct where >= 0; a negative slot skips
  *         the row (its out row is not written); NULL: row r has slot r
+ * out     may be q's own rows and heads (same strides), and k's or v's where
+ *         heads == kv_heads
  */
 mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* attention, mmbev_heads_t q, mmbev_heads_t k,
                                            mmbev_heads_t v, const float* log_decay, const int32_t* slots,

@@ -551,6 +551,12 @@ mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* t, mmbev_hea
       !heads_ok(v, t->rows, t->kv_heads, t->value_dim, t->dtype) || !heads_ok(out, t->rows, t->heads, t->value_dim, t->dtype))
     return MMBEV_ERR_INVALID_ARG;
   if (!log_decay || !aligned(log_decay, 4) || !aligned(slots, 4) || num_slots < 0) return MMBEV_ERR_INVALID_ARG;
+  // a workgroup reads its head's q, k and v before it writes its out: they may be one, unless other heads read them too
+  const bool own = t->heads == t->kv_heads;
+  if ((!same(q, out) && meet(q, t->heads, t->key_dim, out, t->heads, t->value_dim, t->rows, t->dtype)) ||
+      (!(own && same(k, out)) && meet(k, t->kv_heads, t->key_dim, out, t->heads, t->value_dim, t->rows, t->dtype)) ||
+      (!(own && same(v, out)) && meet(v, t->kv_heads, t->value_dim, out, t->heads, t->value_dim, t->rows, t->dtype)))
+    return MMBEV_ERR_INVALID_ARG;
   if (num_slots > kMaxRows) return MMBEV_ERR_UNSUPPORTED;
   if (t->rows > 0 && num_slots > 0 && (!state || !aligned(state, 16))) return MMBEV_ERR_INVALID_ARG;
   if (!slots && num_slots < t->rows) return MMBEV_ERR_INVALID_ARG;

@@ -135,3 +135,19 @@ def test_layer_norm_refuses_shifted_rows(mb):  # noqa: F811
     for bad in (at(BASE, 128, 128), at(3 * BASE, 64, 64), at(BASE, 0, 64)):
         assert back(bad) == mb.ERR_INVALID_ARG
     assert back(at(5 * BASE, 8, 64), skip=skip) == mb.ERR_INVALID_ARG
+
+
+def test_step_output_over_shared_keys_and_values_is_refused(mb):  # noqa: F811
+    """A step's out may be q's own heads, and k's or v's where no heads share them; refused before anything is launched."""
+    L = mb.load()
+
+    def call(q, k, v, out, heads=4, kv=2):
+        t = mb.mmbev_attention_t(rows=10, max_length=0, num_sequences=1, heads=heads, kv_heads=kv, key_dim=8, value_dim=8, dtype=2,
+                                 scale=1.0, reserved=0)
+        return L.mmbev_linear_attention_step(ctypes.byref(t), q, k, v, BASE, None, 10, 9 * BASE, out, None, None)
+
+    at = lambda i, off=0, row=64, head=8: mb.mmbev_heads_t((i + 1) * BASE + 2 * off, row, head)  # noqa: E731
+    q, k, v = at(0), at(1), at(2)
+    for out in (k, v, at(1, 8), at(2, -8), at(0, 8), at(0, 64), at(0, 4), at(0, 0, 32), at(2, 64 * 9)):
+        assert call(q, k, v, out) == mb.ERR_INVALID_ARG
+    assert call(q, k, v, at(2, 8), kv=4) == mb.ERR_INVALID_ARG
