@@ -605,6 +605,13 @@ def _empty_like(stream, like):
         return _torch.empty_like(like)
 
 
+def _written(*tensors) -> None:
+    """Tells autograd that the caller's tensors were written: one that was saved for a backward pass is refused there."""
+    tensors = [t for t in tensors if t is not None]
+    if tensors:
+        _torch.autograd.graph.increment_version(tensors)
+
+
 def _norm_of(x, weight, bias, eps) -> mmbev_norm_t:
     code = _dtype_code(x)
     if x.dim() != 2:
@@ -634,6 +641,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stat
     rows in use (others keep what out holds).
     """
     handle = _issue_on(stream, x, weight, bias, residual, row_count, out, out_sum, fault)
+    given = out, out_sum
     torch = _torch
     desc = _norm_of(x, weight, bias, eps)
     dtype, shape = x.dtype, x.shape
@@ -651,6 +659,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, stat
         desc, _rows("x", x), _rows("residual", residual), _ptr_of(weight), _ptr_of(bias),
         _vector("row_count", row_count, torch.int64, 1), _rows("out", out), _rows("out_sum", out_sum), _ptr_of(mean),
         _ptr_of(rstd), _vector("fault", fault, torch.int32, 1), handle), "mmbev_layer_norm")
+    _written(*given)
     return out, (x if out_sum is None else out_sum), mean, rstd
 
 
@@ -662,6 +671,7 @@ def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, d
     [width], None without `weight_grads`.
     """
     handle = _issue_on(stream, dy, s, weight, mean, rstd, dskip, row_count, dx, dweight, dbias, fault, workspace)
+    given = dx, dweight, dbias
     torch, lib = _torch, _lib or load()
     desc = _norm_of(s, weight, None, 0.0)
     dtype, shape = s.dtype, s.shape
@@ -683,6 +693,7 @@ def layer_norm_backward(dy, s, weight, mean, rstd, dskip=None, row_count=None, d
         _vector("dweight", dweight, torch.float32, shape[1]), _vector("dbias", dbias, torch.float32, shape[1]),
         _vector("fault", fault, torch.int32, 1), _ptr_of(workspace), 0 if workspace is None else workspace.nbytes,
         handle), "mmbev_layer_norm_backward")
+    _written(*given)
     return dx, dweight, dbias
 
 
@@ -702,6 +713,7 @@ def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = Fals
     """Enqueue mmbev_rotary: x [rows][heads][dim]; positions int32 [rows] or [rows][axes] (a view of the voxeliser's
     coordinates will do: coords[:, 1:]); steps, axis: make_rotary's arrays on the GPU.  Returns out (may be x)."""
     handle = _issue_on(stream, x, positions, steps, axis, row_count, out, fault)
+    given = out
     torch = _torch
     xs, shape = _heads("x", x), x.shape
     at, step = positions.shape, positions.stride()
@@ -715,6 +727,7 @@ def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = Fals
         desc, xs, positions.data_ptr(), step[0] if shape[0] > 1 else axes, axes, _vector("steps", steps, torch.int64, pairs),
         _vector("axis", axis, torch.uint8, pairs), _vector("row_count", row_count, torch.int64, 1), _heads("out", out),
         _vector("fault", fault, torch.int32, 1), handle), "mmbev_rotary")
+    _written(given)
     return out
 
 
@@ -752,7 +765,8 @@ def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None
 
     Returns (out, final state or None).  Rows of no sequence keep what `out` holds.
     """
-    handle = _issue_on(stream, q, k, v, log_decay, offsets, initial_state, _given(final_state), out, fault, workspace)
+    given = out, _given(final_state)
+    handle = _issue_on(stream, q, k, v, log_decay, offsets, initial_state, *given, fault, workspace)
     torch = _torch
     n = offsets.numel() - 1
     qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
@@ -769,6 +783,7 @@ def linear_attention(q, k, v, log_decay, offsets, scale=None, initial_state=None
         _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n), _heads("out", out),
         _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), workspace.data_ptr(),
         workspace.nbytes, handle), "mmbev_linear_attention")
+    _written(*given)
     return out, final
 
 
@@ -777,8 +792,8 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
                               workspace=None, stream=None):
     """Enqueue mmbev_linear_attention_backward: the gradients of linear_attention's q, k and v and, where
     `dinitial_state` is True or a tensor to write, of its initial state.  Returns (dq, dk, dv, dinitial_state or None)."""
-    handle = _issue_on(stream, dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, _given(dinitial_state), dq, dk,
-                       dv, fault, workspace)
+    given = dq, dk, dv, _given(dinitial_state)
+    handle = _issue_on(stream, dout, q, k, v, log_decay, offsets, initial_state, dfinal_state, *given, fault, workspace)
     torch = _torch
     n = offsets.numel() - 1
     ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
@@ -797,6 +812,7 @@ def linear_attention_backward(dout, q, k, v, log_decay, offsets, scale=None, ini
         _heads("dk", dk), _heads("dv", dv), _state("dinitial_state", dinitial, desc, n),
         _vector("fault", fault, torch.int32, 1), workspace.data_ptr(), workspace.nbytes, handle),
         "mmbev_linear_attention_backward")
+    _written(*given)
     return dq, dk, dv, dinitial
 
 
@@ -804,6 +820,7 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
     """Enqueue mmbev_linear_attention_step: one row for each of many streams.  state float32 [slots][heads][key_dim]
     [value_dim] is updated in place; slots int32 [rows] names each row's state (negative: the row is skipped)."""
     handle = _issue_on(stream, q, k, v, log_decay, state, slots, out, fault)
+    given = state, out
     torch = _torch
     qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
     desc = _attention_of(q, k, v, 1, scale, 0)
@@ -814,4 +831,5 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
         desc, qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
         _vector("slots", slots, torch.int32, desc.rows), held, _state("state", state, desc, held), _heads("out", out),
         _vector("fault", fault, torch.int32, 1), handle), "mmbev_linear_attention_step")
+    _written(*given)
     return out

@@ -121,3 +121,19 @@ def test_example_trains(gpu_lib):
     losses, encoded, bev = example.main(["--frames", "3", "--steps", "12", "--width", "64"])
     assert losses[-1] < 0.5 * losses[0]
     assert bool(torch.isfinite(encoded).all()) and int((bev != 0).sum()) > 0
+
+
+def test_a_state_updated_in_place_is_not_differentiated_as_it_was(gpu_lib):
+    import torch
+
+    from paper_2608_15437_amd import encoder
+
+    torch.manual_seed(5)
+    q, k, v = (torch.randn(9, 2, 16, device="cuda", requires_grad=True) for _ in range(3))
+    decay, off = torch.full((2,), -0.1, device="cuda"), torch.tensor([0, 9], device="cuda")
+    state = torch.randn(1, 2, 16, 16, device="cuda")
+    out, _ = encoder.linear_attention(q, k, v, decay, off, state)
+    with torch.no_grad():
+        gpu_lib.linear_attention_step(q[:1], k[:1], v[:1], decay, state)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()

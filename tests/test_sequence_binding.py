@@ -72,3 +72,37 @@ def test_a_first_call_with_its_own_workspace_loads_the_library(mb, lib, monkeypa
     mb.linear_attention(q, k, v, decay, off, workspace=room)
     mb.linear_attention_backward(g, q, k, v, decay, off, workspace=room)
     assert len(lib.calls) == 2
+
+
+def norm_tensors():
+    x, y = (gpu(torch.zeros(5, 8)) for _ in range(2))
+    w, mean, rstd = gpu(torch.ones(8)), gpu(torch.zeros(5)), gpu(torch.ones(5))
+    return x, y, w, mean, rstd
+
+
+def test_writes_raise_the_version_that_autograd_checks(mb, lib):  # noqa: F811
+    x, y, w, mean, rstd = norm_tensors()
+    q, k, v, g, decay, off, state = attention_tensors()
+    pos, steps, axis = gpu(torch.zeros(6, dtype=torch.int32)), gpu(torch.zeros(2, dtype=torch.int64)), gpu(torch.zeros(2, dtype=torch.uint8))
+    out, dq, dk, dv, end = (gpu(torch.zeros_like(t)) for t in (q, q, k, v, state))
+
+    def check(call, written, read):
+        before = [t._version for t in written + read]
+        call()
+        after = [t._version for t in written + read]
+        assert [a > b for a, b in zip(after, before)] == [True] * len(written) + [False] * len(read)
+
+    total, dw, db = gpu(torch.zeros(5, 8)), gpu(torch.zeros(8)), gpu(torch.zeros(8))
+    check(lambda: mb.layer_norm(x, w, residual=y, out=x, out_sum=total), [x, total], [y, w])
+    check(lambda: mb.layer_norm_backward(y, x, w, mean, rstd, dx=total, dweight=dw, dbias=db), [total, dw, db], [x, y, w, mean, rstd])
+    check(lambda: mb.rotary(q, pos, steps, axis, out=q), [q], [pos, steps])
+    check(lambda: mb.linear_attention(q, k, v, decay, off, initial_state=state, final_state=end, out=out), [end, out], [q, k, v, state])
+    check(lambda: mb.linear_attention_backward(g, q, k, v, decay, off, initial_state=state, dinitial_state=end, dq=dq, dk=dk, dv=dv),
+          [end, dq, dk, dv], [g, q, k, v, state])
+    check(lambda: mb.linear_attention_step(q, k, v, decay, gpu(torch.zeros(6, 2, 4, 4)), out=out), [out], [q, k, v])
+    held = gpu(torch.zeros(6, 2, 4, 4))
+    check(lambda: mb.linear_attention_step(q, k, v, decay, held), [held], [q, k, v])
+    with torch.inference_mode():
+        held = gpu(torch.zeros(6, 2, 4, 4))
+        mb.linear_attention_step(q, k, v, decay, held)
+    mb.linear_attention_step(q, k, v, decay, held)  # a tensor without a version
