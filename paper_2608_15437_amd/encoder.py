@@ -23,14 +23,17 @@ class _Norm(torch.autograd.Function):
     def forward(ctx, x, residual, weight, bias, eps, row_count):
         out, total, mean, rstd = mmbev.layer_norm(x, weight, bias, eps=eps, residual=residual, stats=True, row_count=row_count)
         ctx.save_for_backward(total, weight, mean, rstd, row_count)
+        ctx.types = [None if t is None else t.dtype for t in (weight, bias)]
         return out, total
 
     @staticmethod
     def backward(ctx, dout, dtotal):
         total, weight, mean, rstd, row_count = ctx.saved_tensors
-        dx, dweight, dbias = mmbev.layer_norm_backward(dout.contiguous(), total, weight, mean, rstd, dskip=dtotal.contiguous(),
-                                                       row_count=row_count)
-        return dx, dx, dweight.to(weight.dtype), dbias.to(weight.dtype), None, None
+        needed = ctx.needs_input_grad  # False where there is no such input
+        dx, *sums = mmbev.layer_norm_backward(dout.contiguous(), total, weight, mean, rstd, dskip=dtotal.contiguous(),
+                                              row_count=row_count, weight_grads=needed[2] or needed[3])
+        dweight, dbias = (t.to(kind) if need else None for t, kind, need in zip(sums, ctx.types, needed[2:4]))
+        return dx if needed[0] else None, dx if needed[1] else None, dweight, dbias, None, None
 
 
 class _Rotary(torch.autograd.Function):

@@ -106,3 +106,22 @@ def test_writes_raise_the_version_that_autograd_checks(mb, lib):  # noqa: F811
         held = gpu(torch.zeros(6, 2, 4, 4))
         mb.linear_attention_step(q, k, v, decay, held)
     mb.linear_attention_step(q, k, v, decay, held)  # a tensor without a version
+
+
+@pytest.fixture
+def anywhere(mb, lib, monkeypatch):
+    """The binding without its look at where tensors are, for what autograd makes by itself."""
+    mb._with_torch()
+    monkeypatch.setattr(mb, "_issue_on", lambda *a: None)
+
+
+@pytest.mark.parametrize("residual", [True, False])
+@pytest.mark.parametrize("weight", [True, False])
+@pytest.mark.parametrize("bias", [True, False])
+def test_every_form_of_the_norm_has_a_gradient(mb, anywhere, residual, weight, bias):  # noqa: F811
+    from paper_2608_15437_amd import encoder
+
+    x, y, w, b = (torch.ones(*s, requires_grad=use) for s, use in (((5, 8), True), ((5, 8), residual), ((8,), weight), ((8,), bias)))
+    out, total = encoder.norm(x, y if residual else None, w if weight else None, b if bias else None)
+    (out.sum() + total.sum()).backward()
+    assert all((t.grad is not None) == t.requires_grad for t in (x, y, w, b))
