@@ -3,7 +3,7 @@
 The voxeliser writes one row per voxel in key order, one range of rows per frame.  A block of the encoder norms the
 rows, turns queries and keys by their voxel coordinates, mixes each frame's rows by linear attention with a decay per
 head and adds the result to the rows; the projections between are plain matrix products of torch.  Gradients come from
-the library's backward calls.  A trained block can also go on row by row (`step`), its state kept between rows.
+the library's backward calls, which have none themselves: a second derivative is refused.  A trained block can also go on row by row (`step`), its state kept between rows.
 
 The rows' number and ranges stay on the device: pass `row_count` (voxel_offsets[-1:]) to encode the voxeliser's full
 buffers without waiting for the count.  Rows past it hold nothing of meaning, so training takes the rows in use alone.
@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from . import mmbev
 
@@ -27,6 +28,7 @@ class _Norm(torch.autograd.Function):
         return out, total
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dtotal):
         total, weight, mean, rstd, row_count = ctx.saved_tensors
         needed = ctx.needs_input_grad  # False where there is no such input
@@ -44,6 +46,7 @@ class _Rotary(torch.autograd.Function):
         return mmbev.rotary(x, positions, steps, axis, layout=layout, row_count=row_count)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         positions, steps, axis, row_count = ctx.saved_tensors
         dx = mmbev.rotary(dout.contiguous(), positions, steps, axis, layout=ctx.layout, inverse=True, row_count=row_count)
@@ -60,6 +63,7 @@ class _Attention(torch.autograd.Function):
         return out, final
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dfinal):
         q, k, v, log_decay, offsets, initial_state = ctx.saved_tensors
         dq, dk, dv, dinitial = mmbev.linear_attention_backward(

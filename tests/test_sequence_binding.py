@@ -125,3 +125,17 @@ def test_every_form_of_the_norm_has_a_gradient(mb, anywhere, residual, weight, b
     out, total = encoder.norm(x, y if residual else None, w if weight else None, b if bias else None)
     (out.sum() + total.sum()).backward()
     assert all((t.grad is not None) == t.requires_grad for t in (x, y, w, b))
+
+
+def test_second_derivatives_are_refused(mb, anywhere):  # noqa: F811
+    from paper_2608_15437_amd import encoder
+
+    rows = lambda *s: torch.ones(*s, requires_grad=True)  # noqa: E731
+    x = rows(5, 8)
+    q, k, v = (rows(6, 2, 4) for _ in range(3))
+    pos, steps, axis = torch.zeros(6, dtype=torch.int32), torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.uint8)
+    for t, out in ((x, encoder.norm(x, None, None, None)[0]), (q, encoder.rotary(q, pos, steps, axis)),
+                   (q, encoder.linear_attention(q, k, v, torch.zeros(2), torch.tensor([0, 6]))[0])):
+        (d,) = torch.autograd.grad(out.sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            (d * t).sum().backward()
