@@ -83,7 +83,9 @@ def rotary(x, positions, steps, axis, layout="half", row_count=None):
 
 
 def linear_attention(q, k, v, log_decay, offsets, initial_state=None, max_length=None):
-    """mmbev.linear_attention's (out, final state), differentiable in q, k, v and the initial state."""
+    """mmbev.linear_attention's (out, final state), differentiable in q, k, v and the initial state; log_decay is a constant."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
+        raise mmbev.MmbevError("log_decay has no gradient: detach it")
     return _Attention.apply(q, k, v, log_decay, offsets, initial_state, max_length)
 
 

@@ -139,3 +139,15 @@ def test_second_derivatives_are_refused(mb, anywhere):  # noqa: F811
         (d,) = torch.autograd.grad(out.sum(), t, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             (d * t).sum().backward()
+
+
+def test_a_decay_that_wants_a_gradient_is_refused(mb, anywhere):  # noqa: F811
+    from paper_2608_15437_amd import encoder
+
+    q, k, v = (torch.ones(6, 2, 4, requires_grad=True) for _ in range(3))
+    decay, off = torch.zeros(2, requires_grad=True), torch.tensor([0, 6])
+    with pytest.raises(mb.MmbevError, match="log_decay"):
+        encoder.linear_attention(q, k, v, decay, off)
+    with torch.no_grad():
+        encoder.linear_attention(q, k, v, decay, off)
+    encoder.linear_attention(q, k, v, decay.detach(), off)
