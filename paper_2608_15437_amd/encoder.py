@@ -10,11 +10,39 @@ buffers without waiting for the count.  Rows past it hold nothing of meaning, so
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 from torch import nn
-from torch.autograd.function import once_differentiable
 
 from . import mmbev
+
+
+class _Refusal(torch.autograd.Function):
+    """A gradient that depends on `sources` in ways that autograd does not know of."""
+
+    @staticmethod
+    def forward(ctx, grad, *sources):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise mmbev.MmbevError("the sequence operators have no second derivatives")
+
+
+def _once(backward):
+    """A backward pass whose results cannot be differentiated: neither by the gradients that come in nor by what it saved."""
+
+    @functools.wraps(backward)
+    def call(ctx, *grads):
+        with torch.no_grad():
+            results = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return results
+        sources = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        return tuple(_Refusal.apply(t, *sources) if t is not None and sources else t for t in results)
+
+    return call
 
 
 class _Norm(torch.autograd.Function):
@@ -28,7 +56,7 @@ class _Norm(torch.autograd.Function):
         return out, total
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dout, dtotal):
         total, weight, mean, rstd, row_count = ctx.saved_tensors
         needed = ctx.needs_input_grad  # False where there is no such input
@@ -46,7 +74,7 @@ class _Rotary(torch.autograd.Function):
         return mmbev.rotary(x, positions, steps, axis, layout=layout, row_count=row_count)
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dout):
         positions, steps, axis, row_count = ctx.saved_tensors
         dx = mmbev.rotary(dout.contiguous(), positions, steps, axis, layout=ctx.layout, inverse=True, row_count=row_count)
@@ -63,7 +91,7 @@ class _Attention(torch.autograd.Function):
         return out, final
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dout, dfinal):
         q, k, v, log_decay, offsets, initial_state = ctx.saved_tensors
         dq, dk, dv, dinitial = mmbev.linear_attention_backward(

@@ -136,9 +136,16 @@ def test_second_derivatives_are_refused(mb, anywhere):  # noqa: F811
     pos, steps, axis = torch.zeros(6, dtype=torch.int32), torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.uint8)
     for t, out in ((x, encoder.norm(x, None, None, None)[0]), (q, encoder.rotary(q, pos, steps, axis)),
                    (q, encoder.linear_attention(q, k, v, torch.zeros(2), torch.tensor([0, 6]))[0])):
-        (d,) = torch.autograd.grad(out.sum(), t, create_graph=True)
-        with pytest.raises(RuntimeError, match="once_differentiable"):
+        (d,) = torch.autograd.grad(out.square().sum(), t, create_graph=True)  # the gradient that comes in depends on t
+        with pytest.raises(mb.MmbevError, match="second derivative"):
             (d * t).sum().backward()
+    out, total = encoder.norm(x, None, None, None)  # what was saved does
+    (d,) = torch.autograd.grad(out.sum(), x, create_graph=True)
+    with pytest.raises(mb.MmbevError, match="second derivative"):
+        (d * x).sum().backward()
+    # a rotation's gradient does not depend on what was turned
+    (d,) = torch.autograd.grad(encoder.rotary(q, pos, steps, axis).sum(), q, create_graph=True)
+    assert not d.requires_grad
 
 
 def test_a_decay_that_wants_a_gradient_is_refused(mb, anywhere):  # noqa: F811
