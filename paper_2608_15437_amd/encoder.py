@@ -6,7 +6,8 @@ head and adds the result to the rows; the projections between are plain matrix p
 the library's backward calls, which have none themselves: a second derivative is refused.  A trained block can also go on row by row (`step`), its state kept between rows.
 
 The rows' number and ranges stay on the device: pass `row_count` (voxel_offsets[-1:]) to encode the voxeliser's full
-buffers without waiting for the count.  Rows past it hold nothing of meaning, so training takes the rows in use alone.
+buffers without waiting for the count.  Results past it hold nothing of meaning; where gradients are wanted they are
+zeros, and so are the gradients of those rows.
 """
 from __future__ import annotations
 
@@ -45,12 +46,21 @@ def _once(backward):
     return call
 
 
+# The library writes the rows in use.  Where a gradient is wanted the others are zeros: they reach the weights' gradients
+# in the products of torch between the operators.
+
+def _rows_like(x, zeros):
+    return torch.zeros_like(x) if zeros else None
+
+
 class _Norm(torch.autograd.Function):
     """layer_norm of x + residual, and the sum itself."""
 
     @staticmethod
     def forward(ctx, x, residual, weight, bias, eps, row_count):
-        out, total, mean, rstd = mmbev.layer_norm(x, weight, bias, eps=eps, residual=residual, stats=True, row_count=row_count)
+        part = row_count is not None and any(ctx.needs_input_grad)
+        out, total, mean, rstd = mmbev.layer_norm(x, weight, bias, eps=eps, residual=residual, stats=True, row_count=row_count,
+                                                  out=_rows_like(x, part), out_sum=_rows_like(x, part and residual is not None))
         ctx.save_for_backward(total, weight, mean, rstd, row_count)
         ctx.types = [None if t is None else t.dtype for t in (weight, bias)]
         return out, total
@@ -61,7 +71,8 @@ class _Norm(torch.autograd.Function):
         total, weight, mean, rstd, row_count = ctx.saved_tensors
         needed = ctx.needs_input_grad  # False where there is no such input
         dx, *sums = mmbev.layer_norm_backward(dout.contiguous(), total, weight, mean, rstd, dskip=dtotal.contiguous(),
-                                              row_count=row_count, weight_grads=needed[2] or needed[3])
+                                              row_count=row_count, weight_grads=needed[2] or needed[3],
+                                              dx=_rows_like(total, row_count is not None))
         dweight, dbias = (t.to(kind) if need else None for t, kind, need in zip(sums, ctx.types, needed[2:4]))
         return dx if needed[0] else None, dx if needed[1] else None, dweight, dbias, None, None
 
@@ -71,21 +82,26 @@ class _Rotary(torch.autograd.Function):
     def forward(ctx, x, positions, steps, axis, layout, row_count):
         ctx.save_for_backward(positions, steps, axis, row_count)
         ctx.layout = layout
-        return mmbev.rotary(x, positions, steps, axis, layout=layout, row_count=row_count)
+        part = row_count is not None and any(ctx.needs_input_grad)
+        return mmbev.rotary(x, positions, steps, axis, layout=layout, row_count=row_count, out=_rows_like(x, part))
 
     @staticmethod
     @_once
     def backward(ctx, dout):
         positions, steps, axis, row_count = ctx.saved_tensors
-        dx = mmbev.rotary(dout.contiguous(), positions, steps, axis, layout=ctx.layout, inverse=True, row_count=row_count)
+        dout = dout.contiguous()
+        dx = mmbev.rotary(dout, positions, steps, axis, layout=ctx.layout, inverse=True, row_count=row_count,
+                          out=_rows_like(dout, row_count is not None))
         return dx, None, None, None, None, None
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, offsets, initial_state, max_length):
+        # the offsets alone know where the rows in use end
+        out = q.new_zeros(*q.shape[:2], v.shape[2]) if any(ctx.needs_input_grad) else None
         out, final = mmbev.linear_attention(q, k, v, log_decay, offsets, initial_state=initial_state, final_state=True,
-                                            max_length=max_length)
+                                            max_length=max_length, out=out)
         ctx.save_for_backward(q, k, v, log_decay, offsets, initial_state)
         ctx.max_length = max_length
         return out, final
@@ -96,7 +112,8 @@ class _Attention(torch.autograd.Function):
         q, k, v, log_decay, offsets, initial_state = ctx.saved_tensors
         dq, dk, dv, dinitial = mmbev.linear_attention_backward(
             dout.contiguous(), q, k, v, log_decay, offsets, initial_state=initial_state, dfinal_state=dfinal.contiguous(),
-            dinitial_state=initial_state is not None, max_length=ctx.max_length)
+            dinitial_state=initial_state is not None, max_length=ctx.max_length, dq=torch.zeros_like(q), dk=torch.zeros_like(k),
+            dv=torch.zeros_like(v))
         return dq, dk, dv, None, None, dinitial, None
 
 
@@ -178,6 +195,8 @@ class VoxelEncoder(nn.Module):
 
     def forward(self, feats, coords, offsets, states=None, max_length=None, row_count=None):
         """Returns (encoded features, the blocks' states after each frame)."""
+        if row_count is not None and torch.is_grad_enabled():  # what lies past the count would enter the weights' gradients
+            feats = torch.where(torch.arange(feats.shape[0], device=feats.device)[:, None] < row_count, feats, 0.0)
         x = feats.to(self.dtype) @ self.embed
         branch, after = torch.zeros_like(x), []
         for i, block in enumerate(self.blocks):
