@@ -297,8 +297,8 @@ struct Exponent {
 };
 
 __device__ __forceinline__ Exponent decay_exponent(const float* log_decay, int h) {
-  // at most 0; -1e4 stands for -inf, whose product with no rows would be NaN
-  const float x = fmaxf(fminf(log_decay[h], 0.0f), -1.0e4f);
+  // at most 0; -1e4 stands for -inf, whose product with no rows would be NaN; NaN stays what it is
+  const float d = log_decay[h], x = d > 0.0f ? 0.0f : d < -1.0e4f ? -1.0e4f : d;
   const float hi = x * 1.44269504088896341f;
   return {hi, __builtin_fmaf(x, 1.44269504088896341f, -hi) + x * 1.92596299e-8f};  // 1 / ln 2 and what fp32 leaves of it
 }

@@ -44,3 +44,29 @@ def test_a_step_of_a_far_decay(gpu_lib):
     gpu_lib.linear_attention_step(z, z, z, g, state)
     want = 3.0 * torch.exp(g.double())[:, None, None]
     assert float((state[0].double() / want - 1.0).abs().max()) < 2e-6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [5, 1500])
+def test_a_decay_of_nan_is_seen_in_its_head_alone(gpu_lib, rows, dtype):
+    """S = nan * S + ...: all of the head's outputs and states are nan, the other heads' keep their bits."""
+    import torch
+
+    from test_gpu_sequence import torch_type
+
+    torch.manual_seed(rows)
+    t = torch_type(dtype)
+    q, k, v = (torch.randn(rows, 3, 32, device="cuda").to(t) for _ in range(3))
+    off = torch.tensor([0, rows], dtype=torch.int64, device="cuda")
+    g = torch.tensor([-0.1, -0.2, -0.3], device="cuda")
+    want, end = gpu_lib.linear_attention(q, k, v, g, off, final_state=True)
+    bad = g.clone()
+    bad[1] = float("nan")
+    out, last = gpu_lib.linear_attention(q, k, v, bad, off, final_state=True)
+    for got, ref, head in ((out, want, 1), (last, end, 1)):
+        assert bool(got.select(head, 1).isnan().all())
+        assert torch.equal(got[:, [0, 2]], ref[:, [0, 2]])
+    state = torch.zeros(rows, 3, 32, 32, device="cuda")
+    out = gpu_lib.linear_attention_step(q, k, v, bad, state)
+    assert bool(out[:, 1].isnan().all()) and bool(state[:, 1].isnan().all())
+    assert bool(out[:, [0, 2]].isfinite().all()) and bool(state[:, [0, 2]].isfinite().all())
