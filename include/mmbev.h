@@ -492,7 +492,9 @@ mmbev_status_t mmbev_voxel_clusters(const int32_t* coords, const int32_t* counts
  * Element types: MMBEV_F32, MMBEV_F16, MMBEV_BF16.  Everything between the
  * loads and the stores is held in 32 bits (a product on the matrix cores takes
  * operands of the element type), and results are rounded once, to nearest
- * even.  Any alignment of the element type and any row stride are taken.
+ * even.  Any alignment of the element type and any stride below 2^40 elements
+ * are taken (linear attention, but not its step: row strides below 2^31, else
+ * MMBEV_ERR_UNSUPPORTED).
  * Arrays that a call writes share no element with its other arrays, except
  * where it says so; they may interleave in rows of one stride.
  *

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "sequence.hpp"
 
@@ -20,21 +21,33 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+
+// Strides and rows that each are in range: the last row's elements lie inside an address space (2^58 bytes or fewer on).
+bool reachable(int64_t rows, int64_t stride) { return rows <= 1 || stride <= ((int64_t)1 << 56) / (rows - 1); }
+
 // Rows of `width` elements: there (or, optional, absent), aligned to the element, rows apart.
 bool rows_ok(const mmbev_rows_t& t, int64_t rows, int32_t width, int32_t dtype, bool optional) {
   if (!t.data) return optional || rows == 0;
-  return aligned(t.data, size_of(dtype)) && (rows <= 1 || t.row_stride >= width) && t.row_stride >= 0 &&
-         t.row_stride < ((int64_t)1 << 40);
+  return aligned(t.data, size_of(dtype)) && (rows <= 1 || t.row_stride >= width) && t.row_stride >= 0 && t.row_stride < kMaxStride &&
+         reachable(rows, t.row_stride);
 }
 
 bool heads_ok(const mmbev_heads_t& t, int64_t rows, int32_t heads, int32_t dim, int32_t dtype) {
   if (!t.data) return rows == 0;
   if (!aligned(t.data, size_of(dtype)) || t.row_stride < 0 || t.head_stride < 0) return false;
-  if (t.row_stride > INT32_MAX || t.head_stride >= ((int64_t)1 << 40)) return false;
+  if (t.row_stride >= kMaxStride || t.head_stride >= kMaxStride || !reachable(rows, t.row_stride)) return false;
   if (heads > 1 && t.head_stride < dim) return false;
   // heads inside a row, or rows inside a head
   const int64_t row = (int64_t)(heads - 1) * t.head_stride + dim;
   return rows <= 1 || t.row_stride >= row || (t.row_stride >= dim && t.head_stride >= (rows - 1) * t.row_stride + dim);
+}
+
+// The attention walks' row strides take 31 bits: a row's address is then one 32 x 32-bit product.
+bool too_wide(std::initializer_list<const mmbev_heads_t*> arrays, int64_t rows) {
+  for (const mmbev_heads_t* t : arrays)
+    if (rows > 1 && t->row_stride > INT32_MAX) return true;
+  return false;
 }
 
 // First and past-the-last byte of rows of heads.
@@ -375,7 +388,8 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* t, mmbev_heads_t x, const int3
   if (!heads_ok(x, t->rows, t->heads, t->dim, t->dtype) || !heads_ok(out, t->rows, t->heads, t->dim, t->dtype))
     return MMBEV_ERR_INVALID_ARG;
   if (t->rows > 0 && (!positions || !aligned(positions, 4) || !steps || !aligned(steps, 8) || !axis)) return MMBEV_ERR_INVALID_ARG;
-  if (position_stride < 0 || (t->rows > 1 && position_stride < axes) || position_stride >= ((int64_t)1 << 40))
+  if (position_stride < 0 || (t->rows > 1 && position_stride < axes) || position_stride >= kMaxStride ||
+      !reachable(t->rows, position_stride))
     return MMBEV_ERR_INVALID_ARG;
   if (!same(x, out) && meet(x, t->heads, t->dim, out, t->heads, t->dim, t->rows, t->dtype)) return MMBEV_ERR_INVALID_ARG;
   RotaryArgs a{};
@@ -420,6 +434,7 @@ mmbev_status_t mmbev_linear_attention(const mmbev_attention_t* t, mmbev_heads_t 
   if (!log_decay || !aligned(log_decay, 4) || !offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) ||
       !aligned(final_state, 4))
     return MMBEV_ERR_INVALID_ARG;
+  if (too_wide({&q, &k, &v, &out}, t->rows)) return MMBEV_ERR_UNSUPPORTED;
   const size_t state = (size_t)t->num_sequences * t->heads * t->key_dim * t->value_dim * 4;
   if (initial_state && final_state &&
       overlap({(uintptr_t)initial_state, (uintptr_t)initial_state + state}, {(uintptr_t)final_state, (uintptr_t)final_state + state}))
@@ -464,6 +479,7 @@ mmbev_status_t mmbev_linear_attention_backward(const mmbev_attention_t* t, mmbev
   if (!log_decay || !aligned(log_decay, 4) || !offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) ||
       !aligned(dfinal_state, 4) || !aligned(dinitial_state, 4))
     return MMBEV_ERR_INVALID_ARG;
+  if (too_wide({&dout, &q, &k, &v, &dq, &dk, &dv}, R)) return MMBEV_ERR_UNSUPPORTED;
   const size_t state = (size_t)t->num_sequences * H * t->key_dim * t->value_dim * 4;
   const Span di = {(uintptr_t)dinitial_state, (uintptr_t)dinitial_state + (dinitial_state ? state : 0)};
   for (const float* in : {initial_state, dfinal_state})

@@ -39,3 +39,25 @@ def test_arrays_interleaved_in_rows_of_one_buffer(gpu_lib):
         dq, dk, dv, rest = (pick(back, i) for i in range(4))
         gpu_lib.linear_attention_backward(c["g"], q, k, v, c["decay"], c["doff"], dq=dq, dk=dk, dv=dv)
         assert all(torch.equal(a, b) for a, b in zip((dq, dk, dv), grads)) and bool((rest == 7.0).all())
+
+
+def test_rows_more_than_31_bits_apart(gpu_lib):
+    """Two rows 2^31 + 64 elements apart: norm, rotary and the step take them; attention says that it does not."""
+    import torch
+
+    wide = (1 << 31) + 64
+    room = torch.zeros(wide + 64, dtype=torch.bfloat16, device="cuda")
+    x = room.as_strided((2, 64), (wide, 1))
+    t = torch.randn(2, 64, device="cuda").bfloat16()
+    x.copy_(t)
+    assert torch.equal(gpu_lib.layer_norm(x)[0], gpu_lib.layer_norm(t)[0])
+    steps, axis = (torch.from_numpy(a).cuda() for a in gpu_lib.make_rotary(32))
+    pos = torch.tensor([7, 9], dtype=torch.int32, device="cuda")
+    h, ht = x.unflatten(1, (2, 32)), t.unflatten(1, (2, 32))
+    assert torch.equal(gpu_lib.rotary(h, pos, steps, axis), gpu_lib.rotary(ht, pos, steps, axis))
+    g = torch.full((2,), -0.1, device="cuda")
+    a, b = torch.zeros(2, 2, 2, 32, 32, device="cuda").unbind(0)
+    assert torch.equal(gpu_lib.linear_attention_step(h, h, h, g, a), gpu_lib.linear_attention_step(ht, ht, ht, g, b))
+    assert torch.equal(a, b)
+    with pytest.raises(gpu_lib.MmbevError, match="-3"):
+        gpu_lib.linear_attention(h, h, h, g, torch.tensor([0, 2], device="cuda"))
