@@ -61,3 +61,44 @@ def test_rows_more_than_31_bits_apart(gpu_lib):
     assert torch.equal(a, b)
     with pytest.raises(gpu_lib.MmbevError, match="-3"):
         gpu_lib.linear_attention(h, h, h, g, torch.tensor([0, 2], device="cuda"))
+
+
+MOST = 1 << 23  # workgroups of a launch: more rows take more launches
+
+
+def whole_of(view, tile, rows):
+    """Every row of a large tensor against a tile that repeats, some of it at a time."""
+    import torch
+
+    n = tile.shape[0]
+    return all(torch.equal(view[a:min(a + n, rows)], tile[:min(n, rows - a)]) for a in range(0, rows, n))
+
+
+@pytest.mark.parametrize("operator", ["layer_norm", "rotary"])
+def test_rows_past_one_launch(gpu_lib, operator):
+    """A row a workgroup, 2^23 + 5 of them with 2^23 + 2 in use, in place: every row is right and those past the count are as
+    they were."""
+    import torch
+
+    rows, used, n = MOST + 5, MOST + 2, 1 << 17
+    if torch.cuda.mem_get_info()[0] < 45e9:
+        pytest.skip("needs 45 GB of memory")
+    count = torch.tensor([used], dtype=torch.int64, device="cuda")
+    if operator == "layer_norm":
+        tile = torch.randn(n, 2050, device="cuda").bfloat16()  # past 2,048 a row takes a whole workgroup
+        run = lambda x, **kw: gpu_lib.layer_norm(x, **kw)[0]  # noqa: E731
+    else:
+        tile = torch.randn(n, 1024, device="cuda")  # 256 packs of two pairs
+        steps, axis = (torch.from_numpy(a).cuda() for a in gpu_lib.make_rotary(1024))
+        pos = (torch.arange(rows, dtype=torch.int32, device="cuda") % n).contiguous()
+        run = lambda x, **kw: gpu_lib.rotary(x[:, None], pos[:x.shape[0]], steps, axis, "interleaved",  # noqa: E731
+                                             **{k: v[:, None] if k == "out" else v for k, v in kw.items()})[:, 0]
+    want = run(tile)
+    x = torch.empty(rows, tile.shape[1], dtype=tile.dtype, device="cuda")
+    for a in range(0, rows, n):
+        x[a:a + n] = tile[:min(n, rows - a)]
+    fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+    run(x, out=x, row_count=count, fault=fault)
+    assert whole_of(x, want, used) and torch.equal(x[used:], tile[used - MOST:rows - MOST]) and int(fault) == 0
+    del x
+    torch.cuda.empty_cache()
