@@ -129,6 +129,10 @@ def load() -> ctypes.CDLL:
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise MmbevError(f"{LIB_PATH} is missing: build it with paper_2608_15437_amd.build.build()")
+        try:
+            import torch  # noqa: F401  (before the library, which then shares torch's HIP runtime instead of bringing another)
+        except ImportError:
+            pass  # the host helpers need none
         L = ctypes.CDLL(LIB_PATH)
         p = ctypes.c_void_p
         L.mmbev_abi_version.argtypes = []

@@ -158,3 +158,17 @@ def test_a_decay_that_wants_a_gradient_is_refused(mb, anywhere):  # noqa: F811
     with torch.no_grad():
         encoder.linear_attention(q, k, v, decay, off)
     encoder.linear_attention(q, k, v, decay.detach(), off)
+
+
+def test_the_library_shares_torchs_hip_runtime(mb):  # noqa: F811
+    """A host helper called before torch is imported must not bring a second HIP runtime: launches on torch's memory and
+    streams then fail."""
+    import os
+    import subprocess
+    import sys
+
+    code = ("from paper_2608_15437_amd import mmbev; mmbev.make_rotary(16); import torch; "
+            "print(len({l.split()[-1] for l in open('/proc/self/maps') if 'libamdhip64' in l}))")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0 and r.stdout.split()[-1] == "1", r.stdout + r.stderr
