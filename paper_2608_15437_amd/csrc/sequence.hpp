@@ -161,8 +161,6 @@ hipError_t launch_attention_step(const AttnStepArgs& a, int32_t dtype, hipStream
 using f16 = _Float16;
 using bf16 = __bf16;
 
-typedef float float4v __attribute__((ext_vector_type(4)));
-
 // N elements as they lie in memory, at any alignment of the element: the
 // loads and stores are still as wide as the elements together (gfx950's
 // global accesses take any byte address; an aligned row is faster).
