@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(AttnSumArgs a) {
 
 // One row of a stream: its state read, decayed, updated and written once.
 // Bound by the state's bytes, and in small calls by its chain of loads (64
-// streams of 8 x 64 x 64, 17 MB: 6.2 us).  A thread has four neighbouring columns of
+// streams of 8 x 64 x 64, 17 MB: 5.8 us).  A thread has four neighbouring columns of
 // every (256 / lanes)-th state row, lanes enough for a row of the state; the
 // rows' parts of the output meet in LDS.
 template <typename T, int LANES>

@@ -22,10 +22,10 @@
 //   rounded copy is put into LDS for the product with a;
 // - the next chunk's loads are issued before this one's products.
 //
-// Heads of 8 x 64 in bf16, forward: 128 frames (921,997 rows) 919 us, 4.1 TB/s;
-// a sequence of 120,000 rows 166 us, where keys and values are read twice, once
-// for the parts' states.  Gradients over 213,879 rows in 8 sequences 525 us:
-// all of them cut, 2.6 GB moved at 5 TB/s.
+// Heads of 8 x 64 in bf16, forward: 128 frames (921,997 rows) 986 us, 3.8 TB/s,
+// bound by the chain of a chunk; a sequence of 120,000 rows 172 us, where keys
+// and values are read twice, once for the parts' states.  Gradients over 213,879
+// rows in 8 sequences 607 us: all of them cut, 2.6 GB moved at 4.3 TB/s.
 //
 // The gradients are the same recurrence: dq forwards as (dout, v, k); dv and dk
 // backwards in time as (k, q, dout) and (v, dout, q), whose states are one
@@ -1097,7 +1097,7 @@ __device__ __forceinline__ void walk_back(const AttnGradArgs& a, int item, WalkS
 // The backward pass: both walks in one launch, the longer one's workgroups
 // first (one after the other their last workgroups, and twice two more
 // launches for the cut sequences' states, left the chip idle: 167 us for one
-// robot frame instead of 113).
+// robot frame instead of 113, both with factors rounded once).
 template <typename T, int D, int GROUP, bool WHOLE>
 __global__ __launch_bounds__(kAttnThreads, (grad_waves(sizeof(T) == 2, D))) void attention_backward_kernel(AttnArgs a, AttnGradArgs b,
                                                                                                        uint32_t back_items) {

@@ -18,8 +18,8 @@ constexpr int64_t kMostGroups = (int64_t)1 << 23;
 
 // Calls that read and write more than this store past the caches: what they
 // write would be evicted before another call reads it, and takes the place of
-// what they read twice.  (Norm of 921,997 x 256 rows 312 -> 299 us, rotary of
-// 213,879 x 16 x 64 163 -> 151, a keyframe's attention 179 -> 166.)  Half of
+// what they read twice.  (Norm of 921,997 x 256 rows 315 -> 309 us, rotary of
+// 213,879 x 16 x 64 169 -> 152, a keyframe's attention 177 -> 169.)  Half of
 // the memory-side cache.
 constexpr int64_t kPastCaches = (int64_t)128 << 20;
 

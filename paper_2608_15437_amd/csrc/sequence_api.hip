@@ -192,8 +192,8 @@ int32_t grad_group(const mmbev_attention_t* t) {
 
 // Rows of a part, at least: enough that its state is a small part of what is
 // read for them.  Short calls want more parts, the backward pass with its two
-// states fewer: a frame's 5,442 rows of 4 x 128 forward in 36 us with 128
-// rows and 43 with 256, the gradients of 18,608 in 127 and 112.
+// states fewer: a frame's 5,442 rows of 4 x 128 forward in 41 us with 128
+// rows and 51 with 256, the gradients of 18,608 in 171 and 165.
 int32_t least_rows(const mmbev_attention_t* t, bool backward) {
   return backward && std::max(t->key_dim, t->value_dim) > 64 ? 256 : 128;
 }
@@ -218,7 +218,7 @@ AttnPlan attention_plan(const mmbev_attention_t* t, bool backward) {
   const bool half = t->dtype != MMBEV_F32;
   const int32_t wide = std::max(t->key_dim, t->value_dim);
   // (three a unit for the gradients of heads of 32, whatever share one's registers allow: 8 frames of 16 heads over 4,
-  // 652 us instead of 760)
+  // 716 us instead of 883)
   p.slots = kComputeUnits * (!backward ? walk_waves(half, wide) : wide <= 32 ? 3 : grad_waves(half, wide));
   p.least = least_rows(t, backward);
   p.cuts = cuts_for(t, t->heads, p.slots, backward);
