@@ -49,6 +49,10 @@ def _once(backward):
 # The library writes the rows in use.  Where a gradient is wanted the others are zeros: they reach the weights' gradients
 # in the products of torch between the operators.
 
+def _wanted(*inputs):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
+
+
 def _rows_like(x, zeros):
     return torch.zeros_like(x) if zeros else None
 
@@ -57,8 +61,8 @@ class _Norm(torch.autograd.Function):
     """layer_norm of x + residual, and the sum itself."""
 
     @staticmethod
-    def forward(ctx, x, residual, weight, bias, eps, row_count):
-        part = row_count is not None and any(ctx.needs_input_grad)
+    def forward(ctx, x, residual, weight, bias, eps, row_count, wanted):
+        part = row_count is not None and wanted
         out, total, mean, rstd = mmbev.layer_norm(x, weight, bias, eps=eps, residual=residual, stats=True, row_count=row_count,
                                                   out=_rows_like(x, part), out_sum=_rows_like(x, part and residual is not None))
         ctx.save_for_backward(total, weight, mean, rstd, row_count)
@@ -74,15 +78,15 @@ class _Norm(torch.autograd.Function):
                                               row_count=row_count, weight_grads=needed[2] or needed[3],
                                               dx=_rows_like(total, row_count is not None))
         dweight, dbias = (t.to(kind) if need else None for t, kind, need in zip(sums, ctx.types, needed[2:4]))
-        return dx if needed[0] else None, dx if needed[1] else None, dweight, dbias, None, None
+        return dx if needed[0] else None, dx if needed[1] else None, dweight, dbias, None, None, None
 
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, positions, steps, axis, layout, row_count):
+    def forward(ctx, x, positions, steps, axis, layout, row_count, wanted):
         ctx.save_for_backward(positions, steps, axis, row_count)
         ctx.layout = layout
-        part = row_count is not None and any(ctx.needs_input_grad)
+        part = row_count is not None and wanted
         return mmbev.rotary(x, positions, steps, axis, layout=layout, row_count=row_count, out=_rows_like(x, part))
 
     @staticmethod
@@ -92,14 +96,14 @@ class _Rotary(torch.autograd.Function):
         dout = dout.contiguous()
         dx = mmbev.rotary(dout, positions, steps, axis, layout=ctx.layout, inverse=True, row_count=row_count,
                           out=_rows_like(dout, row_count is not None))
-        return dx, None, None, None, None, None
+        return dx, None, None, None, None, None, None
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, log_decay, offsets, initial_state, max_length):
+    def forward(ctx, q, k, v, log_decay, offsets, initial_state, max_length, wanted):
         # the offsets alone know where the rows in use end
-        out = q.new_zeros(*q.shape[:2], v.shape[2]) if any(ctx.needs_input_grad) else None
+        out = q.new_zeros(*q.shape[:2], v.shape[2]) if wanted else None
         out, final = mmbev.linear_attention(q, k, v, log_decay, offsets, initial_state=initial_state, final_state=True,
                                             max_length=max_length, out=out)
         ctx.save_for_backward(q, k, v, log_decay, offsets, initial_state)
@@ -114,24 +118,24 @@ class _Attention(torch.autograd.Function):
             dout.contiguous(), q, k, v, log_decay, offsets, initial_state=initial_state, dfinal_state=dfinal.contiguous(),
             dinitial_state=initial_state is not None, max_length=ctx.max_length, dq=torch.zeros_like(q), dk=torch.zeros_like(k),
             dv=torch.zeros_like(v))
-        return dq, dk, dv, None, None, dinitial, None
+        return dq, dk, dv, None, None, dinitial, None, None
 
 
 def norm(x, residual, weight, bias, eps=1e-5, row_count=None):
     """(layer_norm(x + residual), x + residual), differentiable."""
-    return _Norm.apply(x, residual, weight, bias, eps, row_count)
+    return _Norm.apply(x, residual, weight, bias, eps, row_count, _wanted(x, residual, weight, bias))
 
 
 def rotary(x, positions, steps, axis, layout="half", row_count=None):
     """mmbev.rotary, differentiable in x."""
-    return _Rotary.apply(x, positions, steps, axis, layout, row_count)
+    return _Rotary.apply(x, positions, steps, axis, layout, row_count, _wanted(x))
 
 
 def linear_attention(q, k, v, log_decay, offsets, initial_state=None, max_length=None):
     """mmbev.linear_attention's (out, final state), differentiable in q, k, v and the initial state; log_decay is a constant."""
     if log_decay.requires_grad and torch.is_grad_enabled():
         raise mmbev.MmbevError("log_decay has no gradient: detach it")
-    return _Attention.apply(q, k, v, log_decay, offsets, initial_state, max_length)
+    return _Attention.apply(q, k, v, log_decay, offsets, initial_state, max_length, _wanted(q, k, v, initial_state))
 
 
 class Block(nn.Module):

@@ -172,3 +172,28 @@ def test_the_library_shares_torchs_hip_runtime(mb):  # noqa: F811
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=110)
     assert r.returncode == 0 and r.stdout.split()[-1] == "1", r.stdout + r.stderr
+
+
+def test_rows_are_zeroed_only_where_a_gradient_is_wanted(mb, anywhere, monkeypatch):  # noqa: F811
+    """Inference with the module's parameters, over buffers whose rows the device counts, fills nothing."""
+    from paper_2608_15437_amd import encoder
+
+    zeroed = []
+    for name in ("layer_norm", "rotary", "linear_attention"):
+        real = getattr(mb, name)
+        monkeypatch.setattr(mb, name, lambda *a, real=real, **kw: zeroed.append(kw.get("out") is not None) or real(*a, **kw))
+    x, y, w, b = torch.ones(5, 8), torch.ones(5, 8), torch.ones(8, requires_grad=True), torch.zeros(8, requires_grad=True)
+    q, k, v = (torch.ones(6, 2, 4, requires_grad=True) for _ in range(3))
+    pos, steps, axis = torch.zeros(6, dtype=torch.int32), torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.uint8)
+    count = torch.tensor([3])
+
+    def run():
+        zeroed.clear()
+        encoder.norm(x, y, w, b, row_count=count)
+        encoder.rotary(q, pos, steps, axis, row_count=count)
+        encoder.linear_attention(q, k, v, torch.zeros(2), torch.tensor([0, 6]))
+        return list(zeroed)
+
+    assert run() == [True] * 3
+    with torch.no_grad():
+        assert run() == [False] * 3
