@@ -642,8 +642,9 @@ size_t mmbev_linear_attention_workspace_bytes(const mmbev_attention_t* attention
  * NULL) receives the state after the last row (the initial one for an empty
  * sequence).  The two must not overlap.  log_decay (fp32 [heads]) is at most
  * 0, -inf included (a larger value counts as 0, NaN makes the head's results
- * NaN); it is a constant of the model and has no gradient.  A sequence with a NaN or infinity in a row has
- * unspecified outputs; other sequences and heads do not see it.
+ * NaN); it is a constant of the model and has no gradient.  A sequence with a
+ * NaN or infinity in a row or in its initial state has unspecified outputs;
+ * other sequences and heads do not see it.
  * The state is decayed, summed and carried in fp32 over all of a sequence;
  * for 16-bit types what the matrix cores multiply (the state, the pairs'
  * factors scale * lambda^(i-j) * q_i k_j, the decayed rows that enter the
