@@ -617,6 +617,52 @@ mmbev_status_t mmbev_rotary(const mmbev_rotary_t* rotary, mmbev_heads_t x, const
                             const int64_t* row_count, mmbev_heads_t out, int32_t* fault, void* stream);
 
 typedef struct {
+  int64_t rows;         /* 0 .. 2^31-1 */
+  int32_t heads;        /* of queries, 1..1024 */
+  int32_t kv_heads;     /* of keys, 1..1024 */
+  int32_t dim;          /* of a head, 2..256 */
+  int32_t rotary_dim;   /* even, 2..dim; the rest of the head is not turned */
+  int32_t dtype;
+  int32_t weight_dtype; /* MMBEV_F32 or dtype */
+  int32_t layout;       /* MMBEV_ROTARY_HALF or _INTERLEAVED */
+  float eps;            /* >= 0, finite */
+} mmbev_head_norm_t;
+
+/*
+ * Norms of queries and keys for each head, turned by the row's position in
+ * the same pass: every head x of q and of k becomes
+ *   R(x / sqrt(mean(x^2) + eps) * weight)
+ * with q's or k's weight [dim] (NULL: ones) and mmbev_rotary's rotation R
+ * (positions, steps and axis as there).  With the weight dim^-1/2 the heads
+ * have length 1, which the gated delta rule's keys are to have.  The squares
+ * are summed in fp32: a head whose elements pass 2^60 (or, with eps 0, lie
+ * under 2^-60 or are all zero) has unspecified results.  q_out may be q's own
+ * rows and heads (same strides), k_out k's.
+ */
+mmbev_status_t mmbev_head_norm_rotary(const mmbev_head_norm_t* norm, mmbev_heads_t q, mmbev_heads_t k,
+                                      const void* q_weight, const void* k_weight, const int32_t* positions,
+                                      int64_t position_stride, int32_t axes, const uint64_t* steps,
+                                      const uint8_t* axis, const int64_t* row_count, mmbev_heads_t q_out,
+                                      mmbev_heads_t k_out, int32_t* fault, void* stream);
+
+size_t mmbev_head_norm_rotary_backward_workspace_bytes(const mmbev_head_norm_t* norm);
+
+/*
+ * Its gradients, from what it was called with and the gradients of its
+ * results: dq and dk like q and k, dq_weight and dk_weight fp32 [dim] (summed
+ * over rows and heads).  The last two may be NULL; the workspace is needed
+ * where one is asked for (256-byte aligned, no initialisation).  dq may be
+ * dq_out's or q's own rows and heads (same strides), dk dk_out's or k's.
+ */
+mmbev_status_t mmbev_head_norm_rotary_backward(const mmbev_head_norm_t* norm, mmbev_heads_t dq_out,
+                                               mmbev_heads_t dk_out, mmbev_heads_t q, mmbev_heads_t k,
+                                               const void* q_weight, const void* k_weight, const int32_t* positions,
+                                               int64_t position_stride, int32_t axes, const uint64_t* steps,
+                                               const uint8_t* axis, const int64_t* row_count, mmbev_heads_t dq,
+                                               mmbev_heads_t dk, float* dq_weight, float* dk_weight, int32_t* fault,
+                                               void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
   int64_t rows;          /* rows that q, k, v and out hold, 0 .. 2^31-1 */
   int64_t max_length;    /* no sequence is longer (e.g. max_voxels); 0: rows */
   int32_t num_sequences; /* B, 1..65535; (B + 1024) * heads <= 2^23 */

@@ -25,7 +25,6 @@ namespace mmbev {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormGrid = 1024;  // workgroups of the backward pass: four a CU, a partial row each
 
 // Weight or bias of the thread's columns (fp32 or the rows' type).
 template <typename T, int VEC>
@@ -348,6 +347,12 @@ hipError_t launch_norm(const NormArgs& a, int32_t dtype, hipStream_t st) {
                               : norm_of<bf16>(a, s, st);
 }
 
+hipError_t launch_weight_sum(const float* partial, int32_t parts, int32_t width, float* first, float* second, hipStream_t st) {
+  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((uint32_t)((2 * width + kSumCols - 1) / kSumCols)), dim3(kSumCols * kSumParts), 0,
+                     st, partial, parts, width, first, second);
+  return hipGetLastError();
+}
+
 hipError_t launch_norm_backward(const NormArgs& a, int32_t dtype, hipStream_t st) {
   const NormShape s = norm_shape(a.width, dtype);
   const int32_t grid = norm_backward_grid(a.rows, a.width, dtype);
@@ -355,10 +360,7 @@ hipError_t launch_norm_backward(const NormArgs& a, int32_t dtype, hipStream_t st
                        : dtype == MMBEV_F16 ? norm_backward_of<f16>(a, s, grid, st)
                                             : norm_backward_of<bf16>(a, s, grid, st);
   if (e != hipSuccess || !a.partial) return e;
-  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((uint32_t)((2 * a.width + kSumCols - 1) / kSumCols)),
-                     dim3(kSumCols * kSumParts), 0, st, a.partial, grid,
-                     a.width, a.dweight, a.dbias);
-  return hipGetLastError();
+  return launch_weight_sum(a.partial, grid, a.width, a.dweight, a.dbias, st);
 }
 
 }  // namespace mmbev

@@ -50,6 +50,10 @@ hipError_t launch_norm(const NormArgs& a, int32_t dtype, hipStream_t st);
 hipError_t launch_norm_backward(const NormArgs& a, int32_t dtype, hipStream_t st);
 int32_t norm_backward_grid(int64_t rows, int32_t width, int32_t dtype);  // workgroups, hence partial rows
 
+constexpr int kNormGrid = 1024;  // most workgroups of a norm's backward pass: four a CU, a partial row each
+// first and second [width]: partial's `parts` <= kNormGrid rows of 2 * width added up (either may be null)
+hipError_t launch_weight_sum(const float* partial, int32_t parts, int32_t width, float* first, float* second, hipStream_t st);
+
 struct RotaryArgs {
   const void* x;
   void* out;
@@ -66,6 +70,33 @@ struct RotaryArgs {
 };
 
 hipError_t launch_rotary(const RotaryArgs& a, int32_t dtype, hipStream_t st);
+
+// Norm and rotation of every head of two arrays of rows: [0] queries, [1] keys.
+struct HeadNormArgs {
+  const void* x[2];
+  const void* dy[2];     // backward
+  void* out[2];          // backward: dx
+  const void* weight[2]; // null: ones
+  float* partial;        // backward: [grid][2][dim] sums of dweight, or null
+  float* dweight[2];
+  const int32_t* positions;
+  const uint64_t* steps;
+  const uint8_t* axis;
+  const int64_t* row_count;
+  int32_t* fault;
+  int64_t rows, x_row[2], x_head[2], dy_row[2], dy_head[2], out_row[2], out_head[2], position_stride;
+  int64_t first_row;     // of the launch
+  int32_t heads[2];
+  int32_t dim, rotary_dim, axes;
+  int32_t interleaved;
+  int32_t weight_f32;    // weights are fp32 (else of the rows' type)
+  int32_t past;          // store past the caches
+  float eps, inv_dim;
+};
+
+hipError_t launch_head_norm(const HeadNormArgs& a, int32_t dtype, hipStream_t st);
+hipError_t launch_head_norm_backward(const HeadNormArgs& a, int32_t dtype, hipStream_t st);
+int32_t head_norm_backward_grid(const HeadNormArgs& a, int32_t dtype);  // workgroups, hence partial rows
 
 // Waves a SIMD of the walks' kernels, as their registers allow, hence the
 // workgroups of four waves that a compute unit takes; `wide`: 32, 64 or 128.

@@ -72,6 +72,12 @@ class mmbev_rotary_t(ctypes.Structure):
                 ("inverse", ctypes.c_int32)]
 
 
+class mmbev_head_norm_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 class mmbev_attention_t(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("max_length", ctypes.c_int64), ("num_sequences", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("key_dim", ctypes.c_int32),
@@ -179,6 +185,14 @@ def load() -> ctypes.CDLL:
         L.mmbev_make_rotary.restype = i32
         L.mmbev_rotary.argtypes = [ctypes.POINTER(mmbev_rotary_t), heads, p, i64, i32, p, p, p, heads, p, p]
         L.mmbev_rotary.restype = i32
+        head_norm = ctypes.POINTER(mmbev_head_norm_t)
+        L.mmbev_head_norm_rotary.argtypes = [head_norm, heads, heads, p, p, p, i64, i32, p, p, p, heads, heads, p, p]
+        L.mmbev_head_norm_rotary.restype = i32
+        L.mmbev_head_norm_rotary_backward_workspace_bytes.argtypes = [head_norm]
+        L.mmbev_head_norm_rotary_backward_workspace_bytes.restype = size
+        L.mmbev_head_norm_rotary_backward.argtypes = [head_norm, heads, heads, heads, heads, p, p, p, i64, i32, p, p, p, heads,
+                                                      heads, p, p, p, p, size, p]
+        L.mmbev_head_norm_rotary_backward.restype = i32
         L.mmbev_linear_attention_workspace_bytes.argtypes = [attention, i32]
         L.mmbev_linear_attention_workspace_bytes.restype = size
         L.mmbev_linear_attention.argtypes = [attention, heads, heads, heads, p, p, p, heads, p, p, p, size, p]
@@ -712,6 +726,15 @@ def make_rotary(rotary_dim: int, axes: int = 1, base: float = 10000.0, scaling: 
     return steps.view(np.int64), axis
 
 
+def _columns(positions, rows):
+    """Row stride and number of the position columns."""
+    at, step = positions.shape, positions.stride()
+    if positions.dtype != _torch.int32 or at[0] != rows or len(at) > 2 or (len(at) == 2 and at[1] > 1 and step[1] != 1):
+        raise MmbevError("positions must be int32 [rows] or [rows][axes], a row's columns next to each other")
+    axes = at[1] if len(at) == 2 else 1
+    return step[0] if rows > 1 else axes, axes
+
+
 def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = False, row_count=None, out=None, fault=None,
            stream=None):
     """Enqueue mmbev_rotary: x [rows][heads][dim]; positions int32 [rows] or [rows][axes] (a view of the voxeliser's
@@ -720,19 +743,96 @@ def rotary(x, positions, steps, axis, layout: str = "half", inverse: bool = Fals
     given = out
     torch = _torch
     xs, shape = _heads("x", x), x.shape
-    at, step = positions.shape, positions.stride()
-    if positions.dtype != torch.int32 or at[0] != shape[0] or len(at) > 2 or (len(at) == 2 and at[1] > 1 and step[1] != 1):
-        raise MmbevError("positions must be int32 [rows] or [rows][axes], a row's columns next to each other")
-    axes = at[1] if len(at) == 2 else 1
+    stride, axes = _columns(positions, shape[0])
     pairs = steps.numel()
     out = _empty_like(stream, x) if out is None else _like("out", out, x.dtype, shape)
     desc = mmbev_rotary_t(*shape, 2 * pairs, _dtype_code(x), ROTARY_LAYOUTS[layout], 1 if inverse else 0)
     _check((_lib or load()).mmbev_rotary(
-        desc, xs, positions.data_ptr(), step[0] if shape[0] > 1 else axes, axes, _vector("steps", steps, torch.int64, pairs),
+        desc, xs, positions.data_ptr(), stride, axes, _vector("steps", steps, torch.int64, pairs),
         _vector("axis", axis, torch.uint8, pairs), _vector("row_count", row_count, torch.int64, 1), _heads("out", out),
         _vector("fault", fault, torch.int32, 1), handle), "mmbev_rotary")
     _written(given)
     return out
+
+
+def _head_norm_of(q, k, q_weight, k_weight, pairs, eps, layout) -> mmbev_head_norm_t:
+    code = _dtype_code(q)
+    if q.dim() != 3 or k.dim() != 3:
+        raise MmbevError("q and k must be [rows][heads][dim]")
+    (rows, heads, dim), (krows, kv_heads, kdim) = q.shape, k.shape
+    if krows != rows or kdim != dim or k.dtype != q.dtype:
+        raise MmbevError("k must be [rows][kv_heads][dim] of q's type, rows and dim")
+    wcode = F32
+    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if t is not None:
+            if t.numel() != dim or not t.is_contiguous():
+                raise MmbevError(f"{name} must be contiguous with {dim} elements")
+            wcode = _dtype_code(t)
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise MmbevError("q_weight and k_weight must have one type")
+    return mmbev_head_norm_t(rows, heads, kv_heads, dim, 2 * pairs, code, wcode, ROTARY_LAYOUTS[layout], eps)
+
+
+def head_norm_rotary(q, k, q_weight, k_weight, positions, steps, axis, eps: float = 1e-6, layout: str = "half", row_count=None,
+                     q_out=None, k_out=None, fault=None, stream=None):
+    """Enqueue mmbev_head_norm_rotary: q [rows][heads][dim] and k [rows][kv_heads][dim], every head divided by the root of
+    its mean square, multiplied by its weight ([dim] or None; float32 or q's type) and turned as rotary() does.
+
+    Returns (q_out, k_out), which may be q and k.
+    """
+    handle = _issue_on(stream, q, k, q_weight, k_weight, positions, steps, axis, row_count, q_out, k_out, fault)
+    given = q_out, k_out
+    torch = _torch
+    qs, ks = _heads("q", q), _heads("k", k)
+    pairs = steps.numel()
+    desc = _head_norm_of(q, k, q_weight, k_weight, pairs, eps, layout)
+    stride, axes = _columns(positions, desc.rows)
+    q_out = _empty(stream, q, q.shape, q.dtype) if q_out is None else _like("q_out", q_out, q.dtype, q.shape)
+    k_out = _empty(stream, k, k.shape, k.dtype) if k_out is None else _like("k_out", k_out, k.dtype, k.shape)
+    _check((_lib or load()).mmbev_head_norm_rotary(
+        desc, qs, ks, _ptr_of(q_weight), _ptr_of(k_weight), positions.data_ptr(), stride, axes,
+        _vector("steps", steps, torch.int64, pairs), _vector("axis", axis, torch.uint8, pairs),
+        _vector("row_count", row_count, torch.int64, 1), _heads("q_out", q_out), _heads("k_out", k_out),
+        _vector("fault", fault, torch.int32, 1), handle), "mmbev_head_norm_rotary")
+    _written(*given)
+    return q_out, k_out
+
+
+def head_norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, steps, axis, eps: float = 1e-6,
+                              layout: str = "half", row_count=None, dq=None, dk=None, dq_weight=None, dk_weight=None,
+                              weight_grads: bool = True, fault=None, workspace=None, stream=None):
+    """Enqueue mmbev_head_norm_rotary_backward: the gradients of head_norm_rotary's q, k and weights.
+
+    Returns (dq, dk, dq_weight, dk_weight), the last two float32 [dim], None without `weight_grads`.
+    """
+    handle = _issue_on(stream, dq_out, dk_out, q, k, q_weight, k_weight, positions, steps, axis, row_count, dq, dk, dq_weight,
+                       dk_weight, fault, workspace)
+    given = dq, dk, dq_weight, dk_weight
+    torch, lib = _torch, _lib or load()
+    ins = [_heads(name, t) for name, t in (("dq_out", dq_out), ("dk_out", dk_out), ("q", q), ("k", k))]
+    pairs = steps.numel()
+    desc = _head_norm_of(q, k, q_weight, k_weight, pairs, eps, layout)
+    stride, axes = _columns(positions, desc.rows)
+    _like("dq_out", dq_out, q.dtype, q.shape)
+    _like("dk_out", dk_out, q.dtype, k.shape)
+    dq = _empty(stream, q, q.shape, q.dtype) if dq is None else _like("dq", dq, q.dtype, q.shape)
+    dk = _empty(stream, k, k.shape, k.dtype) if dk is None else _like("dk", dk, k.dtype, k.shape)
+    if weight_grads:
+        dq_weight = _empty(stream, q, q.shape[2:], torch.float32) if dq_weight is None else dq_weight
+        dk_weight = _empty(stream, q, q.shape[2:], torch.float32) if dk_weight is None else dk_weight
+        if workspace is None:
+            workspace = _empty(stream, q, (int(lib.mmbev_head_norm_rotary_backward_workspace_bytes(desc)),), torch.uint8)
+    else:
+        workspace = dq_weight = dk_weight = None
+    _check(lib.mmbev_head_norm_rotary_backward(
+        desc, *ins, _ptr_of(q_weight), _ptr_of(k_weight), positions.data_ptr(), stride, axes,
+        _vector("steps", steps, torch.int64, pairs), _vector("axis", axis, torch.uint8, pairs),
+        _vector("row_count", row_count, torch.int64, 1), _heads("dq", dq), _heads("dk", dk),
+        _vector("dq_weight", dq_weight, torch.float32, desc.dim), _vector("dk_weight", dk_weight, torch.float32, desc.dim),
+        _vector("fault", fault, torch.int32, 1), _ptr_of(workspace), 0 if workspace is None else workspace.nbytes, handle),
+        "mmbev_head_norm_rotary_backward")
+    _written(*given)
+    return dq, dk, dq_weight, dk_weight
 
 
 def _attention_of(q, k, v, num_sequences, scale, max_length) -> mmbev_attention_t:
