@@ -475,10 +475,12 @@ mmbev_status_t mmbev_voxel_clusters(const int32_t* coords, const int32_t* counts
 
 /*
  * What a learned VoxelFeatureEncoder (Alg. 1) runs over the voxel rows: layer
- * norm, rotary positions taken from the voxel coordinates, and linear
+ * norm, rotary positions taken from the voxel coordinates, norms of queries
+ * and keys for each head with those positions in the same pass, linear
  * attention with a decay per head, which mixes a frame's rows in key order in
- * time linear in their number.  Each has its forward and backward pass;
- * attention also has the recurrent form for single rows.
+ * time linear in their number, and the gated delta rule, which does so with a
+ * decay and a rate of writing per row.  Each has its forward and backward
+ * pass; the last two also have the recurrent form for single rows.
  *
  * Rows and counts: arrays hold `rows` rows (a capacity, as num_frames *
  * max_voxels of the voxelisation), and how many of them are in use may be
@@ -493,8 +495,8 @@ mmbev_status_t mmbev_voxel_clusters(const int32_t* coords, const int32_t* counts
  * loads and the stores is held in 32 bits (a product on the matrix cores takes
  * operands of the element type), and results are rounded once, to nearest
  * even.  Any alignment of the element type and any stride below 2^40 elements
- * are taken (linear attention, but not its step: row strides below 2^31, else
- * MMBEV_ERR_UNSUPPORTED).
+ * are taken (linear attention and the gated delta rule, but not their steps:
+ * row strides below 2^31, else MMBEV_ERR_UNSUPPORTED).
  * Arrays that a call writes share no element with its other arrays, except
  * where it says so; they may interleave in rows of one stride.
  *
@@ -733,6 +735,64 @@ mmbev_status_t mmbev_linear_attention_step(const mmbev_attention_t* attention, m
                                            mmbev_heads_t v, const float* log_decay, const int32_t* slots,
                                            int64_t num_slots, float* state, mmbev_heads_t out, int32_t* fault,
                                            void* stream);
+
+/* Workspace of a forward (backward = 0) or backward call; 0 where the sizes
+ * are invalid or unsupported, at least 256 otherwise.  A backward call's holds
+ * two states for every 32 rows and two fp32 rows of values for every row. */
+size_t mmbev_gated_delta_workspace_bytes(const mmbev_attention_t* attention, int32_t backward);
+
+/*
+ * The gated delta rule: linear attention whose rows have a decay and a rate of
+ * writing each, and write what the state does not hold for their key yet.
+ * Sequence b is rows [offsets[b], offsets[b+1]); within it, for every head h,
+ * with a_t = exp(log_decay[t][h]):
+ *   S = a_t * S_{t-1};  e_t = v_t - k_t S;  S_t = S + beta[t][h] * k_t^T e_t   [key_dim][value_dim], fp32
+ *   out_t = scale * q_t S_t
+ * S_{-1} is initial_state[b][h] (NULL: zeros); final_state[b][h] (may be
+ * NULL) receives the state after the last row (the initial one for an empty
+ * sequence).  The two must not overlap.
+ * log_decay  fp32 rows of `heads` elements, at most 0, -inf included (a
+ *            larger value counts as 0; what lies under -104 counts as -104,
+ *            whose decay leaves nothing in fp32)
+ * beta       fp32 rows of `heads` elements; with keys of length 1 and beta in
+ *            0..2 no state grows.  Longer keys (beta * |k|^2 > 2) may grow
+ *            without bound, as the rule itself does.
+ * A sequence with a NaN or infinity in a row, a gate or its initial state has
+ * unspecified results; other sequences and heads do not see it.
+ * States, e, and everything between a row and them are as exact as fp32; for
+ * 16-bit types what enters only `out` takes part in 16 bits or more.
+ * max_length only sizes the launches: longer sequences are computed too.
+ * out must not overlap an input.
+ */
+mmbev_status_t mmbev_gated_delta(const mmbev_attention_t* attention, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,
+                                 mmbev_rows_t log_decay, mmbev_rows_t beta, const int64_t* offsets,
+                                 const float* initial_state, mmbev_heads_t out, float* final_state, int32_t* fault,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients.  dfinal_state (may be NULL) is the gradient of final_state;
+ * dinitial_state (may be NULL) receives that of initial_state.  dq is like q,
+ * dk and dv like k and v (the sum over the heads that share them, taken in
+ * fp32), dlog_decay and dbeta fp32 rows of `heads` elements (0 where a
+ * log_decay is over 0).  Written arrays must not overlap an input or each
+ * other.  (rows / 32 + num_sequences) * kv_heads <= 2^23, else
+ * MMBEV_ERR_UNSUPPORTED.
+ */
+mmbev_status_t mmbev_gated_delta_backward(const mmbev_attention_t* attention, mmbev_heads_t dout, mmbev_heads_t q,
+                                          mmbev_heads_t k, mmbev_heads_t v, mmbev_rows_t log_decay, mmbev_rows_t beta,
+                                          const int64_t* offsets, const float* initial_state,
+                                          const float* dfinal_state, mmbev_heads_t dq, mmbev_heads_t dk,
+                                          mmbev_heads_t dv, mmbev_rows_t dlog_decay, mmbev_rows_t dbeta,
+                                          float* dinitial_state, int32_t* fault, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/*
+ * One row for each of many streams, as mmbev_linear_attention_step: row r
+ * updates state[slots[r]] in place by the rule above and reads it.
+ */
+mmbev_status_t mmbev_gated_delta_step(const mmbev_attention_t* attention, mmbev_heads_t q, mmbev_heads_t k,
+                                      mmbev_heads_t v, mmbev_rows_t log_decay, mmbev_rows_t beta, const int32_t* slots,
+                                      int64_t num_slots, float* state, mmbev_heads_t out, int32_t* fault, void* stream);
 
 #ifdef __cplusplus
 }

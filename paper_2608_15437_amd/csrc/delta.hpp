@@ -1,0 +1,1139 @@
+// The gated delta rule: the chunked kernels (one translation unit a type
+// includes this).
+//
+// A row first decays the state, then writes what its key does not hold yet:
+//   S' = a S,  e = v - k S',  S = S' + k^T (beta e),  out = scale q S.
+// In a chunk of 32 rows with G the inclusive sum of log a and
+//   X_ij = e^(G_i - G_j) k_i . k_j for j < i,  P_ij = scale e^(G_i - G_j) q_i . k_j for j <= i,
+// the rows' e solve (1 + X beta) E = R, R = V - e^G K S; with U = beta E
+//   out = scale e^G Q S + P U,  S_after = e^(G_end) S + K^T (e^(G_end - G) U).
+// The system is solved in two blocks of 16 rows, whose own inverses 1 + N beta
+// (N strictly lower: N = -X - N beta X, column by column) are found once a
+// chunk:
+//   E_0 = R_0 + N_00 beta R_0,  R_1' = R_1 - X_10 beta E_0,  E_1 = R_1' + N_11 beta R_1'.
+// Backwards, with D the gradient of the state after the chunk:
+//   W = e^(G_end - G) K D + P^T dout,  Z = (1 + X^T beta)^-1 W (the same blocks, transposed),  dV = beta Z,
+//   D_before = e^(G_end) D + (scale e^G Q)^T dout - (e^G K)^T beta Z.
+//
+// All that a row of the state's columns needs of another is in K, Q, N and P,
+// so a wave walks 16 columns (TV times 16) alone: its state stays in registers
+// from chunk to chunk, and every product's result is the next one's operand
+// where it lies.  What the rows do to each other (N and P) is worked out once a
+// chunk by the workgroup's four waves, through LDS.
+//
+// Precision: the state and the gradients of the gates are fp32 and go through
+// thousands of chunks, so every product is as exact as fp32's: an operand is
+// up to three parts of bf16, whose products of 2^-16 and more are summed (a
+// bf16 row is one part, an fp16 row two, an fp32 value three; bf16 has fp32's
+// exponents, so nothing is scaled).  An fp32 product this way is six products
+// of bf16, 2.7 times as fast as the fp32 ones of the matrix cores.  What only
+// enters a 16-bit result takes two parts, 16 bits.
+#pragma once
+
+#include "common.hpp"
+#include "sequence_parts.hpp"
+
+namespace mmbev {
+namespace {
+
+constexpr int kDeltaThreads = 256;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 b16x4 __attribute__((ext_vector_type(4)));
+
+// Parts of bf16 that a row's element is, and those that enter a result.
+template <typename T>
+constexpr int kPlanes = sizeof(T) == 4 ? 3 : __is_same(T, f16) ? 2 : 1;
+template <typename T>
+constexpr int kOutParts = sizeof(T) == 4 ? 3 : 2;
+
+struct Lane {
+  int w, g, n;  // wave; lane / 16; lane % 16
+};
+__device__ __forceinline__ Lane lane_of() {
+  return {__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), (int)(threadIdx.x & 63) >> 4, (int)threadIdx.x & 15};
+}
+
+// ------------------------------------------------------ products
+
+// Eight elements a lane of a 32-deep product's operand, in N parts.  Lane l
+// holds row (or column) l % 16; with g = l / 16 its elements are 8g .. 8g+7 of
+// the depth or, `split`, 4g .. 4g+3 and 16+4g .. 16+4g+3: two results of 16 x 16
+// (lane l of a result has column l % 16, rows 4g .. 4g+3) are such an operand.
+template <int N>
+struct Parts {
+  b16x8 p[N];
+};
+
+// The sum of the products of two operands' parts, down to those of 2^-8(LEVEL-1).
+template <int LEVEL, int NA, int NB>
+__device__ __forceinline__ f32x4 mma(const Parts<NA>& a, const Parts<NB>& b, f32x4 c) {
+#pragma unroll
+  for (int s = LEVEL - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        if (i + j == s) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c, 0, 0, 0);
+  return c;
+}
+
+template <int N>
+__device__ __forceinline__ Parts<N> split(const float (&x)[8]) {
+  Parts<N> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float left = x[e];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      r.p[i][e] = (bf16)left;
+      left -= (float)r.p[i][e];
+    }
+  }
+  return r;
+}
+
+template <int N>
+__device__ __forceinline__ Parts<N> split(f32x4 x, f32x4 y) {
+  const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  return split<N>(z);
+}
+
+// Four values of an operand, in N parts N arrays of LDS apart.
+template <int N>
+__device__ __forceinline__ void put4(bf16* s, int plane, f32x4 x) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    b16x4 p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[e] = (bf16)x[e];
+      x[e] -= (float)p[e];
+    }
+    __builtin_memcpy(__builtin_assume_aligned(s + i * plane, 8), &p, 8);
+  }
+}
+
+// Operands out of LDS, rows of `stride` elements, parts `plane` apart.
+// A row of memory: row row0 + n, elements c0 + 8g ..
+template <int N>
+__device__ __forceinline__ Parts<N> rows_of(const bf16* s, int plane, int stride, int row0, int c0, const Lane& l) {
+  Parts<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    __builtin_memcpy(&r.p[i], __builtin_assume_aligned(s + i * plane + (row0 + l.n) * stride + c0 + 8 * l.g, 16), 16);
+  return r;
+}
+
+// The same split: elements 4g .. and 16 + 4g ..
+template <int N>
+__device__ __forceinline__ Parts<N> rows_split(const bf16* s, int plane, int stride, int row0, const Lane& l) {
+  Parts<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bf16* p = s + i * plane + (row0 + l.n) * stride + 4 * l.g;
+    b16x4 x, y;
+    __builtin_memcpy(&x, __builtin_assume_aligned(p, 8), 8);
+    __builtin_memcpy(&y, __builtin_assume_aligned(p + 16, 8), 8);
+    r.p[i] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  return r;
+}
+
+// A transposed read: lane n of 16 names 4 neighbouring elements of row n / 4 and gets, of the four rows, element n % 4 of
+// those that lane n / 4 of each row names.
+__device__ __forceinline__ b16x4 read_columns(const bf16* p) {
+  using P = __attribute__((address_space(3))) s16x4*;
+  return __builtin_bit_cast(b16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p)));
+}
+
+// Down columns, split, the 32 rows of a chunk: lane n has column c0 + n or, of a pair of 16-column tiles whose columns
+// are dealt out in fours (STEP 8; the second one's c0 is 4 more), column c0 + 8 (n / 4) + n % 4.
+template <int N, int STEP = 4>
+__device__ __forceinline__ Parts<N> columns_of(const bf16* s, int plane, int stride, int c0, const Lane& l) {
+  Parts<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bf16* p = s + i * plane + (4 * l.g + (l.n >> 2)) * stride + c0 + (l.n & 3) * STEP;
+    r.p[i] = __builtin_shufflevector(read_columns(p), read_columns(p + 16 * stride), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  return r;
+}
+
+// ---- blocks of 16 x 16 in three parts: 16 deep, so a product's 32 take two of the parts' products at once
+
+constexpr int kBlockStride = 20;  // rows of eight-byte steps over all banks
+constexpr int kBlock = 16 * kBlockStride;
+
+struct Block {
+  b16x8 high, ends;  // first and second part; first and third
+};
+
+template <bool TRANSPOSED>
+__device__ __forceinline__ Block block_of(const bf16* s, const Lane& l) {
+  b16x4 p[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if constexpr (TRANSPOSED)
+      p[i] = read_columns(s + i * kBlock + (4 * l.g + (l.n >> 2)) * kBlockStride + (l.n & 3) * 4);
+    else
+      __builtin_memcpy(&p[i], __builtin_assume_aligned(s + i * kBlock + l.n * kBlockStride + 4 * l.g, 8), 8);
+  }
+  return {__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(p[0], p[2], 0, 1, 2, 3, 4, 5, 6, 7)};
+}
+
+// c + block * x
+__device__ __forceinline__ f32x4 mma_block(const Block& a, f32x4 x, f32x4 c) {
+  b16x4 p[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[i][e] = (bf16)x[e];
+      x[e] -= (float)p[i][e];
+    }
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(p[2], p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(p[1], p[1], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(p[0], p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+}
+
+// ------------------------------------------------------ gates
+
+// e^(hi + lo), lo small against hi or both small: the sum's last bits stay in the power.
+__device__ __forceinline__ float exp_of(float hi, float lo) {
+  const float x = hi + lo, rest = lo - (x - hi);
+  const float t = x * 1.44269504088896341f, p = __builtin_amdgcn_exp2f(t);
+  const float more = __builtin_fmaf(x, 1.44269504088896341f, -t) + (x * 1.92596299e-8f + rest * 1.44269504f);
+  return __builtin_fmaf(p, more * 0.693147181f, p);
+}
+
+// A chunk's gates in LDS.  The sums of the log decays are held in two parts,
+// multiples of 2^-10 (whose sums are exact) and what is left over, so that the
+// decay between two rows has its last bits behind a decay of any size too.
+struct Gates {
+  float hi[kDeltaRows], lo[kDeltaRows];      // inclusive sums
+  float beta[kDeltaRows];
+  float fade[kDeltaRows], left[kDeltaRows];  // the decay from before the chunk to a row, and from a row to the chunk's end
+  float whole;
+};
+
+// Inclusive sums over the lanes of each half wave.
+__device__ __forceinline__ float half_wave_sums(float x) {
+  auto moved = [](float v, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl.value, 0xf, 0xf, false));
+  };
+  x += moved(x, std::integral_constant<int, 0x111>{});  // row_shr:1, 2, 4, 8
+  x += moved(x, std::integral_constant<int, 0x112>{});
+  x += moved(x, std::integral_constant<int, 0x114>{});
+  x += moved(x, std::integral_constant<int, 0x118>{});
+  // row_bcast:15 into the second and fourth sixteen lanes
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x142, 0xa, 0xf, false));
+}
+
+__device__ __forceinline__ float last_of_half(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), kDeltaRows - 1));
+}
+
+// A decay of more than e^-104 leaves nothing in fp32; a log decay over 0 counts as 0, NaN stays.
+__device__ __forceinline__ float clamp_gate(float g) { return g > 0.0f ? 0.0f : g < -104.0f ? -104.0f : g; }
+
+// By one wave: lane r < 32 has row r's gates (0 past the rows).
+__device__ __forceinline__ void put_gates(Gates& s, float g, float beta) {
+  const int r = threadIdx.x & 63;
+  g = clamp_gate(g);
+  const float step = __builtin_rintf(g * 1024.0f) * (1.0f / 1024.0f);
+  const float hi = half_wave_sums(step), lo = half_wave_sums(g - step);
+  const float end_hi = last_of_half(hi), end_lo = last_of_half(lo);
+  const float fade = exp_of(hi, lo);
+  if (r < kDeltaRows) {
+    s.hi[r] = hi;
+    s.lo[r] = lo;
+    s.beta[r] = beta;
+    s.fade[r] = fade;
+    s.left[r] = exp_of(end_hi - hi, end_lo - lo);
+    if (r == kDeltaRows - 1) s.whole = fade;
+  }
+}
+
+__device__ __forceinline__ f32x4 four(const float* s) {
+  f32x4 r;
+  __builtin_memcpy(&r, __builtin_assume_aligned(s, 16), 16);
+  return r;
+}
+
+// ------------------------------------------------------ chunks
+
+template <typename T>
+constexpr int kRowPad = 16 / (int)sizeof(T);
+constexpr int kPlanePad = 8;
+
+// Eight elements of each of a chunk's 32 rows, W to a row, shared out among the threads.
+template <int W>
+constexpr int kPacks = W >= 64 ? kDeltaRows * W / 8 / kDeltaThreads : 1;
+
+// Every load is of an element that is there; what is past the rows or the row's end is zeroed on the way into LDS.
+template <typename T, int W>
+__device__ __forceinline__ void fetch_chunk(Pack<T, 8> (&r)[kPacks<W>], const T* p, int32_t stride, int dim, int32_t s0, int32_t hi) {
+#pragma unroll
+  for (int i = 0; i < kPacks<W>; ++i) {
+    const int idx = threadIdx.x + i * kDeltaThreads, c = idx % (W / 8) * 8;
+    const T* row = p + (int64_t)min(s0 + idx / (W / 8), hi - 1) * stride;
+    if (dim % 8 == 0)
+      r[i] = load_pack<T, 8>(row + (c < dim ? c : 0));
+    else
+      r[i] = load_some<T, 8>(row + c, dim - c);
+  }
+}
+
+// f(row, column, pack), zeros where there is nothing.
+template <typename T, int W, typename F>
+__device__ __forceinline__ void each_pack(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n, F&& f) {
+#pragma unroll
+  for (int i = 0; i < kPacks<W>; ++i) {
+    const int idx = threadIdx.x + i * kDeltaThreads, row = idx / (W / 8), c = idx % (W / 8) * 8;
+    if (W < 64 && row >= kDeltaRows) continue;
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * 2)));
+    words x = __builtin_bit_cast(words, r[i]);
+    const bool there = row < n && c < dim;
+#pragma unroll
+    for (int e = 0; e < (int)sizeof(T) * 2; ++e) x[e] = there ? x[e] : 0u;
+    f(row, c, __builtin_bit_cast(Pack<T, 8>, x));
+  }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void put_planes(bf16* s, int plane, const Pack<T, 8>& x) {
+  if constexpr (__is_same(T, bf16)) {
+    __builtin_memcpy(__builtin_assume_aligned(s, 16), &x, 16);
+  } else {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (float)x.v[e];
+    const Parts<N> p = split<N>(f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) __builtin_memcpy(__builtin_assume_aligned(s + i * plane, 16), &p.p[i], 16);
+  }
+}
+
+// A chunk's rows in LDS as operands: parts of W (and a step of 16 bytes) columns.
+template <typename T, int W>
+struct Planes {
+  static constexpr int stride = W + kPlanePad, plane = kDeltaRows * stride;
+  __attribute__((aligned(16))) bf16 v[kPlanes<T> * plane];
+
+  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n) {
+    each_pack<T, W>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { put_planes<kPlanes<T>, T>(v + row * stride + c, plane, x); });
+  }
+  __device__ __forceinline__ Parts<kPlanes<T>> rows(int row0, int c0, const Lane& l) const {
+    return rows_of<kPlanes<T>>(v, plane, stride, row0, c0, l);
+  }
+  template <int STEP = 4>
+  __device__ __forceinline__ Parts<kPlanes<T>> columns(int c0, const Lane& l) const {
+    return columns_of<kPlanes<T>, STEP>(v, plane, stride, c0, l);
+  }
+  // elements c .. c+3 of a row
+  __device__ __forceinline__ f32x4 at(int row, int c) const {
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kPlanes<T>; ++i) {
+      b16x4 p;
+      __builtin_memcpy(&p, __builtin_assume_aligned(v + i * plane + row * stride + c, 8), 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += (float)p[e];
+    }
+    return x;
+  }
+};
+
+// Values as they are.
+template <typename T, int W>
+struct Values {
+  static constexpr int stride = W + kRowPad<T>;
+  __attribute__((aligned(16))) T v[kDeltaRows * stride];
+
+  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n) {
+    each_pack<T, W>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { __builtin_memcpy(__builtin_assume_aligned(v + row * stride + c, 16), &x, sizeof(x)); });
+  }
+  // column c0 + n of rows row0 + 4g ..
+  __device__ __forceinline__ f32x4 down(int row0, int c0, const Lane& l) const {
+    f32x4 x;
+    if constexpr (sizeof(T) == 2) {
+      typedef T t4 __attribute__((ext_vector_type(4)));
+      const bf16* p = reinterpret_cast<const bf16*>(v) + (row0 + 4 * l.g + (l.n >> 2)) * stride + c0 + (l.n & 3) * 4;
+      const t4 t = __builtin_bit_cast(t4, read_columns(p));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (float)t[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = v[(row0 + 4 * l.g + e) * stride + c0 + l.n];
+    }
+    return x;
+  }
+};
+
+// Lane group G's value, known to all four of the same lane % 16.
+template <int G>
+__device__ __forceinline__ float from_group(float x) {
+  const unsigned i = __builtin_bit_cast(unsigned, x);
+  const auto p = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+  const unsigned j = p[G >> 1];
+  const auto q = __builtin_amdgcn_permlane16_swap(j, j, false, false);
+  return __builtin_bit_cast(float, (unsigned)q[G & 1]);
+}
+
+// LDS order between lanes of one wave.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// What the rows of a chunk do to each other.
+constexpr int kPairStride = kDeltaRows + kPlanePad, kPairPlane = kDeltaRows * kPairStride;
+
+template <int PARTS>
+struct Pairs {
+  __attribute__((aligned(16))) bf16 n[3][3 * kBlock];  // N of the first and last 16 rows, X of the last with the first
+  __attribute__((aligned(16))) bf16 p[PARTS ? PARTS * kPairPlane : 8];
+  __attribute__((aligned(16))) float scratch[2][kBlock];
+};
+
+// times e^(G_i - G_j) where j < i (j <= i with the diagonal), else 0; lane n row i, elements j0 + 4g .. of it.
+__device__ __forceinline__ f32x4 decayed(f32x4 x, const Gates& s, int i0, int j0, bool diagonal, float times, const Lane& l) {
+  const int i = i0 + l.n;
+  const float hi = s.hi[i], lo = s.lo[i];
+  const f32x4 jh = four(s.hi + j0 + 4 * l.g), jl = four(s.lo + j0 + 4 * l.g);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int j = j0 + 4 * l.g + r;
+    const float d = exp_of(hi - jh[r], lo - jl[r]) * times;
+    x[r] = j < i || (diagonal && j == i) ? x[r] * d : 0.0f;
+  }
+  return x;
+}
+
+// a_i . b_j over DK columns: lane n row i0 + n, elements j0 + 4g ..
+template <typename T, int DK>
+__device__ __forceinline__ f32x4 dots(const Planes<T, DK>& a, int i0, const Planes<T, DK>& b, int j0, const Lane& l) {
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int s = 0; s < DK / 32; ++s) x = mma<3>(b.rows(j0, 32 * s, l), a.rows(i0, 32 * s, l), x);
+  return x;
+}
+
+// N of 16 rows: N = -X - N beta X, its columns from the last one on.
+__device__ __forceinline__ void put_inverse(bf16* to, float* scratch, f32x4 x, const Gates& s, int i0, const Lane& l) {
+  f32x4 bx;
+  const float beta = s.beta[i0 + l.n];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) bx[r] = beta * x[r];
+  __builtin_memcpy(__builtin_assume_aligned(scratch + l.n * kBlockStride + 4 * l.g, 16), &bx, 16);
+  wave_fence();
+  f32x4 acc = -x;
+  auto column = [&](auto which) {
+    constexpr int J = which.value;
+    const float nj = from_group<J / 4>(acc[J % 4]);
+    const f32x4 row = four(scratch + J * kBlockStride + 4 * l.g);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(-nj, row[r], acc[r]);
+  };
+  column(std::integral_constant<int, 15>{});
+  column(std::integral_constant<int, 14>{});
+  column(std::integral_constant<int, 13>{});
+  column(std::integral_constant<int, 12>{});
+  column(std::integral_constant<int, 11>{});
+  column(std::integral_constant<int, 10>{});
+  column(std::integral_constant<int, 9>{});
+  column(std::integral_constant<int, 8>{});
+  column(std::integral_constant<int, 7>{});
+  column(std::integral_constant<int, 6>{});
+  column(std::integral_constant<int, 5>{});
+  column(std::integral_constant<int, 4>{});
+  column(std::integral_constant<int, 3>{});
+  column(std::integral_constant<int, 2>{});
+  column(std::integral_constant<int, 1>{});
+  put4<3>(to + l.n * kBlockStride + 4 * l.g, kBlock, acc);
+}
+
+// The four waves' shares: two the inverses, the third the last rows with the first, the fourth the rest.  (PARTS 0: no P.)
+template <typename T, int DK, int PARTS>
+__device__ __forceinline__ void put_pairs(Pairs<PARTS>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
+                                          const Lane& l) {
+  auto put_p = [&](int i0, int j0) {
+    const f32x4 x = decayed(dots<T, DK>(*q, i0, k, j0, l), s, i0, j0, true, scale, l);
+    put4<PARTS>(to.p + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, x);
+  };
+  if (l.w < 2) {
+    const int i0 = 16 * l.w;
+    put_inverse(to.n[l.w], to.scratch[l.w], decayed(dots<T, DK>(k, i0, k, i0, l), s, i0, i0, false, 1.0f, l), s, i0, l);
+  } else if (l.w == 2) {
+    put4<3>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed(dots<T, DK>(k, 16, k, 0, l), s, 16, 0, false, 1.0f, l));
+    if constexpr (PARTS) put_p(16, 0);
+  } else if constexpr (PARTS != 0) {
+    put_p(0, 0);
+    put_p(16, 16);
+  }
+}
+
+// ------------------------------------------------------ the state of a wave
+//
+// Columns col0 + 16 tv + n; of a pair of 16-row tiles 2s and 2s + 1 a lane has rows 32 s + 8g .. 8g+7, so a row of K in
+// LDS, read 16 bytes a lane, is the matching operand.
+
+template <int DK, int TV>
+using State = f32x4[DK / 16][TV];
+
+__device__ __forceinline__ int state_row(int tile, int r, const Lane& l) { return 32 * (tile / 2) + 8 * l.g + 4 * (tile % 2) + r; }
+
+template <int DK, int TV>
+__device__ __forceinline__ void load_state(State<DK, TV>& st, const float* from, int kd, int vd, int col0, const Lane& l) {
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = state_row(t, r, l), col = col0 + 16 * v + l.n;
+        st[t][v][r] = from && row < kd && col < vd ? from[row * vd + col] : 0.0f;
+      }
+}
+
+template <int DK, int TV>
+__device__ __forceinline__ void store_state(float* to, const State<DK, TV>& st, int kd, int vd, int col0, const Lane& l) {
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = state_row(t, r, l), col = col0 + 16 * v + l.n;
+        if (row < kd && col < vd) to[row * vd + col] = st[t][v][r];
+      }
+}
+
+// ------------------------------------------------------ the walks
+
+// Where a chunk's states are kept: a sequence's chunks from its first row / 32 + its number on.
+__device__ __forceinline__ int64_t place_of(int32_t first, int32_t b, int32_t s0) {
+  return (int64_t)(first / kDeltaRows) + (s0 - first) / kDeltaRows + b;
+}
+
+enum DeltaMode {
+  kDeltaStates,      // the states at the ends of the parts that go on, and what those parts do to a state
+  kDeltaOut,         // results
+  kDeltaSave,        // what the gradients need: the state before each chunk, the rows' e
+  kDeltaBackStates,  // the gradients of the states at the parts' starts
+  kDeltaBack         // what the gradients need: that of the state after each chunk, Z
+};
+
+template <typename T, int DK, int TV, int MODE>
+struct DeltaShared {
+  static constexpr bool BACK = MODE >= kDeltaBackStates, QUERIES = MODE == kDeltaOut || BACK;
+  static constexpr int PARTS = MODE == kDeltaOut ? kOutParts<T> : BACK ? 3 : 0;
+  static constexpr int BUFFERS = sizeof(T) == 2 && DK <= 64 && TV == 1 ? 2 : 1;
+  Planes<T, DK> k[BUFFERS];
+  Planes<T, QUERIES ? DK : 8> q[BUFFERS];
+  Values<T, BACK ? 8 : 64 * TV> v[BUFFERS];
+  Planes<T, BACK ? 64 * TV : 8> d[BUFFERS];
+  Values<T, MODE == kDeltaOut ? 64 * TV : 8> out;
+  Gates gates[BUFFERS];
+  Pairs<PARTS> pairs;
+};
+
+template <typename T, int DK, int TV, int MODE>
+__global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV)) void delta_walk_kernel(DeltaArgs a) {
+  using Shared = DeltaShared<T, DK, TV, MODE>;
+  constexpr int NP = kPlanes<T>, OUT = kOutParts<T>, W = 64 * TV, BUFFERS = Shared::BUFFERS;
+  constexpr bool BACK = Shared::BACK, QUERIES = Shared::QUERIES, STATES = MODE == kDeltaStates || MODE == kDeltaBackStates;
+  __shared__ Shared sh;
+  const Lane l = lane_of();
+  int unit = blockIdx.x / a.H;
+  const int h = blockIdx.x - unit * a.H;
+  // columns of the state, or of what a part does to it
+  const bool map = MODE == kDeltaStates && blockIdx.y > 0;
+  const int col0 = (l.w + (map ? 4 * ((int)blockIdx.y - 1) : 0)) * 16 * TV, columns = map ? a.kd : a.vd;
+  const Order o = order_of(a);
+  Part q;
+  const bool found = find_part(q, o, a, unit, STATES);
+  if (MODE == kDeltaStates && h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.cut_kind[unit] = !found ? -1 : q.began ? 1 : 0;
+  if (!found) return;
+  int32_t lo = q.lo, hi = q.hi;
+  bool began = q.began, goes_on = q.goes_on && q.before < a.cuts;
+  int32_t boundary = q.before;  // behind the part
+  if constexpr (MODE == kDeltaBackStates) {
+    // the part behind the boundary
+    lo = q.hi;
+    hi = q.next;
+    began = true;
+    goes_on = q.next < q.end && unit + 1 < a.cuts;
+    boundary = unit + 1;
+  }
+  if (map && !began) return;
+  const int64_t each = (int64_t)a.kd * a.vd;
+  const int hk = h / a.group;
+  const T* pk = static_cast<const T*>(a.k) + hk * a.k_head;
+  const T* pq = QUERIES ? static_cast<const T*>(a.q) + h * a.q_head : nullptr;
+  const T* pv = BACK ? static_cast<const T*>(a.dout) + h * a.d_head : static_cast<const T*>(a.v) + hk * a.v_head;
+  const int32_t v_row = BACK ? a.d_row : a.v_row;
+  const bool own = col0 < columns;
+
+  State<DK, TV> st;
+  {
+    const float* from = nullptr;
+    if constexpr (MODE == kDeltaStates)
+      from = !began && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else if constexpr (MODE == kDeltaBackStates)
+      from = !goes_on && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else if constexpr (MODE == kDeltaBack)
+      from = goes_on ? a.cut_grad + ((int64_t)boundary * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else
+      from = began ? a.cut_state + ((int64_t)(boundary - 1) * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    load_state<DK, TV>(st, map ? nullptr : from, a.kd, columns, col0, l);
+    if (map) {
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+        for (int v = 0; v < TV; ++v)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) st[t][v][r] = state_row(t, r, l) == col0 + 16 * v + l.n ? 1.0f : 0.0f;
+    }
+  }
+
+  if constexpr (Shared::PARTS != 0) {
+    // the first rows have nothing of the last ones
+    for (int i = threadIdx.x; i < Shared::PARTS * 16 * 16; i += kDeltaThreads)
+      sh.pairs.p[i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16] = (bf16)0.0f;
+  }
+
+  Pack<T, 8> rk[kPacks<DK>], rq[kPacks<DK>], rv[kPacks<W>];
+  float rg = 0.0f, rb = 0.0f;
+  auto fetch = [&](int32_t s0) {
+    fetch_chunk<T, DK>(rk, pk, a.k_row, a.kd, s0, hi);
+    if constexpr (QUERIES) fetch_chunk<T, DK>(rq, pq, a.q_row, a.kd, s0, hi);
+    if (!map) fetch_chunk<T, W>(rv, pv, v_row, a.vd, s0, hi);
+    if (l.w == 3) {
+      const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
+      rg = a.log_decay[row * a.g_row + h];
+      rb = a.beta[row * a.b_row + h];
+    }
+  };
+  auto put = [&](int32_t s0, int buffer) {
+    const int n = hi - s0;
+    sh.k[buffer].put(rk, a.kd, n);
+    if constexpr (QUERIES) sh.q[buffer].put(rq, a.kd, n);
+    if constexpr (BACK)
+      sh.d[buffer].put(rv, a.vd, n);
+    else if (!map)
+      sh.v[buffer].put(rv, a.vd, n);
+    if (l.w == 3) {
+      const bool there = (int)(threadIdx.x & 31) < n;
+      put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f);
+    }
+  };
+  auto store_out = [&](int32_t s0) {
+    if constexpr (MODE == kDeltaOut) {
+      T* po = static_cast<T*>(a.out) + h * a.o_head;
+#pragma unroll
+      for (int i = 0; i < kPacks<W>; ++i) {
+        const int idx = threadIdx.x + i * kDeltaThreads, row = idx / (W / 8), c = idx % (W / 8) * 8;
+        if (s0 + row >= hi || c >= a.vd) continue;
+        Pack<T, 8> x;
+        __builtin_memcpy(&x, __builtin_assume_aligned(sh.out.v + row * sh.out.stride + c, 16), sizeof(x));
+        store_some<T, 8>(po + (int64_t)(s0 + row) * a.o_row + c, x, a.vd - c, a.past);
+      }
+    }
+  };
+
+  const int chunks = (hi - lo + kDeltaRows - 1) / kDeltaRows;
+  if (chunks > 0) {
+    fetch(BACK ? lo + (chunks - 1) * kDeltaRows : lo);
+    put(BACK ? lo + (chunks - 1) * kDeltaRows : lo, 0);
+    __syncthreads();
+  }
+  for (int c = 0; c < chunks; ++c) {
+    const int32_t s0 = lo + (BACK ? chunks - 1 - c : c) * kDeltaRows, next = BACK ? s0 - kDeltaRows : s0 + kDeltaRows;
+    const int b = BUFFERS == 2 ? c & 1 : 0;
+    const bool more = c + 1 < chunks;
+    const Gates& gates = sh.gates[b];
+    if (more) fetch(next);
+    put_pairs<T, DK, Shared::PARTS>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b]), gates, a.scale, l);
+
+    // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
+    f32x4 ks[2][TV], qs[2][TV];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < TV; ++v) ks[t][v] = qs[t][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (own) {
+#pragma unroll
+      for (int s = 0; s < DK / 32; ++s) {
+        Parts<3> x[TV];
+#pragma unroll
+        for (int v = 0; v < TV; ++v) x[v] = split<3>(st[2 * s][v], st[2 * s + 1][v]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const Parts<NP> k = sh.k[b].rows(16 * t, 32 * s, l);
+#pragma unroll
+          for (int v = 0; v < TV; ++v) ks[t][v] = mma<3>(k, x[v], ks[t][v]);
+          if constexpr (MODE == kDeltaOut) {
+            const Parts<NP> qr = sh.q[b].rows(16 * t, 32 * s, l);
+#pragma unroll
+            for (int v = 0; v < TV; ++v) qs[t][v] = mma<OUT>(x[v], qr, qs[t][v]);
+          }
+        }
+      }
+      if constexpr (MODE == kDeltaSave || MODE == kDeltaBack) {
+        const int64_t place = place_of(o.bound(q.b), q.b, s0);
+        store_state<DK, TV>((BACK ? a.after : a.before) + (place * a.H + h) * each, st, a.kd, a.vd, col0, l);
+      }
+    }
+    __syncthreads();  // the pairs are there
+    if (own) {
+      const float whole = gates.whole;
+      f32x4 beta[2], fade[2], left[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        beta[t] = four(gates.beta + 16 * t + 4 * l.g);
+        fade[t] = four(gates.fade + 16 * t + 4 * l.g);
+        left[t] = four(gates.left + 16 * t + 4 * l.g);
+      }
+      f32x4 e[2][TV];
+      Parts<NP> dout[TV];
+      {
+        // forwards the first 16 rows first, backwards the last
+        constexpr int F = BACK ? 1 : 0, L = 1 - F;
+        if constexpr (BACK) {
+          // W = what the state's gradient and the results' owe the rows
+          const Parts<3> pt[2] = {columns_of<3>(sh.pairs.p, kPairPlane, kPairStride, 0, l),
+                                  columns_of<3>(sh.pairs.p, kPairPlane, kPairStride, 16, l)};
+#pragma unroll
+          for (int v = 0; v < TV; ++v) {
+            dout[v] = sh.d[b].columns(col0 + 16 * v, l);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) e[t][v] = mma<3>(pt[t], dout[v], ks[t][v] * left[t]);
+          }
+        } else {
+#pragma unroll
+          for (int v = 0; v < TV; ++v)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+              if (!map) x = sh.v[b].down(16 * t, col0 + 16 * v, l);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) e[t][v][r] = __builtin_fmaf(-fade[t][r], ks[t][v][r], x[r]);
+            }
+        }
+        const Block first = block_of<BACK>(sh.pairs.n[F], l), cross = block_of<BACK>(sh.pairs.n[2], l),
+                    last = block_of<BACK>(sh.pairs.n[L], l);
+#pragma unroll
+        for (int v = 0; v < TV; ++v) {
+          e[F][v] = mma_block(first, beta[F] * e[F][v], e[F][v]);
+          e[L][v] = mma_block(cross, -(beta[F] * e[F][v]), e[L][v]);
+          e[L][v] = mma_block(last, beta[L] * e[L][v], e[L][v]);
+        }
+      }
+      if constexpr (MODE == kDeltaSave || MODE == kDeltaBack) {
+        float* to = (BACK ? a.due : a.left_over) + (int64_t)h * a.vd;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int32_t row = s0 + 16 * t + 4 * l.g + r;
+#pragma unroll
+            for (int v = 0; v < TV; ++v) {
+              const int col = col0 + 16 * v + l.n;
+              if (row < hi && col < a.vd) to[(int64_t)row * a.H * a.vd + col] = e[t][v][r];
+            }
+          }
+      }
+      if constexpr (MODE == kDeltaOut) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const Parts<OUT> p = rows_split<OUT>(sh.pairs.p, kPairPlane, kPairStride, 16 * t, l);
+          const float f = gates.fade[16 * t + l.n] * a.scale;
+#pragma unroll
+          for (int v = 0; v < TV; ++v) {
+            const f32x4 x = mma<OUT>(split<OUT>(beta[0] * e[0][v], beta[1] * e[1][v]), p, qs[t][v] * f);
+            Pack<T, 4> y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y.v[r] = (T)x[r];
+            __builtin_memcpy(__builtin_assume_aligned(sh.out.v + (16 * t + l.n) * sh.out.stride + col0 + 16 * v + 4 * l.g, 4 * sizeof(T)), &y,
+                             sizeof(y));
+          }
+        }
+      }
+      // the state after the chunk (backwards: its gradient before it)
+      Parts<3> x[TV], y[TV];
+#pragma unroll
+      for (int v = 0; v < TV; ++v) {
+        if constexpr (BACK) {
+          float f[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            f[i] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) f[i] += (float)dout[v].p[p][i];
+            f[i] *= fade[i / 4][i % 4] * a.scale;
+          }
+          y[v] = split<3>(f);
+          x[v] = split<3>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
+        } else {
+          x[v] = split<3>(left[0] * beta[0] * e[0][v], left[1] * beta[1] * e[1][v]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t) {
+        const int c0 = 32 * (t / 2) + 4 * (t % 2);
+        const Parts<NP> k = sh.k[b].template columns<8>(c0, l);
+#pragma unroll
+        for (int v = 0; v < TV; ++v) st[t][v] = mma<3>(k, x[v], st[t][v] * whole);
+        if constexpr (BACK) {
+          const Parts<NP> qc = sh.q[b].template columns<8>(c0, l);
+#pragma unroll
+          for (int v = 0; v < TV; ++v) st[t][v] = mma<3>(qc, y[v], st[t][v]);
+        }
+      }
+    }
+    if (BUFFERS == 2 && more) put(next, b ^ 1);
+    __syncthreads();  // the results are there, the chunk has been read
+    store_out(s0);
+    if (BUFFERS == 1 && more) {
+      put(next, 0);
+      __syncthreads();
+    }
+  }
+  if (!own) return;
+  if constexpr (STATES) {
+    if (map)
+      store_state<DK, TV>(a.cut_map + ((int64_t)unit * a.H + h) * a.kd * a.kd, st, a.kd, a.kd, col0, l);
+    else
+      store_state<DK, TV>((BACK ? a.cut_grad : a.cut_state) + ((int64_t)unit * a.H + h) * each, st, a.kd, a.vd, col0, l);
+  } else {
+    if ((BACK ? !began : !goes_on) && a.final_state)
+      store_state<DK, TV>(a.final_state + ((int64_t)q.b * a.H + h) * each, st, a.kd, a.vd, col0, l);
+  }
+}
+
+// ------------------------------------------------------ the gradients of a chunk
+//
+// With the state S before it, the gradient D of the one after it, and the
+// rows' E and Z (U = beta E, Y = beta Z):
+//   dQ = scale e^G dout S^T + A K,                   A_ij = scale e^(G_i - G_j) dout_i . u_j, j <= i
+//   dK = [-e^G Y S^T - F K] + [e^(G_end - G) U D^T - F^T K + A^T Q],  F_ij = e^(G_i - G_j) y_i . u_j, j < i
+//   dV = Y,  dbeta = Z . E.
+// A row's G scales what it reads (q and, in the first bracket, k) and divides
+// what it writes (the second bracket), so
+//   dG_i = q_i . dQ_i + k_i . (first - second)_i,  and G_end has <D, S_after>;
+// the gradient of a row's log decay is the sum of dG from it on.  With the term
+// in D kept apart, kd_j = k_j . (e^(G_end - G_j) u_j D^T), that is
+//   sum_{i >= t} (dG_i without it) + e^(G_end) <D, S> + sum_{j < t} kd_j.
+
+template <typename T, int DK, int TV>
+struct DeltaGradShared {
+  Planes<T, DK> k, q;
+  Planes<T, 64 * TV> d;
+  Planes<float, 64 * TV> u, y;
+  __attribute__((aligned(16))) bf16 a[3 * kPairPlane], f[3 * kPairPlane];
+  Gates gates;
+  float own[4][kDeltaRows], end[4][kDeltaRows];  // a wave's part of dG and of kd
+  float both[4];                                 // of <D, S>
+};
+
+// Rows of fp32 in global memory as an operand: row `row`, elements c .. c+7; zeros past the matrix.
+__device__ __forceinline__ void load_eight(float (&x)[8], const float* p, int row, int c, int rows, int columns) {
+  const bool there = row < rows;
+  const float* from = p + (int64_t)(there ? row : 0) * columns;
+  if (columns % 8 == 0) {
+    const Pack<float, 8> t = load_pack<float, 8>(from + (c < columns ? c : 0));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = there && c < columns ? t.v[e] : 0.0f;
+  } else {
+    const Pack<float, 8> t = load_some<float, 8>(from + c, columns - c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = there ? t.v[e] : 0.0f;
+  }
+}
+
+// Sum over the four lane groups of the same lane % 16, known to all.
+__device__ __forceinline__ float groups_sum(float x) {
+  unsigned i = __builtin_bit_cast(unsigned, x);
+  const auto p = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+  x = __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
+  i = __builtin_bit_cast(unsigned, x);
+  const auto q = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+  return __builtin_bit_cast(float, (unsigned)q[0]) + __builtin_bit_cast(float, (unsigned)q[1]);
+}
+
+// The sequence whose chunks lie from `place` back, and whether it has one there: first row / 32 + sequence grows with the
+// sequence, so 64 are looked at at a time.
+__device__ __forceinline__ bool chunk_at(int64_t place, const Order& o, int32_t& b, int32_t& s0, int32_t& hi) {
+  const int lane = threadIdx.x & 63;
+  int32_t first = 0, count = o.B;  // candidates
+  while (count > 1) {
+    const int32_t step = (count + 63) / 64, k = first + lane * step;
+    const bool upto = k < first + count && (int64_t)(o.bound(min(k, o.B - 1)) / kDeltaRows) + k <= place;
+    const uint64_t m = __ballot(upto);
+    const int32_t at = m ? 63 - __builtin_clzll(m) : 0;
+    count = min(step, count - at * step);
+    first += at * step;
+  }
+  b = __builtin_amdgcn_readfirstlane(first);
+  const int32_t lo = o.bound(b);
+  hi = o.bound(b + 1);
+  const int64_t begin = lo + (place - lo / kDeltaRows - b) * kDeltaRows;
+  s0 = (int32_t)begin;
+  return begin >= lo && begin < hi;
+}
+
+template <typename T, int DK, int TV>
+__global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
+  constexpr int NP = kPlanes<T>, W = 64 * TV, TD = DK >= 64 ? DK / 64 : 1, PER = W / 8;
+  __shared__ DeltaGradShared<T, DK, TV> sh;
+  const Lane l = lane_of();
+  const int KV = a.H / a.group, hk = blockIdx.x % KV;
+  const int64_t place = blockIdx.x / KV;
+  const Order o = order_of(a);
+  int32_t b, s0, hi;
+  if (!chunk_at(place, o, b, s0, hi)) return;
+  const int n = min(hi - s0, kDeltaRows);
+  const int64_t each = (int64_t)a.kd * a.vd;
+  const bool own = 16 * TD * l.w < DK;
+  for (int i = threadIdx.x; i < 3 * 16 * 16; i += kDeltaThreads) {
+    const int at = i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16;
+    sh.a[at] = sh.f[at] = (bf16)0.0f;
+  }
+  Pack<T, 8> rk[kPacks<DK>];
+  fetch_chunk<T, DK>(rk, static_cast<const T*>(a.k) + hk * a.k_head, a.k_row, a.kd, s0, hi);
+  float dv[kPacks<W>][8];
+  f32x4 dk[2][TD];
+#pragma unroll
+  for (int i = 0; i < kPacks<W>; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dv[i][e] = 0.0f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int d = 0; d < TD; ++d) dk[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  for (int j = 0; j < a.group; ++j) {
+    const int h = hk * a.group + j;
+    {
+      Pack<T, 8> rq[kPacks<DK>], rd[kPacks<W>];
+      Pack<float, 8> re[kPacks<W>], rz[kPacks<W>];
+      fetch_chunk<T, DK>(rq, static_cast<const T*>(a.q) + h * a.q_head, a.q_row, a.kd, s0, hi);
+      fetch_chunk<T, W>(rd, static_cast<const T*>(a.dout) + h * a.d_head, a.d_row, a.vd, s0, hi);
+      fetch_chunk<float, W>(re, a.left_over + h * a.vd, a.H * a.vd, a.vd, s0, hi);
+      fetch_chunk<float, W>(rz, a.due + h * a.vd, a.H * a.vd, a.vd, s0, hi);
+      float g = 0.0f, beta = 0.0f;
+      if (l.w == 3 && (int)(threadIdx.x & 31) < n) {
+        const int64_t row = s0 + (int)(threadIdx.x & 31);
+        g = a.log_decay[row * a.g_row + h];
+        beta = a.beta[row * a.b_row + h];
+      }
+      float rb[kPacks<W>];
+#pragma unroll
+      for (int i = 0; i < kPacks<W>; ++i)
+        rb[i] = a.beta[(int64_t)min(s0 + (int)(threadIdx.x + i * kDeltaThreads) / PER, hi - 1) * a.b_row + h];
+      if (j) __syncthreads();  // the head before has been read
+      if (j == 0) sh.k.put(rk, a.kd, n);
+      sh.q.put(rq, a.kd, n);
+      sh.d.put(rd, a.vd, n);
+      if (l.w == 3) put_gates(sh.gates, g, beta);
+      int i = 0;
+      each_pack<float, W>(re, a.vd, n, [&](int row, int c, Pack<float, 8> x) {
+        float dot = 0.0f;
+        Pack<float, 8> y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float z = row < n && c < a.vd ? rz[i].v[e] : 0.0f;
+          dot = __builtin_fmaf(z, x.v[e], dot);
+          y.v[e] = rb[i] * z;
+          x.v[e] = rb[i] * x.v[e];
+          dv[i][e] += y.v[e];
+        }
+        put_planes<3, float>(sh.u.v + row * sh.u.stride + c, sh.u.plane, x);
+        put_planes<3, float>(sh.y.v + row * sh.y.stride + c, sh.y.plane, y);
+        dot = group_sum<PER>(dot);
+        if (c == 0 && row < n) a.dbeta[(int64_t)(s0 + row) * a.db_row + h] = dot;
+        ++i;
+      });
+    }
+    __syncthreads();
+    const Gates& gates = sh.gates;
+    // A and F: lane n row i, elements j0 + 4g ..
+    auto pairs = [&](int i0, int j0, bool results) {
+      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < W / 32; ++s) {
+        const Parts<3> u = sh.u.rows(j0, 32 * s, l);
+        x = results ? mma<3>(u, sh.d.rows(i0, 32 * s, l), x) : mma<3>(u, sh.y.rows(i0, 32 * s, l), x);
+      }
+      x = decayed(x, gates, i0, j0, results, results ? a.scale : 1.0f, l);
+      put4<3>((results ? sh.a : sh.f) + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, x);
+    };
+    if (l.w < 2) {
+      pairs(16 * l.w, 16 * l.w, true);
+      pairs(16 * l.w, 16 * l.w, false);
+    } else {
+      pairs(16, 0, l.w == 2);
+    }
+    // what comes through the states: lane n row n, elements of dk 4g ..
+    f32x4 read_q[2][TD], read_k[2][TD], written[2][TD];
+    float both = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < TD; ++d) read_q[t][d] = read_k[t][d] = written[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (own) {
+      const float *before = a.before + (place * a.H + h) * each, *after = a.after + (place * a.H + h) * each;
+#pragma unroll
+      for (int s = 0; s < W / 32; ++s) {
+        const Parts<NP> d0 = sh.d.rows(0, 32 * s, l), d1 = sh.d.rows(16, 32 * s, l);
+        const Parts<3> y0 = sh.y.rows(0, 32 * s, l), y1 = sh.y.rows(16, 32 * s, l);
+        const Parts<3> u0 = sh.u.rows(0, 32 * s, l), u1 = sh.u.rows(16, 32 * s, l);
+#pragma unroll
+        for (int d = 0; d < TD; ++d) {
+          const int row = 16 * (l.w * TD + d) + l.n;
+          float x[8], z[8];
+          load_eight(x, before, row, 32 * s + 8 * l.g, a.kd, a.vd);
+          load_eight(z, after, row, 32 * s + 8 * l.g, a.kd, a.vd);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) both = __builtin_fmaf(x[e], z[e], both);
+          const Parts<3> sp = split<3>(x), gp = split<3>(z);
+          read_q[0][d] = mma<3>(sp, d0, read_q[0][d]);
+          read_q[1][d] = mma<3>(sp, d1, read_q[1][d]);
+          read_k[0][d] = mma<3>(sp, y0, read_k[0][d]);
+          read_k[1][d] = mma<3>(sp, y1, read_k[1][d]);
+          written[0][d] = mma<3>(gp, u0, written[0][d]);
+          written[1][d] = mma<3>(gp, u1, written[1][d]);
+        }
+      }
+    }
+    both = group_sum<64>(both);
+    __syncthreads();  // A and F are there
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float own_sum = 0.0f, end_sum = 0.0f;
+      if (own) {
+        const float fade = gates.fade[16 * t + l.n], left = gates.left[16 * t + l.n];
+        const Parts<3> ar = rows_split<3>(sh.a, kPairPlane, kPairStride, 16 * t, l), fr = rows_split<3>(sh.f, kPairPlane, kPairStride, 16 * t, l);
+        const Parts<3> ac = columns_of<3>(sh.a, kPairPlane, kPairStride, 16 * t, l), fc = columns_of<3>(sh.f, kPairPlane, kPairStride, 16 * t, l);
+#pragma unroll
+        for (int d = 0; d < TD; ++d) {
+          const int c0 = 16 * (l.w * TD + d), row = 16 * t + l.n, c = c0 + 4 * l.g;
+          const Parts<NP> kc = sh.k.columns(c0, l), qc = sh.q.columns(c0, l);
+          const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+          const f32x4 dq = mma<3>(kc, ar, read_q[t][d] * (fade * a.scale));
+          const f32x4 reads = -mma<3>(kc, fr, read_k[t][d] * fade);
+          const f32x4 writes = mma<3>(qc, ac, -mma<3>(kc, fc, zero)), end = written[t][d] * left;
+          const f32x4 qv = sh.q.at(row, c), kv = sh.k.at(row, c);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            own_sum += __builtin_fmaf(qv[r], dq[r], kv[r] * (reads[r] - writes[r]));
+            end_sum = __builtin_fmaf(kv[r], end[r], end_sum);
+          }
+          dk[t][d] += reads + writes + end;
+          if (row < n) {
+            Pack<T, 4> x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x.v[r] = (T)dq[r];
+            store_some<T, 4>(static_cast<T*>(a.dq) + (int64_t)(s0 + row) * a.dq_row + h * a.dq_head + c, x, a.kd - c);
+          }
+        }
+      }
+      own_sum = groups_sum(own_sum);
+      end_sum = groups_sum(end_sum);
+      if (l.g == 0) {
+        sh.own[l.w][16 * t + l.n] = own_sum;
+        sh.end[l.w][16 * t + l.n] = end_sum;
+      }
+    }
+    if ((threadIdx.x & 63) == 0) sh.both[l.w] = both;
+    __syncthreads();
+    if (l.w == 0) {
+      const int r = threadIdx.x & 31, back = kDeltaRows - 1 - r;
+      float from = 0.0f, upto = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        from += sh.own[w][back];
+        upto += sh.end[w][r];
+      }
+      const float whole = gates.whole * ((sh.both[0] + sh.both[1]) + (sh.both[2] + sh.both[3]));
+      const float after_row = __shfl(half_wave_sums(from), back), before_row = half_wave_sums(upto) - upto;
+      if ((threadIdx.x & 63) < n) {
+        const int64_t row = s0 + r;
+        const float g = a.log_decay[row * a.g_row + h];
+        a.dlog_decay[row * a.dg_row + h] = g > 0.0f ? 0.0f : after_row + whole + before_row;
+      }
+    }
+  }
+  if (own) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < TD; ++d) {
+        const int row = 16 * t + l.n, c = 16 * (l.w * TD + d) + 4 * l.g;
+        if (row >= n) continue;
+        Pack<T, 4> x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x.v[r] = (T)dk[t][d][r];
+        store_some<T, 4>(static_cast<T*>(a.dk) + (int64_t)(s0 + row) * a.dk_row + hk * a.dk_head + c, x, a.kd - c);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < kPacks<W>; ++i) {
+    const int idx = threadIdx.x + i * kDeltaThreads, row = idx / PER, c = idx % PER * 8;
+    if (row >= n || c >= a.vd) continue;
+    Pack<T, 8> x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = (T)dv[i][e];
+    store_some<T, 8>(static_cast<T*>(a.dv) + (int64_t)(s0 + row) * a.dv_row + hk * a.dv_head + c, x, a.vd - c, a.past);
+  }
+}
+
+// ------------------------------------------------------ launches
+
+// Instances by the key dim padded to 32, 64 or 128 and the value dim to 64 or 128.
+template <typename F>
+void with_dims(int kd, int vd, F&& f) {
+  auto values = [&](auto key) {
+    vd <= 64 ? f(key, std::integral_constant<int, 1>{}) : f(key, std::integral_constant<int, 2>{});
+  };
+  kd <= 32 ? values(std::integral_constant<int, 32>{}) : kd <= 64 ? values(std::integral_constant<int, 64>{}) : values(std::integral_constant<int, 128>{});
+}
+
+template <typename T, int MODE>
+hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
+  with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
+    constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
+    constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
+    const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H), MODE == kDeltaStates ? 1 + (a.kd + 64 * TV - 1) / (64 * TV) : 1);
+    hipLaunchKernelGGL((delta_walk_kernel<T, DK, TV, MODE>), grid, dim3(kDeltaThreads), 0, st, a);
+  });
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t grad_of(const DeltaGradArgs& a, hipStream_t st) {
+  with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
+    constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
+    const dim3 grid((uint32_t)(delta_slots(a.rows, a.B) * (a.H / a.group)));
+    hipLaunchKernelGGL((delta_grad_kernel<T, DK, TV>), grid, dim3(kDeltaThreads), 0, st, a);
+  });
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t delta_walk(const DeltaArgs& a, int mode, hipStream_t st) {
+  switch (mode) {
+    case kDeltaStates: return walk_of<T, kDeltaStates>(a, st);
+    case kDeltaOut: return walk_of<T, kDeltaOut>(a, st);
+    case kDeltaSave: return walk_of<T, kDeltaSave>(a, st);
+    case kDeltaBackStates: return walk_of<T, kDeltaBackStates>(a, st);
+    default: return walk_of<T, kDeltaBack>(a, st);
+  }
+}
+
+}  // namespace
+}  // namespace mmbev

@@ -71,6 +71,126 @@ bool outputs_apart(const mmbev_head_norm_t* t, const mmbev_heads_t (&out)[2], st
   return !meet(out[0], H[0], t->dim, out[1], H[1], t->dim, t->rows, t->dtype);
 }
 
+// ------------------------------------------------------------ gated delta rule
+
+// A sequence and head is a workgroup's work; long sequences are cut so that the workgroups fill the chip's compute units,
+// in parts of at least kDeltaLeast rows, and none where none can be longer than kDeltaWhole or among more sequences
+// than a workgroup can look through in passing.
+constexpr int64_t kComputeUnits = 256;
+constexpr int64_t kDeltaWhole = 512;
+constexpr int32_t kDeltaLeast = 128;
+constexpr int32_t kDeltaCutSequences = 1024;
+
+struct DeltaPlan {
+  int64_t slots;  // workgroups that the chip takes at once
+  int32_t cuts;
+  size_t off_state, off_map, off_grad, off_before, off_after, off_left, off_due, total;  // cut_kind lies first
+};
+
+mmbev_status_t delta_ok(const mmbev_attention_t* t, bool step) {
+  if (!t || t->rows < 0 || t->reserved != 0 || !known_type(t->dtype)) return MMBEV_ERR_INVALID_ARG;
+  if (t->heads < 1 || t->kv_heads < 1 || t->heads % t->kv_heads != 0) return MMBEV_ERR_INVALID_ARG;
+  if (t->key_dim < 1 || t->value_dim < 1) return MMBEV_ERR_INVALID_ARG;
+  if (!std::isfinite(t->scale) || t->scale == 0.0f) return MMBEV_ERR_INVALID_ARG;
+  if (!step && (t->num_sequences < 1 || t->num_sequences > 65535 || t->max_length < 0)) return MMBEV_ERR_INVALID_ARG;
+  if (t->rows > kMaxRows || t->heads > 256 || t->key_dim > 128 || t->value_dim > 128) return MMBEV_ERR_UNSUPPORTED;
+  // a workgroup each, and the parts of cut sequences
+  if ((step ? t->rows : (int64_t)t->num_sequences + 1024) * t->heads > kMostGroups) return MMBEV_ERR_UNSUPPORTED;
+  return MMBEV_OK;
+}
+
+DeltaPlan delta_plan(const mmbev_attention_t* t, bool backward) {
+  DeltaPlan p{};
+  p.slots = kComputeUnits * delta_waves(size_of(t->dtype), t->key_dim, t->value_dim);
+  const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
+  if (longest > kDeltaWhole && t->num_sequences <= kDeltaCutSequences) {
+    // so many parts that with the sequences that are not cut there are about `units` of them: at least half the units
+    const int64_t units = std::max<int64_t>(2, p.slots / t->heads);
+    const int64_t parts = units - std::min<int64_t>(t->num_sequences, units / 2);
+    p.cuts = (int32_t)std::max<int64_t>(1, std::min(parts, (t->rows + kDeltaLeast - 1) / kDeltaLeast));
+  }
+  const size_t state = (size_t)t->heads * t->key_dim * t->value_dim * 4;
+  size_t at = align256((size_t)p.cuts * 4);
+  auto take = [&](size_t bytes) {
+    const size_t from = at;
+    at = align256(at + bytes);
+    return from;
+  };
+  p.off_state = take(p.cuts * state);
+  p.off_map = take((size_t)p.cuts * t->heads * t->key_dim * t->key_dim * 4);
+  if (backward) {
+    const size_t chunks = (size_t)delta_slots(t->rows, t->num_sequences), rows = (size_t)t->rows * t->heads * t->value_dim * 4;
+    p.off_grad = take(p.cuts * state);
+    p.off_before = take(chunks * state);
+    p.off_after = take(chunks * state);
+    p.off_left = take(rows);
+    p.off_due = take(rows);
+  }
+  p.total = std::max<size_t>(at, 256);
+  return p;
+}
+
+// The gradients' launch over chunks.
+bool too_many_chunks(const mmbev_attention_t* t) { return delta_slots(t->rows, t->num_sequences) * t->kv_heads > kMostGroups; }
+
+// Gates: fp32 [rows][heads].
+bool gates_ok(const mmbev_rows_t& g, const mmbev_attention_t* t) { return rows_ok(g, t->rows, t->heads, MMBEV_F32, false); }
+
+bool gates_too_wide(std::initializer_list<const mmbev_rows_t*> arrays, int64_t rows) {
+  for (const mmbev_rows_t* t : arrays)
+    if (rows > 1 && t->row_stride > INT32_MAX) return true;
+  return false;
+}
+
+// An array of rows of heads of any type, in units of two bytes.
+struct Array {
+  mmbev_heads_t t;
+  int32_t heads, dim;
+};
+Array array_of(const mmbev_heads_t& t, int32_t heads, int32_t dim, int32_t dtype) {
+  const int32_t units = size_of(dtype) / 2;
+  return {{t.data, t.row_stride * units, t.head_stride * units}, heads, dim * units};
+}
+Array array_of(const mmbev_rows_t& t, int32_t width) { return array_of(mmbev_heads_t{t.data, t.row_stride, width}, 1, width, MMBEV_F32); }
+
+bool share(const Array& x, const Array& y, int64_t rows) { return meet(x.t, x.heads, x.dim, y.t, y.heads, y.dim, rows, MMBEV_BF16); }
+
+// `written` against each other and against the arrays behind them.
+bool any_meet(std::initializer_list<Array> arrays, int written, int64_t rows) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < (int)arrays.size(); ++j)
+      if (share(arrays.begin()[i], arrays.begin()[j], rows)) return true;
+  return false;
+}
+
+Span states_of(const float* s, size_t bytes) { return {(uintptr_t)s, (uintptr_t)s + (s ? bytes : 0)}; }
+
+void put_delta(DeltaArgs& a, const mmbev_attention_t* t, const mmbev_heads_t& q, const mmbev_heads_t& k, const mmbev_heads_t& v,
+               const mmbev_rows_t& log_decay, const mmbev_rows_t& beta, const int64_t* offsets, const DeltaPlan& p, char* ws) {
+  a.offsets = offsets;
+  a.rows = t->rows;
+  a.B = t->num_sequences;
+  a.cuts = p.cuts;
+  a.longest_first = t->num_sequences <= kOrderedSequences && (int64_t)t->num_sequences * t->heads > p.slots;
+  a.least = kDeltaLeast;
+  put(q, &a.q, &a.q_row, &a.q_head);
+  put(k, &a.k, &a.k_row, &a.k_head);
+  put(v, &a.v, &a.v_row, &a.v_head);
+  a.log_decay = (const float*)log_decay.data;
+  a.g_row = (int32_t)log_decay.row_stride;
+  a.beta = (const float*)beta.data;
+  a.b_row = (int32_t)beta.row_stride;
+  a.H = t->heads;
+  a.group = t->heads / t->kv_heads;
+  a.kd = t->key_dim;
+  a.vd = t->value_dim;
+  a.past = t->rows * (t->heads + t->kv_heads) * (t->key_dim + t->value_dim) * size_of(t->dtype) > kPastCaches;
+  a.scale = t->scale;
+  a.cut_kind = (int32_t*)ws;
+  a.cut_state = (float*)(ws + p.off_state);
+  a.cut_map = (float*)(ws + p.off_map);
+}
+
 }  // namespace
 
 extern "C" {
@@ -134,6 +254,133 @@ mmbev_status_t mmbev_head_norm_rotary_backward(const mmbev_head_norm_t* t, mmbev
   a.dweight[0] = dq_weight;
   a.dweight[1] = dk_weight;
   return status_of(launch_head_norm_backward(a, t->dtype, (hipStream_t)stream));
+}
+
+size_t mmbev_gated_delta_workspace_bytes(const mmbev_attention_t* t, int32_t backward) {
+  if (delta_ok(t, false) != MMBEV_OK || (backward && too_many_chunks(t))) return 0;
+  return delta_plan(t, backward != 0).total;
+}
+
+mmbev_status_t mmbev_gated_delta(const mmbev_attention_t* t, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v, mmbev_rows_t log_decay,
+                                 mmbev_rows_t beta, const int64_t* offsets, const float* initial_state, mmbev_heads_t out,
+                                 float* final_state, int32_t* fault, void* workspace, size_t workspace_bytes, void* stream) {
+  const mmbev_status_t st = delta_ok(t, false);
+  if (st != MMBEV_OK) return st;
+  const int32_t T = t->dtype, H = t->heads, K = t->kv_heads;
+  const int64_t R = t->rows;
+  if (!heads_ok(q, R, H, t->key_dim, T) || !heads_ok(k, R, K, t->key_dim, T) || !heads_ok(v, R, K, t->value_dim, T) ||
+      !heads_ok(out, R, H, t->value_dim, T) || !gates_ok(log_decay, t) || !gates_ok(beta, t))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) || !aligned(final_state, 4)) return MMBEV_ERR_INVALID_ARG;
+  if (too_wide({&q, &k, &v, &out}, R) || gates_too_wide({&log_decay, &beta}, R)) return MMBEV_ERR_UNSUPPORTED;
+  const size_t state = (size_t)t->num_sequences * H * t->key_dim * t->value_dim * 4;
+  if (overlap(states_of(initial_state, state), states_of(final_state, state))) return MMBEV_ERR_INVALID_ARG;
+  if (any_meet({array_of(out, H, t->value_dim, T), array_of(q, H, t->key_dim, T), array_of(k, K, t->key_dim, T),
+                array_of(v, K, t->value_dim, T), array_of(log_decay, H), array_of(beta, H)},
+               1, R))
+    return MMBEV_ERR_INVALID_ARG;
+  const DeltaPlan p = delta_plan(t, false);
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
+  DeltaArgs a{};
+  put_delta(a, t, q, k, v, log_decay, beta, offsets, p, (char*)workspace);
+  put(out, &a.out, &a.o_row, &a.o_head);
+  a.init = initial_state;
+  a.final_state = final_state;
+  a.fault = fault;
+  return status_of(launch_delta(a, T, (hipStream_t)stream));
+}
+
+mmbev_status_t mmbev_gated_delta_backward(const mmbev_attention_t* t, mmbev_heads_t dout, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v,
+                                          mmbev_rows_t log_decay, mmbev_rows_t beta, const int64_t* offsets, const float* initial_state,
+                                          const float* dfinal_state, mmbev_heads_t dq, mmbev_heads_t dk, mmbev_heads_t dv,
+                                          mmbev_rows_t dlog_decay, mmbev_rows_t dbeta, float* dinitial_state, int32_t* fault,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+  const mmbev_status_t st = delta_ok(t, false);
+  if (st != MMBEV_OK) return st;
+  const int32_t T = t->dtype, H = t->heads, K = t->kv_heads;
+  const int64_t R = t->rows;
+  if (!heads_ok(dout, R, H, t->value_dim, T) || !heads_ok(q, R, H, t->key_dim, T) || !heads_ok(k, R, K, t->key_dim, T) ||
+      !heads_ok(v, R, K, t->value_dim, T) || !heads_ok(dq, R, H, t->key_dim, T) || !heads_ok(dk, R, K, t->key_dim, T) ||
+      !heads_ok(dv, R, K, t->value_dim, T))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!gates_ok(log_decay, t) || !gates_ok(beta, t) || !gates_ok(dlog_decay, t) || !gates_ok(dbeta, t)) return MMBEV_ERR_INVALID_ARG;
+  if (!offsets || !aligned(offsets, 8) || !aligned(initial_state, 4) || !aligned(dfinal_state, 4) || !aligned(dinitial_state, 4))
+    return MMBEV_ERR_INVALID_ARG;
+  if (too_wide({&dout, &q, &k, &v, &dq, &dk, &dv}, R) || gates_too_wide({&log_decay, &beta, &dlog_decay, &dbeta}, R) || too_many_chunks(t))
+    return MMBEV_ERR_UNSUPPORTED;
+  const size_t state = (size_t)t->num_sequences * H * t->key_dim * t->value_dim * 4;
+  for (const float* in : {initial_state, dfinal_state})
+    if (overlap(states_of(dinitial_state, state), states_of(in, state))) return MMBEV_ERR_INVALID_ARG;
+  // the gradients against the inputs and against each other
+  if (any_meet({array_of(dq, H, t->key_dim, T), array_of(dk, K, t->key_dim, T), array_of(dv, K, t->value_dim, T), array_of(dlog_decay, H),
+                array_of(dbeta, H), array_of(dout, H, t->value_dim, T), array_of(q, H, t->key_dim, T), array_of(k, K, t->key_dim, T),
+                array_of(v, K, t->value_dim, T), array_of(log_decay, H), array_of(beta, H)},
+               5, R))
+    return MMBEV_ERR_INVALID_ARG;
+  const DeltaPlan p = delta_plan(t, true);
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return MMBEV_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  DeltaGradArgs a{};
+  put_delta(a, t, q, k, v, log_decay, beta, offsets, p, ws);
+  put(dout, &a.dout, &a.d_row, &a.d_head);
+  put(dq, &a.dq, &a.dq_row, &a.dq_head);
+  put(dk, &a.dk, &a.dk_row, &a.dk_head);
+  put(dv, &a.dv, &a.dv_row, &a.dv_head);
+  a.dlog_decay = (float*)dlog_decay.data;
+  a.dg_row = (int32_t)dlog_decay.row_stride;
+  a.dbeta = (float*)dbeta.data;
+  a.db_row = (int32_t)dbeta.row_stride;
+  a.init = initial_state;
+  a.fault = fault;
+  a.cut_grad = (float*)(ws + p.off_grad);
+  a.before = (float*)(ws + p.off_before);
+  a.after = (float*)(ws + p.off_after);
+  a.left_over = (float*)(ws + p.off_left);
+  a.due = (float*)(ws + p.off_due);
+  return status_of(launch_delta_backward(a, dfinal_state, dinitial_state, T, (hipStream_t)stream));
+}
+
+mmbev_status_t mmbev_gated_delta_step(const mmbev_attention_t* t, mmbev_heads_t q, mmbev_heads_t k, mmbev_heads_t v, mmbev_rows_t log_decay,
+                                      mmbev_rows_t beta, const int32_t* slots, int64_t num_slots, float* state, mmbev_heads_t out,
+                                      int32_t* fault, void* stream) {
+  const mmbev_status_t ok = delta_ok(t, true);
+  if (ok != MMBEV_OK) return ok;
+  const int32_t T = t->dtype, H = t->heads, K = t->kv_heads;
+  const int64_t R = t->rows;
+  if (!heads_ok(q, R, H, t->key_dim, T) || !heads_ok(k, R, K, t->key_dim, T) || !heads_ok(v, R, K, t->value_dim, T) ||
+      !heads_ok(out, R, H, t->value_dim, T) || !gates_ok(log_decay, t) || !gates_ok(beta, t))
+    return MMBEV_ERR_INVALID_ARG;
+  if (!aligned(slots, 4) || num_slots < 0) return MMBEV_ERR_INVALID_ARG;
+  // a workgroup reads its head's q, k and v before it writes its out: they may be one, unless other heads read them too
+  const Array to = array_of(out, H, t->value_dim, T);
+  const bool own = H == K;
+  if ((!same(q, out) && share(array_of(q, H, t->key_dim, T), to, R)) || (!(own && same(k, out)) && share(array_of(k, K, t->key_dim, T), to, R)) ||
+      (!(own && same(v, out)) && share(array_of(v, K, t->value_dim, T), to, R)) || share(array_of(log_decay, H), to, R) ||
+      share(array_of(beta, H), to, R))
+    return MMBEV_ERR_INVALID_ARG;
+  if (num_slots > kMaxRows) return MMBEV_ERR_UNSUPPORTED;
+  if (R > 0 && num_slots > 0 && (!state || !aligned(state, 16))) return MMBEV_ERR_INVALID_ARG;
+  if (!slots && num_slots < R) return MMBEV_ERR_INVALID_ARG;
+  DeltaStepArgs a{};
+  put(q, &a.q, &a.q_row, &a.q_head);
+  put(k, &a.k, &a.k_row, &a.k_head);
+  put(v, &a.v, &a.v_row, &a.v_head);
+  put(out, &a.out, &a.o_row, &a.o_head);
+  a.log_decay = (const float*)log_decay.data;
+  a.g_row = log_decay.row_stride;
+  a.beta = (const float*)beta.data;
+  a.b_row = beta.row_stride;
+  a.slots = slots;
+  a.num_slots = num_slots;
+  a.state = state;
+  a.fault = fault;
+  a.rows = R;
+  a.H = H;
+  a.group = H / K;
+  a.kd = t->key_dim;
+  a.vd = t->value_dim;
+  a.scale = t->scale;
+  return status_of(launch_delta_step(a, T, (hipStream_t)stream));
 }
 
 }  // extern "C"

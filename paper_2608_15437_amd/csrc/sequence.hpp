@@ -105,27 +105,33 @@ constexpr int grad_waves(bool half, int wide) { return wide > 64 && !half ? 1 : 
 
 constexpr int kOrderedSequences = 256;
 
-// What the walks over ragged sequences share.  Positions may run backwards;
-// `ad` and `cd` are the state's rows and columns.
-struct AttnWalk {
-  const float* log_decay;
+// Ragged sequences and how the walks over them are cut.  Positions may run
+// backwards.
+struct Ranges {
   const int64_t* offsets;
+  int64_t rows;
+  int32_t B;
+  int32_t reversed;
+  // sequences are cut at shares of (rows in use) / cuts, at least `least` rows; 0: none is
+  int32_t cuts;
+  int32_t longest_first;  // the sequences that are not cut, up to kOrderedSequences of them
+  int32_t least;          // whole chunks
+};
+
+// What the walks of linear attention share; `ad` and `cd` are the state's rows
+// and columns.
+struct AttnWalk : Ranges {
+  const float* log_decay;
   const float* init;      // [B][H][ad][cd], or [B][H][cd][ad] where init_swapped; null: zeros
   float* final_state;     // [B][H][ad][cd]; null: not written
   int32_t* fault;
-  int64_t rows;
-  int32_t B, H;
+  int32_t H;
   int32_t ad, cd;
-  int32_t reversed;
   int32_t init_swapped;
   int32_t exact_state;    // the state is an output: as exact as fp32
   int32_t past;           // store past the caches
   float scale;
   float init_scale, final_scale;  // the state is carried divided by these
-  // sequences are cut at shares of (rows in use) / cuts, at least `least` rows; 0: none is
-  int32_t cuts;
-  int32_t longest_first;  // the sequences that are not cut, up to kOrderedSequences of them
-  int32_t least;          // whole chunks
   float* cut_state;       // [cuts][H][ad][cd]: the state at the end of every part that goes on
   int32_t* cut_rows;      // [cuts] its rows, 0 where it begins its sequence, -1: there is no such part
 };
@@ -186,6 +192,71 @@ struct AttnStepArgs {
   float scale;
 };
 hipError_t launch_attention_step(const AttnStepArgs& a, int32_t dtype, hipStream_t st);
+
+// ---- the gated delta rule
+
+constexpr int kDeltaRows = 32;  // rows of a chunk
+
+// One walk over chunks: forwards over (q, k, v) or, for the gradients,
+// backwards over (q, k, dout).
+struct DeltaArgs : Ranges {
+  const void *q, *k, *v, *dout;
+  void* out;
+  int64_t q_head, k_head, v_head, d_head, o_head;
+  int32_t q_row, k_row, v_row, d_row, o_row;
+  int32_t g_row, b_row;   // of log_decay and beta, fp32 [rows][H]
+  const float *log_decay, *beta;
+  const float* init;      // [B][H][kd][vd]: the state before a sequence; backwards, the gradient of the one after it
+  float* final_state;     // the other end's
+  int32_t* fault;
+  int32_t H, group;       // group: heads that share keys and values
+  int32_t kd, vd;
+  int32_t past;           // store past the caches
+  float scale;
+  // boundaries between parts of a cut sequence: kind -1: there is none, 0: the part before it begins its sequence, 1: it does not
+  int32_t* cut_kind;      // [cuts]
+  float* cut_state;       // [cuts][H][kd][vd]: the state at the boundary
+  float* cut_grad;        // its gradient
+  float* cut_map;         // [cuts][H][kd][kd]: what the part before it does to the state before that part, where kind is 1
+  // the gradients' chunks
+  float* before;          // [slots][H][kd][vd]: the state before a chunk
+  float* after;           // the gradient of the state after it
+  float* left_over;       // [rows][H][vd]: values less what the state holds for their keys
+  float* due;             // its gradient
+};
+
+// Chunks of a sequence lie next to each other from rows / 32 + sequence on, so no two chunks share a place.
+inline int64_t delta_slots(int64_t rows, int64_t B) { return rows / kDeltaRows + B; }
+
+struct DeltaGradArgs : DeltaArgs {
+  void *dq, *dk, *dv;
+  int64_t dq_head, dk_head, dv_head;
+  int32_t dq_row, dk_row, dv_row;
+  int32_t dg_row, db_row;
+  float *dlog_decay, *dbeta;  // fp32 [rows][H]
+};
+
+// Waves a SIMD of the walks' kernels, hence the workgroups of four waves that a compute unit takes, as their registers
+// and LDS allow; keys and values padded to `key` and `value`.
+constexpr int delta_waves(int size, int key, int value) { return size == 4 ? (key > 64 || value > 64 ? 1 : 2) : key > 64 || value > 64 ? 2 : 3; }
+constexpr int delta_grad_waves(int size, int key, int value) { return size == 4 || key > 64 || value > 64 ? 1 : 2; }
+
+hipError_t launch_delta(const DeltaArgs& a, int32_t dtype, hipStream_t st);
+hipError_t launch_delta_backward(const DeltaGradArgs& a, const float* dfinal, float* dinitial, int32_t dtype, hipStream_t st);
+
+struct DeltaStepArgs {
+  const void *q, *k, *v;
+  void* out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, g_row, b_row;
+  const float *log_decay, *beta;
+  const int32_t* slots;
+  float* state;
+  int32_t* fault;
+  int64_t rows, num_slots;
+  int32_t H, group, kd, vd;
+  float scale;
+};
+hipError_t launch_delta_step(const DeltaStepArgs& a, int32_t dtype, hipStream_t st);
 
 // ------------------------------------------------------------ device code
 

@@ -202,6 +202,15 @@ def load() -> ctypes.CDLL:
         L.mmbev_linear_attention_backward.restype = i32
         L.mmbev_linear_attention_step.argtypes = [attention, heads, heads, heads, p, p, i64, p, heads, p, p]
         L.mmbev_linear_attention_step.restype = i32
+        L.mmbev_gated_delta_workspace_bytes.argtypes = [attention, i32]
+        L.mmbev_gated_delta_workspace_bytes.restype = size
+        L.mmbev_gated_delta.argtypes = [attention, heads, heads, heads, rows, rows, p, p, heads, p, p, p, size, p]
+        L.mmbev_gated_delta.restype = i32
+        L.mmbev_gated_delta_backward.argtypes = [attention, heads, heads, heads, heads, rows, rows, p, p, p, heads, heads, heads,
+                                                 rows, rows, p, p, p, size, p]
+        L.mmbev_gated_delta_backward.restype = i32
+        L.mmbev_gated_delta_step.argtypes = [attention, heads, heads, heads, rows, rows, p, i64, p, heads, p, p]
+        L.mmbev_gated_delta_step.restype = i32
         _lib = L
     return _lib
 
@@ -935,5 +944,95 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
         desc, qs, ks, vs, _vector("log_decay", log_decay, torch.float32, desc.heads),
         _vector("slots", slots, torch.int32, desc.rows), held, _state("state", state, desc, held), _heads("out", out),
         _vector("fault", fault, torch.int32, 1), handle), "mmbev_linear_attention_step")
+    _written(*given)
+    return out
+
+
+def _gates(name, t, desc) -> mmbev_rows_t:
+    _like(name, t, _torch.float32, (desc.rows, desc.heads))
+    return _rows(name, t)
+
+
+def gated_delta_workspace_bytes(desc: mmbev_attention_t, backward: bool = False) -> int:
+    return int(load().mmbev_gated_delta_workspace_bytes(desc, 1 if backward else 0))
+
+
+def gated_delta(q, k, v, log_decay, beta, offsets, scale=None, initial_state=None, final_state=False, max_length=None, out=None,
+                fault=None, workspace=None, stream=None):
+    """Enqueue mmbev_gated_delta: q [rows][heads][key_dim], k and v [rows][kv_heads][..], log_decay and beta float32
+    [rows][heads], offsets int64 [B+1] (the voxeliser's out_voxel_offsets).  scale: key_dim ** -0.5 when None.
+    final_state: True, or the tensor to write.  max_length: a bound on the sequences' rows, if known (the grid's max_voxels).
+
+    Returns (out, final state or None).  Rows of no sequence keep what `out` holds.
+    """
+    given = out, _given(final_state)
+    handle = _issue_on(stream, q, k, v, log_decay, beta, offsets, initial_state, *given, fault, workspace)
+    torch = _torch
+    n = offsets.numel() - 1
+    qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
+    desc = _attention_of(q, k, v, n, scale, max_length)
+    shape = (desc.rows, desc.heads, desc.value_dim)
+    out = _empty(stream, q, shape, q.dtype) if out is None else _like("out", out, q.dtype, shape)
+    if final_state is True:
+        final_state = _empty(stream, q, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32)
+    final = None if final_state is False else final_state
+    if workspace is None:
+        workspace = _empty(stream, q, (gated_delta_workspace_bytes(desc),), torch.uint8)
+    _check((_lib or load()).mmbev_gated_delta(
+        desc, qs, ks, vs, _gates("log_decay", log_decay, desc), _gates("beta", beta, desc),
+        _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n), _heads("out", out),
+        _state("final_state", final, desc, n), _vector("fault", fault, torch.int32, 1), workspace.data_ptr(),
+        workspace.nbytes, handle), "mmbev_gated_delta")
+    _written(*given)
+    return out, final
+
+
+def gated_delta_backward(dout, q, k, v, log_decay, beta, offsets, scale=None, initial_state=None, dfinal_state=None,
+                         dinitial_state=False, max_length=None, dq=None, dk=None, dv=None, dlog_decay=None, dbeta=None,
+                         fault=None, workspace=None, stream=None):
+    """Enqueue mmbev_gated_delta_backward: the gradients of gated_delta's q, k, v, log_decay and beta and, where
+    `dinitial_state` is True or a tensor to write, of its initial state.
+
+    Returns (dq, dk, dv, dlog_decay, dbeta, dinitial_state or None)."""
+    given = dq, dk, dv, dlog_decay, dbeta, _given(dinitial_state)
+    handle = _issue_on(stream, dout, q, k, v, log_decay, beta, offsets, initial_state, dfinal_state, *given, fault, workspace)
+    torch = _torch
+    n = offsets.numel() - 1
+    ins = [_heads(name, t) for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v))]
+    desc = _attention_of(q, k, v, n, scale, max_length)
+    _like("dout", dout, q.dtype, (desc.rows, desc.heads, desc.value_dim))
+    gates = _gates("log_decay", log_decay, desc), _gates("beta", beta, desc)
+    dq, dk, dv = (_empty(stream, t, t.shape, t.dtype) if d is None else _like(name, d, t.dtype, t.shape)
+                  for name, d, t in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    dlog_decay, dbeta = (_empty(stream, q, (desc.rows, desc.heads), torch.float32) if d is None else d for d in (dlog_decay, dbeta))
+    if dinitial_state is True:
+        dinitial_state = _empty(stream, q, (n, desc.heads, desc.key_dim, desc.value_dim), torch.float32)
+    dinitial = None if dinitial_state is False else dinitial_state
+    if workspace is None:
+        workspace = _empty(stream, q, (gated_delta_workspace_bytes(desc, True),), torch.uint8)
+    _check((_lib or load()).mmbev_gated_delta_backward(
+        desc, *ins, *gates, _vector("offsets", offsets, torch.int64, 2), _state("initial_state", initial_state, desc, n),
+        _state("dfinal_state", dfinal_state, desc, n), _heads("dq", dq), _heads("dk", dk), _heads("dv", dv),
+        _gates("dlog_decay", dlog_decay, desc), _gates("dbeta", dbeta, desc), _state("dinitial_state", dinitial, desc, n),
+        _vector("fault", fault, torch.int32, 1), workspace.data_ptr(), workspace.nbytes, handle), "mmbev_gated_delta_backward")
+    _written(*given)
+    return dq, dk, dv, dlog_decay, dbeta, dinitial
+
+
+def gated_delta_step(q, k, v, log_decay, beta, state, slots=None, scale=None, out=None, fault=None, stream=None):
+    """Enqueue mmbev_gated_delta_step: one row for each of many streams.  state float32 [slots][heads][key_dim][value_dim]
+    is updated in place; slots int32 [rows] names each row's state (negative: the row is skipped)."""
+    handle = _issue_on(stream, q, k, v, log_decay, beta, state, slots, out, fault)
+    given = state, out
+    torch = _torch
+    qs, ks, vs = _heads("q", q), _heads("k", k), _heads("v", v)
+    desc = _attention_of(q, k, v, 1, scale, 0)
+    shape = (desc.rows, desc.heads, desc.value_dim)
+    out = _empty(stream, q, shape, q.dtype) if out is None else _like("out", out, q.dtype, shape)
+    held = state.shape[0]
+    _check((_lib or load()).mmbev_gated_delta_step(
+        desc, qs, ks, vs, _gates("log_decay", log_decay, desc), _gates("beta", beta, desc),
+        _vector("slots", slots, torch.int32, desc.rows), held, _state("state", state, desc, held), _heads("out", out),
+        _vector("fault", fault, torch.int32, 1), handle), "mmbev_gated_delta_step")
     _written(*given)
     return out
