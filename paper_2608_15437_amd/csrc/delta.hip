@@ -134,7 +134,9 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
     s_k[i] = there ? (float)static_cast<const T*>(a.k)[r * a.k_row + hk * a.k_head + i] : 0.0f;
   }
   const Pack<T, 4> rv = load_some<T, 4>(static_cast<const T*>(a.v) + r * a.v_row + hk * a.v_head + c, a.vd - c);
-  const float decay = exp_of(clamp_gate(a.log_decay[r * a.g_row + h]), 0.0f), beta = a.beta[r * a.b_row + h];
+  float step, rest;
+  base2_of(a.log_decay[r * a.g_row + h], step, rest);
+  const float decay = exp2_of(step, rest), beta = a.beta[r * a.b_row + h];
   __syncthreads();
   float held[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll

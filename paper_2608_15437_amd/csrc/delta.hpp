@@ -80,18 +80,51 @@ __device__ __forceinline__ f32x4 mma(const Parts<NA>& a, const Parts<NB>& b, f32
   return c;
 }
 
+// Two neighbours' next part, taken off them (conversions in pairs: five operations instead of seven).
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef bf16 b16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t take_part(float& x, float& y, bool more) {
+  const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, b16x2));
+  if (more) {
+    x -= __builtin_bit_cast(float, p << 16);
+    y -= __builtin_bit_cast(float, p & 0xffff0000u);
+  }
+  return p;
+}
+
 template <int N>
 __device__ __forceinline__ Parts<N> split(const float (&x)[8]) {
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
+  words w[N];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float u = x[2 * e], v = x[2 * e + 1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i][e] = take_part(u, v, i + 1 < N);
+  }
   Parts<N> r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float left = x[e];
+  for (int i = 0; i < N; ++i) r.p[i] = __builtin_bit_cast(b16x8, w[i]);
+  return r;
+}
+
+template <int N>
+struct Quarter {
+  b16x4 p[N];
+};
+template <int N>
+__device__ __forceinline__ Quarter<N> split(f32x4 x) {
+  typedef uint32_t words __attribute__((ext_vector_type(2)));
+  words w[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      r.p[i][e] = (bf16)left;
-      left -= (float)r.p[i][e];
-    }
+  for (int e = 0; e < 2; ++e) {
+    float u = x[2 * e], v = x[2 * e + 1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i][e] = take_part(u, v, i + 1 < N);
   }
+  Quarter<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.p[i] = __builtin_bit_cast(b16x4, w[i]);
   return r;
 }
 
@@ -104,16 +137,9 @@ __device__ __forceinline__ Parts<N> split(f32x4 x, f32x4 y) {
 // Four values of an operand, in N parts N arrays of LDS apart.
 template <int N>
 __device__ __forceinline__ void put4(bf16* s, int plane, f32x4 x) {
+  const Quarter<N> q = split<N>(x);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    b16x4 p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = (bf16)x[e];
-      x[e] -= (float)p[e];
-    }
-    __builtin_memcpy(__builtin_assume_aligned(s + i * plane, 8), &p, 8);
-  }
+  for (int i = 0; i < N; ++i) __builtin_memcpy(__builtin_assume_aligned(s + i * plane, 8), &q.p[i], 8);
 }
 
 // Operands out of LDS, rows of `stride` elements, parts `plane` apart.
@@ -162,56 +188,51 @@ __device__ __forceinline__ Parts<N> columns_of(const bf16* s, int plane, int str
   return r;
 }
 
-// ---- blocks of 16 x 16 in three parts: 16 deep, so a product's 32 take two of the parts' products at once
+// ---- blocks of 16 x 16: 16 deep, so a product's 32 take two of the parts' products at once
 
 constexpr int kBlockStride = 20;  // rows of eight-byte steps over all banks
 constexpr int kBlock = 16 * kBlockStride;
 
+template <int N>
 struct Block {
   b16x8 high, ends;  // first and second part; first and third
 };
 
-template <bool TRANSPOSED>
-__device__ __forceinline__ Block block_of(const bf16* s, const Lane& l) {
-  b16x4 p[3];
+template <int N, bool TRANSPOSED>
+__device__ __forceinline__ Block<N> block_of(const bf16* s, const Lane& l) {
+  b16x4 p[N];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < N; ++i) {
     if constexpr (TRANSPOSED)
       p[i] = read_columns(s + i * kBlock + (4 * l.g + (l.n >> 2)) * kBlockStride + (l.n & 3) * 4);
     else
       __builtin_memcpy(&p[i], __builtin_assume_aligned(s + i * kBlock + l.n * kBlockStride + 4 * l.g, 8), 8);
   }
-  return {__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(p[0], p[2], 0, 1, 2, 3, 4, 5, 6, 7)};
+  return {__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(p[0], p[N - 1], 0, 1, 2, 3, 4, 5, 6, 7)};
 }
 
 // c + block * x
-__device__ __forceinline__ f32x4 mma_block(const Block& a, f32x4 x, f32x4 c) {
-  b16x4 p[3];
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[i][e] = (bf16)x[e];
-      x[e] -= (float)p[i][e];
-    }
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(p[2], p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(p[1], p[1], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(p[0], p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+template <int N>
+__device__ __forceinline__ f32x4 mma_block(const Block<N>& a, f32x4 x, f32x4 c) {
+  const Quarter<N> q = split<N>(x);
+  if constexpr (N == 3)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(q.p[2], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(q.p[1], q.p[1], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(q.p[0], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
 }
 
 // ------------------------------------------------------ gates
 
-// e^(hi + lo), lo small against hi or both small: the sum's last bits stay in the power.
-__device__ __forceinline__ float exp_of(float hi, float lo) {
-  const float x = hi + lo, rest = lo - (x - hi);
-  const float t = x * 1.44269504088896341f, p = __builtin_amdgcn_exp2f(t);
-  const float more = __builtin_fmaf(x, 1.44269504088896341f, -t) + (x * 1.92596299e-8f + rest * 1.44269504f);
-  return __builtin_fmaf(p, more * 0.693147181f, p);
+// 2^(hi + lo), |lo| under 1: the sum's last bits stay in the power.
+__device__ __forceinline__ float exp2_of(float hi, float lo) {
+  const float x = hi + lo, rest = lo - (x - hi), p = __builtin_amdgcn_exp2f(x);
+  return __builtin_fmaf(p, rest * 0.693147181f, p);
 }
 
-// A chunk's gates in LDS.  The sums of the log decays are held in two parts,
-// multiples of 2^-10 (whose sums are exact) and what is left over, so that the
-// decay between two rows has its last bits behind a decay of any size too.
+// A chunk's gates in LDS.  The sums of the log decays, to base 2, are held in
+// two parts, multiples of 2^-10 (whose sums and differences are exact) and what
+// is left over, so that the decay between two rows has its last bits behind a
+// decay of any size too.
 struct Gates {
   float hi[kDeltaRows], lo[kDeltaRows];      // inclusive sums
   float beta[kDeltaRows];
@@ -239,20 +260,28 @@ __device__ __forceinline__ float last_of_half(float x) {
 // A decay of more than e^-104 leaves nothing in fp32; a log decay over 0 counts as 0, NaN stays.
 __device__ __forceinline__ float clamp_gate(float g) { return g > 0.0f ? 0.0f : g < -104.0f ? -104.0f : g; }
 
+// A log decay to base 2 in its two parts: log2(e) as fp32 and what that leaves of it.
+__device__ __forceinline__ void base2_of(float g, float& step, float& rest) {
+  g = clamp_gate(g);
+  const float x = g * 1.44269504088896341f;
+  step = __builtin_rintf(x * 1024.0f) * (1.0f / 1024.0f);
+  rest = (x - step) + __builtin_fmaf(g, 1.44269504088896341f, -x) + g * 1.92596299e-8f;
+}
+
 // By one wave: lane r < 32 has row r's gates (0 past the rows).
 __device__ __forceinline__ void put_gates(Gates& s, float g, float beta) {
   const int r = threadIdx.x & 63;
-  g = clamp_gate(g);
-  const float step = __builtin_rintf(g * 1024.0f) * (1.0f / 1024.0f);
-  const float hi = half_wave_sums(step), lo = half_wave_sums(g - step);
+  float step, rest;
+  base2_of(g, step, rest);
+  const float hi = half_wave_sums(step), lo = half_wave_sums(rest);
   const float end_hi = last_of_half(hi), end_lo = last_of_half(lo);
-  const float fade = exp_of(hi, lo);
+  const float fade = exp2_of(hi, lo);
   if (r < kDeltaRows) {
     s.hi[r] = hi;
     s.lo[r] = lo;
     s.beta[r] = beta;
     s.fade[r] = fade;
-    s.left[r] = exp_of(end_hi - hi, end_lo - lo);
+    s.left[r] = exp2_of(end_hi - hi, end_lo - lo);
     if (r == kDeltaRows - 1) s.whole = fade;
   }
 }
@@ -273,32 +302,52 @@ constexpr int kPlanePad = 8;
 template <int W>
 constexpr int kPacks = W >= 64 ? kDeltaRows * W / 8 / kDeltaThreads : 1;
 
-// Every load is of an element that is there; what is past the rows or the row's end is zeroed on the way into LDS.
+// An operand's rows as a thread reads them.  Every load is of an element that
+// is there; what is past the rows or the row's end is zeroed on the way into LDS.
 template <typename T, int W>
-__device__ __forceinline__ void fetch_chunk(Pack<T, 8> (&r)[kPacks<W>], const T* p, int32_t stride, int dim, int32_t s0, int32_t hi) {
-#pragma unroll
-  for (int i = 0; i < kPacks<W>; ++i) {
-    const int idx = threadIdx.x + i * kDeltaThreads, c = idx % (W / 8) * 8;
-    const T* row = p + (int64_t)min(s0 + idx / (W / 8), hi - 1) * stride;
-    if (dim % 8 == 0)
-      r[i] = load_pack<T, 8>(row + (c < dim ? c : 0));
-    else
-      r[i] = load_some<T, 8>(row + c, dim - c);
+struct Source {
+  const T* p;  // of the thread's first pack in the chunk at row 0
+  int64_t stride;
+  int dim;
+  static constexpr int kRowsApart = kDeltaThreads / (W / 8);
+
+  __device__ __forceinline__ Source(const void* data, int64_t head, int32_t row_stride, int columns) : stride(row_stride), dim(columns) {
+    const int c = threadIdx.x % (W / 8) * 8;
+    p = static_cast<const T*>(data) + head + row() * stride + (c < dim ? c : 0);
   }
-}
+  static __device__ __forceinline__ int row() { return threadIdx.x / (W / 8); }
+  __device__ __forceinline__ void fetch(Pack<T, 8> (&r)[kPacks<W>], int32_t s0, int32_t hi) const {
+    const bool whole = hi - s0 >= kDeltaRows && W >= 64;
+    const int left = dim - (int)(threadIdx.x % (W / 8)) * 8;
+#pragma unroll
+    for (int i = 0; i < kPacks<W>; ++i) {
+      // (rows past the last one are its copies)
+      const int at = row() + i * kRowsApart;
+      const int64_t up = whole ? s0 + i * kRowsApart : (int64_t)min(s0 + at, hi - 1) - row();
+      const T* from = p + up * stride;
+      if (dim % 8 == 0)
+        r[i] = load_pack<T, 8>(from);
+      else
+        r[i] = load_some<T, 8>(from, left);
+    }
+  }
+};
 
 // f(row, column, pack), zeros where there is nothing.
 template <typename T, int W, typename F>
 __device__ __forceinline__ void each_pack(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n, F&& f) {
+  const bool whole = n >= kDeltaRows && dim >= W;
 #pragma unroll
   for (int i = 0; i < kPacks<W>; ++i) {
     const int idx = threadIdx.x + i * kDeltaThreads, row = idx / (W / 8), c = idx % (W / 8) * 8;
     if (W < 64 && row >= kDeltaRows) continue;
     typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * 2)));
     words x = __builtin_bit_cast(words, r[i]);
-    const bool there = row < n && c < dim;
+    if (!whole) {
+      const bool there = row < n && c < dim;
 #pragma unroll
-    for (int e = 0; e < (int)sizeof(T) * 2; ++e) x[e] = there ? x[e] : 0u;
+      for (int e = 0; e < (int)sizeof(T) * 2; ++e) x[e] = there ? x[e] : 0u;
+    }
     f(row, c, __builtin_bit_cast(Pack<T, 8>, x));
   }
 }
@@ -389,40 +438,50 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// What the rows of a chunk do to each other.
+// What the rows of a chunk do to each other: N and X in NS parts, P in PARTS.
 constexpr int kPairStride = kDeltaRows + kPlanePad, kPairPlane = kDeltaRows * kPairStride;
 
-template <int PARTS>
+template <int NS, int PARTS>
 struct Pairs {
-  __attribute__((aligned(16))) bf16 n[3][3 * kBlock];  // N of the first and last 16 rows, X of the last with the first
+  __attribute__((aligned(16))) bf16 n[3][NS * kBlock];  // N of the first and last 16 rows, X of the last with the first
   __attribute__((aligned(16))) bf16 p[PARTS ? PARTS * kPairPlane : 8];
   __attribute__((aligned(16))) float scratch[2][kBlock];
 };
 
-// times e^(G_i - G_j) where j < i (j <= i with the diagonal), else 0; lane n row i, elements j0 + 4g .. of it.
-__device__ __forceinline__ f32x4 decayed(f32x4 x, const Gates& s, int i0, int j0, bool diagonal, float times, const Lane& l) {
-  const int i = i0 + l.n;
-  const float hi = s.hi[i], lo = s.lo[i];
+// e^(G_i - G_j), lane n row i0 + n, elements j0 + 4g ..: without exp2_of's last bits, off by |G_i - G_j| 2^-25 of itself.
+// (Where j > i it may be infinite.)
+__device__ __forceinline__ f32x4 decays(const Gates& s, int i0, int j0, const Lane& l) {
+  const float hi = s.hi[i0 + l.n], lo = s.lo[i0 + l.n];
   const f32x4 jh = four(s.hi + j0 + 4 * l.g), jl = four(s.lo + j0 + 4 * l.g);
+  f32x4 d;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) d[r] = __builtin_amdgcn_exp2f((hi - jh[r]) + (lo - jl[r]));
+  return d;
+}
+
+// x times them where j < i (j <= i with the diagonal), else 0.  Of two blocks of 16 rows, the diagonal ones have j > i.
+template <bool SAME>
+__device__ __forceinline__ f32x4 decayed(f32x4 x, f32x4 d, bool diagonal, const Lane& l) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int j = j0 + 4 * l.g + r;
-    const float d = exp_of(hi - jh[r], lo - jl[r]) * times;
-    x[r] = j < i || (diagonal && j == i) ? x[r] * d : 0.0f;
+    const int above = l.n - 4 * l.g - r;  // i - j
+    const float y = x[r] * d[r];
+    x[r] = !SAME || above > 0 || (diagonal && above == 0) ? y : 0.0f;
   }
   return x;
 }
 
 // a_i . b_j over DK columns: lane n row i0 + n, elements j0 + 4g ..
-template <typename T, int DK>
+template <int LEVEL, typename T, int DK>
 __device__ __forceinline__ f32x4 dots(const Planes<T, DK>& a, int i0, const Planes<T, DK>& b, int j0, const Lane& l) {
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int s = 0; s < DK / 32; ++s) x = mma<3>(b.rows(j0, 32 * s, l), a.rows(i0, 32 * s, l), x);
+  for (int s = 0; s < DK / 32; ++s) x = mma<LEVEL>(b.rows(j0, 32 * s, l), a.rows(i0, 32 * s, l), x);
   return x;
 }
 
 // N of 16 rows: N = -X - N beta X, its columns from the last one on.
+template <int NS>
 __device__ __forceinline__ void put_inverse(bf16* to, float* scratch, f32x4 x, const Gates& s, int i0, const Lane& l) {
   f32x4 bx;
   const float beta = s.beta[i0 + l.n];
@@ -453,26 +512,26 @@ __device__ __forceinline__ void put_inverse(bf16* to, float* scratch, f32x4 x, c
   column(std::integral_constant<int, 3>{});
   column(std::integral_constant<int, 2>{});
   column(std::integral_constant<int, 1>{});
-  put4<3>(to + l.n * kBlockStride + 4 * l.g, kBlock, acc);
+  put4<NS>(to + l.n * kBlockStride + 4 * l.g, kBlock, acc);
 }
 
 // The four waves' shares: two the inverses, the third the last rows with the first, the fourth the rest.  (PARTS 0: no P.)
-template <typename T, int DK, int PARTS>
-__device__ __forceinline__ void put_pairs(Pairs<PARTS>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
+template <typename T, int DK, int NS, int PARTS>
+__device__ __forceinline__ void put_pairs(Pairs<NS, PARTS>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
                                           const Lane& l) {
-  auto put_p = [&](int i0, int j0) {
-    const f32x4 x = decayed(dots<T, DK>(*q, i0, k, j0, l), s, i0, j0, true, scale, l);
-    put4<PARTS>(to.p + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, x);
-  };
   if (l.w < 2) {
     const int i0 = 16 * l.w;
-    put_inverse(to.n[l.w], to.scratch[l.w], decayed(dots<T, DK>(k, i0, k, i0, l), s, i0, i0, false, 1.0f, l), s, i0, l);
+    const f32x4 x = decayed<true>(dots<NS>(k, i0, k, i0, l), decays(s, i0, i0, l), false, l);
+    put_inverse<NS>(to.n[l.w], to.scratch[l.w], x, s, i0, l);
   } else if (l.w == 2) {
-    put4<3>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed(dots<T, DK>(k, 16, k, 0, l), s, 16, 0, false, 1.0f, l));
-    if constexpr (PARTS) put_p(16, 0);
+    const f32x4 d = decays(s, 16, 0, l);
+    put4<NS>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed<false>(dots<NS>(k, 16, k, 0, l), d, false, l));
+    if constexpr (PARTS) put4<PARTS>(to.p + (16 + l.n) * kPairStride + 4 * l.g, kPairPlane, decayed<false>(dots<PARTS>(*q, 16, k, 0, l), d * scale, false, l));
   } else if constexpr (PARTS != 0) {
-    put_p(0, 0);
-    put_p(16, 16);
+#pragma unroll
+    for (int i0 = 0; i0 < kDeltaRows; i0 += 16)
+      put4<PARTS>(to.p + (i0 + l.n) * kPairStride + i0 + 4 * l.g, kPairPlane,
+                  decayed<true>(dots<PARTS>(*q, i0, k, i0, l), decays(s, i0, i0, l) * scale, true, l));
   }
 }
 
@@ -527,10 +586,10 @@ enum DeltaMode {
   kDeltaBack         // what the gradients need: that of the state after each chunk, Z
 };
 
-template <typename T, int DK, int TV, int MODE>
+template <typename T, int DK, int TV, int MODE, bool EXACT>
 struct DeltaShared {
   static constexpr bool BACK = MODE >= kDeltaBackStates, QUERIES = MODE == kDeltaOut || BACK;
-  static constexpr int PARTS = MODE == kDeltaOut ? kOutParts<T> : BACK ? 3 : 0;
+  static constexpr int PARTS = MODE == kDeltaOut ? kOutParts<T> : BACK ? 3 : 0, NS = EXACT ? 3 : 2;
   static constexpr int BUFFERS = sizeof(T) == 2 && DK <= 64 && TV == 1 ? 2 : 1;
   Planes<T, DK> k[BUFFERS];
   Planes<T, QUERIES ? DK : 8> q[BUFFERS];
@@ -538,12 +597,13 @@ struct DeltaShared {
   Planes<T, BACK ? 64 * TV : 8> d[BUFFERS];
   Values<T, MODE == kDeltaOut ? 64 * TV : 8> out;
   Gates gates[BUFFERS];
-  Pairs<PARTS> pairs;
+  Pairs<NS, PARTS> pairs;
 };
 
-template <typename T, int DK, int TV, int MODE>
+template <typename T, int DK, int TV, int MODE, bool EXACT>
 __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV)) void delta_walk_kernel(DeltaArgs a) {
-  using Shared = DeltaShared<T, DK, TV, MODE>;
+  using Shared = DeltaShared<T, DK, TV, MODE, EXACT>;
+  constexpr int NS = Shared::NS;
   constexpr int NP = kPlanes<T>, OUT = kOutParts<T>, W = 64 * TV, BUFFERS = Shared::BUFFERS;
   constexpr bool BACK = Shared::BACK, QUERIES = Shared::QUERIES, STATES = MODE == kDeltaStates || MODE == kDeltaBackStates;
   __shared__ Shared sh;
@@ -572,10 +632,8 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
   if (map && !began) return;
   const int64_t each = (int64_t)a.kd * a.vd;
   const int hk = h / a.group;
-  const T* pk = static_cast<const T*>(a.k) + hk * a.k_head;
-  const T* pq = QUERIES ? static_cast<const T*>(a.q) + h * a.q_head : nullptr;
-  const T* pv = BACK ? static_cast<const T*>(a.dout) + h * a.d_head : static_cast<const T*>(a.v) + hk * a.v_head;
-  const int32_t v_row = BACK ? a.d_row : a.v_row;
+  const Source<T, DK> from_k(a.k, hk * a.k_head, a.k_row, a.kd), from_q(QUERIES ? a.q : a.k, QUERIES ? h * a.q_head : 0, a.q_row, a.kd);
+  const Source<T, W> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
   const bool own = col0 < columns;
 
   State<DK, TV> st;
@@ -609,9 +667,9 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
   Pack<T, 8> rk[kPacks<DK>], rq[kPacks<DK>], rv[kPacks<W>];
   float rg = 0.0f, rb = 0.0f;
   auto fetch = [&](int32_t s0) {
-    fetch_chunk<T, DK>(rk, pk, a.k_row, a.kd, s0, hi);
-    if constexpr (QUERIES) fetch_chunk<T, DK>(rq, pq, a.q_row, a.kd, s0, hi);
-    if (!map) fetch_chunk<T, W>(rv, pv, v_row, a.vd, s0, hi);
+    from_k.fetch(rk, s0, hi);
+    if constexpr (QUERIES) from_q.fetch(rq, s0, hi);
+    if (!map) from_v.fetch(rv, s0, hi);
     if (l.w == 3) {
       const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
       rg = a.log_decay[row * a.g_row + h];
@@ -657,7 +715,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     const bool more = c + 1 < chunks;
     const Gates& gates = sh.gates[b];
     if (more) fetch(next);
-    put_pairs<T, DK, Shared::PARTS>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b]), gates, a.scale, l);
+    put_pairs<T, DK, NS, Shared::PARTS>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b]), gates, a.scale, l);
 
     // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
     f32x4 ks[2][TV], qs[2][TV];
@@ -668,14 +726,14 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     if (own) {
 #pragma unroll
       for (int s = 0; s < DK / 32; ++s) {
-        Parts<3> x[TV];
+        Parts<NS> x[TV];
 #pragma unroll
-        for (int v = 0; v < TV; ++v) x[v] = split<3>(st[2 * s][v], st[2 * s + 1][v]);
+        for (int v = 0; v < TV; ++v) x[v] = split<NS>(st[2 * s][v], st[2 * s + 1][v]);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const Parts<NP> k = sh.k[b].rows(16 * t, 32 * s, l);
 #pragma unroll
-          for (int v = 0; v < TV; ++v) ks[t][v] = mma<3>(k, x[v], ks[t][v]);
+          for (int v = 0; v < TV; ++v) ks[t][v] = mma<NS>(k, x[v], ks[t][v]);
           if constexpr (MODE == kDeltaOut) {
             const Parts<NP> qr = sh.q[b].rows(16 * t, 32 * s, l);
 #pragma unroll
@@ -724,8 +782,8 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
               for (int r = 0; r < 4; ++r) e[t][v][r] = __builtin_fmaf(-fade[t][r], ks[t][v][r], x[r]);
             }
         }
-        const Block first = block_of<BACK>(sh.pairs.n[F], l), cross = block_of<BACK>(sh.pairs.n[2], l),
-                    last = block_of<BACK>(sh.pairs.n[L], l);
+        const Block<NS> first = block_of<NS, BACK>(sh.pairs.n[F], l), cross = block_of<NS, BACK>(sh.pairs.n[2], l),
+                        last = block_of<NS, BACK>(sh.pairs.n[L], l);
 #pragma unroll
         for (int v = 0; v < TV; ++v) {
           e[F][v] = mma_block(first, beta[F] * e[F][v], e[F][v]);
@@ -764,7 +822,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
         }
       }
       // the state after the chunk (backwards: its gradient before it)
-      Parts<3> x[TV], y[TV];
+      Parts<NS> x[TV], y[TV];
 #pragma unroll
       for (int v = 0; v < TV; ++v) {
         if constexpr (BACK) {
@@ -776,10 +834,10 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
             for (int p = 0; p < NP; ++p) f[i] += (float)dout[v].p[p][i];
             f[i] *= fade[i / 4][i % 4] * a.scale;
           }
-          y[v] = split<3>(f);
-          x[v] = split<3>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
+          y[v] = split<NS>(f);
+          x[v] = split<NS>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
         } else {
-          x[v] = split<3>(left[0] * beta[0] * e[0][v], left[1] * beta[1] * e[1][v]);
+          x[v] = split<NS>(left[0] * beta[0] * e[0][v], left[1] * beta[1] * e[1][v]);
         }
       }
 #pragma unroll
@@ -787,11 +845,11 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
         const int c0 = 32 * (t / 2) + 4 * (t % 2);
         const Parts<NP> k = sh.k[b].template columns<8>(c0, l);
 #pragma unroll
-        for (int v = 0; v < TV; ++v) st[t][v] = mma<3>(k, x[v], st[t][v] * whole);
+        for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(k, x[v], st[t][v] * whole);
         if constexpr (BACK) {
           const Parts<NP> qc = sh.q[b].template columns<8>(c0, l);
 #pragma unroll
-          for (int v = 0; v < TV; ++v) st[t][v] = mma<3>(qc, y[v], st[t][v]);
+          for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(qc, y[v], st[t][v]);
         }
       }
     }
@@ -904,7 +962,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
     sh.a[at] = sh.f[at] = (bf16)0.0f;
   }
   Pack<T, 8> rk[kPacks<DK>];
-  fetch_chunk<T, DK>(rk, static_cast<const T*>(a.k) + hk * a.k_head, a.k_row, a.kd, s0, hi);
+  Source<T, DK>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
   float dv[kPacks<W>][8];
   f32x4 dk[2][TD];
 #pragma unroll
@@ -921,10 +979,10 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
     {
       Pack<T, 8> rq[kPacks<DK>], rd[kPacks<W>];
       Pack<float, 8> re[kPacks<W>], rz[kPacks<W>];
-      fetch_chunk<T, DK>(rq, static_cast<const T*>(a.q) + h * a.q_head, a.q_row, a.kd, s0, hi);
-      fetch_chunk<T, W>(rd, static_cast<const T*>(a.dout) + h * a.d_head, a.d_row, a.vd, s0, hi);
-      fetch_chunk<float, W>(re, a.left_over + h * a.vd, a.H * a.vd, a.vd, s0, hi);
-      fetch_chunk<float, W>(rz, a.due + h * a.vd, a.H * a.vd, a.vd, s0, hi);
+      Source<T, DK>(a.q, h * a.q_head, a.q_row, a.kd).fetch(rq, s0, hi);
+      Source<T, W>(a.dout, h * a.d_head, a.d_row, a.vd).fetch(rd, s0, hi);
+      Source<float, W>(a.left_over, h * a.vd, a.H * a.vd, a.vd).fetch(re, s0, hi);
+      Source<float, W>(a.due, h * a.vd, a.H * a.vd, a.vd).fetch(rz, s0, hi);
       float g = 0.0f, beta = 0.0f;
       if (l.w == 3 && (int)(threadIdx.x & 31) < n) {
         const int64_t row = s0 + (int)(threadIdx.x & 31);
@@ -969,7 +1027,9 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
         const Parts<3> u = sh.u.rows(j0, 32 * s, l);
         x = results ? mma<3>(u, sh.d.rows(i0, 32 * s, l), x) : mma<3>(u, sh.y.rows(i0, 32 * s, l), x);
       }
-      x = decayed(x, gates, i0, j0, results, results ? a.scale : 1.0f, l);
+      f32x4 d = decays(gates, i0, j0, l);
+      if (results) d = d * a.scale;
+      x = i0 == j0 ? decayed<true>(x, d, results, l) : decayed<false>(x, d, results, l);
       put4<3>((results ? sh.a : sh.f) + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, x);
     };
     if (l.w < 2) {
@@ -1103,13 +1163,13 @@ void with_dims(int kd, int vd, F&& f) {
   kd <= 32 ? values(std::integral_constant<int, 32>{}) : kd <= 64 ? values(std::integral_constant<int, 64>{}) : values(std::integral_constant<int, 128>{});
 }
 
-template <typename T, int MODE>
+template <typename T, int MODE, bool EXACT = true>
 hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
   with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
     constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
     constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
     const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H), MODE == kDeltaStates ? 1 + (a.kd + 64 * TV - 1) / (64 * TV) : 1);
-    hipLaunchKernelGGL((delta_walk_kernel<T, DK, TV, MODE>), grid, dim3(kDeltaThreads), 0, st, a);
+    hipLaunchKernelGGL((delta_walk_kernel<T, DK, TV, MODE, EXACT>), grid, dim3(kDeltaThreads), 0, st, a);
   });
   return hipGetLastError();
 }
@@ -1126,6 +1186,8 @@ hipError_t grad_of(const DeltaGradArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t delta_walk(const DeltaArgs& a, int mode, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (!a.exact) return mode == kDeltaStates ? walk_of<T, kDeltaStates, false>(a, st) : walk_of<T, kDeltaOut, false>(a, st);
   switch (mode) {
     case kDeltaStates: return walk_of<T, kDeltaStates>(a, st);
     case kDeltaOut: return walk_of<T, kDeltaOut>(a, st);
