@@ -13,91 +13,164 @@ namespace {
 // a part that does not begin its sequence was walked from nothing, and what it
 // does to a state was found beside that, so
 //   S_e = M_e S_(e-1) + B_e,  backwards  D_e = M_(e+1)^T D_(e+1) + B'_e.
-// A workgroup has 16 columns; its waves take 16 rows of a product each and pass
-// the state on through LDS.  The next boundary's matrices are loaded before
-// this one's product.
+// One boundary after the other, each a product behind its matrix's load, would
+// take longer than the walks (a keyframe's 95: 97 us; 126 of heads of 128,
+// backwards: 1,530).  So the boundaries are taken in runs, all at once, each
+// from nothing together with what the run up to there does to a state (the
+// same recurrence from the unit matrix); then the runs' ends are carried on;
+// and the walk that begins at a boundary adds the product with the end of the
+// run before (add_mapped).
+// A workgroup has 16 columns of B or of the map; its waves take 16 rows of a
+// product each and pass the result on through LDS.  The next boundary's
+// matrices are loaded before this one's product.
 constexpr int kJoinTile = 16;
 
-template <int DK, bool BACK>
-__device__ __forceinline__ void join(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)]) {
+// A boundary's part of the recurrence: X = map X + add, or X = add.
+struct Link {
+  const float *map, *add;
+  float* to;
+  bool there, carries;
+};
+
+// X goes from link to link, from what `first` says: nothing (0), the unit matrix (1).  link(i) is the i-th.
+template <int DK, typename F>
+__device__ __forceinline__ void carry_on(bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)], int count, int col, int kd, int columns, bool unit, F&& link) {
   constexpr int STRIDE = DK + kPlanePad, PLANE = kJoinTile * STRIDE, TD = DK >= 64 ? DK / 64 : 1, STEPS = DK / 32;
   const Lane l = lane_of();
-  const int h = blockIdx.y, col = blockIdx.x * kJoinTile + l.n;
-  const int64_t each = (int64_t)a.kd * a.vd, square = (int64_t)a.kd * a.kd;
-  float* state = (BACK ? a.cut_grad : a.cut_state) + h * each;
   const bool own = 16 * TD * l.w < DK;
-  const int last = a.cuts - 1;
   struct Next {
     float m[TD][STEPS][8];
     f32x4 b[TD];
-    int32_t kind;  // of the boundary, and of the part whose map is there
-    bool carries;
+    Link link;
   };
-  auto fetch = [&](Next& x, int i) {  // the i-th boundary of the walk
-    const int e = BACK ? last - i : i, part = BACK ? e + 1 : e;
-    x.kind = a.cut_kind[e];
-    x.carries = part <= last && a.cut_kind[min(part, last)] == 1;
-    const float* m = a.cut_map + ((int64_t)min(part, last) * a.H + h) * square;
-    const float* b = state + (int64_t)e * a.H * each;
+  auto fetch = [&](Next& x, int i) {
+    x.link = link(i);
 #pragma unroll
     for (int d = 0; d < TD; ++d) {
       const int row0 = 16 * (l.w * TD + d);
+      x.b[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (x.link.there && x.link.add) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x.b[d][r] = b[min(row0 + 4 * l.g + r, a.kd - 1) * a.vd + min(col, a.vd - 1)];
-      if (!x.carries) continue;
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        if constexpr (BACK) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int row = 32 * s + 8 * l.g + k, c = row0 + l.n;
-            const float v = m[min(row, a.kd - 1) * a.kd + min(c, a.kd - 1)];
-            x.m[d][s][k] = row < a.kd && c < a.kd ? v : 0.0f;
-          }
-        } else {
-          load_eight(x.m[d][s], m, row0 + l.n, 32 * s + 8 * l.g, a.kd, a.kd);
-        }
+        for (int r = 0; r < 4; ++r) x.b[d][r] = x.link.add[min(row0 + 4 * l.g + r, kd - 1) * columns + min(col + l.n, columns - 1)];
       }
+      if (!x.link.carries) continue;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) load_eight(x.m[d][s], x.link.map, row0 + l.n, 32 * s + 8 * l.g, kd, kd);
     }
   };
   Next now, next;
-  if (own) fetch(now, 0);
-  int turn = 0;
-  for (int i = 0; i <= last; ++i, turn ^= 1) {
-    if (own && i < last) fetch(next, i + 1);
+  if (own) {
+    // the start
+#pragma unroll
+    for (int d = 0; d < TD; ++d) {
+      const int row = 16 * (l.w * TD + d) + 4 * l.g;
+      f32x4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = unit && row + r == col + l.n ? 1.0f : 0.0f;
+      put4<3>(s_x[1] + l.n * STRIDE + row, PLANE, x);
+    }
+    fetch(now, 0);
+  }
+  __syncthreads();
+  for (int i = 0; i < count; ++i) {
+    const int turn = i & 1;
     if (own) {
-      const int e = BACK ? last - i : i;
+      if (i + 1 < count) fetch(next, i + 1);
 #pragma unroll
       for (int d = 0; d < TD; ++d) {
         const int row = 16 * (l.w * TD + d) + 4 * l.g;
         f32x4 x;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = row + r < a.kd && col < a.vd && now.kind >= 0 ? now.b[d][r] : 0.0f;
-        if (now.kind >= 0 && now.carries && i > 0) {
+        for (int r = 0; r < 4; ++r) x[r] = row + r < kd && col + l.n < columns ? now.b[d][r] : 0.0f;
+        if (now.link.carries) {
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) x = mma<3>(split<3>(now.m[d][s]), rows_of<3>(s_x[turn ^ 1], PLANE, STRIDE, 0, 32 * s, l), x);
+        }
+        if (now.link.there && now.link.to) {
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (row + r < a.kd && col < a.vd) state[(int64_t)e * a.H * each + (row + r) * a.vd + col] = x[r];
+            if (row + r < kd && col + l.n < columns) now.link.to[(row + r) * columns + col + l.n] = x[r];
         }
         put4<3>(s_x[turn] + l.n * STRIDE + row, PLANE, x);
       }
+      now = next;
     }
     __syncthreads();
-    now = next;
   }
+}
+
+// Up to 64 links' flags, lane i of a wave the i-th's, known to all of them.
+struct Flags {
+  uint64_t there, carries;
+  __device__ __forceinline__ bool is_there(int i) const { return there >> i & 1; }
+  __device__ __forceinline__ bool do_carry(int i) const { return carries >> i & 1; }
+};
+
+template <int DK, bool BACK>
+__device__ __forceinline__ void join_run(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)], int run, int tile, int h) {
+  const int64_t each = (int64_t)a.kd * a.vd, square = (int64_t)a.kd * a.kd;
+  const int tiles = (a.vd + kJoinTile - 1) / kJoinTile, first = run * a.run, count = min(a.run, a.cuts - first);
+  const bool map = tile >= tiles;
+  float* state = BACK ? a.cut_grad : a.cut_state;
+  const float* maps = BACK ? a.cut_turned : a.cut_map;
+  auto boundary = [&](int i) { return BACK ? first + count - 1 - i : first + i; };
+  auto coming_in = [&](int e) { return BACK ? min(e + 1, a.cuts - 1) : e; };  // the part whose map comes in
+  const int i = min((int)threadIdx.x & 63, count - 1), e = boundary(i);
+  const bool there = a.cut_kind[e] >= 0, carries = there && a.cut_kind[coming_in(e)] == 1 && !(BACK && e + 1 == a.cuts);
+  const Flags f = {__ballot(there), __ballot(carries)};
+  // boundaries up to the first that does not carry come from the run before
+  const int open = min(f.carries == ~0ull ? 64 : __builtin_ctzll(~f.carries), count);
+  if (h == 0 && tile == 0 && (int)threadIdx.x < count) a.from_run[BACK][e] = i < open;
+  if (map && open == 0) return;
+  carry_on<DK>(s_x, map ? open : count, (map ? tile - tiles : tile) * kJoinTile, a.kd, map ? a.kd : a.vd, map, [&](int i) {
+    const int64_t at = (int64_t)boundary(i) * a.H + h;
+    float* place = map ? a.run_map[BACK] + at * square : state + at * each;
+    return Link{maps + ((int64_t)coming_in(boundary(i)) * a.H + h) * square, map ? nullptr : place, place, f.is_there(i), f.do_carry(i) && (map || i > 0)};
+  });
 }
 
 template <int DK>
 __global__ __launch_bounds__(kDeltaThreads) void delta_join_kernel(DeltaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
-  blockIdx.z == 0 ? join<DK, false>(a, s_x) : join<DK, true>(a, s_x);
+  const int runs = (a.cuts + a.run - 1) / a.run;
+  if ((int)blockIdx.z < runs)
+    join_run<DK, false>(a, s_x, blockIdx.z, blockIdx.x, blockIdx.y);
+  else
+    join_run<DK, true>(a, s_x, blockIdx.z - runs, blockIdx.x, blockIdx.y);
+}
+
+// The runs' ends.
+template <int DK, bool BACK>
+__device__ __forceinline__ void join_ends(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)]) {
+  const int h = blockIdx.y, runs = (a.cuts + a.run - 1) / a.run;
+  const int64_t each = (int64_t)a.kd * a.vd, square = (int64_t)a.kd * a.kd;
+  auto run_of = [&](int i) { return BACK ? runs - 1 - i : i; };
+  auto boundary = [&](int i) { return BACK ? run_of(i) * a.run : min((run_of(i) + 1) * a.run, a.cuts) - 1; };
+  const int e = boundary(min((int)threadIdx.x & 63, runs - 1));
+  const bool there = a.cut_kind[e] >= 0;
+  const Flags f = {__ballot(there), __ballot(there && a.from_run[BACK][e])};
+  carry_on<DK>(s_x, runs, blockIdx.x * kJoinTile, a.kd, a.vd, false, [&](int i) {
+    const int64_t at = (int64_t)boundary(i) * a.H + h;
+    return Link{a.run_map[BACK] + at * square, (BACK ? a.cut_grad : a.cut_state) + at * each, a.run_end[BACK] + ((int64_t)run_of(i) * a.H + h) * each,
+                f.is_there(i), f.do_carry(i) && i > 0};
+  });
+}
+
+template <int DK>
+__global__ __launch_bounds__(kDeltaThreads) void delta_ends_kernel(DeltaArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
+  blockIdx.z == 0 ? join_ends<DK, false>(a, s_x) : join_ends<DK, true>(a, s_x);
 }
 
 hipError_t join_states(const DeltaArgs& a, bool backward, hipStream_t st) {
-  const dim3 grid((a.vd + kJoinTile - 1) / kJoinTile, a.H, backward ? 2 : 1), block(kDeltaThreads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  a.kd <= 32 ? go(delta_join_kernel<32>) : a.kd <= 64 ? go(delta_join_kernel<64>) : go(delta_join_kernel<128>);
+  const int tiles = (a.vd + kJoinTile - 1) / kJoinTile, map_tiles = (a.kd + kJoinTile - 1) / kJoinTile, runs = (a.cuts + a.run - 1) / a.run;
+  auto go = [&](auto join, auto ends) {
+    hipLaunchKernelGGL(join, dim3(tiles + map_tiles, a.H, runs * (backward ? 2 : 1)), dim3(kDeltaThreads), 0, st, a);
+    hipLaunchKernelGGL(ends, dim3(tiles, a.H, backward ? 2 : 1), dim3(kDeltaThreads), 0, st, a);
+  };
+  a.kd <= 32   ? go(delta_join_kernel<32>, delta_ends_kernel<32>)
+  : a.kd <= 64 ? go(delta_join_kernel<64>, delta_ends_kernel<64>)
+               : go(delta_join_kernel<128>, delta_ends_kernel<128>);
   return hipGetLastError();
 }
 

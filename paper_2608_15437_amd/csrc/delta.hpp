@@ -571,6 +571,50 @@ __device__ __forceinline__ void store_state(float* to, const State<DK, TV>& st, 
       }
 }
 
+// Rows of fp32 in global memory as an operand: row `row`, elements c .. c+7; zeros past the matrix.
+__device__ __forceinline__ void load_eight(float (&x)[8], const float* p, int row, int c, int rows, int columns) {
+  const bool there = row < rows;
+  const float* from = p + (int64_t)(there ? row : 0) * columns;
+  if (columns % 8 == 0) {
+    const Pack<float, 8> t = load_pack<float, 8>(from + (c < columns ? c : 0));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = there && c < columns ? t.v[e] : 0.0f;
+  } else {
+    const Pack<float, 8> t = load_some<float, 8>(from + c, columns - c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = there ? t.v[e] : 0.0f;
+  }
+}
+
+// st += map * from, both in global memory: map [kd][kd], from [kd][vd].
+template <int DK, int TV>
+__device__ __forceinline__ void add_mapped(State<DK, TV>& st, const float* map, const float* from, int kd, int vd, int col0, const Lane& l) {
+#pragma unroll
+  for (int s = 0; s < DK / 32; ++s) {
+    Parts<3> x[TV];
+#pragma unroll
+    for (int v = 0; v < TV; ++v) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = 32 * s + 8 * l.g + e, col = col0 + 16 * v + l.n;
+        y[e] = from[min(row, kd - 1) * vd + min(col, vd - 1)];
+        y[e] = row < kd && col < vd ? y[e] : 0.0f;
+      }
+      x[v] = split<3>(y);
+    }
+#pragma unroll
+    for (int t = 0; t < DK / 16; ++t) {
+      float m[8];
+      // lane n has the row that comes out in its place of the state
+      load_eight(m, map, 32 * (t / 2) + 8 * (l.n >> 2) + 4 * (t % 2) + (l.n & 3), 32 * s + 8 * l.g, kd, kd);
+      const Parts<3> p = split<3>(m);
+#pragma unroll
+      for (int v = 0; v < TV; ++v) st[t][v] = mma<3>(p, x[v], st[t][v]);
+    }
+  }
+}
+
 // ------------------------------------------------------ the walks
 
 // Where a chunk's states are kept: a sequence's chunks from its first row / 32 + its number on.
@@ -648,6 +692,13 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     else
       from = began ? a.cut_state + ((int64_t)(boundary - 1) * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
     load_state<DK, TV>(st, map ? nullptr : from, a.kd, columns, col0, l);
+    if constexpr (!STATES) {
+      // the end of the run of boundaries before
+      const int e = BACK ? boundary : boundary - 1, run = BACK ? e / a.run + 1 : e / a.run - 1;
+      if ((BACK ? goes_on : began) && own && a.from_run[BACK][e] && run >= 0 && run * a.run < a.cuts)
+        add_mapped<DK, TV>(st, a.run_map[BACK] + ((int64_t)e * a.H + h) * a.kd * a.kd, a.run_end[BACK] + ((int64_t)run * a.H + h) * each, a.kd,
+                           a.vd, col0, l);
+    }
     if (map) {
 #pragma unroll
       for (int t = 0; t < DK / 16; ++t)
@@ -863,9 +914,21 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
   }
   if (!own) return;
   if constexpr (STATES) {
-    if (map)
-      store_state<DK, TV>(a.cut_map + ((int64_t)unit * a.H + h) * a.kd * a.kd, st, a.kd, a.kd, col0, l);
-    else
+    if (map) {
+      const int64_t at = ((int64_t)unit * a.H + h) * a.kd * a.kd;
+      store_state<DK, TV>(a.cut_map + at, st, a.kd, a.kd, col0, l);
+      if (a.cut_grad) {
+#pragma unroll
+        for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+          for (int v = 0; v < TV; ++v)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int row = state_row(t, r, l), col = col0 + 16 * v + l.n;
+              if (row < a.kd && col < a.kd) a.cut_turned[at + col * a.kd + row] = st[t][v][r];
+            }
+      }
+    } else
       store_state<DK, TV>((BACK ? a.cut_grad : a.cut_state) + ((int64_t)unit * a.H + h) * each, st, a.kd, a.vd, col0, l);
   } else {
     if ((BACK ? !began : !goes_on) && a.final_state)
@@ -897,21 +960,6 @@ struct DeltaGradShared {
   float own[4][kDeltaRows], end[4][kDeltaRows];  // a wave's part of dG and of kd
   float both[4];                                 // of <D, S>
 };
-
-// Rows of fp32 in global memory as an operand: row `row`, elements c .. c+7; zeros past the matrix.
-__device__ __forceinline__ void load_eight(float (&x)[8], const float* p, int row, int c, int rows, int columns) {
-  const bool there = row < rows;
-  const float* from = p + (int64_t)(there ? row : 0) * columns;
-  if (columns % 8 == 0) {
-    const Pack<float, 8> t = load_pack<float, 8>(from + (c < columns ? c : 0));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = there && c < columns ? t.v[e] : 0.0f;
-  } else {
-    const Pack<float, 8> t = load_some<float, 8>(from + c, columns - c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = there ? t.v[e] : 0.0f;
-  }
-}
 
 // Sum over the four lane groups of the same lane % 16, known to all.
 __device__ __forceinline__ float groups_sum(float x) {

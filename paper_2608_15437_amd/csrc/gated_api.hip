@@ -83,8 +83,9 @@ constexpr int32_t kDeltaCutSequences = 1024;
 
 struct DeltaPlan {
   int64_t slots;  // workgroups that the chip takes at once
-  int32_t cuts;
-  size_t off_state, off_map, off_grad, off_before, off_after, off_left, off_due, total;  // cut_kind lies first
+  int32_t cuts, run;
+  // (cut_kind lies first)
+  size_t off_from[2], off_state, off_map, off_run[2], off_end[2], off_grad, off_turned, off_before, off_after, off_left, off_due, total;
 };
 
 mmbev_status_t delta_ok(const mmbev_attention_t* t, bool step) {
@@ -109,16 +110,26 @@ DeltaPlan delta_plan(const mmbev_attention_t* t, bool backward) {
     const int64_t parts = units - std::min<int64_t>(t->num_sequences, units / 2);
     p.cuts = (int32_t)std::max<int64_t>(1, std::min(parts, (t->rows + kDeltaLeast - 1) / kDeltaLeast));
   }
-  const size_t state = (size_t)t->heads * t->key_dim * t->value_dim * 4;
+  // steps one after the other: a run's boundaries and the runs
+  p.run = 1;
+  while (p.run * p.run < p.cuts) ++p.run;
+  const size_t state = (size_t)t->heads * t->key_dim * t->value_dim * 4, maps = (size_t)p.cuts * t->heads * t->key_dim * t->key_dim * 4;
+  const size_t runs = (p.cuts + p.run - 1) / p.run;
   size_t at = align256((size_t)p.cuts * 4);
   auto take = [&](size_t bytes) {
     const size_t from = at;
     at = align256(at + bytes);
     return from;
   };
+  for (int i = 0; i < (backward ? 2 : 1); ++i) {
+    p.off_from[i] = take((size_t)p.cuts * 4);
+    p.off_run[i] = take(maps);
+    p.off_end[i] = take(runs * state);
+  }
   p.off_state = take(p.cuts * state);
-  p.off_map = take((size_t)p.cuts * t->heads * t->key_dim * t->key_dim * 4);
+  p.off_map = take(maps);
   if (backward) {
+    p.off_turned = take(maps);
     const size_t chunks = (size_t)delta_slots(t->rows, t->num_sequences), rows = (size_t)t->rows * t->heads * t->value_dim * 4;
     p.off_grad = take(p.cuts * state);
     p.off_before = take(chunks * state);
@@ -189,6 +200,12 @@ void put_delta(DeltaArgs& a, const mmbev_attention_t* t, const mmbev_heads_t& q,
   a.cut_kind = (int32_t*)ws;
   a.cut_state = (float*)(ws + p.off_state);
   a.cut_map = (float*)(ws + p.off_map);
+  a.run = p.run;
+  for (int i = 0; i < 2; ++i) {
+    a.from_run[i] = (int32_t*)(ws + p.off_from[i]);
+    a.run_map[i] = (float*)(ws + p.off_run[i]);
+    a.run_end[i] = (float*)(ws + p.off_end[i]);
+  }
 }
 
 }  // namespace
@@ -335,6 +352,7 @@ mmbev_status_t mmbev_gated_delta_backward(const mmbev_attention_t* t, mmbev_head
   a.exact = 1;
   a.fault = fault;
   a.cut_grad = (float*)(ws + p.off_grad);
+  a.cut_turned = (float*)(ws + p.off_turned);
   a.before = (float*)(ws + p.off_before);
   a.after = (float*)(ws + p.off_after);
   a.left_over = (float*)(ws + p.off_left);

@@ -217,8 +217,15 @@ struct DeltaArgs : Ranges {
   // boundaries between parts of a cut sequence: kind -1: there is none, 0: the part before it begins its sequence, 1: it does not
   int32_t* cut_kind;      // [cuts]
   float* cut_state;       // [cuts][H][kd][vd]: the state at the boundary
-  float* cut_grad;        // its gradient
+  float* cut_grad;        // its gradient; null: forwards alone
   float* cut_map;         // [cuts][H][kd][kd]: what the part before it does to the state before that part, where kind is 1
+  float* cut_turned;      // its transpose (with cut_grad)
+  // Boundaries are joined in runs of `run`: [0] forwards, [1] backwards.  Where from_run is set, what lies at a boundary
+  // has run_map times the state at the end of the run before it yet to come.
+  int32_t run;
+  int32_t* from_run[2];   // [cuts]
+  float* run_map[2];      // [cuts][H][kd][kd]
+  float* run_end[2];      // [runs][H][kd][vd]: the state at a run's last boundary, backwards the gradient at its first
   // the gradients' chunks
   float* before;          // [slots][H][kd][vd]: the state before a chunk
   float* after;           // the gradient of the state after it
