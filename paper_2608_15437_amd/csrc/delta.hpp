@@ -303,32 +303,31 @@ template <int W>
 constexpr int kPacks = W >= 64 ? kDeltaRows * W / 8 / kDeltaThreads : 1;
 
 // An operand's rows as a thread reads them.  Every load is of an element that
-// is there; what is past the rows or the row's end is zeroed on the way into LDS.
-template <typename T, int W>
+// is there, unconditional where the dim is a multiple of eight (WHOLE: a load
+// under a condition is waited for where the paths meet); what is past the rows
+// or the row's end is zeroed on the way into LDS.
+template <typename T, int W, bool WHOLE>
 struct Source {
-  const T* p;  // of the thread's first pack in the chunk at row 0
+  const T* p;  // row 0, the thread's columns
   int64_t stride;
   int dim;
   static constexpr int kRowsApart = kDeltaThreads / (W / 8);
 
   __device__ __forceinline__ Source(const void* data, int64_t head, int32_t row_stride, int columns) : stride(row_stride), dim(columns) {
     const int c = threadIdx.x % (W / 8) * 8;
-    p = static_cast<const T*>(data) + head + row() * stride + (c < dim ? c : 0);
+    p = static_cast<const T*>(data) + head + (c < dim ? c : 0);
   }
-  static __device__ __forceinline__ int row() { return threadIdx.x / (W / 8); }
   __device__ __forceinline__ void fetch(Pack<T, 8> (&r)[kPacks<W>], int32_t s0, int32_t hi) const {
-    const bool whole = hi - s0 >= kDeltaRows && W >= 64;
-    const int left = dim - (int)(threadIdx.x % (W / 8)) * 8;
+    const T* chunk = p + s0 * stride;
 #pragma unroll
     for (int i = 0; i < kPacks<W>; ++i) {
       // (rows past the last one are its copies)
-      const int at = row() + i * kRowsApart;
-      const int64_t up = whole ? s0 + i * kRowsApart : (int64_t)min(s0 + at, hi - 1) - row();
-      const T* from = p + up * stride;
-      if (dim % 8 == 0)
+      const uint32_t row = min((int)threadIdx.x / (W / 8) + i * kRowsApart, hi - s0 - 1);
+      const T* from = chunk + (uint64_t)row * (uint32_t)stride;
+      if constexpr (WHOLE)
         r[i] = load_pack<T, 8>(from);
       else
-        r[i] = load_some<T, 8>(from, left);
+        r[i] = load_some<T, 8>(from, dim - (int)(threadIdx.x % (W / 8)) * 8);
     }
   }
 };
@@ -644,7 +643,7 @@ struct DeltaShared {
   Pairs<NS, PARTS> pairs;
 };
 
-template <typename T, int DK, int TV, int MODE, bool EXACT>
+template <typename T, int DK, int TV, int MODE, bool EXACT, bool WHOLE>
 __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV)) void delta_walk_kernel(DeltaArgs a) {
   using Shared = DeltaShared<T, DK, TV, MODE, EXACT>;
   constexpr int NS = Shared::NS;
@@ -676,8 +675,8 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
   if (map && !began) return;
   const int64_t each = (int64_t)a.kd * a.vd;
   const int hk = h / a.group;
-  const Source<T, DK> from_k(a.k, hk * a.k_head, a.k_row, a.kd), from_q(QUERIES ? a.q : a.k, QUERIES ? h * a.q_head : 0, a.q_row, a.kd);
-  const Source<T, W> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
+  const Source<T, DK, WHOLE> from_k(a.k, hk * a.k_head, a.k_row, a.kd), from_q(QUERIES ? a.q : a.k, QUERIES ? h * a.q_head : 0, a.q_row, a.kd);
+  const Source<T, W, WHOLE> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
   const bool own = col0 < columns;
 
   State<DK, TV> st;
@@ -708,6 +707,12 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
           for (int r = 0; r < 4; ++r) st[t][v][r] = state_row(t, r, l) == col0 + 16 * v + l.n ? 1.0f : 0.0f;
     }
   }
+
+  // arrived: else its first use in the loop would wait, in every round, for all loads that are on their way by then
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v) asm volatile("" : "+v"(st[t][v]));
 
   if constexpr (Shared::PARTS != 0) {
     // the first rows have nothing of the last ones
@@ -761,11 +766,12 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     __syncthreads();
   }
   for (int c = 0; c < chunks; ++c) {
-    const int32_t s0 = lo + (BACK ? chunks - 1 - c : c) * kDeltaRows, next = BACK ? s0 - kDeltaRows : s0 + kDeltaRows;
+    const int32_t s0 = lo + (BACK ? chunks - 1 - c : c) * kDeltaRows;
+    // (the last chunk is read twice: loads under a condition would be waited for together with the results' stores)
+    const int32_t next = c + 1 == chunks ? s0 : BACK ? s0 - kDeltaRows : s0 + kDeltaRows;
     const int b = BUFFERS == 2 ? c & 1 : 0;
-    const bool more = c + 1 < chunks;
     const Gates& gates = sh.gates[b];
-    if (more) fetch(next);
+    fetch(next);
     put_pairs<T, DK, NS, Shared::PARTS>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b]), gates, a.scale, l);
 
     // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
@@ -904,10 +910,10 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
         }
       }
     }
-    if (BUFFERS == 2 && more) put(next, b ^ 1);
+    if (BUFFERS == 2) put(next, b ^ 1);
     __syncthreads();  // the results are there, the chunk has been read
     store_out(s0);
-    if (BUFFERS == 1 && more) {
+    if (BUFFERS == 1) {
       put(next, 0);
       __syncthreads();
     }
@@ -992,7 +998,7 @@ __device__ __forceinline__ bool chunk_at(int64_t place, const Order& o, int32_t&
   return begin >= lo && begin < hi;
 }
 
-template <typename T, int DK, int TV>
+template <typename T, int DK, int TV, bool WHOLE>
 __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
   constexpr int NP = kPlanes<T>, W = 64 * TV, TD = DK >= 64 ? DK / 64 : 1, PER = W / 8;
   __shared__ DeltaGradShared<T, DK, TV> sh;
@@ -1010,7 +1016,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
     sh.a[at] = sh.f[at] = (bf16)0.0f;
   }
   Pack<T, 8> rk[kPacks<DK>];
-  Source<T, DK>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
+  Source<T, DK, WHOLE>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
   float dv[kPacks<W>][8];
   f32x4 dk[2][TD];
 #pragma unroll
@@ -1027,10 +1033,10 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
     {
       Pack<T, 8> rq[kPacks<DK>], rd[kPacks<W>];
       Pack<float, 8> re[kPacks<W>], rz[kPacks<W>];
-      Source<T, DK>(a.q, h * a.q_head, a.q_row, a.kd).fetch(rq, s0, hi);
-      Source<T, W>(a.dout, h * a.d_head, a.d_row, a.vd).fetch(rd, s0, hi);
-      Source<float, W>(a.left_over, h * a.vd, a.H * a.vd, a.vd).fetch(re, s0, hi);
-      Source<float, W>(a.due, h * a.vd, a.H * a.vd, a.vd).fetch(rz, s0, hi);
+      Source<T, DK, WHOLE>(a.q, h * a.q_head, a.q_row, a.kd).fetch(rq, s0, hi);
+      Source<T, W, WHOLE>(a.dout, h * a.d_head, a.d_row, a.vd).fetch(rd, s0, hi);
+      Source<float, W, WHOLE>(a.left_over, h * a.vd, a.H * a.vd, a.vd).fetch(re, s0, hi);
+      Source<float, W, WHOLE>(a.due, h * a.vd, a.H * a.vd, a.vd).fetch(rz, s0, hi);
       float g = 0.0f, beta = 0.0f;
       if (l.w == 3 && (int)(threadIdx.x & 31) < n) {
         const int64_t row = s0 + (int)(threadIdx.x & 31);
@@ -1211,13 +1217,16 @@ void with_dims(int kd, int vd, F&& f) {
   kd <= 32 ? values(std::integral_constant<int, 32>{}) : kd <= 64 ? values(std::integral_constant<int, 64>{}) : values(std::integral_constant<int, 128>{});
 }
 
+bool whole_packs(const DeltaArgs& a) { return a.kd % 8 == 0 && a.vd % 8 == 0; }
+
 template <typename T, int MODE, bool EXACT = true>
 hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
   with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
     constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
     constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
     const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H), MODE == kDeltaStates ? 1 + (a.kd + 64 * TV - 1) / (64 * TV) : 1);
-    hipLaunchKernelGGL((delta_walk_kernel<T, DK, TV, MODE, EXACT>), grid, dim3(kDeltaThreads), 0, st, a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDeltaThreads), 0, st, a); };
+    whole_packs(a) ? go(delta_walk_kernel<T, DK, TV, MODE, EXACT, true>) : go(delta_walk_kernel<T, DK, TV, MODE, EXACT, false>);
   });
   return hipGetLastError();
 }
@@ -1227,7 +1236,8 @@ hipError_t grad_of(const DeltaGradArgs& a, hipStream_t st) {
   with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
     constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
     const dim3 grid((uint32_t)(delta_slots(a.rows, a.B) * (a.H / a.group)));
-    hipLaunchKernelGGL((delta_grad_kernel<T, DK, TV>), grid, dim3(kDeltaThreads), 0, st, a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDeltaThreads), 0, st, a); };
+    whole_packs(a) ? go(delta_grad_kernel<T, DK, TV, true>) : go(delta_grad_kernel<T, DK, TV, false>);
   });
   return hipGetLastError();
 }
