@@ -23,7 +23,7 @@ namespace {
 // A workgroup has 16 columns of B or of the map; its waves take 16 rows of a
 // product each and pass the result on through LDS.  The next boundary's
 // matrices are loaded before this one's product.
-constexpr int kJoinTile = 16;
+constexpr int kJoinTile = 16, kJoinThreads = 256;
 
 // A boundary's part of the recurrence: X = map X + add, or X = add.
 struct Link {
@@ -130,7 +130,7 @@ __device__ __forceinline__ void join_run(const DeltaArgs& a, bf16 (*s_x)[3 * kJo
 }
 
 template <int DK>
-__global__ __launch_bounds__(kDeltaThreads) void delta_join_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void delta_join_kernel(DeltaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
   const int runs = (a.cuts + a.run - 1) / a.run;
   if ((int)blockIdx.z < runs)
@@ -157,7 +157,7 @@ __device__ __forceinline__ void join_ends(const DeltaArgs& a, bf16 (*s_x)[3 * kJ
 }
 
 template <int DK>
-__global__ __launch_bounds__(kDeltaThreads) void delta_ends_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void delta_ends_kernel(DeltaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
   blockIdx.z == 0 ? join_ends<DK, false>(a, s_x) : join_ends<DK, true>(a, s_x);
 }
@@ -165,8 +165,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_ends_kernel(DeltaArgs a) 
 hipError_t join_states(const DeltaArgs& a, bool backward, hipStream_t st) {
   const int tiles = (a.vd + kJoinTile - 1) / kJoinTile, map_tiles = (a.kd + kJoinTile - 1) / kJoinTile, runs = (a.cuts + a.run - 1) / a.run;
   auto go = [&](auto join, auto ends) {
-    hipLaunchKernelGGL(join, dim3(tiles + map_tiles, a.H, runs * (backward ? 2 : 1)), dim3(kDeltaThreads), 0, st, a);
-    hipLaunchKernelGGL(ends, dim3(tiles, a.H, backward ? 2 : 1), dim3(kDeltaThreads), 0, st, a);
+    hipLaunchKernelGGL(join, dim3(tiles + map_tiles, a.H, runs * (backward ? 2 : 1)), dim3(kJoinThreads), 0, st, a);
+    hipLaunchKernelGGL(ends, dim3(tiles, a.H, backward ? 2 : 1), dim3(kJoinThreads), 0, st, a);
   };
   a.kd <= 32   ? go(delta_join_kernel<32>, delta_ends_kernel<32>)
   : a.kd <= 64 ? go(delta_join_kernel<64>, delta_ends_kernel<64>)

@@ -30,13 +30,14 @@
 // enters a 16-bit result takes two parts, 16 bits.
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "sequence_parts.hpp"
 
 namespace mmbev {
 namespace {
 
-constexpr int kDeltaThreads = 256;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -134,6 +135,15 @@ __device__ __forceinline__ Parts<N> split(f32x4 x, f32x4 y) {
   return split<N>(z);
 }
 
+// The first N parts of two results as an operand.
+template <int N, int M>
+__device__ __forceinline__ Parts<N> both(const Quarter<M>& x, const Quarter<M>& y) {
+  Parts<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.p[i] = __builtin_shufflevector(x.p[i], y.p[i], 0, 1, 2, 3, 4, 5, 6, 7);
+  return r;
+}
+
 // Four values of an operand, in N parts N arrays of LDS apart.
 template <int N>
 __device__ __forceinline__ void put4(bf16* s, int plane, f32x4 x) {
@@ -213,8 +223,7 @@ __device__ __forceinline__ Block<N> block_of(const bf16* s, const Lane& l) {
 
 // c + block * x
 template <int N>
-__device__ __forceinline__ f32x4 mma_block(const Block<N>& a, f32x4 x, f32x4 c) {
-  const Quarter<N> q = split<N>(x);
+__device__ __forceinline__ f32x4 mma_block(const Block<N>& a, const Quarter<N>& q, f32x4 c) {
   if constexpr (N == 3)
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(q.p[2], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
   c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(q.p[1], q.p[1], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
@@ -233,7 +242,7 @@ __device__ __forceinline__ float exp2_of(float hi, float lo) {
 // two parts, multiples of 2^-10 (whose sums and differences are exact) and what
 // is left over, so that the decay between two rows has its last bits behind a
 // decay of any size too.
-struct Gates {
+struct alignas(16) Gates {
   float hi[kDeltaRows], lo[kDeltaRows];      // inclusive sums
   float beta[kDeltaRows];
   float fade[kDeltaRows], left[kDeltaRows];  // the decay from before the chunk to a row, and from a row to the chunk's end
@@ -268,8 +277,8 @@ __device__ __forceinline__ void base2_of(float g, float& step, float& rest) {
   rest = (x - step) + __builtin_fmaf(g, 1.44269504088896341f, -x) + g * 1.92596299e-8f;
 }
 
-// By one wave: lane r < 32 has row r's gates (0 past the rows).
-__device__ __forceinline__ void put_gates(Gates& s, float g, float beta) {
+// By one wave: lane r < 32 has row r's gates (0 past the rows).  `left` is multiplied by `times`.
+__device__ __forceinline__ void put_gates(Gates& s, float g, float beta, float times) {
   const int r = threadIdx.x & 63;
   float step, rest;
   base2_of(g, step, rest);
@@ -281,7 +290,7 @@ __device__ __forceinline__ void put_gates(Gates& s, float g, float beta) {
     s.lo[r] = lo;
     s.beta[r] = beta;
     s.fade[r] = fade;
-    s.left[r] = exp2_of(end_hi - hi, end_lo - lo);
+    s.left[r] = exp2_of(end_hi - hi, end_lo - lo) * times;
     if (r == kDeltaRows - 1) s.whole = fade;
   }
 }
@@ -298,31 +307,32 @@ template <typename T>
 constexpr int kRowPad = 16 / (int)sizeof(T);
 constexpr int kPlanePad = 8;
 
-// Eight elements of each of a chunk's 32 rows, W to a row, shared out among the threads.
-template <int W>
-constexpr int kPacks = W >= 64 ? kDeltaRows * W / 8 / kDeltaThreads : 1;
+// Eight elements of each of a chunk's 32 rows, W to a row, shared out among the threads of NW waves.
+template <int W, int NW>
+constexpr int kPacks = (kDeltaRows * W / 8 + 64 * NW - 1) / (64 * NW);
+template <int W, int NW>
+constexpr int kRowsApart = 64 * NW / (W / 8);  // of a thread's packs
 
 // An operand's rows as a thread reads them.  Every load is of an element that
 // is there, unconditional where the dim is a multiple of eight (WHOLE: a load
 // under a condition is waited for where the paths meet); what is past the rows
 // or the row's end is zeroed on the way into LDS.
-template <typename T, int W, bool WHOLE>
+template <typename T, int W, int NW, bool WHOLE>
 struct Source {
   const T* p;  // row 0, the thread's columns
   int64_t stride;
   int dim;
-  static constexpr int kRowsApart = kDeltaThreads / (W / 8);
 
   __device__ __forceinline__ Source(const void* data, int64_t head, int32_t row_stride, int columns) : stride(row_stride), dim(columns) {
     const int c = threadIdx.x % (W / 8) * 8;
     p = static_cast<const T*>(data) + head + (c < dim ? c : 0);
   }
-  __device__ __forceinline__ void fetch(Pack<T, 8> (&r)[kPacks<W>], int32_t s0, int32_t hi) const {
+  __device__ __forceinline__ void fetch(Pack<T, 8> (&r)[kPacks<W, NW>], int32_t s0, int32_t hi) const {
     const T* chunk = p + s0 * stride;
 #pragma unroll
-    for (int i = 0; i < kPacks<W>; ++i) {
+    for (int i = 0; i < kPacks<W, NW>; ++i) {
       // (rows past the last one are its copies)
-      const uint32_t row = min((int)threadIdx.x / (W / 8) + i * kRowsApart, hi - s0 - 1);
+      const uint32_t row = min((int)threadIdx.x / (W / 8) + i * kRowsApart<W, NW>, hi - s0 - 1);
       const T* from = chunk + (uint64_t)row * (uint32_t)stride;
       if constexpr (WHOLE)
         r[i] = load_pack<T, 8>(from);
@@ -333,21 +343,21 @@ struct Source {
 };
 
 // f(row, column, pack), zeros where there is nothing.
-template <typename T, int W, typename F>
-__device__ __forceinline__ void each_pack(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n, F&& f) {
-  const bool whole = n >= kDeltaRows && dim >= W;
+template <typename T, int W, int NW, typename F>
+__device__ __forceinline__ void each_pack(const Pack<T, 8> (&r)[kPacks<W, NW>], int dim, int n, F&& f) {
+  const int row = threadIdx.x / (W / 8), c = threadIdx.x % (W / 8) * 8;
 #pragma unroll
-  for (int i = 0; i < kPacks<W>; ++i) {
-    const int idx = threadIdx.x + i * kDeltaThreads, row = idx / (W / 8), c = idx % (W / 8) * 8;
-    if (W < 64 && row >= kDeltaRows) continue;
+  for (int i = 0; i < kPacks<W, NW>; ++i) {
+    if (kPacks<W, NW> * kRowsApart<W, NW> > kDeltaRows && row + i * kRowsApart<W, NW> >= kDeltaRows) continue;
     typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * 2)));
     words x = __builtin_bit_cast(words, r[i]);
-    if (!whole) {
-      const bool there = row < n && c < dim;
+    if (n < kDeltaRows || dim < W) {
+      const bool there = row + i * kRowsApart<W, NW> < n && c < dim;
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) * 2; ++e) x[e] = there ? x[e] : 0u;
+      asm volatile("");  // a branch over the selections: most chunks are whole
     }
-    f(row, c, __builtin_bit_cast(Pack<T, 8>, x));
+    f(row + i * kRowsApart<W, NW>, c, __builtin_bit_cast(Pack<T, 8>, x));
   }
 }
 
@@ -371,8 +381,9 @@ struct Planes {
   static constexpr int stride = W + kPlanePad, plane = kDeltaRows * stride;
   __attribute__((aligned(16))) bf16 v[kPlanes<T> * plane];
 
-  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n) {
-    each_pack<T, W>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { put_planes<kPlanes<T>, T>(v + row * stride + c, plane, x); });
+  template <int NW>
+  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W, NW>], int dim, int n) {
+    each_pack<T, W, NW>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { put_planes<kPlanes<T>, T>(v + row * stride + c, plane, x); });
   }
   __device__ __forceinline__ Parts<kPlanes<T>> rows(int row0, int c0, const Lane& l) const {
     return rows_of<kPlanes<T>>(v, plane, stride, row0, c0, l);
@@ -401,8 +412,9 @@ struct Values {
   static constexpr int stride = W + kRowPad<T>;
   __attribute__((aligned(16))) T v[kDeltaRows * stride];
 
-  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W>], int dim, int n) {
-    each_pack<T, W>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { __builtin_memcpy(__builtin_assume_aligned(v + row * stride + c, 16), &x, sizeof(x)); });
+  template <int NW>
+  __device__ __forceinline__ void put(const Pack<T, 8> (&r)[kPacks<W, NW>], int dim, int n) {
+    each_pack<T, W, NW>(r, dim, n, [&](int row, int c, const Pack<T, 8>& x) { __builtin_memcpy(__builtin_assume_aligned(v + row * stride + c, 16), &x, sizeof(x)); });
   }
   // column c0 + n of rows row0 + 4g ..
   __device__ __forceinline__ f32x4 down(int row0, int c0, const Lane& l) const {
@@ -421,30 +433,21 @@ struct Values {
   }
 };
 
-// Lane group G's value, known to all four of the same lane % 16.
-template <int G>
-__device__ __forceinline__ float from_group(float x) {
-  const unsigned i = __builtin_bit_cast(unsigned, x);
-  const auto p = __builtin_amdgcn_permlane32_swap(i, i, false, false);
-  const unsigned j = p[G >> 1];
-  const auto q = __builtin_amdgcn_permlane16_swap(j, j, false, false);
-  return __builtin_bit_cast(float, (unsigned)q[G & 1]);
-}
-
 // LDS order between lanes of one wave.
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
-// What the rows of a chunk do to each other: N and X in NS parts, P in PARTS.
-constexpr int kPairStride = kDeltaRows + kPlanePad, kPairPlane = kDeltaRows * kPairStride;
+// What the rows of a chunk do to each other, in NS parts (P: PARTS), with the rows' beta multiplied in: forwards that of
+// the row that is read (N beta, -X beta, P beta), backwards that of the row that reads (beta N, -beta X, P as it is).
+constexpr int kPairStride = kDeltaRows + 4, kPairPlane = kDeltaRows * kPairStride;
 
 template <int NS, int PARTS>
 struct Pairs {
-  __attribute__((aligned(16))) bf16 n[3][NS * kBlock];  // N of the first and last 16 rows, X of the last with the first
+  __attribute__((aligned(16))) bf16 n[3][NS * kBlock];  // N of the first and last 16 rows, -X of the last with the first
   __attribute__((aligned(16))) bf16 p[PARTS ? PARTS * kPairPlane : 8];
-  __attribute__((aligned(16))) float scratch[2][kBlock];
+  __attribute__((aligned(16))) float x[2][kBlock];      // X of the first and last 16 rows
 };
 
 // e^(G_i - G_j), lane n row i0 + n, elements j0 + 4g ..: without exp2_of's last bits, off by |G_i - G_j| 2^-25 of itself.
@@ -479,58 +482,89 @@ __device__ __forceinline__ f32x4 dots(const Planes<T, DK>& a, int i0, const Plan
   return x;
 }
 
-// N of 16 rows: N = -X - N beta X, its columns from the last one on.
-template <int NS>
-__device__ __forceinline__ void put_inverse(bf16* to, float* scratch, f32x4 x, const Gates& s, int i0, const Lane& l) {
-  f32x4 bx;
-  const float beta = s.beta[i0 + l.n];
+// N = -X - N beta X of both blocks of 16 rows, by one wave: lane i of each half has row i of a block (twice), and takes
+// its columns from the last one on, X's rows read out of LDS.  A row needs no other's, so there is no exchange between
+// lanes: 120 multiply-adds behind each other's loads, not their results.
+template <int NS, int PARTS, bool BACK>
+__device__ __forceinline__ void put_inverses(Pairs<NS, PARTS>& to, const Gates& s) {
+  const int lane = threadIdx.x & 63, block = lane >> 5, i = lane & 15, columns = lane >> 4 & 1;
+  const float* x = to.x[block];
+  float n[16], beta[16];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) bx[r] = beta * x[r];
-  __builtin_memcpy(__builtin_assume_aligned(scratch + l.n * kBlockStride + 4 * l.g, 16), &bx, 16);
-  wave_fence();
-  f32x4 acc = -x;
-  auto column = [&](auto which) {
-    constexpr int J = which.value;
-    const float nj = from_group<J / 4>(acc[J % 4]);
-    const f32x4 row = four(scratch + J * kBlockStride + 4 * l.g);
+  for (int c = 0; c < 16; c += 4) {
+    const f32x4 mine = four(x + i * kBlockStride + c), b = four(s.beta + 16 * block + c);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(-nj, row[r], acc[r]);
+    for (int e = 0; e < 4; ++e) {
+      n[c + e] = -mine[e];
+      beta[c + e] = b[e];
+    }
+  }
+  f32x4 row[2][4];  // of X: this column's and the next one's
+  auto load = [&](int j) {
+#pragma unroll
+    for (int c = 0; c < j; c += 4) row[j & 1][c / 4] = four(x + j * kBlockStride + c);
   };
-  column(std::integral_constant<int, 15>{});
-  column(std::integral_constant<int, 14>{});
-  column(std::integral_constant<int, 13>{});
-  column(std::integral_constant<int, 12>{});
-  column(std::integral_constant<int, 11>{});
-  column(std::integral_constant<int, 10>{});
-  column(std::integral_constant<int, 9>{});
-  column(std::integral_constant<int, 8>{});
-  column(std::integral_constant<int, 7>{});
-  column(std::integral_constant<int, 6>{});
-  column(std::integral_constant<int, 5>{});
-  column(std::integral_constant<int, 4>{});
-  column(std::integral_constant<int, 3>{});
-  column(std::integral_constant<int, 2>{});
-  column(std::integral_constant<int, 1>{});
-  put4<NS>(to + l.n * kBlockStride + 4 * l.g, kBlock, acc);
+  load(15);
+#pragma unroll
+  for (int j = 15; j > 0; --j) {
+    if (j > 1) load(j - 1);
+    const float m = n[j] * beta[j];
+#pragma unroll
+    for (int c = 0; c < j; ++c) n[c] = __builtin_fmaf(-m, row[j & 1][c / 4][c % 4], n[c]);
+    // done before further rows are loaded: else all of them are at once, and the registers of the whole kernel are gone
+#pragma unroll
+    for (int c = 0; c < j; ++c) asm volatile("" : "+v"(n[c])::"memory");
+  }
+  // half of the row a lane
+  const float own = s.beta[16 * block + i];
+  f32x4 y[2];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float u = n[e] * (BACK ? own : beta[e]), v = n[8 + e] * (BACK ? own : beta[8 + e]);
+    y[e / 4][e % 4] = columns ? v : u;
+  }
+  bf16* p = to.n[block] + i * kBlockStride + 8 * columns;
+  put4<NS>(p, kBlock, y[0]);
+  put4<NS>(p + 4, kBlock, y[1]);
 }
 
-// The four waves' shares: two the inverses, the third the last rows with the first, the fourth the rest.  (PARTS 0: no P.)
-template <typename T, int DK, int NS, int PARTS>
+// The waves' shares of a chunk's preparation: the inverses, the last rows with the first, the rest (none where there is no
+// P), and the gates, a wave each; of two waves the first has the inverses, the second the others.
+template <int NW>
+__device__ __forceinline__ bool has_share(int share, const Lane& l) {
+  return NW >= 4 ? l.w == share : NW == 3 ? l.w == (share == 3 ? 2 : share) : l.w == (share ? 1 : 0);
+}
+
+// (PARTS 0: no P.)
+template <typename T, int DK, int NW, int NS, int PARTS, bool BACK>
 __device__ __forceinline__ void put_pairs(Pairs<NS, PARTS>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
                                           const Lane& l) {
-  if (l.w < 2) {
-    const int i0 = 16 * l.w;
-    const f32x4 x = decayed<true>(dots<NS>(k, i0, k, i0, l), decays(s, i0, i0, l), false, l);
-    put_inverse<NS>(to.n[l.w], to.scratch[l.w], x, s, i0, l);
-  } else if (l.w == 2) {
-    const f32x4 d = decays(s, 16, 0, l);
-    put4<NS>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed<false>(dots<NS>(k, 16, k, 0, l), d, false, l));
-    if constexpr (PARTS) put4<PARTS>(to.p + (16 + l.n) * kPairStride + 4 * l.g, kPairPlane, decayed<false>(dots<PARTS>(*q, 16, k, 0, l), d * scale, false, l));
-  } else if constexpr (PARTS != 0) {
+  const f32x4 one = {1.0f, 1.0f, 1.0f, 1.0f};
+  if (has_share<NW>(0, l)) {
 #pragma unroll
-    for (int i0 = 0; i0 < kDeltaRows; i0 += 16)
-      put4<PARTS>(to.p + (i0 + l.n) * kPairStride + i0 + 4 * l.g, kPairPlane,
-                  decayed<true>(dots<PARTS>(*q, i0, k, i0, l), decays(s, i0, i0, l) * scale, true, l));
+    for (int b = 0; b < 2; ++b) {
+      const f32x4 x = decayed<true>(dots<NS>(k, 16 * b, k, 16 * b, l), decays(s, 16 * b, 16 * b, l), false, l);
+      __builtin_memcpy(__builtin_assume_aligned(to.x[b] + l.n * kBlockStride + 4 * l.g, 16), &x, 16);
+    }
+    wave_fence();
+    put_inverses<NS, PARTS, BACK>(to, s);
+  }
+  if (has_share<NW>(1, l)) {
+    const f32x4 d = decays(s, 16, 0, l), beta = BACK ? one : four(s.beta + 4 * l.g);
+    const f32x4 x = d * (BACK ? one * -s.beta[16 + l.n] : -beta);
+    put4<NS>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed<false>(dots<NS>(k, 16, k, 0, l), x, false, l));
+    if constexpr (PARTS)
+      put4<PARTS>(to.p + (16 + l.n) * kPairStride + 4 * l.g, kPairPlane, decayed<false>(dots<PARTS>(*q, 16, k, 0, l), d * scale * beta, false, l));
+  }
+  if constexpr (PARTS != 0) {
+    if (has_share<NW>(2, l)) {
+#pragma unroll
+      for (int i0 = 0; i0 < kDeltaRows; i0 += 16) {
+        const f32x4 d = decays(s, i0, i0, l) * scale;
+        put4<PARTS>(to.p + (i0 + l.n) * kPairStride + i0 + 4 * l.g, kPairPlane,
+                    decayed<true>(dots<PARTS>(*q, i0, k, i0, l), BACK ? d : d * four(s.beta + i0 + 4 * l.g), true, l));
+      }
+    }
   }
 }
 
@@ -629,37 +663,56 @@ enum DeltaMode {
   kDeltaBack         // what the gradients need: that of the state after each chunk, Z
 };
 
-template <typename T, int DK, int TV, int MODE, bool EXACT>
+struct Nothing {};
+
+// A wave has two tiles of 16 columns: what it reads of the rows' operands serves both, and one's products run in the
+// other's shadow.  Value columns are padded to W; beside the states of the parts, further waves of the same workgroup walk
+// the columns of what the part does to a state.
+constexpr int kWalkTiles = 2;
+template <int DK, int W, int MODE>
+constexpr int kWalkWaves = (MODE == kDeltaStates ? W + DK : W) / (16 * kWalkTiles);
+
+template <typename T, int DK, int W, int MODE, bool EXACT>
 struct DeltaShared {
   static constexpr bool BACK = MODE >= kDeltaBackStates, QUERIES = MODE == kDeltaOut || BACK;
   static constexpr int PARTS = MODE == kDeltaOut ? kOutParts<T> : BACK ? 3 : 0, NS = EXACT ? 3 : 2;
-  static constexpr int BUFFERS = sizeof(T) == 2 && DK <= 64 && TV == 1 ? 2 : 1;
+  // (two: a keyframe's results with the state 215 us instead of 204, 128 frames' without 1,276 instead of 1,500)
+  static constexpr int BUFFERS = __is_same(T, bf16) && DK <= 64 && W <= 64 && !EXACT ? 2 : 1;
+  template <bool THERE, typename X>
+  using If = std::conditional_t<THERE, X, Nothing>;
+  // a chunk's results take its queries' place where that is not written again at once
+  union Queries {
+    If<QUERIES, Planes<T, DK>> rows;
+    If<MODE == kDeltaOut && BUFFERS == 2, Values<T, W>> out;
+    __device__ Queries() {}
+  };
   Planes<T, DK> k[BUFFERS];
-  Planes<T, QUERIES ? DK : 8> q[BUFFERS];
-  Values<T, BACK ? 8 : 64 * TV> v[BUFFERS];
-  Planes<T, BACK ? 64 * TV : 8> d[BUFFERS];
-  Values<T, MODE == kDeltaOut ? 64 * TV : 8> out;
+  Queries q[BUFFERS];
+  If<!BACK, Values<T, W>> v[BUFFERS];
+  If<BACK, Planes<T, W>> d[BUFFERS];
+  If<MODE == kDeltaOut && BUFFERS == 1, Values<T, W>> out;
   Gates gates[BUFFERS];
   Pairs<NS, PARTS> pairs;
 };
 
-template <typename T, int DK, int TV, int MODE, bool EXACT, bool WHOLE>
-__global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV)) void delta_walk_kernel(DeltaArgs a) {
-  using Shared = DeltaShared<T, DK, TV, MODE, EXACT>;
+template <typename T, int DK, int W, int MODE, bool EXACT, bool WHOLE>
+__global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(T), DK, W)) void delta_walk_kernel(DeltaArgs a) {
+  using Shared = DeltaShared<T, DK, W, MODE, EXACT>;
+  constexpr int NW = kWalkWaves<DK, W, MODE>, TV = kWalkTiles, THREADS = 64 * NW;
   constexpr int NS = Shared::NS;
-  constexpr int NP = kPlanes<T>, OUT = kOutParts<T>, W = 64 * TV, BUFFERS = Shared::BUFFERS;
+  constexpr int NP = kPlanes<T>, OUT = kOutParts<T>, BUFFERS = Shared::BUFFERS;
   constexpr bool BACK = Shared::BACK, QUERIES = Shared::QUERIES, STATES = MODE == kDeltaStates || MODE == kDeltaBackStates;
   __shared__ Shared sh;
   const Lane l = lane_of();
   int unit = blockIdx.x / a.H;
   const int h = blockIdx.x - unit * a.H;
   // columns of the state, or of what a part does to it
-  const bool map = MODE == kDeltaStates && blockIdx.y > 0;
-  const int col0 = (l.w + (map ? 4 * ((int)blockIdx.y - 1) : 0)) * 16 * TV, columns = map ? a.kd : a.vd;
+  const bool map = MODE == kDeltaStates && l.w >= W / (16 * TV);
+  const int col0 = 16 * TV * l.w - (map ? W : 0), columns = map ? a.kd : a.vd;
   const Order o = order_of(a);
   Part q;
   const bool found = find_part(q, o, a, unit, STATES);
-  if (MODE == kDeltaStates && h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.cut_kind[unit] = !found ? -1 : q.began ? 1 : 0;
+  if (MODE == kDeltaStates && h == 0 && threadIdx.x == 0) a.cut_kind[unit] = !found ? -1 : q.began ? 1 : 0;
   if (!found) return;
   int32_t lo = q.lo, hi = q.hi;
   bool began = q.began, goes_on = q.goes_on && q.before < a.cuts;
@@ -672,12 +725,11 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     goes_on = q.next < q.end && unit + 1 < a.cuts;
     boundary = unit + 1;
   }
-  if (map && !began) return;
   const int64_t each = (int64_t)a.kd * a.vd;
   const int hk = h / a.group;
-  const Source<T, DK, WHOLE> from_k(a.k, hk * a.k_head, a.k_row, a.kd), from_q(QUERIES ? a.q : a.k, QUERIES ? h * a.q_head : 0, a.q_row, a.kd);
-  const Source<T, W, WHOLE> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
-  const bool own = col0 < columns;
+  const Source<T, DK, NW, WHOLE> from_k(a.k, hk * a.k_head, a.k_row, a.kd), from_q(QUERIES ? a.q : a.k, QUERIES ? h * a.q_head : 0, a.q_row, a.kd);
+  const Source<T, W, NW, WHOLE> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
+  const bool own = col0 < columns && !(map && !began);
 
   State<DK, TV> st;
   {
@@ -716,17 +768,17 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
 
   if constexpr (Shared::PARTS != 0) {
     // the first rows have nothing of the last ones
-    for (int i = threadIdx.x; i < Shared::PARTS * 16 * 16; i += kDeltaThreads)
+    for (int i = threadIdx.x; i < Shared::PARTS * 16 * 16; i += THREADS)
       sh.pairs.p[i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16] = (bf16)0.0f;
   }
 
-  Pack<T, 8> rk[kPacks<DK>], rq[kPacks<DK>], rv[kPacks<W>];
+  Pack<T, 8> rk[kPacks<DK, NW>], rq[kPacks<DK, NW>], rv[kPacks<W, NW>];
   float rg = 0.0f, rb = 0.0f;
   auto fetch = [&](int32_t s0) {
     from_k.fetch(rk, s0, hi);
     if constexpr (QUERIES) from_q.fetch(rq, s0, hi);
-    if (!map) from_v.fetch(rv, s0, hi);
-    if (l.w == 3) {
+    from_v.fetch(rv, s0, hi);
+    if (has_share<NW>(3, l)) {
       const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
       rg = a.log_decay[row * a.g_row + h];
       rb = a.beta[row * a.b_row + h];
@@ -734,26 +786,33 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
   };
   auto put = [&](int32_t s0, int buffer) {
     const int n = hi - s0;
-    sh.k[buffer].put(rk, a.kd, n);
-    if constexpr (QUERIES) sh.q[buffer].put(rq, a.kd, n);
+    sh.k[buffer].template put<NW>(rk, a.kd, n);
+    if constexpr (QUERIES) sh.q[buffer].rows.template put<NW>(rq, a.kd, n);
     if constexpr (BACK)
-      sh.d[buffer].put(rv, a.vd, n);
-    else if (!map)
-      sh.v[buffer].put(rv, a.vd, n);
-    if (l.w == 3) {
+      sh.d[buffer].template put<NW>(rv, a.vd, n);
+    else
+      sh.v[buffer].template put<NW>(rv, a.vd, n);
+    if (has_share<NW>(3, l)) {
       const bool there = (int)(threadIdx.x & 31) < n;
-      put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f);
+      put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f, BACK ? 1.0f : there ? rb : 0.0f);
     }
   };
-  auto store_out = [&](int32_t s0) {
+  auto results = [&](int buffer) -> auto& {
+    if constexpr (BUFFERS == 2)
+      return sh.q[buffer].out;
+    else
+      return sh.out;
+  };
+  auto store_out = [&](int32_t s0, int buffer) {
     if constexpr (MODE == kDeltaOut) {
+      const auto& from = results(buffer);
       T* po = static_cast<T*>(a.out) + h * a.o_head;
 #pragma unroll
-      for (int i = 0; i < kPacks<W>; ++i) {
-        const int idx = threadIdx.x + i * kDeltaThreads, row = idx / (W / 8), c = idx % (W / 8) * 8;
-        if (s0 + row >= hi || c >= a.vd) continue;
+      for (int i = 0; i < kPacks<W, NW>; ++i) {
+        const int idx = threadIdx.x + i * THREADS, row = idx / (W / 8), c = idx % (W / 8) * 8;
+        if (s0 + row >= hi || c >= a.vd || row >= kDeltaRows) continue;
         Pack<T, 8> x;
-        __builtin_memcpy(&x, __builtin_assume_aligned(sh.out.v + row * sh.out.stride + c, 16), sizeof(x));
+        __builtin_memcpy(&x, __builtin_assume_aligned(from.v + row * from.stride + c, 16), sizeof(x));
         store_some<T, 8>(po + (int64_t)(s0 + row) * a.o_row + c, x, a.vd - c, a.past);
       }
     }
@@ -772,7 +831,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     const int b = BUFFERS == 2 ? c & 1 : 0;
     const Gates& gates = sh.gates[b];
     fetch(next);
-    put_pairs<T, DK, NS, Shared::PARTS>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b]), gates, a.scale, l);
+    put_pairs<T, DK, NW, NS, Shared::PARTS, BACK>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b].rows), gates, a.scale, l);
 
     // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
     f32x4 ks[2][TV], qs[2][TV];
@@ -792,7 +851,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
 #pragma unroll
           for (int v = 0; v < TV; ++v) ks[t][v] = mma<NS>(k, x[v], ks[t][v]);
           if constexpr (MODE == kDeltaOut) {
-            const Parts<NP> qr = sh.q[b].rows(16 * t, 32 * s, l);
+            const Parts<NP> qr = sh.q[b].rows.rows(16 * t, 32 * s, l);
 #pragma unroll
             for (int v = 0; v < TV; ++v) qs[t][v] = mma<OUT>(x[v], qr, qs[t][v]);
           }
@@ -806,14 +865,14 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     __syncthreads();  // the pairs are there
     if (own) {
       const float whole = gates.whole;
-      f32x4 beta[2], fade[2], left[2];
+      f32x4 fade[2], left[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        beta[t] = four(gates.beta + 16 * t + 4 * l.g);
         fade[t] = four(gates.fade + 16 * t + 4 * l.g);
         left[t] = four(gates.left + 16 * t + 4 * l.g);
       }
       f32x4 e[2][TV];
+      Quarter<NS> ep[2][TV];  // forwards e's parts
       Parts<NP> dout[TV];
       {
         // forwards the first 16 rows first, backwards the last
@@ -843,9 +902,11 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
                         last = block_of<NS, BACK>(sh.pairs.n[L], l);
 #pragma unroll
         for (int v = 0; v < TV; ++v) {
-          e[F][v] = mma_block(first, beta[F] * e[F][v], e[F][v]);
-          e[L][v] = mma_block(cross, -(beta[F] * e[F][v]), e[L][v]);
-          e[L][v] = mma_block(last, beta[L] * e[L][v], e[L][v]);
+          e[F][v] = mma_block(first, split<NS>(e[F][v]), e[F][v]);
+          ep[F][v] = split<NS>(e[F][v]);
+          e[L][v] = mma_block(cross, ep[F][v], e[L][v]);
+          e[L][v] = mma_block(last, split<NS>(e[L][v]), e[L][v]);
+          if constexpr (MODE == kDeltaOut) ep[L][v] = split<NS>(e[L][v]);
         }
       }
       if constexpr (MODE == kDeltaSave || MODE == kDeltaBack) {
@@ -869,17 +930,18 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
           const float f = gates.fade[16 * t + l.n] * a.scale;
 #pragma unroll
           for (int v = 0; v < TV; ++v) {
-            const f32x4 x = mma<OUT>(split<OUT>(beta[0] * e[0][v], beta[1] * e[1][v]), p, qs[t][v] * f);
+            const f32x4 x = mma<OUT>(both<OUT>(ep[0][v], ep[1][v]), p, qs[t][v] * f);
             Pack<T, 4> y;
 #pragma unroll
             for (int r = 0; r < 4; ++r) y.v[r] = (T)x[r];
-            __builtin_memcpy(__builtin_assume_aligned(sh.out.v + (16 * t + l.n) * sh.out.stride + col0 + 16 * v + 4 * l.g, 4 * sizeof(T)), &y,
-                             sizeof(y));
+            auto& to = results(b);
+            __builtin_memcpy(__builtin_assume_aligned(to.v + (16 * t + l.n) * to.stride + col0 + 16 * v + 4 * l.g, 4 * sizeof(T)), &y, sizeof(y));
           }
         }
       }
       // the state after the chunk (backwards: its gradient before it)
       Parts<NS> x[TV], y[TV];
+      const f32x4 beta[2] = {four(gates.beta + 4 * l.g), four(gates.beta + 16 + 4 * l.g)};
 #pragma unroll
       for (int v = 0; v < TV; ++v) {
         if constexpr (BACK) {
@@ -894,7 +956,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
           y[v] = split<NS>(f);
           x[v] = split<NS>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
         } else {
-          x[v] = split<NS>(left[0] * beta[0] * e[0][v], left[1] * beta[1] * e[1][v]);
+          x[v] = split<NS>(left[0] * e[0][v], left[1] * e[1][v]);  // (beta is in there)
         }
       }
 #pragma unroll
@@ -904,7 +966,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
 #pragma unroll
         for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(k, x[v], st[t][v] * whole);
         if constexpr (BACK) {
-          const Parts<NP> qc = sh.q[b].template columns<8>(c0, l);
+          const Parts<NP> qc = sh.q[b].rows.template columns<8>(c0, l);
 #pragma unroll
           for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(qc, y[v], st[t][v]);
         }
@@ -912,7 +974,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
     }
     if (BUFFERS == 2) put(next, b ^ 1);
     __syncthreads();  // the results are there, the chunk has been read
-    store_out(s0);
+    store_out(s0, b);
     if (BUFFERS == 1) {
       put(next, 0);
       __syncthreads();
@@ -955,6 +1017,8 @@ __global__ __launch_bounds__(kDeltaThreads, delta_waves(sizeof(T), DK, 64 * TV))
 // the gradient of a row's log decay is the sum of dG from it on.  With the term
 // in D kept apart, kd_j = k_j . (e^(G_end - G_j) u_j D^T), that is
 //   sum_{i >= t} (dG_i without it) + e^(G_end) <D, S> + sum_{j < t} kd_j.
+
+constexpr int kGradWaves = 4;
 
 template <typename T, int DK, int TV>
 struct DeltaGradShared {
@@ -999,7 +1063,7 @@ __device__ __forceinline__ bool chunk_at(int64_t place, const Order& o, int32_t&
 }
 
 template <typename T, int DK, int TV, bool WHOLE>
-__global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
+__global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
   constexpr int NP = kPlanes<T>, W = 64 * TV, TD = DK >= 64 ? DK / 64 : 1, PER = W / 8;
   __shared__ DeltaGradShared<T, DK, TV> sh;
   const Lane l = lane_of();
@@ -1011,16 +1075,16 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
   const int n = min(hi - s0, kDeltaRows);
   const int64_t each = (int64_t)a.kd * a.vd;
   const bool own = 16 * TD * l.w < DK;
-  for (int i = threadIdx.x; i < 3 * 16 * 16; i += kDeltaThreads) {
+  for (int i = threadIdx.x; i < 3 * 16 * 16; i += 64 * kGradWaves) {
     const int at = i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16;
     sh.a[at] = sh.f[at] = (bf16)0.0f;
   }
-  Pack<T, 8> rk[kPacks<DK>];
-  Source<T, DK, WHOLE>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
-  float dv[kPacks<W>][8];
+  Pack<T, 8> rk[kPacks<DK, kGradWaves>];
+  Source<T, DK, kGradWaves, WHOLE>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
+  float dv[kPacks<W, kGradWaves>][8];
   f32x4 dk[2][TD];
 #pragma unroll
-  for (int i = 0; i < kPacks<W>; ++i)
+  for (int i = 0; i < kPacks<W, kGradWaves>; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dv[i][e] = 0.0f;
 #pragma unroll
@@ -1031,29 +1095,29 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
   for (int j = 0; j < a.group; ++j) {
     const int h = hk * a.group + j;
     {
-      Pack<T, 8> rq[kPacks<DK>], rd[kPacks<W>];
-      Pack<float, 8> re[kPacks<W>], rz[kPacks<W>];
-      Source<T, DK, WHOLE>(a.q, h * a.q_head, a.q_row, a.kd).fetch(rq, s0, hi);
-      Source<T, W, WHOLE>(a.dout, h * a.d_head, a.d_row, a.vd).fetch(rd, s0, hi);
-      Source<float, W, WHOLE>(a.left_over, h * a.vd, a.H * a.vd, a.vd).fetch(re, s0, hi);
-      Source<float, W, WHOLE>(a.due, h * a.vd, a.H * a.vd, a.vd).fetch(rz, s0, hi);
+      Pack<T, 8> rq[kPacks<DK, kGradWaves>], rd[kPacks<W, kGradWaves>];
+      Pack<float, 8> re[kPacks<W, kGradWaves>], rz[kPacks<W, kGradWaves>];
+      Source<T, DK, kGradWaves, WHOLE>(a.q, h * a.q_head, a.q_row, a.kd).fetch(rq, s0, hi);
+      Source<T, W, kGradWaves, WHOLE>(a.dout, h * a.d_head, a.d_row, a.vd).fetch(rd, s0, hi);
+      Source<float, W, kGradWaves, WHOLE>(a.left_over, h * a.vd, a.H * a.vd, a.vd).fetch(re, s0, hi);
+      Source<float, W, kGradWaves, WHOLE>(a.due, h * a.vd, a.H * a.vd, a.vd).fetch(rz, s0, hi);
       float g = 0.0f, beta = 0.0f;
       if (l.w == 3 && (int)(threadIdx.x & 31) < n) {
         const int64_t row = s0 + (int)(threadIdx.x & 31);
         g = a.log_decay[row * a.g_row + h];
         beta = a.beta[row * a.b_row + h];
       }
-      float rb[kPacks<W>];
+      float rb[kPacks<W, kGradWaves>];
 #pragma unroll
-      for (int i = 0; i < kPacks<W>; ++i)
-        rb[i] = a.beta[(int64_t)min(s0 + (int)(threadIdx.x + i * kDeltaThreads) / PER, hi - 1) * a.b_row + h];
+      for (int i = 0; i < kPacks<W, kGradWaves>; ++i)
+        rb[i] = a.beta[(int64_t)min(s0 + (int)(threadIdx.x + i * 64 * kGradWaves) / PER, hi - 1) * a.b_row + h];
       if (j) __syncthreads();  // the head before has been read
-      if (j == 0) sh.k.put(rk, a.kd, n);
-      sh.q.put(rq, a.kd, n);
-      sh.d.put(rd, a.vd, n);
-      if (l.w == 3) put_gates(sh.gates, g, beta);
+      if (j == 0) sh.k.template put<kGradWaves>(rk, a.kd, n);
+      sh.q.template put<kGradWaves>(rq, a.kd, n);
+      sh.d.template put<kGradWaves>(rd, a.vd, n);
+      if (l.w == 3) put_gates(sh.gates, g, beta, 1.0f);
       int i = 0;
-      each_pack<float, W>(re, a.vd, n, [&](int row, int c, Pack<float, 8> x) {
+      each_pack<float, W, kGradWaves>(re, a.vd, n, [&](int row, int c, Pack<float, 8> x) {
         float dot = 0.0f;
         Pack<float, 8> y;
 #pragma unroll
@@ -1196,8 +1260,8 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
       }
   }
 #pragma unroll
-  for (int i = 0; i < kPacks<W>; ++i) {
-    const int idx = threadIdx.x + i * kDeltaThreads, row = idx / PER, c = idx % PER * 8;
+  for (int i = 0; i < kPacks<W, kGradWaves>; ++i) {
+    const int idx = threadIdx.x + i * 64 * kGradWaves, row = idx / PER, c = idx % PER * 8;
     if (row >= n || c >= a.vd) continue;
     Pack<T, 8> x;
 #pragma unroll
@@ -1212,7 +1276,7 @@ __global__ __launch_bounds__(kDeltaThreads, delta_grad_waves(sizeof(T), DK, 64 *
 template <typename F>
 void with_dims(int kd, int vd, F&& f) {
   auto values = [&](auto key) {
-    vd <= 64 ? f(key, std::integral_constant<int, 1>{}) : f(key, std::integral_constant<int, 2>{});
+    vd <= 64 ? f(key, std::integral_constant<int, 64>{}) : f(key, std::integral_constant<int, 128>{});
   };
   kd <= 32 ? values(std::integral_constant<int, 32>{}) : kd <= 64 ? values(std::integral_constant<int, 64>{}) : values(std::integral_constant<int, 128>{});
 }
@@ -1221,22 +1285,22 @@ bool whole_packs(const DeltaArgs& a) { return a.kd % 8 == 0 && a.vd % 8 == 0; }
 
 template <typename T, int MODE, bool EXACT = true>
 hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
-  with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
-    constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
+  with_dims(a.kd, a.vd, [&](auto key, auto value) {
+    constexpr int DK = decltype(key)::value, W = decltype(value)::value;
     constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
-    const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H), MODE == kDeltaStates ? 1 + (a.kd + 64 * TV - 1) / (64 * TV) : 1);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDeltaThreads), 0, st, a); };
-    whole_packs(a) ? go(delta_walk_kernel<T, DK, TV, MODE, EXACT, true>) : go(delta_walk_kernel<T, DK, TV, MODE, EXACT, false>);
+    const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWalkWaves<DK, W, MODE>), 0, st, a); };
+    whole_packs(a) ? go(delta_walk_kernel<T, DK, W, MODE, EXACT, true>) : go(delta_walk_kernel<T, DK, W, MODE, EXACT, false>);
   });
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t grad_of(const DeltaGradArgs& a, hipStream_t st) {
-  with_dims(a.kd, a.vd, [&](auto key, auto tiles) {
-    constexpr int DK = decltype(key)::value, TV = decltype(tiles)::value;
+  with_dims(a.kd, a.vd, [&](auto key, auto value) {
+    constexpr int DK = decltype(key)::value, TV = decltype(value)::value / 64;
     const dim3 grid((uint32_t)(delta_slots(a.rows, a.B) * (a.H / a.group)));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDeltaThreads), 0, st, a); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kGradWaves), 0, st, a); };
     whole_packs(a) ? go(delta_grad_kernel<T, DK, TV, true>) : go(delta_grad_kernel<T, DK, TV, false>);
   });
   return hipGetLastError();

@@ -82,7 +82,6 @@ constexpr int32_t kDeltaLeast = 128;
 constexpr int32_t kDeltaCutSequences = 1024;
 
 struct DeltaPlan {
-  int64_t slots;  // workgroups that the chip takes at once
   int32_t cuts, run;
   // (cut_kind lies first)
   size_t off_from[2], off_state, off_map, off_run[2], off_end[2], off_grad, off_turned, off_before, off_after, off_left, off_due, total;
@@ -102,11 +101,12 @@ mmbev_status_t delta_ok(const mmbev_attention_t* t, bool step) {
 
 DeltaPlan delta_plan(const mmbev_attention_t* t, bool backward) {
   DeltaPlan p{};
-  p.slots = kComputeUnits * delta_waves(size_of(t->dtype), t->key_dim, t->value_dim);
+  // workgroups that the chip takes at once
+  const int64_t slots = kComputeUnits * delta_groups(size_of(t->dtype), t->key_dim, t->value_dim);
   const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
   if (longest > kDeltaWhole && t->num_sequences <= kDeltaCutSequences) {
     // so many parts that with the sequences that are not cut there are about `units` of them: at least half the units
-    const int64_t units = std::max<int64_t>(2, p.slots / t->heads);
+    const int64_t units = std::max<int64_t>(2, slots / t->heads);
     const int64_t parts = units - std::min<int64_t>(t->num_sequences, units / 2);
     p.cuts = (int32_t)std::max<int64_t>(1, std::min(parts, (t->rows + kDeltaLeast - 1) / kDeltaLeast));
   }
@@ -182,7 +182,7 @@ void put_delta(DeltaArgs& a, const mmbev_attention_t* t, const mmbev_heads_t& q,
   a.rows = t->rows;
   a.B = t->num_sequences;
   a.cuts = p.cuts;
-  a.longest_first = t->num_sequences <= kOrderedSequences && (int64_t)t->num_sequences * t->heads > p.slots;
+  a.longest_first = t->num_sequences <= kOrderedSequences && (int64_t)t->num_sequences * t->heads > kComputeUnits;
   a.least = kDeltaLeast;
   put(q, &a.q, &a.q_row, &a.q_head);
   put(k, &a.k, &a.k_row, &a.k_head);

@@ -244,9 +244,13 @@ struct DeltaGradArgs : DeltaArgs {
   float *dlog_decay, *dbeta;  // fp32 [rows][H]
 };
 
-// Waves a SIMD of the walks' kernels, hence the workgroups of four waves that a compute unit takes, as their registers
-// and LDS allow; keys and values padded to `key` and `value`.
-constexpr int delta_waves(int size, int key, int value) { return size == 4 ? (key > 64 || value > 64 ? 1 : 2) : key > 64 || value > 64 ? 2 : 3; }
+// Waves a SIMD that the walks' kernels have registers for, and the workgroups that a compute unit takes, as their LDS
+// allows; keys and values padded to `key` and `value`.
+constexpr int delta_waves(int size, int key, int value) { return size == 4 && (key > 64 || value > 64) ? 1 : 2; }
+constexpr int delta_groups(int size, int key, int value) {
+  const bool wide = key > 64 || value > 64;
+  return size == 4 ? (wide ? 1 : 2) : wide ? 2 : 4;
+}
 constexpr int delta_grad_waves(int size, int key, int value) { return size == 4 || key > 64 || value > 64 ? 1 : 2; }
 
 hipError_t launch_delta(const DeltaArgs& a, int32_t dtype, hipStream_t st);
