@@ -1024,8 +1024,14 @@ template <typename T, int DK, int TV>
 struct DeltaGradShared {
   Planes<T, DK> k, q;
   Planes<T, 64 * TV> d;
-  Planes<float, 64 * TV> u, y;
-  __attribute__((aligned(16))) bf16 a[3 * kPairPlane], f[3 * kPairPlane];
+  Planes<float, 64 * TV> y;
+  union {  // A and F take U's place when it has been read
+    Planes<float, 64 * TV> u;
+    struct {
+      __attribute__((aligned(16))) bf16 a[3 * kPairPlane], f[3 * kPairPlane];
+    };
+  };
+  __device__ DeltaGradShared() {}
   Gates gates;
   float own[4][kDeltaRows], end[4][kDeltaRows];  // a wave's part of dG and of kd
   float both[4];                                 // of <D, S>
@@ -1075,10 +1081,6 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
   const int n = min(hi - s0, kDeltaRows);
   const int64_t each = (int64_t)a.kd * a.vd;
   const bool own = 16 * TD * l.w < DK;
-  for (int i = threadIdx.x; i < 3 * 16 * 16; i += 64 * kGradWaves) {
-    const int at = i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16;
-    sh.a[at] = sh.f[at] = (bf16)0.0f;
-  }
   Pack<T, 8> rk[kPacks<DK, kGradWaves>];
   Source<T, DK, kGradWaves, WHOLE>(a.k, hk * a.k_head, a.k_row, a.kd).fetch(rk, s0, hi);
   float dv[kPacks<W, kGradWaves>][8];
@@ -1137,7 +1139,7 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
     }
     __syncthreads();
     const Gates& gates = sh.gates;
-    // A and F: lane n row i, elements j0 + 4g ..
+    // A (results) and F: lane n row i, elements j0 + 4g ..
     auto pairs = [&](int i0, int j0, bool results) {
       f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -1147,14 +1149,14 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
       }
       f32x4 d = decays(gates, i0, j0, l);
       if (results) d = d * a.scale;
-      x = i0 == j0 ? decayed<true>(x, d, results, l) : decayed<false>(x, d, results, l);
-      put4<3>((results ? sh.a : sh.f) + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, x);
+      return i0 == j0 ? decayed<true>(x, d, results, l) : decayed<false>(x, d, results, l);
     };
+    f32x4 one_pair, other_pair = {0.0f, 0.0f, 0.0f, 0.0f};
     if (l.w < 2) {
-      pairs(16 * l.w, 16 * l.w, true);
-      pairs(16 * l.w, 16 * l.w, false);
+      one_pair = pairs(16 * l.w, 16 * l.w, true);
+      other_pair = pairs(16 * l.w, 16 * l.w, false);
     } else {
-      pairs(16, 0, l.w == 2);
+      one_pair = pairs(16, 0, l.w == 2);
     }
     // what comes through the states: lane n row n, elements of dk 4g ..
     f32x4 read_q[2][TD], read_k[2][TD], written[2][TD];
@@ -1167,9 +1169,6 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
       const float *before = a.before + (place * a.H + h) * each, *after = a.after + (place * a.H + h) * each;
 #pragma unroll
       for (int s = 0; s < W / 32; ++s) {
-        const Parts<NP> d0 = sh.d.rows(0, 32 * s, l), d1 = sh.d.rows(16, 32 * s, l);
-        const Parts<3> y0 = sh.y.rows(0, 32 * s, l), y1 = sh.y.rows(16, 32 * s, l);
-        const Parts<3> u0 = sh.u.rows(0, 32 * s, l), u1 = sh.u.rows(16, 32 * s, l);
 #pragma unroll
         for (int d = 0; d < TD; ++d) {
           const int row = 16 * (l.w * TD + d) + l.n;
@@ -1179,16 +1178,26 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
 #pragma unroll
           for (int e = 0; e < 8; ++e) both = __builtin_fmaf(x[e], z[e], both);
           const Parts<3> sp = split<3>(x), gp = split<3>(z);
-          read_q[0][d] = mma<3>(sp, d0, read_q[0][d]);
-          read_q[1][d] = mma<3>(sp, d1, read_q[1][d]);
-          read_k[0][d] = mma<3>(sp, y0, read_k[0][d]);
-          read_k[1][d] = mma<3>(sp, y1, read_k[1][d]);
-          written[0][d] = mma<3>(gp, u0, written[0][d]);
-          written[1][d] = mma<3>(gp, u1, written[1][d]);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            read_q[t][d] = mma<3>(sp, sh.d.rows(16 * t, 32 * s, l), read_q[t][d]);
+            read_k[t][d] = mma<3>(sp, sh.y.rows(16 * t, 32 * s, l), read_k[t][d]);
+            written[t][d] = mma<3>(gp, sh.u.rows(16 * t, 32 * s, l), written[t][d]);
+          }
         }
       }
     }
     both = group_sum<64>(both);
+    __syncthreads();  // U has been read
+    {
+      const int i0 = l.w < 2 ? 16 * l.w : 16, j0 = l.w < 2 ? i0 : 0;
+      const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+      put4<3>((l.w == 3 ? sh.f : sh.a) + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, one_pair);
+      if (l.w < 2)
+        put4<3>(sh.f + (i0 + l.n) * kPairStride + j0 + 4 * l.g, kPairPlane, other_pair);
+      else  // the first rows have nothing of the last ones
+        put4<3>((l.w == 3 ? sh.f : sh.a) + l.n * kPairStride + 16 + 4 * l.g, kPairPlane, zero);
+    }
     __syncthreads();  // A and F are there
 #pragma unroll
     for (int t = 0; t < 2; ++t) {

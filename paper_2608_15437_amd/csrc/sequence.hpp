@@ -251,7 +251,7 @@ constexpr int delta_groups(int size, int key, int value) {
   const bool wide = key > 64 || value > 64;
   return size == 4 ? (wide ? 1 : 2) : wide ? 2 : 4;
 }
-constexpr int delta_grad_waves(int size, int key, int value) { return size == 4 || key > 64 || value > 64 ? 1 : 2; }
+constexpr int delta_grad_waves(int size, int key, int value) { return size == 4 || key > 64 || value > 64 ? 1 : 3; }
 
 hipError_t launch_delta(const DeltaArgs& a, int32_t dtype, hipStream_t st);
 hipError_t launch_delta_backward(const DeltaGradArgs& a, const float* dfinal, float* dinitial, int32_t dtype, hipStream_t st);
