@@ -35,7 +35,7 @@ bool positions_ok(const mmbev_head_norm_t* t, const Positions& p) {
   return p.stride >= 0 && (t->rows <= 1 || p.stride >= p.axes) && p.stride < kMaxStride && reachable(t->rows, p.stride);
 }
 
-HeadNormArgs head_norm_args(const mmbev_head_norm_t* t, int32_t arrays, const Positions& p, const void* q_weight, const void* k_weight,
+HeadNormArgs head_norm_args(const mmbev_head_norm_t* t, const Positions& p, const void* q_weight, const void* k_weight,
                             const int64_t* row_count, int32_t* fault) {
   HeadNormArgs a{};
   a.weight[0] = q_weight;
@@ -54,7 +54,6 @@ HeadNormArgs head_norm_args(const mmbev_head_norm_t* t, int32_t arrays, const Po
   a.rotary_dim = t->rotary_dim;
   a.interleaved = t->layout == MMBEV_ROTARY_INTERLEAVED;
   a.weight_f32 = t->weight_dtype == MMBEV_F32;
-  a.past = arrays * t->rows * (t->heads + t->kv_heads) * t->dim * size_of(t->dtype) > kPastCaches;
   a.eps = t->eps;
   a.inv_dim = (float)(1.0 / t->dim);
   return a;
@@ -227,7 +226,7 @@ mmbev_status_t mmbev_head_norm_rotary(const mmbev_head_norm_t* t, mmbev_heads_t 
     return MMBEV_ERR_INVALID_ARG;
   const mmbev_heads_t out[2] = {q_out, k_out};
   if (!outputs_apart(t, out, {&q}, {&k})) return MMBEV_ERR_INVALID_ARG;
-  HeadNormArgs a = head_norm_args(t, 2, p, q_weight, k_weight, row_count, fault);
+  HeadNormArgs a = head_norm_args(t, p, q_weight, k_weight, row_count, fault);
   put(q, &a.x[0], &a.x_row[0], &a.x_head[0]);
   put(k, &a.x[1], &a.x_row[1], &a.x_head[1]);
   put(q_out, &a.out[0], &a.out_row[0], &a.out_head[0]);
@@ -237,7 +236,7 @@ mmbev_status_t mmbev_head_norm_rotary(const mmbev_head_norm_t* t, mmbev_heads_t 
 
 size_t mmbev_head_norm_rotary_backward_workspace_bytes(const mmbev_head_norm_t* t) {
   if (head_norm_ok(t) != MMBEV_OK) return 0;
-  const HeadNormArgs a = head_norm_args(t, 3, {}, nullptr, nullptr, nullptr, nullptr);
+  const HeadNormArgs a = head_norm_args(t, {}, nullptr, nullptr, nullptr, nullptr);
   return align256((size_t)head_norm_backward_grid(a, t->dtype) * 2 * t->dim * 4);
 }
 
@@ -260,7 +259,7 @@ mmbev_status_t mmbev_head_norm_rotary_backward(const mmbev_head_norm_t* t, mmbev
   if (!outputs_apart(t, out, {&dq_out, &q}, {&dk_out, &k})) return MMBEV_ERR_INVALID_ARG;
   const bool sums = dq_weight || dk_weight;
   if (sums && !workspace_ok(workspace, workspace_bytes, mmbev_head_norm_rotary_backward_workspace_bytes(t))) return MMBEV_ERR_WORKSPACE;
-  HeadNormArgs a = head_norm_args(t, 3, p, q_weight, k_weight, row_count, fault);
+  HeadNormArgs a = head_norm_args(t, p, q_weight, k_weight, row_count, fault);
   put(q, &a.x[0], &a.x_row[0], &a.x_head[0]);
   put(k, &a.x[1], &a.x_row[1], &a.x_head[1]);
   put(dq_out, &a.dy[0], &a.dy_row[0], &a.dy_head[0]);

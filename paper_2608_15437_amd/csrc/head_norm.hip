@@ -5,18 +5,26 @@
 //
 // LANES neighbouring lanes hold a head, two 16-byte packs each: of the part
 // that turns, the packs of the pairs' first and second elements or two packs of
-// neighbouring pairs; of the rest, two packs that turn by nothing.  A group of
+// neighbouring pairs; of the rest, two packs that turn by nothing.  Where both
+// parts have a whole pack (FULL) every access is one: the last pack of a part
+// begins so that it ends with the part, lanes with none of their own do the
+// last one's work, and what two lanes have counts once in the sums and is
+// stored twice, the same.  A group of
 // lanes takes several heads of one row and one array, so that it works the
 // sines and cosines out and loads the weights once for all of them (the fewer
 // rows, the fewer heads, so that small calls spread out).
 // The operator moves bytes; beside them are some 15 operations an element and
-// 50 a pair for its angle.
+// 50 a pair for its angle.  (Storing past the caches, as the other sequence
+// operators' large calls do, costs here, where a store has 64 bytes a head:
+// 921,997 rows of 8 + 4 heads 701 us instead of 566, gradients of 213,879 in
+// fp32 676 instead of 554.)
 //
 // The weights' gradients: a group stays with its heads and walks the rows that
 // its workgroup takes (every grid-th block of them) with its columns' sums in
 // registers; the workgroup's groups add theirs in LDS, and a second launch adds
 // the workgroups' rows, all in a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "rotary.hpp"
 
@@ -32,37 +40,59 @@ struct HeadShape {
   int32_t turned, items;     // of them with pairs, and with elements
   int32_t parts[2], each;    // a row's groups of lanes, of queries and of keys, and the heads of one
   int32_t rows_block;
+  int32_t full, ragged;      // see FULL; some elements are two lanes'
 };
 
 // What a lane has of every head: where its packs are, and its pairs' angles.
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, bool FULL>
 struct Place {
   static constexpr int V = kPackOf<T>;
-  int at[2], left[2];  // first element of a pack, elements from there on
-  bool turned;
+  int at[2];    // first element of a pack
+  int left[2];  // elements from there on (not FULL)
+  int skip[2];  // elements that are another lane's too (FULL)
+  bool turned, ragged;
   float sn[V], cs[V];
 
+  // The i-th of a part's packs, of its `size` elements from `begin` on.
+  __device__ __forceinline__ void put(int which, int i, int begin, int size, bool there) {
+    const int first = begin + i * V, last = begin + size - V;
+    at[which] = FULL ? min(first, last) : first;
+    left[which] = there ? begin + size - first : 0;
+    skip[which] = there ? min(max(first - last, 0), V) : V;
+  }
   __device__ __forceinline__ void set(const HeadNormArgs& a, const HeadShape& s, int lane) {
-    const int half = a.rotary_dim / 2;
+    const bool there = lane < s.items;
+    if (FULL) lane = min(lane, s.items - 1);
     turned = lane < s.turned;
+    ragged = s.ragged;
+    // neighbouring lanes' first packs lie next to each other, and so do their second ones
     if (!turned) {
-      const int c = a.rotary_dim + (lane - s.turned) * 2 * V;
-      at[0] = c;
-      at[1] = c + V;
-      left[0] = lane < s.items ? a.dim - c : 0;
-      left[1] = left[0] - V;
+      put(0, lane - s.turned, a.rotary_dim, a.dim - a.rotary_dim, there);
+      put(1, lane - s.turned + s.items - s.turned, a.rotary_dim, a.dim - a.rotary_dim, there);
     } else if (INTERLEAVED) {
-      at[0] = lane * 2 * V;
-      at[1] = at[0] + V;
-      left[0] = a.rotary_dim - at[0];
-      left[1] = left[0] - V;
+      put(0, lane, 0, a.rotary_dim, there);
+      put(1, lane + s.turned, 0, a.rotary_dim, there);
     } else {
-      at[0] = lane * V;
-      at[1] = half + at[0];
-      left[0] = left[1] = half - at[0];
+      put(0, lane, 0, a.rotary_dim / 2, there);
+      put(1, lane, a.rotary_dim / 2, a.rotary_dim / 2, there);
     }
   }
-  __device__ __forceinline__ void angles(const HeadNormArgs& a, int64_t row, int lane) {
+  // an element of the lane's own
+  __device__ __forceinline__ bool own(int which, int e) const { return FULL ? e >= skip[which] : e < left[which]; }
+  __device__ __forceinline__ int width(int which) const { return FULL ? V : left[which]; }
+  __device__ __forceinline__ Pack<T, V> load(const T* x, int which) const {
+    if constexpr (FULL)
+      return load_pack<T, V>(x + at[which]);
+    else
+      return load_some<T, V>(x + at[which], left[which]);
+  }
+  __device__ __forceinline__ void store(T* x, int which, const Pack<T, V>& r) const {
+    if constexpr (FULL)
+      store_pack<T, V>(x + at[which], r);
+    else
+      store_some<T, V>(x + at[which], r, left[which]);
+  }
+  __device__ __forceinline__ void angles(const HeadNormArgs& a, int64_t row) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       sn[e] = 0.0f;
@@ -70,11 +100,19 @@ struct Place {
     }
     if (!turned) return;
     const int half = a.rotary_dim / 2;
+    const int32_t* positions = a.positions + row * a.position_stride;
+    // of up to four axes all are loaded together with the table, not after it
+    int32_t of_axis[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) of_axis[i] = positions[min(i, a.axes - 1)];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       // pairs past the last turn by its angle; they are not stored
-      const int j = min(lane * V + e, half - 1), ax = min((int)a.axis[j], a.axes - 1);
-      const uint64_t phase = (uint64_t)(int64_t)a.positions[row * a.position_stride + ax] * a.steps[j];
+      const int pair = INTERLEAVED ? at[e / (V / 2)] / 2 + e % (V / 2) : at[0] + e;
+      const int j = min(pair, half - 1), ax = min((int)a.axis[j], a.axes - 1);
+      int32_t p = ax == 0 ? of_axis[0] : ax == 1 ? of_axis[1] : ax == 2 ? of_axis[2] : of_axis[3];
+      if (a.axes > 4) p = positions[ax];
+      const uint64_t phase = (uint64_t)(int64_t)p * a.steps[j];
       sincos_of_phase((uint32_t)(phase >> 32), sn[e], cs[e]);
     }
   }
@@ -96,12 +134,9 @@ struct Two {
   Pack<T, V> p[2];
 };
 
-template <typename T, int V>
-__device__ __forceinline__ Two<T, V> load_two(const T* x, const int (&at)[2], const int (&left)[2], bool past) {
-  Two<T, V> r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) r.p[i] = past && left[i] >= V ? load_past<T, V>(x + at[i]) : load_some<T, V>(x + at[i], left[i]);
-  return r;
+template <typename P, typename T, int V>
+__device__ __forceinline__ Two<T, V> load_two(const P& place, const T* x) {
+  return {{place.load(x, 0), place.load(x, 1)}};
 }
 
 template <typename T, int V>
@@ -112,8 +147,8 @@ __device__ __forceinline__ void widen(float (&to)[2][V], const Two<T, V>& from) 
     for (int e = 0; e < V; ++e) to[i][e] = (float)from.p[i].v[e];
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void store_two(T* x, const float (&f)[2][V], const int (&at)[2], const int (&left)[2], bool past) {
+template <typename P, typename T, int V>
+__device__ __forceinline__ void store_two(const P& place, T* x, const float (&f)[2][V]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     Pack<T, V> r;
@@ -125,38 +160,51 @@ __device__ __forceinline__ void store_two(T* x, const float (&f)[2][V], const in
       if constexpr (__is_same(T, f16)) asm("" : "+v"(y));
       r.v[e] = (T)y;
     }
-    store_some<T, V>(x + at[i], r, left[i], past);
+    place.store(x, i, r);
   }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void load_weights(float (&w)[2][V], const void* p, bool f32, const int (&at)[2], const int (&left)[2]) {
+template <typename P, typename T, int V>
+__device__ __forceinline__ void load_weights(const P& place, float (&w)[2][V], const void* p, bool f32) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (!p) {
 #pragma unroll
       for (int e = 0; e < V; ++e) w[i][e] = 1.0f;
     } else if (f32) {
-      const Pack<float, V> r = load_some<float, V>(static_cast<const float*>(p) + at[i], left[i]);
+      const Pack<float, V> r = load_some<float, V>(static_cast<const float*>(p) + place.at[i], place.width(i));
 #pragma unroll
       for (int e = 0; e < V; ++e) w[i][e] = r.v[e];
     } else {
-      const Pack<T, V> r = load_some<T, V>(static_cast<const T*>(p) + at[i], left[i]);
+      const Pack<T, V> r = load_some<T, V>(static_cast<const T*>(p) + place.at[i], place.width(i));
 #pragma unroll
       for (int e = 0; e < V; ++e) w[i][e] = (float)r.v[e];
     }
   }
 }
 
-// Reciprocal root of the mean square (elements past the head are zeros).
-template <int LANES, int V>
-__device__ __forceinline__ float head_rstd(const float (&x)[2][V], const HeadNormArgs& a) {
-  float sq = 0.0f;
+// Sum over the head of x * y, the lane's own elements (past the head both are zeros).
+template <int LANES, typename P, int V>
+__device__ __forceinline__ float head_sum(const P& place, const float (&x)[2][V], const float (&y)[2][V]) {
+  float t = 0.0f;
+  if (place.ragged) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int e = 0; e < V; ++e) sq = __builtin_fmaf(x[i][e], x[i][e], sq);
-  return 1.0f / __builtin_sqrtf(__builtin_fmaf(group_sum<LANES>(sq), a.inv_dim, a.eps));
+      for (int e = 0; e < V; ++e) t = __builtin_fmaf(place.own(i, e) ? x[i][e] : 0.0f, y[i][e], t);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) t = __builtin_fmaf(x[i][e], y[i][e], t);
+  }
+  return group_sum<LANES>(t);
+}
+
+// Reciprocal root of the mean square, off by a step at most.
+template <int LANES, typename P, int V>
+__device__ __forceinline__ float head_rstd(const P& place, const float (&x)[2][V], const HeadNormArgs& a) {
+  return __builtin_amdgcn_rsqf(__builtin_fmaf(head_sum<LANES, P, V>(place, x, x), a.inv_dim, a.eps));
 }
 
 // The group's array and heads.
@@ -169,7 +217,7 @@ struct Share {
   }
 };
 
-template <typename T, bool INTERLEAVED, int LANES>
+template <typename T, bool INTERLEAVED, int LANES, bool FULL>
 __global__ __launch_bounds__(kHeadThreads) void head_norm_kernel(HeadNormArgs a, HeadShape s) {
   constexpr int V = kPackOf<T>;
   const int64_t n = rows_in_use(a.row_count, a.rows, a.fault);
@@ -179,37 +227,44 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_kernel(HeadNormArgs a,
   if (r >= s.rows_block || row >= n) return;
   const Share share(a, s, group - r * parts);
   const int which = share.which;
-  Place<T, INTERLEAVED> place;
+  using P = Place<T, INTERLEAVED, FULL>;
+  P place;
   place.set(a, s, lane);
   float w[2][V];
-  load_weights<T, V>(w, which ? a.weight[1] : a.weight[0], a.weight_f32, place.at, place.left);
+  load_weights<P, T, V>(place, w, which ? a.weight[1] : a.weight[0], a.weight_f32);
   const int64_t x_head = which ? a.x_head[1] : a.x_head[0], out_head = which ? a.out_head[1] : a.out_head[0];
-  const T* x = static_cast<const T*>(which ? a.x[1] : a.x[0]) + row * (which ? a.x_row[1] : a.x_row[0]) + share.h0 * x_head;
-  T* out = static_cast<T*>(which ? a.out[1] : a.out[0]) + row * (which ? a.out_row[1] : a.out_row[0]) + share.h0 * out_head;
-  place.angles(a, row, lane);
+  const T* x = static_cast<const T*>(which ? a.x[1] : a.x[0]) + row * (which ? a.x_row[1] : a.x_row[0]);
+  T* out = static_cast<T*>(which ? a.out[1] : a.out[0]) + row * (which ? a.out_row[1] : a.out_row[0]);
+  auto load = [&](Two<T, V> (&t)[kHeadsAtOnce], int h) {
+#pragma unroll
+    for (int i = 0; i < kHeadsAtOnce; ++i) t[i] = load_two<P, T, V>(place, x + (int64_t)min(h + i, share.h1 - 1) * x_head);
+  };
   auto finish = [&](const Two<T, V>& from, T* to) {
     float f[2][V];
     widen<T, V>(f, from);
-    const float rstd = head_rstd<LANES, V>(f, a);
+    const float rstd = head_rstd<LANES, P, V>(place, f, a);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) f[i][e] = f[i][e] * rstd * w[i][e];
     place.turn(f, false);
-    store_two<T, V>(to, f, place.at, place.left, a.past);
+    store_two<P, T, V>(place, to, f);
   };
-  int h = share.h0;
-  for (; h + kHeadsAtOnce <= share.h1; h += kHeadsAtOnce, x += kHeadsAtOnce * x_head, out += kHeadsAtOnce * out_head) {
-    Two<T, V> t[kHeadsAtOnce];
+  // the first heads' loads before the angles' work, the next ones' before these are stored
+  Two<T, V> t[kHeadsAtOnce], next[kHeadsAtOnce];
+  load(t, share.h0);
+  place.angles(a, row);
+  for (int h = share.h0; h < share.h1; h += kHeadsAtOnce) {
+    if (h + kHeadsAtOnce < share.h1) load(next, h + kHeadsAtOnce);
 #pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) t[i] = load_two<T, V>(x + i * x_head, place.at, place.left, a.past);
-#pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) finish(t[i], out + i * out_head);
+    for (int i = 0; i < kHeadsAtOnce; ++i) {
+      if (h + i < share.h1) finish(t[i], out + (int64_t)(h + i) * out_head);
+      t[i] = next[i];
+    }
   }
-  for (; h < share.h1; ++h, x += x_head, out += out_head) finish(load_two<T, V>(x, place.at, place.left, a.past), out);
 }
 
-template <typename T, bool INTERLEAVED, int LANES>
+template <typename T, bool INTERLEAVED, int LANES, bool FULL>
 __global__ __launch_bounds__(kHeadThreads) void head_norm_backward_kernel(HeadNormArgs a, HeadShape s) {
   constexpr int V = kPackOf<T>;
   __shared__ float s_sum[kHeadThreads / LANES][LANES * 2 * V + 1];
@@ -218,10 +273,11 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_backward_kernel(HeadNo
   const int r = group / parts;
   const Share share(a, s, group - r * parts);
   const int which = share.which;
-  Place<T, INTERLEAVED> place;
+  using P = Place<T, INTERLEAVED, FULL>;
+  P place;
   place.set(a, s, lane);
   float w[2][V], dw[2][V];
-  load_weights<T, V>(w, which ? a.weight[1] : a.weight[0], a.weight_f32, place.at, place.left);
+  load_weights<P, T, V>(place, w, which ? a.weight[1] : a.weight[0], a.weight_f32);
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -229,10 +285,10 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_backward_kernel(HeadNo
   const int64_t x_head = which ? a.x_head[1] : a.x_head[0], dy_head = which ? a.dy_head[1] : a.dy_head[0],
                 out_head = which ? a.out_head[1] : a.out_head[0];
   auto finish = [&](const Two<T, V>& from, const Two<T, V>& grad, T* to) {
-    float f[2][V], d[2][V], dot = 0.0f;
+    float f[2][V], d[2][V];
     widen<T, V>(f, from);
     widen<T, V>(d, grad);
-    const float rstd = head_rstd<LANES, V>(f, a);
+    const float rstd = head_rstd<LANES, P, V>(place, f, a);
     place.turn(d, true);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -241,40 +297,34 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_backward_kernel(HeadNo
         f[i][e] *= rstd;
         dw[i][e] = __builtin_fmaf(d[i][e], f[i][e], dw[i][e]);
         d[i][e] *= w[i][e];
-        dot = __builtin_fmaf(d[i][e], f[i][e], dot);
       }
-    dot = group_sum<LANES>(dot) * a.inv_dim;
+    const float dot = head_sum<LANES, P, V>(place, d, f) * a.inv_dim;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) d[i][e] = rstd * __builtin_fmaf(-f[i][e], dot, d[i][e]);
-    store_two<T, V>(to, d, place.at, place.left, a.past);
+    store_two<P, T, V>(place, to, d);
   };
   if (r < s.rows_block)
     for (int64_t row = (int64_t)blockIdx.x * s.rows_block + r; row < n; row += (int64_t)gridDim.x * s.rows_block) {
-      const T* x = static_cast<const T*>(which ? a.x[1] : a.x[0]) + row * (which ? a.x_row[1] : a.x_row[0]) + share.h0 * x_head;
-      const T* dy = static_cast<const T*>(which ? a.dy[1] : a.dy[0]) + row * (which ? a.dy_row[1] : a.dy_row[0]) + share.h0 * dy_head;
-      T* out = static_cast<T*>(which ? a.out[1] : a.out[0]) + row * (which ? a.out_row[1] : a.out_row[0]) + share.h0 * out_head;
-      place.angles(a, row, lane);
-      int h = share.h0;
-      for (; h + 2 <= share.h1; h += 2, x += 2 * x_head, dy += 2 * dy_head, out += 2 * out_head) {
-        Two<T, V> t[2], g[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          t[i] = load_two<T, V>(x + i * x_head, place.at, place.left, a.past);
-          g[i] = load_two<T, V>(dy + i * dy_head, place.at, place.left, a.past);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) finish(t[i], g[i], out + i * out_head);
+      const T* x = static_cast<const T*>(which ? a.x[1] : a.x[0]) + row * (which ? a.x_row[1] : a.x_row[0]);
+      const T* dy = static_cast<const T*>(which ? a.dy[1] : a.dy[0]) + row * (which ? a.dy_row[1] : a.dy_row[0]);
+      T* out = static_cast<T*>(which ? a.out[1] : a.out[0]) + row * (which ? a.out_row[1] : a.out_row[0]);
+      for (int h = share.h0; h < share.h1; h += 2) {
+        const int other = min(h + 1, share.h1 - 1);
+        const Two<T, V> t[2] = {load_two<P, T, V>(place, x + h * x_head), load_two<P, T, V>(place, x + other * x_head)};
+        const Two<T, V> g[2] = {load_two<P, T, V>(place, dy + h * dy_head), load_two<P, T, V>(place, dy + other * dy_head)};
+        if (h == share.h0) place.angles(a, row);
+        finish(t[0], g[0], out + h * out_head);
+        if (other != h) finish(t[1], g[1], out + other * out_head);
       }
-      if (h < share.h1) finish(load_two<T, V>(x, place.at, place.left, a.past), load_two<T, V>(dy, place.at, place.left, a.past), out);
     }
   if (!a.partial) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (e < place.left[i]) s_sum[group][place.at[i] + e] = dw[i][e];
+      if (place.own(i, e)) s_sum[group][place.at[i] + e] = dw[i][e];
   __syncthreads();
   for (int c = threadIdx.x; c < 2 * a.dim; c += kHeadThreads) {
     const int k = c >= a.dim, at = c - (k ? a.dim : 0);
@@ -291,35 +341,45 @@ HeadShape head_shape(const HeadNormArgs& a, int32_t vec) {
   const int32_t half = a.rotary_dim / 2;
   s.turned = (half + vec - 1) / vec;  // vec pairs a lane
   s.items = s.turned + (a.dim - a.rotary_dim + 2 * vec - 1) / (2 * vec);
+  const int32_t rest = a.dim - a.rotary_dim, part = a.interleaved ? a.rotary_dim : half;
+  s.full = part >= vec && (rest == 0 || rest >= vec);
   s.lanes = 4;
   while (s.lanes < s.items) s.lanes *= 2;
-  // sixteen heads share an angle unless that leaves the chip under four waves a SIMD, or a row with more groups than
-  // a workgroup has
+  s.ragged = s.lanes > s.items || part % (a.interleaved ? 2 * vec : vec) != 0 || rest % (2 * vec) != 0;
+  // At most sixteen heads share their angles, and no more than leave the chip two waves a SIMD; a workgroup has room for
+  // a row's groups.  Groups wait for those with most heads, and an angle costs about as much as three heads: of 8 + 4 heads
+  // in groups of 4, 921,997 rows take X us, in groups of 8 864.
   const int32_t heads = a.heads[0] + a.heads[1], groups = kHeadThreads / s.lanes;
-  const int64_t wanted = 256 * 4 * 4 * 64;
-  s.each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(16, a.rows * s.lanes * heads / wanted));
-  auto count = [&](int i) { return (a.heads[i] + s.each - 1) / s.each; };
-  while (count(0) + count(1) > groups) ++s.each;
-  s.parts[0] = count(0);
-  s.parts[1] = count(1);
+  const int64_t wanted = 256 * 4 * 2 * 64;
+  const int32_t most = (int32_t)std::max<int64_t>(1, std::min<int64_t>(16, a.rows * s.lanes * heads / wanted));
+  auto count = [&](int i, int32_t each) { return (a.heads[i] + each - 1) / each; };
+  int64_t best = INT64_MAX;
+  for (int32_t each = 1; each <= 1024; ++each) {
+    const int64_t parts = count(0, each) + count(1, each);
+    if (parts > groups) continue;
+    if (each > most && best != INT64_MAX) break;
+    if (parts * (each + 3) < best) {
+      best = parts * (each + 3);
+      s.each = each;
+    }
+  }
+  s.parts[0] = count(0, s.each);
+  s.parts[1] = count(1, s.each);
   s.rows_block = groups / (s.parts[0] + s.parts[1]);
   return s;
 }
 
 template <typename T, bool BACKWARD, int LANES>
 void launch_lanes(const HeadNormArgs& a, const HeadShape& s, int64_t groups, hipStream_t st) {
-  const dim3 grid((uint32_t)groups), block(kHeadThreads);
-  if constexpr (BACKWARD) {
-    if (a.interleaved)
-      hipLaunchKernelGGL((head_norm_backward_kernel<T, true, LANES>), grid, block, 0, st, a, s);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kHeadThreads), 0, st, a, s); };
+  auto full = [&](auto which) {
+    constexpr bool FULL = decltype(which)::value;
+    if constexpr (BACKWARD)
+      a.interleaved ? go(head_norm_backward_kernel<T, true, LANES, FULL>) : go(head_norm_backward_kernel<T, false, LANES, FULL>);
     else
-      hipLaunchKernelGGL((head_norm_backward_kernel<T, false, LANES>), grid, block, 0, st, a, s);
-  } else {
-    if (a.interleaved)
-      hipLaunchKernelGGL((head_norm_kernel<T, true, LANES>), grid, block, 0, st, a, s);
-    else
-      hipLaunchKernelGGL((head_norm_kernel<T, false, LANES>), grid, block, 0, st, a, s);
-  }
+      a.interleaved ? go(head_norm_kernel<T, true, LANES, FULL>) : go(head_norm_kernel<T, false, LANES, FULL>);
+  };
+  s.full ? full(std::true_type{}) : full(std::false_type{});
 }
 
 // dim <= 256, so at most 64 lanes of 2 packs hold a head.

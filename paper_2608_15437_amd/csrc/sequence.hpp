@@ -90,7 +90,6 @@ struct HeadNormArgs {
   int32_t dim, rotary_dim, axes;
   int32_t interleaved;
   int32_t weight_f32;    // weights are fp32 (else of the rows' type)
-  int32_t past;          // store past the caches
   float eps, inv_dim;
 };
 
