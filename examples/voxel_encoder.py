@@ -1,7 +1,7 @@
 """From points to an encoded bird's-eye-view map: voxelise a batch of frames, train a small voxel encoder on them, encode
 the voxeliser's buffers without waiting for their counts, and scatter the result.
 
-    python examples/voxel_encoder.py [--frames 4] [--steps 20] [--width 128] [--heads 4] [--depth 2]
+    python examples/voxel_encoder.py [--frames 4] [--steps 20] [--width 128] [--heads 4] [--depth 2] [--gated]
 
 The frames are synthetic; the target is each voxel's mean intensity, smoothed over the voxels before it in its frame.
 """
@@ -31,13 +31,14 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, default in (("frames", 4), ("steps", 20), ("width", 128), ("heads", 4), ("depth", 2)):
         ap.add_argument("--" + name, type=int, default=default)
+    ap.add_argument("--gated", action="store_true", help="blocks with the gated delta rule")
     a = ap.parse_args(argv)
     torch.manual_seed(0)
     vz, feats, rows = inputs(a.frames)
     coords, offsets = vz.out_coords, vz.out_voxel_offsets
     print(f"{a.frames} frames, {rows} voxels of {feats.shape[1]} features", flush=True)
 
-    net = VoxelEncoder(feats.shape[1], a.width, a.heads, a.depth)
+    net = VoxelEncoder(feats.shape[1], a.width, a.heads, a.depth, gated=a.gated)
     opt = torch.optim.AdamW(net.parameters(), lr=2e-3)
     frame = coords[:rows, 0].long()
     total = feats[:rows, 3].cumsum(0)

@@ -2,8 +2,10 @@
 
 The voxeliser writes one row per voxel in key order, one range of rows per frame.  A block of the encoder norms the
 rows, turns queries and keys by their voxel coordinates, mixes each frame's rows by linear attention with a decay per
-head and adds the result to the rows; the projections between are plain matrix products of torch.  Gradients come from
-the library's backward calls, which have none themselves: a second derivative is refused.  A trained block can also go on row by row (`step`), its state kept between rows.
+head and adds the result to the rows; the projections between are plain matrix products of torch.  A gated block
+takes the gated delta rule instead, over queries and keys that are normed for each head as they are turned.  Gradients
+come from the library's backward calls, which have none themselves: a second derivative is refused.  A trained block can
+also go on row by row (`step`), its state kept between rows.
 
 The rows' number and ranges stay on the device: pass `row_count` (voxel_offsets[-1:]) to encode the voxeliser's full
 buffers without waiting for the count.  Results past it hold nothing of meaning; where gradients are wanted they are
@@ -12,6 +14,7 @@ zeros, and so are the gradients of those rows.
 from __future__ import annotations
 
 import functools
+import math
 
 import torch
 from torch import nn
@@ -121,6 +124,50 @@ class _Attention(torch.autograd.Function):
         return dq, dk, dv, None, None, dinitial, None, None
 
 
+class _HeadNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, steps, axis, eps, layout, row_count, wanted):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, steps, axis, row_count)
+        ctx.form = eps, layout
+        part = row_count is not None and wanted
+        return mmbev.head_norm_rotary(q, k, q_weight, k_weight, positions, steps, axis, eps=eps, layout=layout, row_count=row_count,
+                                      q_out=_rows_like(q, part), k_out=_rows_like(k, part))
+
+    @staticmethod
+    @_once
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, positions, steps, axis, row_count = ctx.saved_tensors
+        eps, layout = ctx.form
+        needed, part = ctx.needs_input_grad, row_count is not None
+        dq, dk, *sums = mmbev.head_norm_rotary_backward(
+            dq_out.contiguous(), dk_out.contiguous(), q, k, q_weight, k_weight, positions, steps, axis, eps=eps, layout=layout,
+            row_count=row_count, dq=_rows_like(q, part), dk=_rows_like(k, part), weight_grads=needed[2] or needed[3])
+        dqw, dkw = (t.to(w.dtype) if need else None for t, w, need in zip(sums, (q_weight, k_weight), needed[2:4]))
+        return dq if needed[0] else None, dk if needed[1] else None, dqw, dkw, None, None, None, None, None, None, None
+
+
+class _GatedDelta(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, beta, offsets, initial_state, max_length, wanted):
+        # the offsets alone know where the rows in use end
+        out = q.new_zeros(*q.shape[:2], v.shape[2]) if wanted else None
+        out, final = mmbev.gated_delta(q, k, v, log_decay, beta, offsets, initial_state=initial_state, final_state=True,
+                                       max_length=max_length, out=out)
+        ctx.save_for_backward(q, k, v, log_decay, beta, offsets, initial_state)
+        ctx.max_length = max_length
+        return out, final
+
+    @staticmethod
+    @_once
+    def backward(ctx, dout, dfinal):
+        q, k, v, log_decay, beta, offsets, initial_state = ctx.saved_tensors
+        *grads, dinitial = mmbev.gated_delta_backward(
+            dout.contiguous(), q, k, v, log_decay, beta, offsets, initial_state=initial_state, dfinal_state=dfinal.contiguous(),
+            dinitial_state=initial_state is not None, max_length=ctx.max_length, dq=torch.zeros_like(q), dk=torch.zeros_like(k),
+            dv=torch.zeros_like(v), dlog_decay=torch.zeros_like(log_decay), dbeta=torch.zeros_like(beta))
+        return *grads, None, dinitial, None, None
+
+
 def norm(x, residual, weight, bias, eps=1e-5, row_count=None):
     """(layer_norm(x + residual), x + residual), differentiable."""
     return _Norm.apply(x, residual, weight, bias, eps, row_count, _wanted(x, residual, weight, bias))
@@ -136,6 +183,17 @@ def linear_attention(q, k, v, log_decay, offsets, initial_state=None, max_length
     if log_decay.requires_grad and torch.is_grad_enabled():
         raise mmbev.MmbevError("log_decay has no gradient: detach it")
     return _Attention.apply(q, k, v, log_decay, offsets, initial_state, max_length, _wanted(q, k, v, initial_state))
+
+
+def head_norm_rotary(q, k, q_weight, k_weight, positions, steps, axis, eps=1e-6, layout="half", row_count=None):
+    """mmbev.head_norm_rotary, differentiable in q, k and the weights."""
+    return _HeadNorm.apply(q, k, q_weight, k_weight, positions, steps, axis, eps, layout, row_count, _wanted(q, k, q_weight, k_weight))
+
+
+def gated_delta(q, k, v, log_decay, beta, offsets, initial_state=None, max_length=None):
+    """mmbev.gated_delta's (out, final state), differentiable in all but the offsets."""
+    return _GatedDelta.apply(q, k, v, log_decay, beta, offsets, initial_state, max_length,
+                             _wanted(q, k, v, log_decay, beta, initial_state))
 
 
 class Block(nn.Module):
@@ -181,14 +239,53 @@ class Block(nn.Module):
         return x, out.flatten(1) @ self.out
 
 
-class VoxelEncoder(nn.Module):
-    """Voxel features [rows][features] to encoded ones [rows][out_features], fp32, as mmbev.scatter_to_bev takes them."""
+class GatedBlock(Block):
+    """The same with the gated delta rule: queries and keys normed for each head (keys to length 1, as the rule wants them)
+    and turned in one pass; decays and rates of writing per row and head from the normed rows."""
 
-    def __init__(self, features, width=128, heads=4, depth=2, out_features=32, dtype=torch.bfloat16, device="cuda", **block):
+    def __init__(self, width, heads, kv_heads=None, head_dim=None, axes=3, base=1000.0, dtype=torch.bfloat16, device="cuda"):
+        super().__init__(width, heads, kv_heads, head_dim, axes, base, dtype, device)
+        self.q_weight = nn.Parameter(torch.full((self.dim,), self.dim ** -0.5, device=device))
+        self.register_buffer("k_weight", torch.full((self.dim,), self.dim ** -0.5, device=device))
+        self.gates = nn.Parameter(torch.randn(width, 2 * heads, device=device) * width ** -0.5)
+        # the decays that Block's heads have, times softplus(gate) / ln 2, which is 1 at a gate of 0
+        self.rate = nn.Parameter((-self.log_decay).log())
+
+    def _project(self, x, branch, positions, row_count):
+        y, x = norm(x, branch, self.norm_weight, self.norm_bias, row_count=row_count)
+        rows = y @ self.qkv
+        q, k, v = (t.unflatten(1, (-1, self.dim)) for t in
+                   rows.split([self.heads * self.dim, self.kv_heads * self.dim, self.kv_heads * self.dim], dim=1))
+        q, k = head_norm_rotary(q, k, self.q_weight, self.k_weight, positions, self.steps, self.axis, row_count=row_count)
+        decay, beta = (y.float() @ self.gates).chunk(2, dim=1)
+        log_decay = -self.rate.exp() * nn.functional.softplus(decay) / math.log(2.0)
+        return x, q, k, v, log_decay, torch.sigmoid(beta)
+
+    def forward(self, x, branch, coords, offsets, state=None, max_length=None, row_count=None):
+        """As Block's."""
+        x, q, k, v, log_decay, beta = self._project(x, branch, coords[:, 1:], row_count)
+        out, state = gated_delta(q, k, v, log_decay, beta, offsets, state, max_length)
+        return x, out.flatten(1) @ self.out, state
+
+    @torch.no_grad()
+    def step(self, x, branch, coords, state, slots=None):
+        """One new row for each of many streams, whose states are updated in place."""
+        x, q, k, v, log_decay, beta = self._project(x, branch, coords[:, 1:], None)
+        out = mmbev.gated_delta_step(q, k, v, log_decay, beta, state, slots)
+        return x, out.flatten(1) @ self.out
+
+
+class VoxelEncoder(nn.Module):
+    """Voxel features [rows][features] to encoded ones [rows][out_features], fp32, as mmbev.scatter_to_bev takes them.
+    gated: its blocks are GatedBlocks."""
+
+    def __init__(self, features, width=128, heads=4, depth=2, out_features=32, dtype=torch.bfloat16, device="cuda", gated=False,
+                 **block):
         super().__init__()
         self.dtype = dtype
         self.embed = nn.Parameter(torch.randn(features, width, device=device, dtype=dtype) * features ** -0.5)
-        self.blocks = nn.ModuleList(Block(width, heads, dtype=dtype, device=device, **block) for _ in range(depth))
+        kind = GatedBlock if gated else Block
+        self.blocks = nn.ModuleList(kind(width, heads, dtype=dtype, device=device, **block) for _ in range(depth))
         self.norm_weight = nn.Parameter(torch.ones(width, device=device))
         self.norm_bias = nn.Parameter(torch.zeros(width, device=device))
         self.head = nn.Parameter(torch.randn(width, out_features, device=device, dtype=dtype) * width ** -0.5)
