@@ -499,18 +499,19 @@ __device__ __forceinline__ void put_inverses(Pairs<NS, PARTS>& to, const Gates& 
       beta[c + e] = b[e];
     }
   }
-  f32x4 row[2][4];  // of X: this column's and the next one's
+  f32x4 row[3][4];  // of X: this column's and the next two
   auto load = [&](int j) {
 #pragma unroll
-    for (int c = 0; c < j; c += 4) row[j & 1][c / 4] = four(x + j * kBlockStride + c);
+    for (int c = 0; c < j; c += 4) row[j % 3][c / 4] = four(x + j * kBlockStride + c);
   };
   load(15);
+  load(14);
 #pragma unroll
   for (int j = 15; j > 0; --j) {
-    if (j > 1) load(j - 1);
+    if (j > 2) load(j - 2);
     const float m = n[j] * beta[j];
 #pragma unroll
-    for (int c = 0; c < j; ++c) n[c] = __builtin_fmaf(-m, row[j & 1][c / 4][c % 4], n[c]);
+    for (int c = 0; c < j; ++c) n[c] = __builtin_fmaf(-m, row[j % 3][c / 4][c % 4], n[c]);
     // done before further rows are loaded: else all of them are at once, and the registers of the whole kernel are gone
 #pragma unroll
     for (int c = 0; c < j; ++c) asm volatile("" : "+v"(n[c])::"memory");
@@ -691,7 +692,7 @@ struct DeltaShared {
   If<!BACK, Values<T, W>> v[BUFFERS];
   If<BACK, Planes<T, W>> d[BUFFERS];
   If<MODE == kDeltaOut && BUFFERS == 1, Values<T, W>> out;
-  Gates gates[BUFFERS];
+  Gates gates[2];
   Pairs<NS, PARTS> pairs;
 };
 
@@ -778,11 +779,16 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
     from_k.fetch(rk, s0, hi);
     if constexpr (QUERIES) from_q.fetch(rq, s0, hi);
     from_v.fetch(rv, s0, hi);
-    if (has_share<NW>(3, l)) {
-      const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
-      rg = a.log_decay[row * a.g_row + h];
-      rb = a.beta[row * a.b_row + h];
-    }
+  };
+  // a chunk's gates are loaded two chunks ahead of it, and made one ahead
+  auto fetch_gates = [&](int32_t s0) {
+    const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
+    rg = a.log_decay[row * a.g_row + h];
+    rb = a.beta[row * a.b_row + h];
+  };
+  auto make_gates = [&](int32_t s0, int buffer) {
+    const bool there = (int)(threadIdx.x & 31) < hi - s0;
+    put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f, BACK ? 1.0f : there ? rb : 0.0f);
   };
   auto put = [&](int32_t s0, int buffer) {
     const int n = hi - s0;
@@ -792,10 +798,6 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
       sh.d[buffer].template put<NW>(rv, a.vd, n);
     else
       sh.v[buffer].template put<NW>(rv, a.vd, n);
-    if (has_share<NW>(3, l)) {
-      const bool there = (int)(threadIdx.x & 31) < n;
-      put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f, BACK ? 1.0f : there ? rb : 0.0f);
-    }
   };
   auto results = [&](int buffer) -> auto& {
     if constexpr (BUFFERS == 2)
@@ -819,18 +821,30 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
   };
 
   const int chunks = (hi - lo + kDeltaRows - 1) / kDeltaRows;
+  // (past the last chunk the last one again: loads under a condition would be waited for together with the results' stores)
+  auto begin = [&](int c) {
+    c = min(c, chunks - 1);
+    return lo + (BACK ? chunks - 1 - c : c) * kDeltaRows;
+  };
   if (chunks > 0) {
-    fetch(BACK ? lo + (chunks - 1) * kDeltaRows : lo);
-    put(BACK ? lo + (chunks - 1) * kDeltaRows : lo, 0);
+    fetch(begin(0));
+    if (has_share<NW>(3, l)) {
+      fetch_gates(begin(0));
+      make_gates(begin(0), 0);
+      fetch_gates(begin(1));
+    }
+    put(begin(0), 0);
     __syncthreads();
   }
   for (int c = 0; c < chunks; ++c) {
-    const int32_t s0 = lo + (BACK ? chunks - 1 - c : c) * kDeltaRows;
-    // (the last chunk is read twice: loads under a condition would be waited for together with the results' stores)
-    const int32_t next = c + 1 == chunks ? s0 : BACK ? s0 - kDeltaRows : s0 + kDeltaRows;
+    const int32_t s0 = begin(c), next = begin(c + 1);
     const int b = BUFFERS == 2 ? c & 1 : 0;
-    const Gates& gates = sh.gates[b];
+    const Gates& gates = sh.gates[c & 1];
     fetch(next);
+    if (has_share<NW>(3, l)) {
+      make_gates(next, (c + 1) & 1);
+      fetch_gates(begin(c + 2));
+    }
     put_pairs<T, DK, NW, NS, Shared::PARTS, BACK>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b].rows), gates, a.scale, l);
 
     // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
