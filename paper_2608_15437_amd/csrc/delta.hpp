@@ -581,15 +581,23 @@ __device__ __forceinline__ int state_row(int tile, int r, const Lane& l) { retur
 
 template <int DK, int TV>
 __device__ __forceinline__ void load_state(State<DK, TV>& st, const float* from, int kd, int vd, int col0, const Lane& l) {
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v) st[t][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (!from) return;
+  // unconditional loads of an element that is there: they do not wait for each other
 #pragma unroll
   for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
     for (int v = 0; v < TV; ++v)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = state_row(t, r, l), col = col0 + 16 * v + l.n;
-        st[t][v][r] = from && row < kd && col < vd ? from[row * vd + col] : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r) st[t][v][r] = from[min(state_row(t, r, l), kd - 1) * vd + min(col0 + 16 * v + l.n, vd - 1)];
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st[t][v][r] = state_row(t, r, l) < kd && col0 + 16 * v + l.n < vd ? st[t][v][r] : 0.0f;
 }
 
 template <int DK, int TV>
@@ -732,41 +740,6 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
   const Source<T, W, NW, WHOLE> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
   const bool own = col0 < columns && !(map && !began);
 
-  State<DK, TV> st;
-  {
-    const float* from = nullptr;
-    if constexpr (MODE == kDeltaStates)
-      from = !began && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
-    else if constexpr (MODE == kDeltaBackStates)
-      from = !goes_on && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
-    else if constexpr (MODE == kDeltaBack)
-      from = goes_on ? a.cut_grad + ((int64_t)boundary * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
-    else
-      from = began ? a.cut_state + ((int64_t)(boundary - 1) * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
-    load_state<DK, TV>(st, map ? nullptr : from, a.kd, columns, col0, l);
-    if constexpr (!STATES) {
-      // the end of the run of boundaries before
-      const int e = BACK ? boundary : boundary - 1, run = BACK ? e / a.run + 1 : e / a.run - 1;
-      if ((BACK ? goes_on : began) && own && a.from_run[BACK][e] && run >= 0 && run * a.run < a.cuts)
-        add_mapped<DK, TV>(st, a.run_map[BACK] + ((int64_t)e * a.H + h) * a.kd * a.kd, a.run_end[BACK] + ((int64_t)run * a.H + h) * each, a.kd,
-                           a.vd, col0, l);
-    }
-    if (map) {
-#pragma unroll
-      for (int t = 0; t < DK / 16; ++t)
-#pragma unroll
-        for (int v = 0; v < TV; ++v)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) st[t][v][r] = state_row(t, r, l) == col0 + 16 * v + l.n ? 1.0f : 0.0f;
-    }
-  }
-
-  // arrived: else its first use in the loop would wait, in every round, for all loads that are on their way by then
-#pragma unroll
-  for (int t = 0; t < DK / 16; ++t)
-#pragma unroll
-    for (int v = 0; v < TV; ++v) asm volatile("" : "+v"(st[t][v]));
-
   if constexpr (Shared::PARTS != 0) {
     // the first rows have nothing of the last ones
     for (int i = threadIdx.x; i < Shared::PARTS * 16 * 16; i += THREADS)
@@ -828,8 +801,46 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
   };
   if (chunks > 0) {
     fetch(begin(0));
+    if (has_share<NW>(3, l)) fetch_gates(begin(0));
+  }
+
+  State<DK, TV> st;
+  {
+    const float* from = nullptr;
+    if constexpr (MODE == kDeltaStates)
+      from = !began && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else if constexpr (MODE == kDeltaBackStates)
+      from = !goes_on && a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else if constexpr (MODE == kDeltaBack)
+      from = goes_on ? a.cut_grad + ((int64_t)boundary * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    else
+      from = began ? a.cut_state + ((int64_t)(boundary - 1) * a.H + h) * each : a.init ? a.init + ((int64_t)q.b * a.H + h) * each : nullptr;
+    load_state<DK, TV>(st, map ? nullptr : from, a.kd, columns, col0, l);
+    if constexpr (!STATES) {
+      // the end of the run of boundaries before
+      const int e = BACK ? boundary : boundary - 1, run = BACK ? e / a.run + 1 : e / a.run - 1;
+      if ((BACK ? goes_on : began) && own && a.from_run[BACK][e] && run >= 0 && run * a.run < a.cuts)
+        add_mapped<DK, TV>(st, a.run_map[BACK] + ((int64_t)e * a.H + h) * a.kd * a.kd, a.run_end[BACK] + ((int64_t)run * a.H + h) * each, a.kd,
+                           a.vd, col0, l);
+    }
+    if (map) {
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+        for (int v = 0; v < TV; ++v)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) st[t][v][r] = state_row(t, r, l) == col0 + 16 * v + l.n ? 1.0f : 0.0f;
+    }
+  }
+
+  // arrived: else its first use in the loop would wait, in every round, for all loads that are on their way by then
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int v = 0; v < TV; ++v) asm volatile("" : "+v"(st[t][v]));
+
+  if (chunks > 0) {
     if (has_share<NW>(3, l)) {
-      fetch_gates(begin(0));
       make_gates(begin(0), 0);
       fetch_gates(begin(1));
     }
