@@ -24,7 +24,7 @@ namespace {
 // product each and pass the result on through LDS.  The next boundary's
 // matrices are loaded before this one's product.  Bound by that chain, 1 to 2
 // us a boundary: a keyframe's 127 boundaries of 8 heads of 64 33 us, the ends
-// 14; 128 of 4 heads of 128, both ways, 133 and 35.  (Four boundaries' loads
+// 17; 127 of 4 heads of 128, both ways, 133 and 35.  (Four boundaries' loads
 // ahead took as long: 40 and 18, 182 and 39.)
 constexpr int kJoinTile = 16, kJoinThreads = 256;
 
