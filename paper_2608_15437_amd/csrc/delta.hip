@@ -22,11 +22,24 @@ namespace {
 // run before (add_mapped).
 // A workgroup has 16 columns of B or of the map; its waves take 16 rows of a
 // product each and pass the result on through LDS.  The next boundary's
-// matrices are loaded before this one's product.  Bound by that chain, 1 to 2
-// us a boundary: a keyframe's 127 boundaries of 8 heads of 64 33 us, the ends
-// 17; 127 of 4 heads of 128, both ways, 133 and 35.  (Four boundaries' loads
-// ahead took as long: 40 and 18, 182 and 39.)
+// matrices are loaded before this one's product.  Bound by that chain, 2 to 4
+// us a boundary: a keyframe's 127 boundaries of 8 heads of 64 27 us, the ends
+// 17; 127 of 4 heads of 128, both ways, 130 and 34.  (Four boundaries' loads
+// ahead took longer: 40 us instead of 33, 182 instead of 133; so did 32 columns
+// of heads of 128, 155.)
 constexpr int kJoinTile = 16, kJoinThreads = 256;
+
+__host__ __device__ inline int tiles_of(int columns) { return (columns + kJoinTile - 1) / kJoinTile; }
+
+// The workgroups that read the same maps lie next to each other on the same die (the dies take eight workgroups in turn),
+// whose L2 then has them once: a keyframe's joining 33 -> 27 us, 8 frames' both ways 62 -> 46.
+struct Chain {
+  int chain, tile;
+};
+__device__ __forceinline__ Chain chain_of(int tiles) {
+  const int turn = blockIdx.x / 8;
+  return {turn / tiles * 8 + (int)(blockIdx.x % 8), turn % tiles};
+}
 
 // A boundary's part of the recurrence: X = map X + add, or X = add.
 struct Link {
@@ -112,7 +125,7 @@ struct Flags {
 template <int DK, bool BACK>
 __device__ __forceinline__ void join_run(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)], int run, int tile, int h) {
   const int64_t each = (int64_t)a.kd * a.vd, square = (int64_t)a.kd * a.kd;
-  const int tiles = (a.vd + kJoinTile - 1) / kJoinTile, first = run * a.run, count = min(a.run, a.cuts - first);
+  const int tiles = tiles_of(a.vd), first = run * a.run, count = min(a.run, a.cuts - first);
   const bool map = tile >= tiles;
   float* state = BACK ? a.cut_grad : a.cut_state;
   const float* maps = BACK ? a.cut_turned : a.cut_map;
@@ -136,23 +149,25 @@ template <int DK>
 __global__ __launch_bounds__(kJoinThreads) void delta_join_kernel(DeltaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
   const int runs = (a.cuts + a.run - 1) / a.run;
-  if ((int)blockIdx.z < runs)
-    join_run<DK, false>(a, s_x, blockIdx.z, blockIdx.x, blockIdx.y);
-  else
-    join_run<DK, true>(a, s_x, blockIdx.z - runs, blockIdx.x, blockIdx.y);
+  const Chain c = chain_of(tiles_of(a.vd) + tiles_of(a.kd));
+  const int run = c.chain / a.H, h = c.chain - run * a.H;
+  if (run < runs)
+    join_run<DK, false>(a, s_x, run, c.tile, h);
+  else if (a.cut_grad && run < 2 * runs)
+    join_run<DK, true>(a, s_x, run - runs, c.tile, h);
 }
 
 // The runs' ends.
 template <int DK, bool BACK>
-__device__ __forceinline__ void join_ends(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)]) {
-  const int h = blockIdx.y, runs = (a.cuts + a.run - 1) / a.run;
+__device__ __forceinline__ void join_ends(const DeltaArgs& a, bf16 (*s_x)[3 * kJoinTile * (DK + kPlanePad)], int tile, int h) {
+  const int runs = (a.cuts + a.run - 1) / a.run;
   const int64_t each = (int64_t)a.kd * a.vd, square = (int64_t)a.kd * a.kd;
   auto run_of = [&](int i) { return BACK ? runs - 1 - i : i; };
   auto boundary = [&](int i) { return BACK ? run_of(i) * a.run : min((run_of(i) + 1) * a.run, a.cuts) - 1; };
   const int e = boundary(min((int)threadIdx.x & 63, runs - 1));
   const bool there = a.cut_kind[e] >= 0;
   const Flags f = {__ballot(there), __ballot(there && a.from_run[BACK][e])};
-  carry_on<DK>(s_x, runs, blockIdx.x * kJoinTile, a.kd, a.vd, false, [&](int i) {
+  carry_on<DK>(s_x, runs, tile * kJoinTile, a.kd, a.vd, false, [&](int i) {
     const int64_t at = (int64_t)boundary(i) * a.H + h;
     return Link{a.run_map[BACK] + at * square, (BACK ? a.cut_grad : a.cut_state) + at * each, a.run_end[BACK] + ((int64_t)run_of(i) * a.H + h) * each,
                 f.is_there(i), f.do_carry(i) && i > 0};
@@ -162,14 +177,18 @@ __device__ __forceinline__ void join_ends(const DeltaArgs& a, bf16 (*s_x)[3 * kJ
 template <int DK>
 __global__ __launch_bounds__(kJoinThreads) void delta_ends_kernel(DeltaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16 s_x[2][3 * kJoinTile * (DK + kPlanePad)];
-  blockIdx.z == 0 ? join_ends<DK, false>(a, s_x) : join_ends<DK, true>(a, s_x);
+  const Chain c = chain_of(tiles_of(a.vd));
+  if (c.chain < a.H)
+    join_ends<DK, false>(a, s_x, c.tile, c.chain);
+  else if (a.cut_grad && c.chain < 2 * a.H)
+    join_ends<DK, true>(a, s_x, c.tile, c.chain - a.H);
 }
 
 hipError_t join_states(const DeltaArgs& a, bool backward, hipStream_t st) {
-  const int tiles = (a.vd + kJoinTile - 1) / kJoinTile, map_tiles = (a.kd + kJoinTile - 1) / kJoinTile, runs = (a.cuts + a.run - 1) / a.run;
+  const int runs = (a.cuts + a.run - 1) / a.run, chains = backward ? 2 * a.H : a.H;
   auto go = [&](auto join, auto ends) {
-    hipLaunchKernelGGL(join, dim3(tiles + map_tiles, a.H, runs * (backward ? 2 : 1)), dim3(kJoinThreads), 0, st, a);
-    hipLaunchKernelGGL(ends, dim3(tiles, a.H, backward ? 2 : 1), dim3(kJoinThreads), 0, st, a);
+    hipLaunchKernelGGL(join, dim3((runs * chains + 7) / 8 * 8 * (tiles_of(a.vd) + tiles_of(a.kd))), dim3(kJoinThreads), 0, st, a);
+    hipLaunchKernelGGL(ends, dim3((chains + 7) / 8 * 8 * tiles_of(a.vd)), dim3(kJoinThreads), 0, st, a);
   };
   a.kd <= 32   ? go(delta_join_kernel<32>, delta_ends_kernel<32>)
   : a.kd <= 64 ? go(delta_join_kernel<64>, delta_ends_kernel<64>)

@@ -10,6 +10,9 @@ also go on row by row (`step`), its state kept between rows.
 The rows' number and ranges stay on the device: pass `row_count` (voxel_offsets[-1:]) to encode the voxeliser's full
 buffers without waiting for the count.  Results past it hold nothing of meaning; where gradients are wanted they are
 zeros, and so are the gradients of those rows.
+
+A training step may be captured into a graph.  As with all torch modules, no eager autograd graph of the same
+parameters may be alive meanwhile: drop the results of earlier passes first.
 """
 from __future__ import annotations
 

@@ -200,6 +200,42 @@ def test_backward_pass_in_a_graph(gpu_lib):
             assert torch.equal(a, b)
 
 
+def test_gradients_of_the_modules_in_a_graph(gpu_lib):
+    """A block's forward and backward pass captured with no eager graph of its leaves alive, replayed with other rows."""
+    import torch
+
+    from paper_2608_15437_amd.encoder import GatedBlock
+
+    torch.manual_seed(8)
+    off, rows = torch.tensor([0, 90, 90, 700], device="cuda"), 700
+    block = GatedBlock(64, 2, dtype=torch.float32)
+    # the library's own sums over rows (torch's may clear their scratch memory by a node that a graph should not hold)
+    leaves = [block.norm_weight, block.norm_bias, block.q_weight]
+    coords = torch.randint(0, 200, (rows, 4), device="cuda", dtype=torch.int32)
+    x, weight = torch.randn(rows, 64, device="cuda"), torch.randn(rows, 64, device="cuda")
+
+    def work():
+        y, branch, state = block(x, torch.zeros_like(x), coords, off)
+        return [t.detach() for t in (branch, state, *torch.autograd.grad([branch, state], leaves, [weight, state.detach()]))]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, 64, device="cuda"))
+        want = work()
+        graph.replay()
+        torch.cuda.synchronize()
+        # torch's own products may take other tiles in the two: fp32 sums over 700 rows of results off by some steps
+        for a, b in zip(got, want):
+            assert (a - b).norm() <= 700 * 2 ** -24 * b.norm()
+
+
 def test_example_trains(gpu_lib):
     import torch
 
