@@ -33,9 +33,9 @@
 // splitting results into parts, masks, addresses) and the chain through a
 // chunk, with two waves a SIMD, which the registers of a state allow; the
 // matrix cores are busy for 25%, LDS for 40%.  128 frames of 921,997 rows, 8
-// heads of 64 in bf16: 1,261 us, 3.0 TB/s.  Rows fetched two chunks ahead
+// heads of 64 in bf16: 1,252 us, 3.1 TB/s.  Rows fetched two chunks ahead
 // instead of one took registers and 6% longer.  A single sequence is walked in
-// parts, its keys and values read twice: 120,000 rows 430 us.
+// parts, its keys and values read twice: 120,000 rows 416 us.
 #pragma once
 
 #include <type_traits>
