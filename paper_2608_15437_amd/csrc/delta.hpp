@@ -1109,6 +1109,9 @@ __device__ __forceinline__ bool chunk_at(int64_t place, const Order& o, int32_t&
 template <typename T, int DK, int TV, bool WHOLE>
 __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
   constexpr int NP = kPlanes<T>, W = 64 * TV, TD = DK >= 64 ? DK / 64 : 1, PER = W / 8;
+  // where one workgroup has a compute unit's LDS the states are on their way while the rows are worked on (heads of 128 214
+  // -> 186 us); where it has three, the registers run out (890 -> 1,114)
+  constexpr bool EARLY = delta_grad_waves(sizeof(T), DK, W) == 1;
   __shared__ DeltaGradShared<T, DK, TV> sh;
   const Lane l = lane_of();
   const int KV = a.H / a.group, hk = blockIdx.x % KV;
@@ -1134,6 +1137,8 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
 
   for (int j = 0; j < a.group; ++j) {
     const int h = hk * a.group + j;
+    Pack<float, 8> before[W / 32][TD], after[W / 32][TD];
+    const float *pb = a.before + (place * a.H + h) * each, *pa = a.after + (place * a.H + h) * each;
     {
       Pack<T, 8> rq[kPacks<DK, kGradWaves>], rd[kPacks<W, kGradWaves>];
       Pack<float, 8> re[kPacks<W, kGradWaves>], rz[kPacks<W, kGradWaves>];
@@ -1151,6 +1156,22 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
 #pragma unroll
       for (int i = 0; i < kPacks<W, kGradWaves>; ++i)
         rb[i] = a.beta[(int64_t)min(s0 + (int)(threadIdx.x + i * 64 * kGradWaves) / PER, hi - 1) * a.b_row + h];
+      if constexpr (EARLY) {
+#pragma unroll
+        for (int s = 0; s < W / 32; ++s)
+#pragma unroll
+          for (int d = 0; d < TD; ++d) {
+            // (rows past the last one are its copies)
+            const int row = min(16 * (l.w * TD + d) + l.n, a.kd - 1) * a.vd, c = 32 * s + 8 * l.g;
+            if constexpr (WHOLE) {
+              before[s][d] = load_pack<float, 8>(pb + row + min(c, a.vd - 8));
+              after[s][d] = load_pack<float, 8>(pa + row + min(c, a.vd - 8));
+            } else {
+              before[s][d] = load_some<float, 8>(pb + row + c, a.vd - c);
+              after[s][d] = load_some<float, 8>(pa + row + c, a.vd - c);
+            }
+          }
+      }
       if (j) __syncthreads();  // the head before has been read
       if (j == 0) sh.k.template put<kGradWaves>(rk, a.kd, n);
       sh.q.template put<kGradWaves>(rq, a.kd, n);
@@ -1204,15 +1225,23 @@ __global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64
 #pragma unroll
       for (int d = 0; d < TD; ++d) read_q[t][d] = read_k[t][d] = written[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (own) {
-      const float *before = a.before + (place * a.H + h) * each, *after = a.after + (place * a.H + h) * each;
 #pragma unroll
       for (int s = 0; s < W / 32; ++s) {
 #pragma unroll
         for (int d = 0; d < TD; ++d) {
           const int row = 16 * (l.w * TD + d) + l.n;
           float x[8], z[8];
-          load_eight(x, before, row, 32 * s + 8 * l.g, a.kd, a.vd);
-          load_eight(z, after, row, 32 * s + 8 * l.g, a.kd, a.vd);
+          if constexpr (EARLY) {
+            const bool there = row < a.kd && 32 * s + 8 * l.g < a.vd;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              x[e] = there ? before[s][d].v[e] : 0.0f;
+              z[e] = there ? after[s][d].v[e] : 0.0f;
+            }
+          } else {
+            load_eight(x, pb, row, 32 * s + 8 * l.g, a.kd, a.vd);
+            load_eight(z, pa, row, 32 * s + 8 * l.g, a.kd, a.vd);
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) both = __builtin_fmaf(x[e], z[e], both);
           const Parts<3> sp = split<3>(x), gp = split<3>(z);
