@@ -759,11 +759,10 @@ size_t mmbev_gated_delta_workspace_bytes(const mmbev_attention_t* attention, int
  *            without bound, as the rule itself does.
  * A sequence with a NaN or infinity in a row, a gate or its initial state has
  * unspecified results; other sequences and heads do not see it.
- * States, e, and everything between a row and them are as exact as fp32 where
- * final_state is asked for (for 16-bit types what enters only `out` takes part
- * in 16 bits or more; without a final state so does everything).  32 rows are
- * solved at a time: rows that repeat one key with a beta near 2 pass a
- * rounding on up to 63 times as large, with a beta of 1 twice.
+ * States, e, and everything between a row and a result are as exact as fp32;
+ * a result is rounded once.  32 rows are solved at a time: rows that repeat one
+ * key with a beta near 2 pass a rounding on up to 63 times as large, with a
+ * beta of 1 twice.
  * max_length only sizes the launches: longer sequences are computed too.
  * out must not overlap an input.
  */

@@ -27,15 +27,19 @@
 // bf16 row is one part, an fp16 row two, an fp32 value three; bf16 has fp32's
 // exponents, so nothing is scaled).  An fp32 product this way is six products
 // of bf16, 2.7 times as fast as the fp32 ones of the matrix cores.  What only
-// enters a 16-bit result takes two parts, 16 bits.
+// enters a 16-bit result has three parts too: with two, 0.4% of the results
+// were not the nearest value to their sum instead of 0.03%, and a state that
+// was no output lost bits in every chunk.  (128 frames' results took 1,260 us
+// that way instead of 1,700, a frame's 68 instead of 77, a keyframe's 420
+// instead of 432.)
 //
 // What bounds the walks: issue of vector instructions (58 to 72% of the time:
 // splitting results into parts, masks, addresses) and the chain through a
 // chunk, with two waves a SIMD, which the registers of a state allow; the
 // matrix cores are busy for 25%, LDS for 40%.  128 frames of 921,997 rows, 8
-// heads of 64 in bf16: 1,252 us, 3.1 TB/s.  Rows fetched two chunks ahead
+// heads of 64 in bf16: 1,700 us, 2.3 TB/s.  Rows fetched two chunks ahead
 // instead of one took registers and 6% longer.  A single sequence is walked in
-// parts, its keys and values read twice: 120,000 rows 416 us.
+// parts, its keys and values read twice: 120,000 rows 432 us.
 #pragma once
 
 #include <type_traits>
@@ -51,11 +55,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 b16x4 __attribute__((ext_vector_type(4)));
 
-// Parts of bf16 that a row's element is, and those that enter a result.
+// Parts of bf16 that a row's element is, and those of an fp32 value.
 template <typename T>
 constexpr int kPlanes = sizeof(T) == 4 ? 3 : __is_same(T, f16) ? 2 : 1;
-template <typename T>
-constexpr int kOutParts = sizeof(T) == 4 ? 3 : 2;
+constexpr int kParts = 3;
 
 struct Lane {
   int w, g, n;  // wave; lane / 16; lane % 16
@@ -210,29 +213,26 @@ __device__ __forceinline__ Parts<N> columns_of(const bf16* s, int plane, int str
 constexpr int kBlockStride = 20;  // rows of eight-byte steps over all banks
 constexpr int kBlock = 16 * kBlockStride;
 
-template <int N>
 struct Block {
   b16x8 high, ends;  // first and second part; first and third
 };
 
-template <int N, bool TRANSPOSED>
-__device__ __forceinline__ Block<N> block_of(const bf16* s, const Lane& l) {
-  b16x4 p[N];
+template <bool TRANSPOSED>
+__device__ __forceinline__ Block block_of(const bf16* s, const Lane& l) {
+  b16x4 p[kParts];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < kParts; ++i) {
     if constexpr (TRANSPOSED)
       p[i] = read_columns(s + i * kBlock + (4 * l.g + (l.n >> 2)) * kBlockStride + (l.n & 3) * 4);
     else
       __builtin_memcpy(&p[i], __builtin_assume_aligned(s + i * kBlock + l.n * kBlockStride + 4 * l.g, 8), 8);
   }
-  return {__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(p[0], p[N - 1], 0, 1, 2, 3, 4, 5, 6, 7)};
+  return {__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(p[0], p[2], 0, 1, 2, 3, 4, 5, 6, 7)};
 }
 
 // c + block * x
-template <int N>
-__device__ __forceinline__ f32x4 mma_block(const Block<N>& a, const Quarter<N>& q, f32x4 c) {
-  if constexpr (N == 3)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(q.p[2], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mma_block(const Block& a, const Quarter<kParts>& q, f32x4 c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.ends, __builtin_shufflevector(q.p[2], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
   c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(q.p[1], q.p[1], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.high, __builtin_shufflevector(q.p[0], q.p[0], 0, 1, 2, 3, 4, 5, 6, 7), c, 0, 0, 0);
 }
@@ -446,14 +446,14 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// What the rows of a chunk do to each other, in NS parts (P: PARTS), with the rows' beta multiplied in: forwards that of
+// What the rows of a chunk do to each other (P: where WITH_P), with the rows' beta multiplied in: forwards that of
 // the row that is read (N beta, -X beta, P beta), backwards that of the row that reads (beta N, -beta X, P as it is).
 constexpr int kPairStride = kDeltaRows + 4, kPairPlane = kDeltaRows * kPairStride;
 
-template <int NS, int PARTS>
+template <bool WITH_P>
 struct Pairs {
-  __attribute__((aligned(16))) bf16 n[3][NS * kBlock];  // N of the first and last 16 rows, -X of the last with the first
-  __attribute__((aligned(16))) bf16 p[PARTS ? PARTS * kPairPlane : 8];
+  __attribute__((aligned(16))) bf16 n[3][kParts * kBlock];  // N of the first and last 16 rows, -X of the last with the first
+  __attribute__((aligned(16))) bf16 p[WITH_P ? kParts * kPairPlane : 8];
   __attribute__((aligned(16))) float x[2][kBlock];      // X of the first and last 16 rows
 };
 
@@ -492,8 +492,8 @@ __device__ __forceinline__ f32x4 dots(const Planes<T, DK>& a, int i0, const Plan
 // N = -X - N beta X of both blocks of 16 rows, by one wave: lane i of each half has row i of a block (twice), and takes
 // its columns from the last one on, X's rows read out of LDS.  A row needs no other's, so there is no exchange between
 // lanes: 120 multiply-adds behind each other's loads, not their results.
-template <int NS, int PARTS, bool BACK>
-__device__ __forceinline__ void put_inverses(Pairs<NS, PARTS>& to, const Gates& s) {
+template <bool WITH_P, bool BACK>
+__device__ __forceinline__ void put_inverses(Pairs<WITH_P>& to, const Gates& s) {
   const int lane = threadIdx.x & 63, block = lane >> 5, i = lane & 15, columns = lane >> 4 & 1;
   const float* x = to.x[block];
   float n[16], beta[16];
@@ -532,8 +532,8 @@ __device__ __forceinline__ void put_inverses(Pairs<NS, PARTS>& to, const Gates& 
     y[e / 4][e % 4] = columns ? v : u;
   }
   bf16* p = to.n[block] + i * kBlockStride + 8 * columns;
-  put4<NS>(p, kBlock, y[0]);
-  put4<NS>(p + 4, kBlock, y[1]);
+  put4<kParts>(p, kBlock, y[0]);
+  put4<kParts>(p + 4, kBlock, y[1]);
 }
 
 // The waves' shares of a chunk's preparation: the inverses, the last rows with the first, the rest (none where there is no
@@ -543,34 +543,33 @@ __device__ __forceinline__ bool has_share(int share, const Lane& l) {
   return NW >= 4 ? l.w == share : NW == 3 ? l.w == (share == 3 ? 2 : share) : l.w == (share ? 1 : 0);
 }
 
-// (PARTS 0: no P.)
-template <typename T, int DK, int NW, int NS, int PARTS, bool BACK>
-__device__ __forceinline__ void put_pairs(Pairs<NS, PARTS>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
+template <typename T, int DK, int NW, bool WITH_P, bool BACK>
+__device__ __forceinline__ void put_pairs(Pairs<WITH_P>& to, const Planes<T, DK>& k, const Planes<T, DK>* q, const Gates& s, float scale,
                                           const Lane& l) {
   const f32x4 one = {1.0f, 1.0f, 1.0f, 1.0f};
   if (has_share<NW>(0, l)) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const f32x4 x = decayed<true>(dots<NS>(k, 16 * b, k, 16 * b, l), decays(s, 16 * b, 16 * b, l), false, l);
+      const f32x4 x = decayed<true>(dots<kParts>(k, 16 * b, k, 16 * b, l), decays(s, 16 * b, 16 * b, l), false, l);
       __builtin_memcpy(__builtin_assume_aligned(to.x[b] + l.n * kBlockStride + 4 * l.g, 16), &x, 16);
     }
     wave_fence();
-    put_inverses<NS, PARTS, BACK>(to, s);
+    put_inverses<WITH_P, BACK>(to, s);
   }
   if (has_share<NW>(1, l)) {
     const f32x4 d = decays(s, 16, 0, l), beta = BACK ? one : four(s.beta + 4 * l.g);
     const f32x4 x = d * (BACK ? one * -s.beta[16 + l.n] : -beta);
-    put4<NS>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed<false>(dots<NS>(k, 16, k, 0, l), x, false, l));
-    if constexpr (PARTS)
-      put4<PARTS>(to.p + (16 + l.n) * kPairStride + 4 * l.g, kPairPlane, decayed<false>(dots<PARTS>(*q, 16, k, 0, l), d * scale * beta, false, l));
+    put4<kParts>(to.n[2] + l.n * kBlockStride + 4 * l.g, kBlock, decayed<false>(dots<kParts>(k, 16, k, 0, l), x, false, l));
+    if constexpr (WITH_P)
+      put4<kParts>(to.p + (16 + l.n) * kPairStride + 4 * l.g, kPairPlane, decayed<false>(dots<kParts>(*q, 16, k, 0, l), d * scale * beta, false, l));
   }
-  if constexpr (PARTS != 0) {
+  if constexpr (WITH_P) {
     if (has_share<NW>(2, l)) {
 #pragma unroll
       for (int i0 = 0; i0 < kDeltaRows; i0 += 16) {
         const f32x4 d = decays(s, i0, i0, l) * scale;
-        put4<PARTS>(to.p + (i0 + l.n) * kPairStride + i0 + 4 * l.g, kPairPlane,
-                    decayed<true>(dots<PARTS>(*q, i0, k, i0, l), BACK ? d : d * four(s.beta + i0 + 4 * l.g), true, l));
+        put4<kParts>(to.p + (i0 + l.n) * kPairStride + i0 + 4 * l.g, kPairPlane,
+                    decayed<true>(dots<kParts>(*q, i0, k, i0, l), BACK ? d : d * four(s.beta + i0 + 4 * l.g), true, l));
       }
     }
   }
@@ -689,35 +688,25 @@ constexpr int kWalkTiles = 2;
 template <int DK, int W, int MODE>
 constexpr int kWalkWaves = (MODE == kDeltaStates ? W + DK : W) / (16 * kWalkTiles);
 
-template <typename T, int DK, int W, int MODE, bool EXACT>
+template <typename T, int DK, int W, int MODE>
 struct DeltaShared {
   static constexpr bool BACK = MODE >= kDeltaBackStates, QUERIES = MODE == kDeltaOut || BACK;
-  static constexpr int PARTS = MODE == kDeltaOut ? kOutParts<T> : BACK ? 3 : 0, NS = EXACT ? 3 : 2;
-  // (two: a keyframe's results with the state 215 us instead of 204, 128 frames' without 1,276 instead of 1,500)
-  static constexpr int BUFFERS = __is_same(T, bf16) && DK <= 64 && W <= 64 && !EXACT ? 2 : 1;
   template <bool THERE, typename X>
   using If = std::conditional_t<THERE, X, Nothing>;
-  // a chunk's results take its queries' place where that is not written again at once
-  union Queries {
-    If<QUERIES, Planes<T, DK>> rows;
-    If<MODE == kDeltaOut && BUFFERS == 2, Values<T, W>> out;
-    __device__ Queries() {}
-  };
-  Planes<T, DK> k[BUFFERS];
-  Queries q[BUFFERS];
-  If<!BACK, Values<T, W>> v[BUFFERS];
-  If<BACK, Planes<T, W>> d[BUFFERS];
-  If<MODE == kDeltaOut && BUFFERS == 1, Values<T, W>> out;
+  Planes<T, DK> k;
+  If<QUERIES, Planes<T, DK>> q;
+  If<!BACK, Values<T, W>> v;
+  If<BACK, Planes<T, W>> d;
+  If<MODE == kDeltaOut, Values<T, W>> out;
   Gates gates[2];
-  Pairs<NS, PARTS> pairs;
+  Pairs<QUERIES> pairs;
 };
 
-template <typename T, int DK, int W, int MODE, bool EXACT, bool WHOLE>
+template <typename T, int DK, int W, int MODE, bool WHOLE>
 __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(T), DK, W)) void delta_walk_kernel(DeltaArgs a) {
-  using Shared = DeltaShared<T, DK, W, MODE, EXACT>;
+  using Shared = DeltaShared<T, DK, W, MODE>;
   constexpr int NW = kWalkWaves<DK, W, MODE>, TV = kWalkTiles, THREADS = 64 * NW;
-  constexpr int NS = Shared::NS;
-  constexpr int NP = kPlanes<T>, OUT = kOutParts<T>, BUFFERS = Shared::BUFFERS;
+  constexpr int NP = kPlanes<T>;
   constexpr bool BACK = Shared::BACK, QUERIES = Shared::QUERIES, STATES = MODE == kDeltaStates || MODE == kDeltaBackStates;
   __shared__ Shared sh;
   const Lane l = lane_of();
@@ -748,9 +737,9 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
   const Source<T, W, NW, WHOLE> from_v(BACK ? a.dout : a.v, BACK ? h * a.d_head : hk * a.v_head, BACK ? a.d_row : a.v_row, a.vd);
   const bool own = col0 < columns && !(map && !began);
 
-  if constexpr (Shared::PARTS != 0) {
+  if constexpr (QUERIES) {
     // the first rows have nothing of the last ones
-    for (int i = threadIdx.x; i < Shared::PARTS * 16 * 16; i += THREADS)
+    for (int i = threadIdx.x; i < kParts * 16 * 16; i += THREADS)
       sh.pairs.p[i / 256 * kPairPlane + i % 256 / 16 * kPairStride + 16 + i % 16] = (bf16)0.0f;
   }
 
@@ -771,31 +760,24 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
     const bool there = (int)(threadIdx.x & 31) < hi - s0;
     put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f, BACK ? 1.0f : there ? rb : 0.0f);
   };
-  auto put = [&](int32_t s0, int buffer) {
+  auto put = [&](int32_t s0) {
     const int n = hi - s0;
-    sh.k[buffer].template put<NW>(rk, a.kd, n);
-    if constexpr (QUERIES) sh.q[buffer].rows.template put<NW>(rq, a.kd, n);
+    sh.k.template put<NW>(rk, a.kd, n);
+    if constexpr (QUERIES) sh.q.template put<NW>(rq, a.kd, n);
     if constexpr (BACK)
-      sh.d[buffer].template put<NW>(rv, a.vd, n);
+      sh.d.template put<NW>(rv, a.vd, n);
     else
-      sh.v[buffer].template put<NW>(rv, a.vd, n);
+      sh.v.template put<NW>(rv, a.vd, n);
   };
-  auto results = [&](int buffer) -> auto& {
-    if constexpr (BUFFERS == 2)
-      return sh.q[buffer].out;
-    else
-      return sh.out;
-  };
-  auto store_out = [&](int32_t s0, int buffer) {
+  auto store_out = [&](int32_t s0) {
     if constexpr (MODE == kDeltaOut) {
-      const auto& from = results(buffer);
       T* po = static_cast<T*>(a.out) + h * a.o_head;
 #pragma unroll
       for (int i = 0; i < kPacks<W, NW>; ++i) {
         const int idx = threadIdx.x + i * THREADS, row = idx / (W / 8), c = idx % (W / 8) * 8;
         if (s0 + row >= hi || c >= a.vd || row >= kDeltaRows) continue;
         Pack<T, 8> x;
-        __builtin_memcpy(&x, __builtin_assume_aligned(from.v + row * from.stride + c, 16), sizeof(x));
+        __builtin_memcpy(&x, __builtin_assume_aligned(sh.out.v + row * sh.out.stride + c, 16), sizeof(x));
         store_some<T, 8>(po + (int64_t)(s0 + row) * a.o_row + c, x, a.vd - c, a.past);
       }
     }
@@ -852,19 +834,18 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
       make_gates(begin(0), 0);
       fetch_gates(begin(1));
     }
-    put(begin(0), 0);
+    put(begin(0));
     __syncthreads();
   }
   for (int c = 0; c < chunks; ++c) {
     const int32_t s0 = begin(c), next = begin(c + 1);
-    const int b = BUFFERS == 2 ? c & 1 : 0;
     const Gates& gates = sh.gates[c & 1];
     fetch(next);
     if (has_share<NW>(3, l)) {
       make_gates(next, (c + 1) & 1);
       fetch_gates(begin(c + 2));
     }
-    put_pairs<T, DK, NW, NS, Shared::PARTS, BACK>(sh.pairs, sh.k[b], reinterpret_cast<const Planes<T, DK>*>(&sh.q[b].rows), gates, a.scale, l);
+    put_pairs<T, DK, NW, QUERIES, BACK>(sh.pairs, sh.k, reinterpret_cast<const Planes<T, DK>*>(&sh.q), gates, a.scale, l);
 
     // the products with the state: K S, lane n column n of it; and (Q S) transposed, lane n row n
     f32x4 ks[2][TV], qs[2][TV];
@@ -875,18 +856,18 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
     if (own) {
 #pragma unroll
       for (int s = 0; s < DK / 32; ++s) {
-        Parts<NS> x[TV];
+        Parts<kParts> x[TV];
 #pragma unroll
-        for (int v = 0; v < TV; ++v) x[v] = split<NS>(st[2 * s][v], st[2 * s + 1][v]);
+        for (int v = 0; v < TV; ++v) x[v] = split<kParts>(st[2 * s][v], st[2 * s + 1][v]);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const Parts<NP> k = sh.k[b].rows(16 * t, 32 * s, l);
+          const Parts<NP> k = sh.k.rows(16 * t, 32 * s, l);
 #pragma unroll
-          for (int v = 0; v < TV; ++v) ks[t][v] = mma<NS>(k, x[v], ks[t][v]);
+          for (int v = 0; v < TV; ++v) ks[t][v] = mma<kParts>(k, x[v], ks[t][v]);
           if constexpr (MODE == kDeltaOut) {
-            const Parts<NP> qr = sh.q[b].rows.rows(16 * t, 32 * s, l);
+            const Parts<NP> qr = sh.q.rows(16 * t, 32 * s, l);
 #pragma unroll
-            for (int v = 0; v < TV; ++v) qs[t][v] = mma<OUT>(x[v], qr, qs[t][v]);
+            for (int v = 0; v < TV; ++v) qs[t][v] = mma<kParts>(x[v], qr, qs[t][v]);
           }
         }
       }
@@ -905,7 +886,7 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
         left[t] = four(gates.left + 16 * t + 4 * l.g);
       }
       f32x4 e[2][TV];
-      Quarter<NS> ep[2][TV];  // forwards e's parts
+      Quarter<kParts> ep[2][TV];  // forwards e's parts
       Parts<NP> dout[TV];
       {
         // forwards the first 16 rows first, backwards the last
@@ -916,7 +897,7 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
                                   columns_of<3>(sh.pairs.p, kPairPlane, kPairStride, 16, l)};
 #pragma unroll
           for (int v = 0; v < TV; ++v) {
-            dout[v] = sh.d[b].columns(col0 + 16 * v, l);
+            dout[v] = sh.d.columns(col0 + 16 * v, l);
 #pragma unroll
             for (int t = 0; t < 2; ++t) e[t][v] = mma<3>(pt[t], dout[v], ks[t][v] * left[t]);
           }
@@ -926,20 +907,19 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
               f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-              if (!map) x = sh.v[b].down(16 * t, col0 + 16 * v, l);
+              if (!map) x = sh.v.down(16 * t, col0 + 16 * v, l);
 #pragma unroll
               for (int r = 0; r < 4; ++r) e[t][v][r] = __builtin_fmaf(-fade[t][r], ks[t][v][r], x[r]);
             }
         }
-        const Block<NS> first = block_of<NS, BACK>(sh.pairs.n[F], l), cross = block_of<NS, BACK>(sh.pairs.n[2], l),
-                        last = block_of<NS, BACK>(sh.pairs.n[L], l);
+        const Block first = block_of<BACK>(sh.pairs.n[F], l), cross = block_of<BACK>(sh.pairs.n[2], l), last = block_of<BACK>(sh.pairs.n[L], l);
 #pragma unroll
         for (int v = 0; v < TV; ++v) {
-          e[F][v] = mma_block(first, split<NS>(e[F][v]), e[F][v]);
-          ep[F][v] = split<NS>(e[F][v]);
+          e[F][v] = mma_block(first, split<kParts>(e[F][v]), e[F][v]);
+          ep[F][v] = split<kParts>(e[F][v]);
           e[L][v] = mma_block(cross, ep[F][v], e[L][v]);
-          e[L][v] = mma_block(last, split<NS>(e[L][v]), e[L][v]);
-          if constexpr (MODE == kDeltaOut) ep[L][v] = split<NS>(e[L][v]);
+          e[L][v] = mma_block(last, split<kParts>(e[L][v]), e[L][v]);
+          if constexpr (MODE == kDeltaOut) ep[L][v] = split<kParts>(e[L][v]);
         }
       }
       if constexpr (MODE == kDeltaSave || MODE == kDeltaBack) {
@@ -959,21 +939,20 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
       if constexpr (MODE == kDeltaOut) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const Parts<OUT> p = rows_split<OUT>(sh.pairs.p, kPairPlane, kPairStride, 16 * t, l);
+          const Parts<kParts> p = rows_split<kParts>(sh.pairs.p, kPairPlane, kPairStride, 16 * t, l);
           const float f = gates.fade[16 * t + l.n] * a.scale;
 #pragma unroll
           for (int v = 0; v < TV; ++v) {
-            const f32x4 x = mma<OUT>(both<OUT>(ep[0][v], ep[1][v]), p, qs[t][v] * f);
+            const f32x4 x = mma<kParts>(both<kParts>(ep[0][v], ep[1][v]), p, qs[t][v] * f);
             Pack<T, 4> y;
 #pragma unroll
             for (int r = 0; r < 4; ++r) y.v[r] = (T)x[r];
-            auto& to = results(b);
-            __builtin_memcpy(__builtin_assume_aligned(to.v + (16 * t + l.n) * to.stride + col0 + 16 * v + 4 * l.g, 4 * sizeof(T)), &y, sizeof(y));
+            __builtin_memcpy(__builtin_assume_aligned(sh.out.v + (16 * t + l.n) * sh.out.stride + col0 + 16 * v + 4 * l.g, 4 * sizeof(T)), &y, sizeof(y));
           }
         }
       }
       // the state after the chunk (backwards: its gradient before it)
-      Parts<NS> x[TV], y[TV];
+      Parts<kParts> x[TV], y[TV];
       const f32x4 beta[2] = {four(gates.beta + 4 * l.g), four(gates.beta + 16 + 4 * l.g)};
 #pragma unroll
       for (int v = 0; v < TV; ++v) {
@@ -986,32 +965,29 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
             for (int p = 0; p < NP; ++p) f[i] += (float)dout[v].p[p][i];
             f[i] *= fade[i / 4][i % 4] * a.scale;
           }
-          y[v] = split<NS>(f);
-          x[v] = split<NS>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
+          y[v] = split<kParts>(f);
+          x[v] = split<kParts>(-(fade[0] * beta[0] * e[0][v]), -(fade[1] * beta[1] * e[1][v]));
         } else {
-          x[v] = split<NS>(left[0] * e[0][v], left[1] * e[1][v]);  // (beta is in there)
+          x[v] = split<kParts>(left[0] * e[0][v], left[1] * e[1][v]);  // (beta is in there)
         }
       }
 #pragma unroll
       for (int t = 0; t < DK / 16; ++t) {
         const int c0 = 32 * (t / 2) + 4 * (t % 2);
-        const Parts<NP> k = sh.k[b].template columns<8>(c0, l);
+        const Parts<NP> k = sh.k.template columns<8>(c0, l);
 #pragma unroll
-        for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(k, x[v], st[t][v] * whole);
+        for (int v = 0; v < TV; ++v) st[t][v] = mma<kParts>(k, x[v], st[t][v] * whole);
         if constexpr (BACK) {
-          const Parts<NP> qc = sh.q[b].rows.template columns<8>(c0, l);
+          const Parts<NP> qc = sh.q.template columns<8>(c0, l);
 #pragma unroll
-          for (int v = 0; v < TV; ++v) st[t][v] = mma<NS>(qc, y[v], st[t][v]);
+          for (int v = 0; v < TV; ++v) st[t][v] = mma<kParts>(qc, y[v], st[t][v]);
         }
       }
     }
-    if (BUFFERS == 2) put(next, b ^ 1);
     __syncthreads();  // the results are there, the chunk has been read
-    store_out(s0, b);
-    if (BUFFERS == 1) {
-      put(next, 0);
-      __syncthreads();
-    }
+    store_out(s0);
+    put(next);
+    __syncthreads();
   }
   if (!own) return;
   if constexpr (STATES) {
@@ -1359,14 +1335,14 @@ void with_dims(int kd, int vd, F&& f) {
 
 bool whole_packs(const DeltaArgs& a) { return a.kd % 8 == 0 && a.vd % 8 == 0; }
 
-template <typename T, int MODE, bool EXACT = true>
+template <typename T, int MODE>
 hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
   with_dims(a.kd, a.vd, [&](auto key, auto value) {
     constexpr int DK = decltype(key)::value, W = decltype(value)::value;
     constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
     const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWalkWaves<DK, W, MODE>), 0, st, a); };
-    whole_packs(a) ? go(delta_walk_kernel<T, DK, W, MODE, EXACT, true>) : go(delta_walk_kernel<T, DK, W, MODE, EXACT, false>);
+    whole_packs(a) ? go(delta_walk_kernel<T, DK, W, MODE, true>) : go(delta_walk_kernel<T, DK, W, MODE, false>);
   });
   return hipGetLastError();
 }
@@ -1384,8 +1360,6 @@ hipError_t grad_of(const DeltaGradArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t delta_walk(const DeltaArgs& a, int mode, hipStream_t st) {
-  if constexpr (sizeof(T) == 2)
-    if (!a.exact) return mode == kDeltaStates ? walk_of<T, kDeltaStates, false>(a, st) : walk_of<T, kDeltaOut, false>(a, st);
   switch (mode) {
     case kDeltaStates: return walk_of<T, kDeltaStates>(a, st);
     case kDeltaOut: return walk_of<T, kDeltaOut>(a, st);

@@ -302,7 +302,6 @@ mmbev_status_t mmbev_gated_delta(const mmbev_attention_t* t, mmbev_heads_t q, mm
   put(out, &a.out, &a.o_row, &a.o_head);
   a.init = initial_state;
   a.final_state = final_state;
-  a.exact = final_state != nullptr;
   a.fault = fault;
   return status_of(launch_delta(a, T, (hipStream_t)stream));
 }
@@ -348,7 +347,6 @@ mmbev_status_t mmbev_gated_delta_backward(const mmbev_attention_t* t, mmbev_head
   a.dbeta = (float*)dbeta.data;
   a.db_row = (int32_t)dbeta.row_stride;
   a.init = initial_state;
-  a.exact = 1;
   a.fault = fault;
   a.cut_grad = (float*)(ws + p.off_grad);
   a.cut_turned = (float*)(ws + p.off_turned);

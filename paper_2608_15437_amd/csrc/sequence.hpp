@@ -211,7 +211,6 @@ struct DeltaArgs : Ranges {
   int32_t H, group;       // group: heads that share keys and values
   int32_t kd, vd;
   int32_t past;           // store past the caches
-  int32_t exact;          // the state is an output, or what the gradients need: as exact as fp32
   float scale;
   // boundaries between parts of a cut sequence: kind -1: there is none, 0: the part before it begins its sequence, 1: it does not
   int32_t* cut_kind;      // [cuts]
