@@ -752,12 +752,12 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
   };
   // a chunk's gates are loaded two chunks ahead of it, and made one ahead
   auto fetch_gates = [&](int32_t s0) {
-    const int64_t row = min(s0 + (int)(threadIdx.x & 31), hi - 1);
+    const int64_t row = delta_row(s0, threadIdx.x & 31, hi);
     rg = a.log_decay[row * a.g_row + h];
     rb = a.beta[row * a.b_row + h];
   };
   auto make_gates = [&](int32_t s0, int buffer) {
-    const bool there = (int)(threadIdx.x & 31) < hi - s0;
+    const bool there = delta_row_there(s0, threadIdx.x & 31, hi);
     put_gates(sh.gates[buffer], there ? rg : 0.0f, there ? rb : 0.0f, BACK ? 1.0f : there ? rb : 0.0f);
   };
   auto put = [&](int32_t s0) {
@@ -775,7 +775,7 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
 #pragma unroll
       for (int i = 0; i < kPacks<W, NW>; ++i) {
         const int idx = threadIdx.x + i * THREADS, row = idx / (W / 8), c = idx % (W / 8) * 8;
-        if (s0 + row >= hi || c >= a.vd || row >= kDeltaRows) continue;
+        if (!delta_row_there(s0, row, hi) || c >= a.vd || row >= kDeltaRows) continue;
         Pack<T, 8> x;
         __builtin_memcpy(&x, __builtin_assume_aligned(sh.out.v + row * sh.out.stride + c, 16), sizeof(x));
         store_some<T, 8>(po + (int64_t)(s0 + row) * a.o_row + c, x, a.vd - c, a.past);
@@ -783,11 +783,11 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
     }
   };
 
-  const int chunks = (hi - lo + kDeltaRows - 1) / kDeltaRows;
+  const int chunks = delta_chunks(lo, hi);
   // (past the last chunk the last one again: loads under a condition would be waited for together with the results' stores)
   auto begin = [&](int c) {
     c = min(c, chunks - 1);
-    return lo + (BACK ? chunks - 1 - c : c) * kDeltaRows;
+    return delta_chunk(lo, BACK ? chunks - 1 - c : c);
   };
   if (chunks > 0) {
     fetch(begin(0));
@@ -928,11 +928,11 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int32_t row = s0 + 16 * t + 4 * l.g + r;
+            const int row = 16 * t + 4 * l.g + r;
 #pragma unroll
             for (int v = 0; v < TV; ++v) {
               const int col = col0 + 16 * v + l.n;
-              if (row < hi && col < a.vd) to[(int64_t)row * a.H * a.vd + col] = e[t][v][r];
+              if (delta_row_there(s0, row, hi) && col < a.vd) to[((int64_t)s0 + row) * a.H * a.vd + col] = e[t][v][r];
             }
           }
       }

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "delta_rows.hpp"
 #include "mmbev.h"
 
 namespace mmbev {
@@ -193,8 +194,6 @@ struct AttnStepArgs {
 hipError_t launch_attention_step(const AttnStepArgs& a, int32_t dtype, hipStream_t st);
 
 // ---- the gated delta rule
-
-constexpr int kDeltaRows = 32;  // rows of a chunk
 
 // One walk over chunks: forwards over (q, k, v) or, for the gradients,
 // backwards over (q, k, dout).
