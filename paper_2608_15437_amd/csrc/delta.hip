@@ -316,7 +316,7 @@ hipError_t walk(const DeltaArgs& a, DeltaMode mode, int32_t dtype, hipStream_t s
 
 hipError_t launch_delta(const DeltaArgs& a, int32_t dtype, hipStream_t st) {
   check_offsets(a, st);
-  if (a.cuts) {
+  if (a.cuts >= kDeltaLeastCuts) {
     hipError_t e = walk(a, kDeltaStates, dtype, st);
     if (e == hipSuccess) e = join_states(a, false, st);
     if (e != hipSuccess) return e;
@@ -330,7 +330,7 @@ hipError_t launch_delta_backward(const DeltaGradArgs& a, const float* dfinal, fl
   back.init = dfinal;
   back.final_state = dinitial;
   hipError_t e = hipSuccess;
-  if (a.cuts) {
+  if (a.cuts >= kDeltaLeastCuts) {
     e = walk(a, kDeltaStates, dtype, st);
     if (e == hipSuccess) e = walk(back, kDeltaBackStates, dtype, st);
     if (e == hipSuccess) e = join_states(a, true, st);

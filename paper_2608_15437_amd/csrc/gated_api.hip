@@ -73,8 +73,9 @@ bool outputs_apart(const mmbev_head_norm_t* t, const mmbev_heads_t (&out)[2], st
 // ------------------------------------------------------------ gated delta rule
 
 // A sequence and head is a workgroup's work; long sequences are cut so that the workgroups fill the chip's compute units,
-// in parts of at least kDeltaLeast rows, and none where none can be longer than kDeltaWhole or among more sequences
-// than a workgroup can look through in passing.
+// in parts of at least kDeltaLeast rows, and none where none can be longer than kDeltaWhole, among more sequences than a
+// workgroup can look through in passing, or where the heads alone come to so many that there are under kDeltaLeastCuts
+// shares (then a single sequence has a workgroup a head, of fp32 heads over 64 from 86 on, be that fewer than there are units).
 constexpr int64_t kComputeUnits = 256;
 constexpr int64_t kDeltaWhole = 512;
 constexpr int32_t kDeltaLeast = 128;
@@ -112,25 +113,25 @@ DeltaPlan delta_plan(const mmbev_attention_t* t, bool backward) {
   // steps one after the other: a run's boundaries and the runs
   p.run = 1;
   while (p.run * p.run < p.cuts) ++p.run;
-  const size_t state = (size_t)t->heads * t->key_dim * t->value_dim * 4, maps = (size_t)p.cuts * t->heads * t->key_dim * t->key_dim * 4;
-  const size_t runs = (p.cuts + p.run - 1) / p.run;
-  size_t at = align256((size_t)p.cuts * 4);
+  const size_t cuts = p.cuts >= kDeltaLeastCuts ? p.cuts : 0, runs = (cuts + p.run - 1) / p.run;
+  const size_t state = (size_t)t->heads * t->key_dim * t->value_dim * 4, maps = cuts * t->heads * t->key_dim * t->key_dim * 4;
+  size_t at = align256(cuts * 4);
   auto take = [&](size_t bytes) {
     const size_t from = at;
     at = align256(at + bytes);
     return from;
   };
   for (int i = 0; i < (backward ? 2 : 1); ++i) {
-    p.off_from[i] = take((size_t)p.cuts * 4);
+    p.off_from[i] = take(cuts * 4);
     p.off_run[i] = take(maps);
     p.off_end[i] = take(runs * state);
   }
-  p.off_state = take(p.cuts * state);
+  p.off_state = take(cuts * state);
   p.off_map = take(maps);
   if (backward) {
     p.off_turned = take(maps);
     const size_t chunks = (size_t)delta_slots(t->rows, t->num_sequences), rows = (size_t)t->rows * t->heads * t->value_dim * 4;
-    p.off_grad = take(p.cuts * state);
+    p.off_grad = take(cuts * state);
     p.off_before = take(chunks * state);
     p.off_after = take(chunks * state);
     p.off_left = take(rows);

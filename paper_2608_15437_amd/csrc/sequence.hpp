@@ -230,6 +230,10 @@ struct DeltaArgs : Ranges {
   float* due;             // its gradient
 };
 
+// Of one or two shares of the rows none is less than half of a sequence, so none is cut: nothing is launched for parts, and
+// they have no room.
+constexpr int32_t kDeltaLeastCuts = 3;
+
 // Chunks of a sequence lie next to each other from rows / 32 + sequence on, so no two chunks share a place.
 inline int64_t delta_slots(int64_t rows, int64_t B) { return rows / kDeltaRows + B; }
 

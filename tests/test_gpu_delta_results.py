@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import gated as og
-from test_gpu_delta import CASES, DEEP, LONG, delta_case, near
+from test_gpu_delta import CASES, DEEP, LONG, check_backward, check_forward, delta_case, near
 from test_gpu_sequence import U, close, up
 
 pytestmark = pytest.mark.gpu
@@ -99,3 +99,11 @@ def test_whole_sequences_longest_first(gpu_lib, dtype, B, H):
     near(got[:used], want[:used], U[dtype], "out")
     for b in range(B):
         near(final[b], last[b], U["f32"], f"final state {b}")
+
+
+@pytest.mark.parametrize("H,kv,lengths", [(90, 45, [600, 30]), (64, 64, [520, 0, 40]), (64, 1, [700])])
+def test_heads_that_leave_few_shares(gpu_lib, H, kv, lengths):
+    """fp32 heads over 64 wide: two shares of the rows and fewer, where no sequence is cut, and three, where one is."""
+    c, ref = delta_case(400 + H, lengths, H, kv, 66, 8, "f32", carry=True)
+    check_forward(gpu_lib, c, ref)
+    check_backward(gpu_lib, c, ref)
