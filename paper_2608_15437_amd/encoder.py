@@ -11,8 +11,10 @@ The rows' number and ranges stay on the device: pass `row_count` (voxel_offsets[
 buffers without waiting for the count.  Results past it hold nothing of meaning; where gradients are wanted they are
 zeros, and so are the gradients of those rows.
 
-A training step may be captured into a graph.  As with all torch modules, no eager autograd graph of the same
-parameters may be alive meanwhile: drop the results of earlier passes first.
+The operators and the gradients that they sum themselves (of rows, norms' weights and biases) may be captured into a graph.
+As with all torch modules, no eager autograd graph of the same parameters may be alive meanwhile: drop the results of
+earlier passes first.  The other parameters' gradients are torch's own products and sums over rows (a gated block's
+`rate` is one), which may clear scratch memory by nodes of the graph: compare replays of such a step with eager ones.
 """
 from __future__ import annotations
 
