@@ -1083,11 +1083,12 @@ __device__ __forceinline__ bool chunk_at(int64_t place, const Order& o, int32_t&
 }
 
 template <typename T, int DK, int TV, bool WHOLE>
-__global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
+__global__ __launch_bounds__(64 * kGradWaves, delta_grad_waves(__is_same(T, f16), sizeof(T), DK, 64 * TV)) void delta_grad_kernel(DeltaGradArgs a) {
   constexpr int NP = kPlanes<T>, W = 64 * TV, TD = DK >= 64 ? DK / 64 : 1, PER = W / 8;
-  // where one workgroup has a compute unit's LDS the states are on their way while the rows are worked on (heads of 128 214
-  // -> 186 us); where it has three, the registers run out (890 -> 1,114)
-  constexpr bool EARLY = delta_grad_waves(sizeof(T), DK, W) == 1;
+  // where a compute unit has one or two workgroups the states are on their way while the rows are worked on (fp16 heads of
+  // 128 214 -> 186 us; the whole call of 8 crowded frames in fp32 4,090 -> 4,050, in fp16 3,195 -> 3,140); where it has
+  // three, the registers run out (bf16 890 -> 1,114)
+  constexpr bool EARLY = delta_grad_waves(__is_same(T, f16), sizeof(T), DK, W) < 3;
   __shared__ DeltaGradShared<T, DK, TV> sh;
   const Lane l = lane_of();
   const int KV = a.H / a.group, hk = blockIdx.x % KV;
@@ -1340,6 +1341,7 @@ hipError_t walk_of(const DeltaArgs& a, hipStream_t st) {
   with_dims(a.kd, a.vd, [&](auto key, auto value) {
     constexpr int DK = decltype(key)::value, W = decltype(value)::value;
     constexpr bool states = MODE == kDeltaStates || MODE == kDeltaBackStates;
+    static_assert(delta_groups(__is_same(T, f16), sizeof(T), DK, W) * sizeof(DeltaShared<T, DK, W, MODE>) <= 160 * 1024, "the plan's workgroups fit");
     const dim3 grid((uint32_t)((states ? a.cuts : a.cuts + a.B) * (int64_t)a.H));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWalkWaves<DK, W, MODE>), 0, st, a); };
     whole_packs(a) ? go(delta_walk_kernel<T, DK, W, MODE, true>) : go(delta_walk_kernel<T, DK, W, MODE, false>);

@@ -102,7 +102,7 @@ mmbev_status_t delta_ok(const mmbev_attention_t* t, bool step) {
 DeltaPlan delta_plan(const mmbev_attention_t* t, bool backward) {
   DeltaPlan p{};
   // workgroups that the chip takes at once
-  const int64_t slots = kComputeUnits * delta_groups(size_of(t->dtype), t->key_dim, t->value_dim);
+  const int64_t slots = kComputeUnits * delta_groups(t->dtype == MMBEV_F16, size_of(t->dtype), t->key_dim, t->value_dim);
   const int64_t longest = t->max_length > 0 ? std::min(t->max_length, t->rows) : t->rows;
   if (longest > kDeltaWhole && t->num_sequences <= kDeltaCutSequences) {
     // so many parts that with the sequences that are not cut there are about `units` of them: at least half the units

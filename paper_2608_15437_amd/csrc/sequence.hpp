@@ -245,14 +245,18 @@ struct DeltaGradArgs : DeltaArgs {
   float *dlog_decay, *dbeta;  // fp32 [rows][H]
 };
 
-// Waves a SIMD that the walks' kernels have registers for, and the workgroups that a compute unit takes, as their LDS
-// allows; keys and values padded to `key` and `value`.
+// Waves a SIMD that the walks' kernels are compiled for, the workgroups that a compute unit takes of them, as LDS and
+// those waves allow, and the waves that the gradients' kernel is compiled for; keys and values padded to `key` and `value`.
+// (fp16 heads over 32 have three workgroups: with a plan for four, whose last ones begin when the others end, a keyframe
+// of 8 heads of 64 took 631 us instead of 575, gradients of 8 crowded frames 3,500 instead of 3,180.)
 constexpr int delta_waves(int size, int key, int value) { return size == 4 && (key > 64 || value > 64) ? 1 : 2; }
-constexpr int delta_groups(int size, int key, int value) {
+constexpr int delta_groups(bool f16, int size, int key, int value) {
   const bool wide = key > 64 || value > 64;
-  return size == 4 ? (wide ? 1 : 2) : wide ? 2 : 4;
+  return size == 4 ? (wide ? 1 : 2) : wide ? 2 : f16 && key > 32 ? 3 : 4;
 }
-constexpr int delta_grad_waves(int size, int key, int value) { return size == 4 || key > 64 || value > 64 ? 1 : 3; }
+constexpr int delta_grad_waves(bool f16, int size, int key, int value) {
+  return size == 4 || key > 64 || value > 64 ? 1 : f16 && key > 32 ? 2 : 3;
+}
 
 hipError_t launch_delta(const DeltaArgs& a, int32_t dtype, hipStream_t st);
 hipError_t launch_delta_backward(const DeltaGradArgs& a, const float* dfinal, float* dinitial, int32_t dtype, hipStream_t st);

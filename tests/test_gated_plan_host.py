@@ -16,3 +16,16 @@ def test_no_room_for_cuts_that_cannot_be(mb):  # noqa: F811
     # backwards the chunks' states and rows alone
     chunks, rows = (100000 // 32 + 1) * 128 * 128 * 128 * 4, 100000 * 128 * 128 * 4
     assert 0 <= size(128, 1) - 2 * (chunks + rows) < 4 * 256
+
+
+def test_parts_for_the_workgroups_that_fit(mb):  # noqa: F811
+    """A long sequence of 8 heads is cut so that its parts fill the chip's 256 units once: four workgroups a unit in bf16, three
+    in fp16, whose rows take more LDS, but of heads up to 32 four; the room is proportional to the parts."""
+    def room(dtype, dim):
+        return mb.load().mmbev_gated_delta_workspace_bytes(ctypes.byref(attention(mb, rows=120000, num_sequences=1, heads=8, kv_heads=8, key_dim=dim,
+                                                                                  value_dim=64, dtype=dtype)), 0)
+
+    for dtype, dim, parts in ((2, 64, 127), (1, 64, 95), (1, 40, 95), (0, 64, 63)):
+        one = 8 * dim * (64 + 2 * dim) * 4  # a state and two maps
+        assert parts * one < room(dtype, dim) < (parts + 1) * one + 16 * 8 * dim * 64 * 4, (dtype, dim)
+    assert room(1, 32) == room(2, 32)
