@@ -928,11 +928,11 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int row = 16 * t + 4 * l.g + r;
+            const int32_t row = s0 + 16 * t + 4 * l.g + r;  // (a call with gradients has fewer than 2^29 rows)
 #pragma unroll
             for (int v = 0; v < TV; ++v) {
               const int col = col0 + 16 * v + l.n;
-              if (delta_row_there(s0, row, hi) && col < a.vd) to[((int64_t)s0 + row) * a.H * a.vd + col] = e[t][v][r];
+              if (row < hi && col < a.vd) to[(int64_t)row * a.H * a.vd + col] = e[t][v][r];
             }
           }
       }
