@@ -23,8 +23,8 @@ namespace {
 // A workgroup has 16 columns of B or of the map; its waves take 16 rows of a
 // product each and pass the result on through LDS.  The next boundary's
 // matrices are loaded before this one's product.  Bound by that chain, 2 to 4
-// us a boundary: a keyframe's 127 boundaries of 8 heads of 64 27 us, the ends
-// 17; 127 of 4 heads of 128, both ways, 130 and 34.  (Four boundaries' loads
+// us a boundary: a keyframe's 127 boundaries of 8 heads of 64 24 us, the ends
+// 16; 127 of 4 heads of 128, both ways, 123 and 34.  (Four boundaries' loads
 // ahead took longer: 40 us instead of 33, 182 instead of 133; so did 32 columns
 // of heads of 128, 155.)
 constexpr int kJoinTile = 16, kJoinThreads = 256;
@@ -32,7 +32,7 @@ constexpr int kJoinTile = 16, kJoinThreads = 256;
 __host__ __device__ inline int tiles_of(int columns) { return (columns + kJoinTile - 1) / kJoinTile; }
 
 // The workgroups that read the same maps lie next to each other on the same die (the dies take eight workgroups in turn),
-// whose L2 then has them once: a keyframe's joining 33 -> 27 us, 8 frames' both ways 62 -> 46.
+// whose L2 then has them once: a keyframe's joining 33 -> 24 us, 8 frames' both ways 59 -> 43.
 struct Chain {
   int chain, tile;
 };
@@ -202,7 +202,7 @@ hipError_t join_states(const DeltaArgs& a, bool backward, hipStream_t st) {
 // neighbouring columns of every (256 / lanes)-th state row in registers, lanes
 // enough for a row of the state; the rows' parts of both sums meet in LDS.
 // 1,024 streams of 8 heads of 128 x 128: 211 us, 5.1 TB/s; 64 of 8 heads of
-// 64 x 64: 6.2 us.
+// 64 x 64: 6.1 us.
 template <typename T, int LANES, int ROWS>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
   constexpr int PARTS = 256 / LANES;

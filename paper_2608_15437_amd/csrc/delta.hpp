@@ -16,10 +16,10 @@
 //   D_before = e^(G_end) D + (scale e^G Q)^T dout - (e^G K)^T beta Z.
 //
 // All that a row of the state's columns needs of another is in K, Q, N and P,
-// so a wave walks 16 columns (TV times 16) alone: its state stays in registers
-// from chunk to chunk, and every product's result is the next one's operand
-// where it lies.  What the rows do to each other (N and P) is worked out once a
-// chunk by the workgroup's four waves, through LDS.
+// so a wave walks 32 columns (two tiles of 16) alone: its state stays in
+// registers from chunk to chunk, and every product's result is the next one's
+// operand where it lies.  What the rows do to each other (N and P) is worked out
+// once a chunk by the workgroup's waves, two to eight of them, through LDS.
 //
 // Precision: the state and the gradients of the gates are fp32 and go through
 // thousands of chunks, so every product is as exact as fp32's: an operand is
@@ -33,13 +33,19 @@
 // that way instead of 1,700, a frame's 68 instead of 77, a keyframe's 420
 // instead of 432.)
 //
-// What bounds the walks: issue of vector instructions (58 to 72% of the time:
-// splitting results into parts, masks, addresses) and the chain through a
-// chunk, with two waves a SIMD, which the registers of a state allow; the
-// matrix cores are busy for 25%, LDS for 40%.  128 frames of 921,997 rows, 8
-// heads of 64 in bf16: 1,700 us, 2.3 TB/s.  Rows fetched two chunks ahead
-// instead of one took registers and 6% longer.  A single sequence is walked in
-// parts, its keys and values read twice: 120,000 rows 432 us.
+// What bounds the walks: issue of vector instructions (heads of 64 in bf16: 64
+// to 73% of the time forwards, 51 to 65% in the gradients' walks: splitting
+// results into parts, masks, addresses) and the chain through a chunk, with two
+// waves a SIMD, which the registers of a state allow; the matrix cores are busy
+// for 15 to 30%, LDS for 18 to 34%.  128 frames of 921,997 rows, 8 heads of 64
+// in bf16: 1,680 us, 2.3 TB/s.  Rows fetched two chunks ahead instead of one
+// took registers and 6% longer.  A single sequence is walked in parts, its keys
+// and values read twice: 120,000 rows 432 us.  Of 16-bit keys over 64 the two
+// walks that leave what the gradients need have a state too large for their 256
+// registers and spill about 100 of them (344 to 500 bytes of scratch a lane; not
+// the one backwards of fp16 values up to 64, which has one wave a SIMD): vector
+// instructions are 20% of the time, 18,608 rows of 4 heads of 128 in fp16 take
+// 173 and 206 us.
 #pragma once
 
 #include <type_traits>
@@ -1029,7 +1035,7 @@ __global__ __launch_bounds__((64 * kWalkWaves<DK, W, MODE>), delta_waves(sizeof(
 //
 // A workgroup has a chunk and the heads that share its key; the walks left S,
 // D, E and Z in memory.  Reading them is what bounds it (213,879 rows, 8 heads
-// of 64 over 4 in bf16: 3.5 GB in 890 us, 3.9 TB/s): states between chunks of
+// of 64 over 4 in bf16: 3.5 GB in 852 us, 4.1 TB/s): states between chunks of
 // 32 rows are four times a chunk's keys and values.
 
 constexpr int kGradWaves = 4;

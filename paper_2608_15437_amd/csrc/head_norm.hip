@@ -20,8 +20,10 @@
 // fp32 676 instead of 554.)  Measured: 921,997 rows of 8 + 4 heads of 64 in
 // bf16 571 us, 5.0 TB/s; gradients of 213,879 rows of 8 + 8 heads in fp32 501
 // us, 5.2 TB/s, HBM's; of 18,608 rows of 4 + 4 heads of 100 in fp16 31 us, 2.9
-// TB/s (400-byte heads, lanes that share elements, three axes' angles); a frame's
-// 5,442 rows in 10 us, the chain from position to angle to row.
+// TB/s (200-byte heads, lanes that share elements, three axes' angles, and 1,163
+// blocks of rows over 1,024 workgroups, of which 139 go round twice: with the
+// sums' launch 33.6 us, of 16,384 rows, once round, 29.4, of 32,768, twice,
+// 44.3); a frame's 5,442 rows in 10 us, the chain from position to angle to row.
 //
 // The weights' gradients: a group stays with its heads and walks the rows that
 // its workgroup takes (every grid-th block of them) with its columns' sums in
